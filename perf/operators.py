@@ -1,0 +1,473 @@
+"""Cases for the 8-bit key-value cache and the operators around it: rotary positions,
+rows quantised as they are appended to a paged cache and read back, and attention of
+one new token or of a prompt's rows over that cache.
+
+The cache.  `pool` is a byte tensor [n_pages, 2, n_kv_heads, page * (head_dim + 4)]: for
+each page, keys (0) then values (1), and each KV head, `page * head_dim` codes followed by
+`page` float32 scales, one for each position.  A stored value is (code - 128) * scale.
+The codes of a key block lie position by position ([page][head_dim]); those of a value
+block in groups of four positions, each dimension's four side by side
+([page / 4][head_dim][4]).  With a = the row's largest magnitude: scale = a / 127 rounded
+to float32, code = 128 + the integer nearest to 127 x / a (the exact quotient, ties to
+even), and 0 and 128 for a < 2^-100.
+`table` [n_seqs, max_pages] names a sequence's pages in order.
+
+Rows.  `length` [n_seqs] counts each sequence's positions, new rows included; the new
+rows of sequence b are rows row_start[b] .. row_start[b + 1] of the arrays and its last
+positions (one row for each sequence where row_start is absent).
+
+A case is one call (or an append and the read of what it wrote):
+
+* op: "rope", "append", "read", "attend".
+* n_seqs, rows, length: sequences, the most new rows of one, the most positions of one;
+  spread: whether the other sequences have fewer rows and positions.
+* heads, kv_heads, head_dim, page, dtype ("bf16", "f32"): shapes and the rows' type.
+* rope: "" or layout/rotated dimensions/scaling of the rotary tables.
+"""
+
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+TINY = 2.0 ** -100
+
+
+def _case(name, op, n_seqs, rows, length, heads, kv_heads, head_dim, *, page=64, dtype="bf16",
+          spread=True, rope=""):
+    c = dict(op=op, n_seqs=n_seqs, rows=rows, length=length, heads=heads, kv_heads=kv_heads,
+             head_dim=head_dim, page=page, dtype=dtype, spread=spread, rope=rope)
+    return dict(name=name, **c) if name else c
+
+
+def listed():
+    return [
+        # the queries of 32 clients, one token each, far into a stretched context
+        _case("rope_tokens_32", "rope", 32, 1, 16384, 40, 8, 128, rope="half/128/bands"),
+        # a long prompt's queries, half of each head rotated, neighbouring pairs
+        _case("rope_prompt_8192", "rope", 1, 8192, 8192, 32, 8, 128, rope="pairs/64/ramp"),
+        # one batched decode step's projection rows: queries and keys rotated, keys and
+        # values stored, as between the projection and the attention of a layer
+        _case("append_tokens_48", "append", 48, 1, 4000, 32, 8, 128, dtype="f32",
+              rope="half/128/bands"),
+        # the last chunk of a long prompt, rows already rotated
+        _case("append_prompt_2048", "append", 1, 2048, 8192, 32, 8, 128),
+        # several prompts of different lengths packed into one pass, small pages and heads
+        _case("append_packed_12", "append", 12, 500, 1500, 32, 8, 64, page=16, dtype="f32"),
+        # a whole long context taken out of the cache
+        _case("read_context_8192", "read", 2, 8192, 8192, 32, 8, 128, spread=False),
+        # a single client's token after a short prompt: latency
+        _case("token_1_at_700", "attend", 1, 1, 700, 32, 8, 128),
+        # a single client at the library's longest context, fp32 rows as its decode step has
+        _case("token_1_at_16384", "attend", 1, 1, 16384, 32, 8, 128, dtype="f32"),
+        # a batch of clients at different lengths, the small shape's heads, small pages
+        _case("token_48_at_4000", "attend", 48, 1, 4000, 32, 8, 64, page=16),
+        # a large batch at the longest context, five query heads a KV head
+        _case("token_32_at_16384", "attend", 32, 1, 16384, 40, 8, 128, spread=False),
+        # three short prompts of odd lengths in one pass, fp32 rows
+        _case("prompt_3_of_333", "attend", 3, 333, 333, 32, 8, 128, dtype="f32"),
+        # a chunk of 2048 rows that ends a prompt of 8192
+        _case("prompt_2048_of_8192", "attend", 1, 2048, 8192, 32, 8, 128, spread=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case: 1 to 64 sequences of 1 to 16384 positions (at most 400000 in all), 1 to
+    8 query heads for each of 1 to 8 KV heads, both head sizes, every page size and both
+    types; prompts of 2 to 2048 rows at depths of up to 8192 positions."""
+    op = rng.choice(["rope", "append", "append", "read", "token", "token", "token", "prompt",
+                     "prompt"])
+    kv_heads = rng.choice([1, 2, 4, 8, 8])
+    heads = kv_heads * rng.choice([1, 2, 4, 4, 5, 8])
+    head_dim = rng.choice([64, 128, 128])
+    page = rng.choice([16, 32, 64, 128])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    spread = rng.random() < 0.7
+    part = rng.choice([head_dim, head_dim, head_dim // 2, head_dim // 4])
+    rope = "%s/%d/%s" % (rng.choice(["half", "pairs"]), part,
+                         rng.choice(["plain", "linear", "base", "bands", "ramp"]))
+    if op == "token":
+        length = _log_int(rng, 1, 16384)
+        n = _log_int(rng, 1, max(1, min(64, 400000 // length)))
+        return _case(None, "attend", n, 1, length, heads, kv_heads, head_dim, page=page,
+                     dtype=dtype, spread=spread)
+    if op == "prompt":
+        rows = _log_int(rng, 2, 2048)
+        n = _log_int(rng, 1, max(1, min(16, 2048 // rows)))
+        most = 2048 * 8192 * 32 // (rows * n * heads)
+        length = rng.randint(rows, max(rows, min(8192, most)))
+        return _case(None, "attend", n, rows, length, heads, kv_heads, head_dim, page=page,
+                     dtype=dtype, spread=spread)
+    if rng.random() < 0.5:
+        n, rows = _log_int(rng, 1, 64), 1
+    else:
+        rows = _log_int(rng, 2, 8192)
+        n = _log_int(rng, 1, max(1, min(16, 8192 // rows)))
+    length = rng.randint(rows, 16384)
+    if op == "append" and rng.random() < 0.5:
+        rope = ""
+    return _case(None, op, n, rows, length, heads, kv_heads, head_dim, page=page, dtype=dtype,
+                 spread=spread, rope="" if op == "read" else rope)
+
+
+# ---------------------------------------------------------------- inputs
+def _counts(case):
+    """New rows and positions of each sequence: the most for the first, and with `spread`
+    down to half of that for the others."""
+    n, t, p, on = case["n_seqs"], case["rows"], case["length"], case["spread"]
+    rows = [t - (on * 53 * b) % (t // 2 + 1) for b in range(n)]
+    return rows, [max(r, p - (on * 97 * b) % (p // 2 + 1)) for b, r in enumerate(rows)]
+
+
+def frequencies(rope, base=500000.0):
+    """Angle step of each rotated pair, and the factor on cosines and sines, of the
+    tables' scalings: eight times the context of 2048 positions."""
+    _, dim, scaling = rope.split("/")
+    dim, stretch, trained = int(dim), 8.0, 2048.0
+    j = torch.arange(dim // 2, dtype=torch.float64)
+    if scaling == "base":
+        return (base * stretch ** (dim / (dim - 2.0))) ** (-2.0 * j / dim), 1.0
+    f = base ** (-2.0 * j / dim)
+    if scaling == "linear":
+        return f / stretch, 1.0
+    if scaling == "bands":      # by wavelength: long ones stretched, short ones kept
+        turns = trained * f / (2 * math.pi)
+        keep = ((turns - 1.0) / (4.0 - 1.0)).clamp(0, 1)
+        return f / stretch * (1 - keep) + f * keep, 1.0
+    if scaling == "ramp":       # by dimension, between 32 turns and one
+        at = [dim * math.log(trained / (t * 2 * math.pi)) / (2 * math.log(base)) for t in (32.0, 1.0)]
+        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), dim - 1)
+        move = ((j - lo) / max(hi - lo, 0.001)).clamp(0, 1)
+        return f / stretch * move + f * (1 - move), 0.1 * math.log(stretch) + 1.0
+    return f, 1.0
+
+
+def _pool(n_pages, case, gen):
+    """Pages of quantised rows: normal values, a few large dimensions among the keys."""
+    H, hd, page = case["kv_heads"], case["head_dim"], case["page"]
+    blocks = []
+    for which in (0, 1):
+        x = torch.randn(n_pages, H, page, hd, device="cuda", generator=gen)
+        if which == 0:
+            x *= torch.where(torch.arange(hd, device="cuda") % 29 == 3, 4.0, 0.9)
+        top = x.abs().amax(-1, keepdim=True)
+        codes = (x.mul_(127.0 / top).round_() + 128.0).to(torch.uint8)
+        del x
+        if which == 1:
+            codes = codes.view(n_pages, H, page // 4, 4, hd).transpose(3, 4).contiguous()
+        scales = (top.view(n_pages, H, page) / 127.0).view(torch.uint8)
+        blocks.append(torch.cat([codes.view(n_pages, H, page * hd), scales], -1))
+    return torch.stack(blocks, 1)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    H, G, hd, page = case["kv_heads"], case["heads"], case["head_dim"], case["page"]
+    t = DTYPES[case["dtype"]]
+    rows, lens = _counts(case)
+    need = [-(-n // page) for n in lens]
+    n_rows, n_pages = sum(rows), sum(need) + 3
+
+    def normal(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen)
+
+    s = {"case": dict(case), "length": torch.tensor(lens, dtype=torch.int32, device="cuda"),
+         "row_start": None}
+    if case["rows"] > 1:
+        start = torch.tensor([0] + rows).cumsum(0)
+        s["row_start"] = start.to(torch.int32).to("cuda")
+    if case["op"] != "rope":
+        order = torch.randperm(n_pages, device="cuda", generator=gen).to(torch.int32)
+        s["table"] = torch.zeros(len(lens), max(need), dtype=torch.int32, device="cuda")
+        at = 0
+        for b, n in enumerate(need):
+            s["table"][b, :n] = order[at:at + n]
+            at += n
+    if case["op"] in ("read", "attend"):
+        s["pool"] = _pool(n_pages, case, gen)
+    elif case["op"] == "append":
+        s["pool"] = torch.randint(0, 256, (n_pages, 2, H, page * (hd + 4)), dtype=torch.uint8,
+                                  device="cuda", generator=gen)
+        s["k"] = normal(n_rows, H, hd).to(t)
+        s["v"] = normal(n_rows, H, hd).to(t)
+    if case["op"] in ("rope", "attend") or case["rope"]:
+        s["q"] = (1.5 * normal(n_rows, G, hd)).to(t)
+    if case["rope"]:
+        f, factor = frequencies(case["rope"])
+        ang = torch.arange(max(lens), dtype=torch.float64, device="cuda")[:, None] * f.to("cuda")
+        s["cos"] = (factor * ang.cos()).to(torch.float32)
+        s["sin"] = (factor * ang.sin()).to(torch.float32)
+    if case["op"] == "rope":
+        s["positions"] = _where(s)[1].to(torch.int32)
+    return s
+
+
+# ---------------------------------------------------------------- the plain form
+def _where(s):
+    """Sequence and position of each new row."""
+    length = s["length"].long()
+    if s["row_start"] is None:
+        return torch.arange(len(length), device="cuda"), length - 1
+    start = s["row_start"].long()
+    i = torch.arange(sum(_counts(s["case"])[0]), device="cuda")
+    b = torch.searchsorted(start, i, right=True) - 1
+    return b, length[b] - start[b + 1] + i
+
+
+def _rotate(s, x, pos):
+    """x [rows, heads, head_dim] in float32, rotated at its rows' positions."""
+    layout, dim, _ = s["case"]["rope"].split("/")
+    dim = int(dim)
+    c, n = s["cos"][pos][:, None], s["sin"][pos][:, None]
+    x = x.float()
+    r, rest = x[..., :dim], x[..., dim:]
+    if layout == "half":
+        a, b = r[..., :dim // 2], r[..., dim // 2:]
+        r = torch.cat([a * c - b * n, a * n + b * c], -1)
+    else:
+        a, b = r[..., 0::2], r[..., 1::2]
+        r = torch.stack([a * c - b * n, a * n + b * c], -1).flatten(-2)
+    return torch.cat([r, rest], -1)
+
+
+def _quantise(x):
+    """Codes (bytes) and scales of rows x [..., head_dim]: the quotients in 64 bits, where
+    a value next to the border between two codes keeps its side."""
+    x = x.double()
+    top = x.abs().amax(-1, keepdim=True)
+    small = top < TINY
+    code = torch.where(small, 0.0, x * 127.0 / top).round() + 128.0
+    return code.to(torch.uint8), torch.where(small, 0.0, top / 127.0)[..., 0].float()
+
+
+def _slots(s, b, pos):
+    page = s["case"]["page"]
+    return s["table"][b, pos // page].long(), pos % page
+
+
+def _store(s, which, x, b, pos):
+    page, hd = s["case"]["page"], s["case"]["head_dim"]
+    code, scale = _quantise(x.float())
+    phys, slot = _slots(s, b, pos)
+    n, h = s["pool"].shape[0], s["pool"].shape[2]
+    block = s["pool"][:, which]
+    codes = block[..., :page * hd]
+    heads = torch.arange(h, device="cuda")
+    d = torch.arange(hd, device="cuda")
+    if which == 0:
+        at = slot[:, None] * hd + d
+    else:
+        at = (slot // 4)[:, None] * (4 * hd) + 4 * d + (slot % 4)[:, None]
+    codes[phys[:, None, None], heads[:, None], at[:, None]] = code
+    at = page * hd + 4 * slot[:, None] + torch.arange(4, device="cuda")
+    block[phys[:, None, None], heads[:, None], at[:, None]] = scale[..., None].view(torch.uint8)
+
+
+def _values(s, pages, which):
+    """Float32 values of the named pages: [..., page, n_kv_heads, head_dim]."""
+    page, hd = s["case"]["page"], s["case"]["head_dim"]
+    block = s["pool"][:, which][pages.long()]
+    lead = block.shape[:-1]
+    scale = block[..., page * hd:].contiguous().view(torch.float32)
+    code = block[..., :page * hd].float() - 128.0
+    if which == 0:
+        code = code.view(*lead, page, hd)
+    else:
+        code = code.view(*lead, page // 4, hd, 4).transpose(-1, -2).reshape(*lead, page, hd)
+    return (code * scale[..., None]).transpose(-3, -2)
+
+
+def _read(s, t):
+    page, hd = s["case"]["page"], s["case"]["head_dim"]
+    b, pos = _where(s)
+    phys, slot = _slots(s, b, pos)
+    heads, d = torch.arange(s["pool"].shape[2], device="cuda"), torch.arange(hd, device="cuda")
+    out = []
+    for which in (0, 1):
+        block = s["pool"][:, which]
+        if which == 0:
+            at = slot[:, None] * hd + d
+        else:
+            at = (slot // 4)[:, None] * (4 * hd) + 4 * d + (slot % 4)[:, None]
+        code = block[phys[:, None, None], heads[:, None], at[:, None]]
+        at = page * hd + 4 * slot[:, None] + torch.arange(4, device="cuda")
+        scale = block[phys[:, None, None], heads[:, None], at[:, None]].view(torch.float32)
+        out.append(((code.float() - 128.0) * scale).to(t))
+    return out
+
+
+def _attend(s):
+    c = s["case"]
+    B, H, hd, t = c["n_seqs"], c["kv_heads"], c["head_dim"], s["q"].dtype
+    G = c["heads"] // H
+    b, pos = _where(s)
+    k = _values(s, s["table"], 0).flatten(1, 2).permute(0, 2, 3, 1)   # [B, H, hd, positions]
+    v = _values(s, s["table"], 1).flatten(1, 2).transpose(1, 2)       # [B, H, positions, hd]
+    n = k.shape[-1]
+    T = c["rows"]
+    i = torch.zeros_like(b) if s["row_start"] is None else \
+        torch.arange(len(b), device="cuda") - s["row_start"].long()[b]
+    q = torch.zeros(B, T, H, G, hd, device="cuda")
+    q[b, i] = s["q"].float().view(-1, H, G, hd)
+    last = torch.full((B, T), -1, device="cuda")
+    last[b, i] = pos
+    q = q.permute(0, 2, 1, 3, 4).reshape(B, H, T * G, hd)
+    x = torch.matmul(q, k.contiguous()).view(B, H, T, G, n) * (1.0 / math.sqrt(hd))
+    seen = torch.arange(n, device="cuda") <= last[..., None]
+    x = x.masked_fill_(~seen[:, None, :, None], float("-inf"))
+    e = (x - x.amax(-1, keepdim=True)).exp()
+    e = torch.where(seen[:, None, :, None], e, torch.zeros((), device="cuda"))
+    o = torch.matmul(e.view(B, H, T * G, n), v.contiguous()).view(B, H, T, G, hd)
+    o = o / e.sum(-1, keepdim=True)
+    return o.permute(0, 2, 1, 3, 4).reshape(B, T, H * G, hd)[b, i].to(t)
+
+
+def _plain(s):
+    c = s["case"]
+    if c["op"] == "rope":
+        return _rotate(s, s["q"], s["positions"].long()).to(s["q"].dtype)
+    if c["op"] == "attend":
+        return _attend(s)
+    if c["op"] == "read":
+        return _read(s, DTYPES[c["dtype"]])
+    b, pos = _where(s)
+    k, got = s["k"], []
+    if c["rope"]:
+        k = _rotate(s, k, pos)
+        got = [_rotate(s, s["q"], pos).to(s["q"].dtype)]
+    _store(s, 0, k, b, pos)
+    _store(s, 1, s["v"], b, pos)
+    return got + _read(s, torch.bfloat16 if c["rope"] else torch.float32)
+
+
+# ---------------------------------------------------------------- the framework's calls
+def _calls(s):
+    from paper_2608_24204_amd import ops
+    c = s["case"]
+    if "rope" not in s:     # what a program keeps between calls: its tables and its cache
+        layout = c["rope"].split("/")[0]
+        s["rope"] = ops.RopeTable(s["cos"], s["sin"], layout=layout) if c["rope"] else None
+        s["cache"] = None if c["op"] == "rope" else \
+            ops.KvCache(s["pool"], s["table"], page=c["page"], head_dim=c["head_dim"])
+    if c["op"] == "rope":
+        return ops.rope(s["q"], s["positions"], s["rope"])
+    at = dict(row_start=s["row_start"])
+    if c["op"] == "attend":
+        return s["cache"].attend(s["q"], s["length"], max_rows=c["rows"], **at)
+    if c["op"] == "read":
+        return s["cache"].read(s["length"], n_rows=sum(_counts(c)[0]), dtype=DTYPES[c["dtype"]],
+                               **at)
+    q = s["cache"].append(s["k"], s["v"], s["length"], rope=s["rope"], q=s.get("q"), **at)
+    k, v = s["cache"].read(s["length"], n_rows=s["k"].shape[0],
+                           dtype=torch.bfloat16 if c["rope"] else torch.float32, **at)
+    return [k, v] if q is None else [q, k, v]
+
+
+def run(s):
+    return _calls(s) if own else _plain(s)
+
+
+# ---------------------------------------------------------------- work and the exact values
+def work(case):
+    rows, lens = _counts(case)
+    H, hd = case["kv_heads"], case["head_dim"]
+    size = 2 if case["dtype"] == "bf16" else 4
+    n = sum(rows)
+    cached = 2 * H * (hd + 4)                  # bytes of one position
+    q = n * case["heads"] * hd * size          # the queries, or the output
+    dim = int(case["rope"].split("/")[1]) if case["rope"] else 0
+    tables = n * dim * 4
+    turn = 3 * n * dim                          # operations on one head's rotated values
+    if case["op"] == "rope":
+        return {"bytes": 2 * q + tables + 4 * n, "flops": turn * case["heads"]}
+    if case["op"] == "read":
+        return {"bytes": n * (cached + 2 * H * hd * size), "flops": 2 * n * H * hd}
+    if case["op"] == "append":
+        out = 2 if case["rope"] else 4
+        return {"bytes": n * (2 * H * hd * size + cached + 2 * H * hd * out) +
+                (2 * q + tables if dim else 0),
+                "flops": 8 * n * H * hd + turn * (case["heads"] + H)}
+    seen = sum(r * p - r * (r - 1) // 2 for r, p in zip(rows, lens))
+    return {"bytes": sum(lens) * cached + 2 * q, "flops": 4 * case["heads"] * hd * seen}
+
+
+def exact(case, seed):
+    """The same outputs from the definitions, in 64 bits, one sequence at a time."""
+    s = prepare(case, seed)
+    rows, lens = _counts(case)
+    H, hd, page = case["kv_heads"], case["head_dim"], case["page"]
+    G = case["heads"] // H
+    dev = "cuda"
+
+    def turned(x, pos):
+        layout, dim, _ = case["rope"].split("/")
+        dim = int(dim)
+        f, factor = frequencies(case["rope"])
+        z = torch.polar(torch.full((len(pos), dim // 2), factor, dtype=torch.float64, device=dev),
+                        pos.double()[:, None] * f.to(dev))[:, None]
+        x = x.double()
+        first = torch.arange(dim // 2, device=dev) * (1 if layout == "half" else 2)
+        second = first + (dim // 2 if layout == "half" else 1)
+        y = torch.complex(x[..., first], x[..., second]) * z
+        out = x.clone()
+        out[..., first], out[..., second] = y.real, y.imag
+        return out
+
+    def held(x):
+        """What 8-bit rows of x stand for."""
+        x = x.double()
+        top = x.abs().amax(-1, keepdim=True)
+        return torch.where(top >= TINY, torch.round(127.0 * x / top) * (top / 127.0), 0.0)
+
+    def context(b, n):
+        """Keys and values of the first n positions of sequence b."""
+        flat = s["pool"].reshape(-1)
+        p = torch.arange(n, device=dev)
+        block = s["table"][b].long()[p // page]
+        slot, got = p % page, []
+        head, d = torch.arange(H, device=dev)[None, :, None], torch.arange(hd, device=dev)
+        for which in (0, 1):
+            at = ((block * 2 + which)[:, None, None] * H + head) * (page * (hd + 4))
+            place = slot[:, None, None]
+            code = at + (place * hd + d if which == 0 else
+                         torch.div(place, 4, rounding_mode="floor") * 4 * hd + 4 * d + place % 4)
+            byte = at + page * hd + 4 * place + torch.arange(4, device=dev)
+            scale = flat[byte].view(torch.float32).double()
+            got.append((flat[code].double() - 128.0) * scale)
+        return got
+
+    first = [sum(rows[:b]) for b in range(len(rows))]
+    parts = []
+    for b, (r, n) in enumerate(zip(rows, lens)):
+        pos = torch.arange(n - r, n, device=dev)
+        at = slice(first[b], first[b] + r)
+        if case["op"] == "rope":
+            parts.append([turned(s["q"][at], pos)])
+        elif case["op"] == "append":
+            k, got = s["k"][at], []
+            if case["rope"]:
+                k, got = turned(k, pos), [turned(s["q"][at], pos)]
+            parts.append(got + [held(k), held(s["v"][at])])
+        else:
+            k, v = context(b, n)
+            if case["op"] == "read":
+                parts.append([k[n - r:], v[n - r:]])
+                continue
+            q = s["q"][at].double()
+            o = torch.empty_like(q)
+            past = torch.arange(n, device=dev)[None] > pos[:, None]
+            for h in range(case["heads"]):
+                x = (q[:, h] @ k[:, h // G].T) / math.sqrt(hd)
+                x = torch.softmax(x.masked_fill(past, -math.inf), -1)
+                o[:, h] = x @ v[:, h // G]
+            parts.append([o])
+    out = [torch.cat(p) for p in zip(*parts)]
+    return out[0] if case["op"] in ("rope", "attend") else out
