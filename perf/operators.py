@@ -7,9 +7,9 @@ each page, keys (0) then values (1), and each KV head, `page * head_dim` codes f
 `page` float32 scales, one for each position.  A stored value is (code - 128) * scale.
 The codes of a key block lie position by position ([page][head_dim]); those of a value
 block in groups of four positions, each dimension's four side by side
-([page / 4][head_dim][4]).  With a = the row's largest magnitude: scale = a / 127 rounded
-to float32, code = 128 + the integer nearest to 127 x / a (the exact quotient, ties to
-even), and 0 and 128 for a < 2^-100.
+([page / 4][head_dim][4]).  With a = the row's largest magnitude, at least 2^-60: scale =
+a / 127 rounded to float32, code = 128 + the integer nearest to 127 x / a (the exact
+quotient, ties to even).
 `table` [n_seqs, max_pages] names a sequence's pages in order.
 
 Rows.  `length` [n_seqs] counts each sequence's positions, new rows included; the new
@@ -34,7 +34,7 @@ import torch
 own = False
 
 DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
-TINY = 2.0 ** -100
+LEAST = 2.0 ** -60
 
 
 def _case(name, op, n_seqs, rows, length, heads, kv_heads, head_dim, *, page=64, dtype="bf16",
@@ -242,10 +242,9 @@ def _quantise(x):
     """Codes (bytes) and scales of rows x [..., head_dim]: the quotients in 64 bits, where
     a value next to the border between two codes keeps its side."""
     x = x.double()
-    top = x.abs().amax(-1, keepdim=True)
-    small = top < TINY
-    code = torch.where(small, 0.0, x * 127.0 / top).round() + 128.0
-    return code.to(torch.uint8), torch.where(small, 0.0, top / 127.0)[..., 0].float()
+    top = x.abs().amax(-1, keepdim=True).clamp(min=LEAST)
+    code = (x * 127.0 / top).round() + 128.0
+    return code.to(torch.uint8), (top / 127.0)[..., 0].float()
 
 
 def _slots(s, b, pos):
@@ -424,8 +423,8 @@ def exact(case, seed):
     def held(x):
         """What 8-bit rows of x stand for."""
         x = x.double()
-        top = x.abs().amax(-1, keepdim=True)
-        return torch.where(top >= TINY, torch.round(127.0 * x / top) * (top / 127.0), 0.0)
+        top = x.abs().amax(-1, keepdim=True).clamp(min=LEAST)
+        return torch.round(127.0 * x / top) * (top / 127.0)
 
     def context(b, n):
         """Keys and values of the first n positions of sequence b."""
