@@ -55,8 +55,9 @@ typedef enum {
 
 /* Element types.  WICI_Q8 is a weight storage format only (wici_config's
  * weight_dtype): block-scaled 8-bit codes, see wici_quantize_q8; its weight
- * tensors are given as WICI_BF16 or WICI_F32 and quantised at load. */
-typedef enum { WICI_F32 = 0, WICI_BF16 = 1, WICI_Q8 = 2 } wici_dtype;
+ * tensors are given as WICI_BF16 or WICI_F32 and quantised at load.  WICI_KV8 is
+ * a KV cache storage format only (see wici_kv8). */
+typedef enum { WICI_F32 = 0, WICI_BF16 = 1, WICI_Q8 = 2, WICI_KV8 = 3 } wici_dtype;
 
 /* Arithmetic of the prefill projections (decode always multiplies bf16/fp32
  * weights by fp32 activations with fp32 accumulation). */
@@ -360,6 +361,162 @@ wici_status wici_stream_read(const void* d_buf, size_t bytes, int32_t grid, int3
  * 16384, grid outside [1, 4096]), WICI_E_HIP (a HIP call failed). */
 wici_status wici_stream_read_noalloc(const void* d_buf, size_t bytes, int32_t grid,
                                      void* hip_stream, uint32_t* checksum);
+
+/* ---- Operators on caller-owned device tensors (no model) -------------------------
+ *
+ * Rotary positions, an 8-bit paged KV cache and causal attention over it, for callers
+ * that run their own layers.  Conventions of these calls:
+ *  - every pointer marked device is device memory of the stream's GPU; tensors stay with
+ *    the caller, and the calls allocate nothing;
+ *  - a call enqueues on hip_stream (NULL: the null stream of the current device) and
+ *    returns without waiting; it may be captured into a HIP graph.  Two calls (or
+ *    captured graphs) may overlap unless one writes what the other uses: the cache, an
+ *    output or the workspace;
+ *  - arguments are checked before anything is enqueued.  Errors: WICI_E_ARG, WICI_E_HIP
+ *    (the launch failed);
+ *  - what lies in device memory (lengths, rows, page tables, positions) is not seen by
+ *    those checks.  The kernels bound it: no value there makes them leave their tensors. */
+
+/* Head rows: element (row, head, d) at data[row * row_stride + head * head_stride + d].
+ * dtype WICI_F32 or WICI_BF16; data 16-byte aligned, strides (in elements, positive) multiples
+ * of 8 and no overlap between rows or heads. */
+typedef struct {
+  void* data; /* device */
+  int32_t dtype;
+  int64_t row_stride, head_stride;
+} wici_head_rows;
+
+typedef enum {
+  WICI_ROPE_HALF = 0, /* pairs (j, j + dim / 2) */
+  WICI_ROPE_PAIRS = 1 /* pairs (2 j, 2 j + 1) */
+} wici_rope_layout;
+
+/* Angle steps f_j of pair j of a rotary embedding of `dim` dimensions, with
+ * b_j = base^(-2 j / dim), s = factor, n = original (the positions trained on): */
+typedef enum {
+  WICI_ROPE_PLAIN = 0,  /* f_j = b_j */
+  WICI_ROPE_LINEAR = 1, /* f_j = b_j / s */
+  WICI_ROPE_BASE = 2,   /* f_j = (base s^(dim / (dim - 2)))^(-2 j / dim) */
+  WICI_ROPE_BANDS = 3,  /* by the turns r_j = n b_j / 2 pi within the trained positions:
+                           k_j = clamp((r_j - low) / (high - low), 0, 1),
+                           f_j = (1 - k_j) b_j / s + k_j b_j */
+  WICI_ROPE_RAMP = 4    /* by dimension: j_lo = floor(D(high)), j_hi = ceil(D(low)), limited
+                           to [0, dim - 1], with D(t) = dim ln(n / 2 pi t) / (2 ln base);
+                           m_j = clamp((j - j_lo) / max(j_hi - j_lo, 0.001), 0, 1),
+                           f_j = m_j b_j / s + (1 - m_j) b_j, and cosines and sines are
+                           multiplied by 1 + 0.1 ln s */
+} wici_rope_scaling;
+
+typedef struct {
+  int32_t dim;     /* rotated dimensions of a head, a multiple of 8, 8..128 */
+  int32_t layout;  /* wici_rope_layout */
+  int32_t scaling; /* wici_rope_scaling; PLAIN ignores the fields below base */
+  double base;     /* > 1 */
+  double factor;   /* s >= 1 */
+  double original; /* n > 0 (BANDS, RAMP) */
+  double low, high;/* 0 < low < high (BANDS, RAMP; both 0: 1 and 4 for BANDS, 1 and 32 for
+                      RAMP) */
+} wici_rope;
+
+/* Tables of a rotary embedding: cosines and sines [n_pos][dim / 2], 16-byte aligned.
+ * Dimensions from dim on pass through unchanged. */
+typedef struct {
+  const float* cos_t; /* device */
+  const float* sin_t; /* device */
+  int64_t n_pos;
+  int32_t dim;
+  int32_t layout;
+} wici_rope_tab;
+
+/* Fill the tables of positions 0 .. n_pos - 1 (angles in 64 bits, rounded to fp32).
+ * n_pos <= 2^24. */
+wici_status wici_rope_table(const wici_rope* rope, int64_t n_pos, float* cos_t, float* sin_t,
+                            void* hip_stream);
+
+/* y[row, head] = x[row, head] rotated at positions[row] (device), n_rows rows of n_heads heads
+ * of head_dim (64 or 128) dimensions.  y may be x itself.  The arithmetic is fp32, each
+ * product and sum rounded, and one rounding to y's type.  A row at a negative position
+ * (padding) is left as it is; at a position past the tables it is NaN in the rotated
+ * dimensions. */
+wici_status wici_rope_rows(const wici_rope_tab* rope, int32_t head_dim, int32_t n_rows,
+                           int32_t n_heads, const int32_t* positions, wici_head_rows x,
+                           wici_head_rows y, void* hip_stream);
+
+/* An 8-bit paged KV cache (WICI_KV8).  For each page, keys then values, and each KV head, the
+ * pool holds a block of page * head_dim codes (bytes) and then page fp32 scales, one for each
+ * position: blocks follow each other as [n_pages][2][n_kv_heads].  A stored row of
+ * head_dim values x has, with a = max(max_d |x_d|, 2^-60),
+ *   scale = a / 127 (rounded to fp32),
+ *   code_d = 128 + the integer nearest to 127 x_d / a (the exact quotient, ties to even),
+ * and stands for (code_d - 128) * scale.  A row holding an infinity or a NaN is stored as
+ * all NaN (scale NaN).  Key codes lie as [page][head_dim], value codes as
+ * [page / 4][head_dim][4]: the codes of four neighbouring positions side by side.  68 (64
+ * dimensions) or 132 (128) bytes for each position, head, key or value.
+ * table[seq * table_stride + i] names the page of the sequence's positions page * i ..; an
+ * entry outside [0, n_pages) names none: those positions are not attended, appending to them
+ * does nothing, and they read as zero.  So do positions past max_pages pages. */
+typedef struct {
+  void* pool;           /* device, 16-byte aligned, wici_kv8_bytes bytes */
+  int32_t n_pages;
+  int32_t page;         /* positions per page: 16, 32, 64 or 128 */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  const int32_t* table; /* device */
+  int64_t table_stride; /* entries between sequences' tables */
+  int32_t max_pages;    /* entries of each sequence's table */
+} wici_kv8;
+
+/* Bytes of a pool (uses n_pages, page, n_kv_heads, head_dim).  No GPU call. */
+wici_status wici_kv8_bytes(const wici_kv8* cache, size_t* bytes);
+
+/* The new rows of a call.  Sequence b has length[b] positions, the new ones included, and its
+ * new rows, row_start[b] .. row_start[b + 1] of the arrays, are its last positions.  Without
+ * row_start every sequence has one new row (n_rows == n_seqs).  Rows before row_start[0] or
+ * from row_start[n_seqs] on belong to no sequence: whatever they hold is not used, and outputs
+ * there are left as they are.  A sequence with more new rows than positions has its first
+ * rows at negative positions: they are not appended or read, and attend to nothing.
+ * row_start must not decrease. */
+typedef struct {
+  int32_t n_seqs, n_rows;
+  const int32_t* row_start; /* device [n_seqs + 1], or NULL */
+  const int32_t* length;    /* device [n_seqs] */
+  int32_t max_rows;         /* the most new rows of a sequence and the most positions, as far as */
+  int32_t max_length;       /* the caller knows (0: no idea).  They only shape the launch: */
+                            /* results do not depend on them, beyond the order of sums. */
+} wici_kv8_batch;
+
+/* Quantise the rows k and v (n_kv_heads heads) into the cache.  With rope, keys are rotated at
+ * their positions first (in fp32, as by wici_rope_rows, with no rounding before the
+ * quantisation), and with q.data set the n_heads query heads too, into q_out (which may be
+ * q): the work between a layer's projection and its attention in one launch.  q.data needs
+ * rope; rope.dim at most head_dim.  At most 65535 sequences. */
+wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
+                            const wici_rope_tab* rope, int32_t n_heads, wici_head_rows q,
+                            wici_head_rows q_out, wici_head_rows k, wici_head_rows v,
+                            void* hip_stream);
+
+/* Read the batch's rows back: k and v (either data may be NULL) receive the values that the
+ * cache holds at the rows' positions, rounded once to their type. */
+wici_status wici_kv8_read(const wici_kv8* cache, const wici_kv8_batch* batch, wici_head_rows k,
+                          wici_head_rows v, void* hip_stream);
+
+/* Bytes of device workspace wici_kv8_attend needs for this cache and batch (0: none): uses the
+ * geometry, counts and hints, no device memory.  No GPU call. */
+wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batch* batch,
+                                      int32_t n_heads, size_t* bytes);
+
+/* Causal grouped-query attention of the batch's rows over the cache: query head h reads KV
+ * head h / (n_heads / n_kv_heads), a row at position p sees the sequence's positions <= p
+ * (append first),
+ *   out = sum_j e^(scale q . k_j) v_j / sum_j e^(scale q . k_j),
+ * with scores, weights and sums in fp32; q and the weights enter the matrix products as one
+ * fp16 term where q and out are bf16 (exact for q; within 2^-11 of a weight), else two (2^-22).  A row
+ * that sees nothing gives zeros.  q and out are n_heads heads, of any of the two types each;
+ * out may be q only if they are the same rows exactly.  workspace: device, 16-byte aligned,
+ * undefined before and after. */
+wici_status wici_kv8_attend(const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,
+                            float scale, wici_head_rows q, wici_head_rows out, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
 
 /* Message of the last failed call on this model ("" if none).  Valid until the
  * next call on the model. */

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libwici.so"
 WICI_OK, WICI_E_ARG, WICI_E_STATE, WICI_E_CAPACITY, WICI_E_HIP, WICI_E_NUMERIC = 0, -1, -2, -3, -4, -5
 STATUS_NAMES = {0: "WICI_OK", -1: "WICI_E_ARG", -2: "WICI_E_STATE", -3: "WICI_E_CAPACITY",
                 -4: "WICI_E_HIP", -5: "WICI_E_NUMERIC"}
-WICI_F32, WICI_BF16, WICI_Q8 = 0, 1, 2
+WICI_F32, WICI_BF16, WICI_Q8, WICI_KV8 = 0, 1, 2, 3
 PREFILL_MODES = {"bf16x2": 0, "bf16": 1, "f32": 2, "bf16x3": 3, "bf16x3q": 4}
 WICI_FLAG_NO_GRAPH = 1
 WICI_FLAG_FAULT_DRILL = 2
@@ -31,7 +31,9 @@ EXPORTED = ["wici_create", "wici_memory_requirements", "wici_bind_memory", "wici
             "wici_prefill", "wici_decode_step", "wici_decode_n", "wici_reset_kv", "wici_position",
             "wici_read_kv", "wici_profile_decode_step", "wici_quantize_q8", "wici_md5",
             "wici_load_weights_cached", "wici_bind_memory_shared", "wici_decode_batch",
-            "wici_stream_read", "wici_stream_read_noalloc", "wici_last_error", "wici_destroy"]
+            "wici_stream_read", "wici_stream_read_noalloc", "wici_last_error", "wici_destroy",
+            "wici_rope_table", "wici_rope_rows", "wici_kv8_bytes", "wici_kv8_append",
+            "wici_kv8_read", "wici_kv8_attend_workspace", "wici_kv8_attend"]
 
 
 class WiciConfig(ctypes.Structure):
@@ -51,6 +53,35 @@ class WiciTensor(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("dtype", ctypes.c_int32), ("ndim", ctypes.c_int32),
                 ("shape", ctypes.c_int64 * 2), ("data", ctypes.c_void_p),
                 ("on_device", ctypes.c_int32)]
+
+
+class WiciHeadRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class WiciRope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class WiciRopeTab(ctypes.Structure):
+    _fields_ = [("cos_t", ctypes.c_void_p), ("sin_t", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
+                ("dim", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class WiciKv8(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_int32)]
+
+
+class WiciKv8Batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("row_start", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("max_rows", ctypes.c_int32), ("max_length", ctypes.c_int32)]
 
 
 class WiciError(RuntimeError):
@@ -97,6 +128,19 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
                              ctypes.c_int),
         "wici_stream_read_noalloc": ([P, sz, i32, P, ctypes.POINTER(ctypes.c_uint32)],
                                      ctypes.c_int),
+        "wici_rope_table": ([ctypes.POINTER(WiciRope), ctypes.c_int64, P, P, P], ctypes.c_int),
+        "wici_rope_rows": ([ctypes.POINTER(WiciRopeTab), i32, i32, i32, P, WiciHeadRows,
+                            WiciHeadRows, P], ctypes.c_int),
+        "wici_kv8_bytes": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(sz)], ctypes.c_int),
+        "wici_kv8_append": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch),
+                             ctypes.POINTER(WiciRopeTab), i32, WiciHeadRows, WiciHeadRows,
+                             WiciHeadRows, WiciHeadRows, P], ctypes.c_int),
+        "wici_kv8_read": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), WiciHeadRows,
+                           WiciHeadRows, P], ctypes.c_int),
+        "wici_kv8_attend_workspace": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), i32,
+                                       ctypes.POINTER(sz)], ctypes.c_int),
+        "wici_kv8_attend": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), i32,
+                             ctypes.c_float, WiciHeadRows, WiciHeadRows, P, sz, P], ctypes.c_int),
         "wici_last_error": ([P], ctypes.c_char_p),
         "wici_destroy": ([P], None),
     }

@@ -20,8 +20,8 @@ OUT = os.path.join(PKG, "libwici.so")
 BUILD = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["gemv.hip", "misc.hip", "attention.hip", "gemm.hip", "batch.hip", "model.cpp", "quant.cpp",
-           "cache.cpp", "noalloc.cpp"]
+SOURCES = ["gemv.hip", "misc.hip", "attention.hip", "gemm.hip", "batch.hip", "kv8.hip", "kv8_attn.hip",
+           "model.cpp", "ops.cpp", "quant.cpp", "cache.cpp", "noalloc.cpp"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

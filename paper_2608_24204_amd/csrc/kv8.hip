@@ -1,0 +1,338 @@
+// Rotary positions, and the 8-bit key-value cache as it is written and read back.
+//
+// All three kernels are bound by memory: each row is read once and written once.  A
+// head row of hd values is a unit of hd / 8 lanes, eight values a lane, so a unit's
+// maximum is a reduction within one row of DPP lanes and no unit waits for another.
+#include "kv8.h"
+
+#include "launch.h"
+
+namespace wici {
+
+// Four consecutive elements at element offset `at` (a multiple of 4).
+__device__ __forceinline__ void load4(const HeadRows& x, int64_t at, float* o) {
+  if (x.bf16) {
+    const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(x.p) + at);
+    o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xffff0000u);
+    o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xffff0000u);
+  } else {
+    const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(x.p) + at);
+    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+  }
+}
+__device__ __forceinline__ void put4(const HeadRows& x, int64_t at, const float* v) {
+  if (x.bf16) {
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(x.p) + at) =
+        make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+                   (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(x.p) + at) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// The eight dimensions of lane c of a unit, as two runs of four: consecutive, or (a
+// rotated run of the half layout) the first members of four pairs and the second.
+struct Runs {
+  int a, b;
+  bool turn;  // rotated
+};
+__device__ __forceinline__ Runs runs(const RopeTab& rope, int c) {
+  Runs r{8 * c, 8 * c + 4, false};
+  if (rope.cos && 8 * c < rope.dim) {
+    r.turn = true;
+    if (rope.layout == 0) {
+      r.a = 4 * c;
+      r.b = rope.dim / 2 + 4 * c;
+    }
+  }
+  return r;
+}
+
+// (a, b) -> (a cos - b sin, a sin + b cos) for each pair, every product and sum rounded
+// to fp32 by itself: the codes of a rotated key are then a function of the row alone
+// and not of how a compiler joins the products.
+__device__ __forceinline__ void turn8(float (&x)[8], const float4& c, const float4& s, int layout) {
+#pragma clang fp contract(off)
+  const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float& u = layout ? x[2 * i] : x[i];
+    float& w = layout ? x[2 * i + 1] : x[4 + i];
+    const float a = u, b = w;
+    const float ac = a * cc[i], bs = b * ss[i], as = a * ss[i], bc = b * cc[i];
+    u = ac - bs;
+    w = as + bc;
+  }
+}
+
+// A unit's rotation at position pos; past the table the row is NaN (no angle is known).
+__device__ __forceinline__ void turn_row(const RopeTab& rope, const Runs& r, int c, int pos,
+                                         float (&x)[8]) {
+  if (!r.turn) return;
+  const size_t at = (size_t)min(pos, rope.n_pos - 1) * (rope.dim / 2) + 4 * c;
+  const float4 cs = *reinterpret_cast<const float4*>(rope.cos + at);
+  const float4 sn = *reinterpret_cast<const float4*>(rope.sin + at);
+  turn8(x, cs, sn, rope.layout);
+  if (pos >= rope.n_pos) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7fc00000u);
+  }
+}
+
+// ------------------------------------------------------------------- rotary positions
+// The table is read where another head of the row has read it before; a row's heads are
+// neighbouring units.
+template <int HD>
+__global__ __launch_bounds__(256) void k_rope_rows(HeadRows x, HeadRows y, int n_rows, int n_heads,
+                                                   const int32_t* __restrict__ positions,
+                                                   RopeTab rope) {
+  constexpr int LPU = HD / 8, UPB = 256 / LPU;
+  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
+  const int c = threadIdx.x % LPU;
+  if (u >= (int64_t)n_rows * n_heads) return;
+  const int row = (int)(u / n_heads), h = (int)(u - (int64_t)row * n_heads);
+  const int pos = positions[row];
+  if (pos < 0) return;  // padding: left as it is
+  const Runs r = runs(rope, c);
+  float v[8];
+  const int64_t in = row * x.row_stride + h * x.head_stride;
+  load4(x, in + r.a, v);
+  load4(x, in + r.b, v + 4);
+  turn_row(rope, r, c, pos, v);
+  const int64_t out = row * y.row_stride + h * y.head_stride;
+  put4(y, out + r.a, v);
+  put4(y, out + r.b, v + 4);
+}
+
+__global__ __launch_bounds__(256) void k_rope_table(RopeFreqs f, int half, int64_t n,
+                                                    float* __restrict__ cos_t,
+                                                    float* __restrict__ sin_t) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  // angles of far positions need more than fp32: at position 100000 its step is 2^-7
+  const double a = (double)(i / half) * f.f[i % half];
+  cos_t[i] = (float)(f.factor * cos(a));
+  sin_t[i] = (float)(f.factor * sin(a));
+}
+
+// ------------------------------------------------------------------- the cache
+// The largest of a unit's values as bits: for magnitudes the order of the bits is the
+// order of the values, and infinities and NaN come out above every finite one.
+template <int LPU>
+__device__ __forceinline__ unsigned unit_max(unsigned v) {
+#pragma unroll
+  for (int m = LPU / 2; m >= 1; m >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, m));
+  return v;
+}
+
+// 128 + the integer nearest to 127 x / top, ties to even, exactly: the fp32 quotient t is
+// within 2^-15 of it, so only a t next to a border is decided again, by comparing
+// 254 |x| with (2 m + 1) top, both of which 53 bits hold.
+__device__ __forceinline__ unsigned code_of(float x, float top, float inv) {
+  const float u = fabsf(x) * inv;
+  const float m = floorf(u);
+  float k = rintf(u);
+  if (fabsf((u - m) - 0.5f) < 1e-4f) {
+    const double l = 254.0 * (double)fabsf(x), r = (2.0 * (double)m + 1.0) * (double)top;
+    k = l > r ? m + 1.f : l < r ? m : m + (float)((int)m & 1);
+  }
+  return 128u + (unsigned)(int)copysignf(k, x);
+}
+
+// The eight codes of a lane (two words) and the unit's scale.
+template <int LPU>
+__device__ __forceinline__ float quantise(const float (&x)[8], unsigned (&w)[2]) {
+  unsigned b = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b = max(b, __float_as_uint(x[i]) & 0x7fffffffu);
+  b = unit_max<LPU>(b);
+  w[0] = w[1] = 0x80808080u;
+  // a row holding an infinity or a NaN is kept as NaN, so that what reads it shows it
+  if (b >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
+  const float top = fmaxf(__uint_as_float(b), kKv8Least), inv = __fdiv_rn(127.f, top);
+  unsigned q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = code_of(x[i], top, inv);
+  w[0] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+  w[1] = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+  return __fdiv_rn(top, 127.f);
+}
+
+// Sequence and position of row t: found by counting the sequences that start at or
+// before it, the unit's lanes side by side.
+struct RowAt {
+  bool there;
+  char* base;
+  const int32_t* table;
+  int pos;
+};
+template <int LPU>
+__device__ __forceinline__ RowAt row_at(const Kv8& c, const Kv8Rows& r, int t, int lane) {
+  int b = t;
+  if (r.kind == KV8_ARRAYS && r.row_start) {
+    int n = 0;
+    for (int j = lane; j <= r.n_seqs; j += LPU) n += r.row_start[j] <= t;
+#pragma unroll
+    for (int m = LPU / 2; m >= 1; m >>= 1) n += __shfl_xor(n, m);
+    b = n - 1;
+  } else if (r.kind == KV8_CHUNK) {
+    b = 0;
+  }
+  if (b < 0 || b >= r.n_seqs) return RowAt{false, nullptr, nullptr, 0};
+  const Kv8Seq s = kv8_seq(c, r, b);
+  const int pos = s.len - s.rows + (t - s.row0);
+  return RowAt{t < s.row0 + s.rows && pos >= 0, s.base, s.table, pos};
+}
+// The block of a position's page, or nullptr when no page holds it.
+template <int HD>
+__device__ __forceinline__ char* block_of(const Kv8& c, const RowAt& w, int which, int h) {
+  const int phys = kv8_page(w.table, w.pos >> c.page_shift, c.max_pages, c.n_pages);
+  return phys < 0 ? nullptr
+                  : w.base + kv8_block_at(phys, which, h, c.n_kv, 1 << c.page_shift, HD);
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab rope, int n_q,
+                                                    HeadRows q, HeadRows q_out, float q_scale,
+                                                    HeadRows k, HeadRows v) {
+  constexpr int LPU = HD / 8, UPB = 256 / LPU;
+  const int lane = threadIdx.x % LPU, per = n_q + 2 * c.n_kv;
+  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
+  if (u >= (int64_t)r.n_rows * per) return;  // whole units leave together
+  const int t = (int)(u / per), item = (int)(u - (int64_t)t * per);
+  const RowAt w = row_at<LPU>(c, r, t, lane);
+  if (!w.there) return;
+  const bool is_q = item < n_q, is_v = item >= n_q + c.n_kv;
+  const int h = is_q ? item : is_v ? item - n_q - c.n_kv : item - n_q;
+  const HeadRows& x = is_q ? q : is_v ? v : k;
+  RopeTab none = rope;
+  none.cos = nullptr;
+  const Runs run = runs(is_v ? none : rope, lane);
+  const int64_t in = t * x.row_stride + h * x.head_stride;
+  float e[8];
+  load4(x, in + run.a, e);
+  load4(x, in + run.b, e + 4);
+  turn_row(rope, run, lane, w.pos, e);
+  if (is_q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] *= q_scale;
+    const int64_t out = t * q_out.row_stride + h * q_out.head_stride;
+    put4(q_out, out + run.a, e);
+    put4(q_out, out + run.b, e + 4);
+    return;
+  }
+  const int page = 1 << c.page_shift, slot = w.pos & (page - 1);
+  char* blk = block_of<HD>(c, w, is_v, h);
+  unsigned code[2];
+  const float scale = quantise<LPU>(e, code);
+  if (!blk) return;
+  if (is_v) {
+    char* d = blk + kv8_value_at(slot, 8 * lane, HD);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[4 * i] = (char)(code[i >> 2] >> (8 * (i & 3)));
+  } else {
+    *reinterpret_cast<unsigned*>(blk + kv8_key_at(slot, run.a, HD)) = code[0];
+    *reinterpret_cast<unsigned*>(blk + kv8_key_at(slot, run.b, HD)) = code[1];
+  }
+  if (lane == 0) *reinterpret_cast<float*>(blk + kv8_scale_at(slot, page, HD)) = scale;
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv8_read(Kv8 c, Kv8Rows r, HeadRows k, HeadRows v) {
+  constexpr int LPU = HD / 8, UPB = 256 / LPU;
+  const int lane = threadIdx.x % LPU, per = 2 * c.n_kv;
+  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
+  if (u >= (int64_t)r.n_rows * per) return;
+  const int t = (int)(u / per), item = (int)(u - (int64_t)t * per);
+  const RowAt w = row_at<LPU>(c, r, t, lane);
+  const bool is_v = item >= c.n_kv;
+  const int h = is_v ? item - c.n_kv : item;
+  const HeadRows& y = is_v ? v : k;
+  if (!w.there || !y.p) return;
+  const int page = 1 << c.page_shift, slot = w.pos & (page - 1);
+  const char* blk = block_of<HD>(c, w, is_v, h);
+  float e[8] = {};  // a position without a page reads as zero
+  if (blk) {
+    const float scale = *reinterpret_cast<const float*>(blk + kv8_scale_at(slot, page, HD));
+    unsigned code[8];
+    if (is_v) {
+      const uint4* s =
+          reinterpret_cast<const uint4*>(blk + kv8_value_at(slot & ~3, 8 * lane, HD));
+      const uint4 a = s[0], b = s[1];
+      const unsigned words[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) code[i] = words[i] >> (8 * (slot & 3)) & 0xffu;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(blk + kv8_key_at(slot, 8 * lane, HD));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) code[i] = (i < 4 ? a.x : a.y) >> (8 * (i & 3)) & 0xffu;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = (float)((int)code[i] - 128) * scale;
+  }
+  const int64_t out = t * y.row_stride + h * y.head_stride + 8 * lane;
+  put4(y, out, e);
+  put4(y, out + 4, e + 4);
+}
+
+// ------------------------------------------------------------------- launchers
+// Workgroups of `units` head rows, or 0 when there are none or more than a grid holds.
+static unsigned unit_blocks(int hd, int64_t units) {
+  const int64_t per = 256 / (hd / 8), n = (units + per - 1) / per;
+  return n < 1 || n > 0x7fffffff ? 0 : (unsigned)n;
+}
+
+hipError_t launch_rope_rows(int hd, const HeadRows& x, const HeadRows& y, int n_rows, int n_heads,
+                            const int32_t* positions, const RopeTab& rope, hipStream_t st) {
+  const unsigned grid = unit_blocks(hd, (int64_t)n_rows * n_heads);
+  if (!grid) return hipErrorInvalidValue;
+  if (hd == 128)
+    launch_k(k_rope_rows<128>, dim3(grid), dim3(256), 0, st, kOnly, x, y, n_rows, n_heads,
+             positions, rope);
+  else if (hd == 64)
+    launch_k(k_rope_rows<64>, dim3(grid), dim3(256), 0, st, kOnly, x, y, n_rows, n_heads,
+             positions, rope);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_table(const RopeFreqs& f, int half, int64_t n_pos, float* cos, float* sin,
+                             hipStream_t st) {
+  const int64_t n = n_pos * half, grid = (n + 255) / 256;
+  if (half < 1 || half > 64 || grid < 1 || grid > 0x7fffffff) return hipErrorInvalidValue;
+  launch_k(k_rope_table, dim3((unsigned)grid), dim3(256), 0, st, kOnly, f, half, n, cos, sin);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_append(int hd, const Kv8& c, const Kv8Rows& r, const RopeTab& rope, int n_q,
+                             const HeadRows& q, const HeadRows& q_out, float q_scale,
+                             const HeadRows& k, const HeadRows& v, hipStream_t st) {
+  if (!q.p) n_q = 0;
+  const unsigned grid = unit_blocks(hd, (int64_t)r.n_rows * (n_q + 2 * c.n_kv));
+  if (!grid) return hipErrorInvalidValue;
+  if (hd == 128)
+    launch_k(k_kv8_append<128>, dim3(grid), dim3(256), 0, st, kOnly, c, r, rope, n_q, q, q_out,
+             q_scale, k, v);
+  else if (hd == 64)
+    launch_k(k_kv8_append<64>, dim3(grid), dim3(256), 0, st, kOnly, c, r, rope, n_q, q, q_out,
+             q_scale, k, v);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_read(int hd, const Kv8& c, const Kv8Rows& r, const HeadRows& k,
+                           const HeadRows& v, hipStream_t st) {
+  const unsigned grid = unit_blocks(hd, (int64_t)r.n_rows * 2 * c.n_kv);
+  if (!grid) return hipErrorInvalidValue;
+  if (hd == 128)
+    launch_k(k_kv8_read<128>, dim3(grid), dim3(256), 0, st, kOnly, c, r, k, v);
+  else if (hd == 64)
+    launch_k(k_kv8_read<64>, dim3(grid), dim3(256), 0, st, kOnly, c, r, k, v);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace wici

@@ -1,0 +1,447 @@
+// Causal grouped-query attention over the 8-bit key-value cache.
+//
+// Mathematics.  For a row with query q over positions j with key codes a_j (scale s_j)
+// and value codes c_j (scale t_j):
+//   y_j = s_j (q . a_j) scale log2(e),   out = sum_j 2^y_j t_j c_j / sum_j 2^y_j.
+// The codes are small integers, exact in fp16, so both products run on the fp16 matrix
+// cores with the scales outside them: the keys' on the scores, the values' on the
+// weights w_j = 2^(y_j - ref) t_j.  `ref` runs with the largest y_j + log2 t_j (an online
+// softmax on the weights themselves), so the weights stay inside fp16's range whatever
+// the values' scales are, and one factor 2^-ref cancels in the quotient.  It moves only
+// when a weight would pass 2^15 (it is set 2^6 below the largest), so most steps rescale
+// nothing.  (Where scores pass 2^24 a reference cannot hold log2 t_j beside them: such a
+// row goes on with the largest score and a power of two of its own, `lift`.)  Scores, weights, sums and the output are fp32; q and w enter the products as
+// NT fp16 terms: one for bf16 rows (q is exact in it, a weight within 2^-11, an eighth of
+// the output's own rounding), two where queries or output are fp32 (2^-22).
+//
+// Layout.  S^T = A Q^T and O^T = C^T W^T on v_mfma_f32_16x16x32_f16: lane l holds query
+// row l % 16 in both results, so maximum, sum and rescaling of a row are that lane's own
+// (lanes l, l + 16, .. join their sums at the end).  A tile of S^T leaves lane l with
+// positions 4 (l / 16) .. + 3, which are the positions the second product takes from that
+// lane: the weights go from one product to the next in place, and the value cache keeps
+// four positions of a dimension in one word because that word is the other operand.
+// Codes go from memory to registers to the matrix cores with no exchange between lanes.
+#include "kv8.h"
+
+#include <algorithm>
+
+#include "launch.h"
+
+namespace wici {
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNoRef = -3e38f;    // ref before the first weight
+constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
+constexpr float kMaxWeight = 32768.f;
+constexpr float kHugeScore = 16777216.f;
+constexpr int kStep = 32;           // positions a wavefront takes at a time: two tiles of 16
+
+// Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
+// Both steps are exact.
+__device__ __forceinline__ void codes4(unsigned w, unsigned& lo, unsigned& hi) {
+  const unsigned p = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u);
+  const unsigned q = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
+  const half2_t off = {(_Float16)1152.f, (_Float16)1152.f};
+  lo = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2_t, p) - off);
+  hi = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2_t, q) - off);
+}
+__device__ __forceinline__ half8_t codes8(unsigned a, unsigned b) {
+  uint4 v;
+  codes4(a, v.x, v.y);
+  codes4(b, v.z, v.w);
+  return __builtin_bit_cast(half8_t, v);
+}
+
+// The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
+template <int HD>
+struct RowState {
+  float ref, sum;           // sum over this lane's positions
+  float lift;               // o holds 2^-lift of its sum (0 until a score passes kHugeScore)
+  floatx4_t o[HD / 16];     // tile 4 h + t, element i: dimension 64 h + 16 (l / 16) + 4 i + t
+};
+
+// The codes and scales of 32 positions, as one lane holds them.
+template <int HD>
+struct Step {
+  uint4 k[2][HD / 64];      // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
+  uint4 v[2][HD / 64];      // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
+  float4 ks[2], vs[2];      // scales of positions 4 (l / 16) .. + 3
+  bool there[2];            // the tile's page exists
+};
+
+template <int HD>
+__device__ __forceinline__ void load_step(Step<HD>& s, const Kv8& c, const Kv8Seq& q, int h, int j0,
+                                          int lane) {
+  const int r16 = lane & 15, g = lane >> 4, page = 1 << c.page_shift;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int j = j0 + 16 * t, slot = j & (page - 1);
+    const int phys = kv8_page(q.table, j >> c.page_shift, c.max_pages, c.n_pages);
+    s.there[t] = phys >= 0;
+    const char* kb = q.base + kv8_block_at(max(phys, 0), 0, h, c.n_kv, page, HD);
+    const char* vb = kb + c.n_kv * kv8_block_bytes(page, HD);
+    const char* kp = kb + kv8_key_at(slot + r16, g * (HD / 4), HD);
+    const char* vp = vb + kv8_value_at(slot + 4 * g, 4 * r16, HD);
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) {
+      s.k[t][i] = reinterpret_cast<const uint4*>(kp)[i];
+      s.v[t][i] = *reinterpret_cast<const uint4*>(vp + 256 * i);
+    }
+    s.ks[t] = *reinterpret_cast<const float4*>(kb + kv8_scale_at(slot + 4 * g, page, HD));
+    s.vs[t] = *reinterpret_cast<const float4*>(vb + kv8_scale_at(slot + 4 * g, page, HD));
+  }
+}
+
+// One step: positions j0 .. j0 + 31 for the 16 query rows qf (NT terms, scaled so that a
+// score is dot * key scale * q_unit); row l % 16 sees positions below `limit`.  MASKED:
+// some row does not see all of them (or a page is missing).
+template <int HD, int NT, bool MASKED>
+__device__ __forceinline__ void attend_step(RowState<HD>& st, bool& huge, const Step<HD>& s,
+                                            const half8_t (&qf)[NT][HD / 32], float q_unit, int j0,
+                                            int limit, int lane) {
+  const int g = lane >> 4;
+  floatx4_t sc[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const unsigned* w = reinterpret_cast<const unsigned*>(&s.k[t][0]);
+    sc[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+      const half8_t a = codes8(w[2 * d], w[2 * d + 1]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, qf[n][d], sc[t], 0, 0, 0);
+    }
+  }
+  float y[8], vs[8], e[8], w[8];
+  bool on[8];
+  float most = 0.f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = 4 * t + i;
+      on[x] = !MASKED || (s.there[t] && j0 + 16 * t + 4 * g + i < limit);
+      const float unit = (&s.ks[t].x)[i] * q_unit;
+      y[x] = on[x] ? sc[t][i] * unit : -INFINITY;
+      vs[x] = (&s.vs[t].x)[i];
+      e[x] = __builtin_amdgcn_exp2f(on[x] ? __builtin_fmaf(sc[t][i], unit, -st.ref) : -INFINITY);
+      w[x] = on[x] ? e[x] * vs[x] : 0.f;
+      most = fmaxf(most, w[x]);
+    }
+  // weights from the rounded scores, which huge scores of a tie share
+  auto weigh = [&]() {
+    const float down = __builtin_amdgcn_exp2f(-st.lift);
+    most = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      e[x] = __builtin_amdgcn_exp2f(y[x] - st.ref);
+      w[x] = on[x] ? e[x] * vs[x] * down : 0.f;
+      most = fmaxf(most, w[x]);
+    }
+  };
+  if (huge) weigh();
+  if (__any(most > kMaxWeight)) {  // move the reference, rare after a row's first step
+    // the largest of f over this row's positions
+    auto largest = [&](auto f) {
+      float z = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (on[x]) z = fmaxf(z, f(x));
+      z = fmaxf(z, __shfl_xor(z, 16));
+      return fmaxf(z, __shfl_xor(z, 32));
+    };
+    const float z = largest([&](int x) { return y[x] + __builtin_amdgcn_logf(vs[x]); });
+    huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
+    float ref = fmaxf(st.ref, z - kTopWeight), lift = 0.f;
+    if (huge) {
+      ref = fmaxf(st.ref, largest([&](int x) { return y[x]; }));
+      lift = fmaxf(st.lift + (st.ref - ref),
+                   largest([&](int x) { return y[x] - ref + __builtin_amdgcn_logf(vs[x]); }) -
+                       kTopWeight);
+      lift = lift > -1e30f ? lift : 0.f;  // a row that sees nothing yet
+    }
+    const float corr = __builtin_amdgcn_exp2f(st.ref - ref);
+    const float corr_o = __builtin_amdgcn_exp2f(st.ref - ref + (st.lift - lift));
+    st.ref = ref;
+    st.lift = lift;
+    st.sum *= corr;
+#pragma unroll
+    for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.o[u][i] *= corr_o;
+    weigh();
+  }
+  half8_t wf[NT];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    st.sum += e[x];
+    float rest = w[x];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      wf[n][x] = (_Float16)rest;
+      rest -= (float)wf[n][x];
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < HD / 64; ++h) {
+    const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[0][h]);
+    const unsigned* v1 = reinterpret_cast<const unsigned*>(&s.v[1][h]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const half8_t a = codes8(v0[t], v1[t]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        st.o[4 * h + t] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(a, wf[n], st.o[4 * h + t], 0, 0, 0);
+    }
+  }
+}
+
+// Eight elements of a row from element offset `at` (a multiple of 8).
+__device__ __forceinline__ void load_row8(const HeadRows& x, int64_t at, float* o) {
+  if (x.bf16) load8(static_cast<const bf16_t*>(x.p) + at, o);
+  else load8(static_cast<const float*>(x.p) + at, o);
+}
+
+// 16 query rows (row l % 16 of the tile, zero where `on` is false) as NT fp16 terms,
+// scaled by a power of two that brings the largest finite magnitude of the 16 into
+// [2^6, 2^7); `unit` undoes it.  Infinities and NaN stay in their own rows.
+template <int HD, int NT>
+__device__ __forceinline__ void load_queries(const HeadRows& q, int64_t at, bool on, int lane,
+                                             half8_t (&qf)[NT][HD / 32], float& unit) {
+  const int g = lane >> 4;
+  float v[HD / 32][8], most = 0.f;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) {
+    load_row8(q, at + g * (HD / 4) + 8 * d, v[d]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[d][i] = on ? v[d][i] : 0.f;
+      const float a = fabsf(v[d][i]);
+      most = a < INFINITY ? fmaxf(most, a) : most;
+    }
+  }
+  most = wave_max(most);
+  const int ex = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 100);
+  const float up = __uint_as_float((unsigned)(127 + 6 - ex) << 23);
+  unit = __uint_as_float((unsigned)(127 - 6 + ex) << 23);
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float rest = v[d][i] * up;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        qf[n][d][i] = (_Float16)rest;
+        rest -= (float)qf[n][d][i];
+      }
+    }
+}
+
+// A lane's 16 consecutive output values of one half-row.
+__device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int d, const float* v) {
+  if (!a.out.p) {
+    const size_t at = ((size_t)row * a.n_q + head) * a.hd + d;
+    store_act4(a.act, at, make_float4(v[0], v[1], v[2], v[3]));
+    return;
+  }
+  const int64_t at = row * a.out.row_stride + head * a.out.head_stride + d;
+  if (a.out.bf16) {
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out.p) + at) =
+        make_uint2((uint32_t)f32_to_bf16(v[0]) | ((uint32_t)f32_to_bf16(v[1]) << 16),
+                   (uint32_t)f32_to_bf16(v[2]) | ((uint32_t)f32_to_bf16(v[3]) << 16));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out.p) + at) =
+        make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// ------------------------------------------------------------------- split over positions
+// Workgroup (KV head, sequence, split): four wavefronts take the split's steps of 32
+// positions in turn for a tile of 16 of the sequence's rows x query heads of the group
+// (row r: new row r / G, query head r % G), and are joined at the end.  A split's range
+// follows from the sequence's own length, so one launch serves any length.  With one
+// split the output is written here, otherwise (ref, sum, output) to `part` for the merge.
+template <int HD, int NT>
+__global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+                                                        int ntile) {
+  __shared__ float s_o[4][16][HD + 4];
+  __shared__ float s_ref[4][16], s_sum[4][16];
+  const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
+  const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, g = lane >> 4, G = a.n_q / c.n_kv;
+  const Kv8Seq q = kv8_seq(c, r, b);
+  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+  float* part_ml = a.work;
+  float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
+
+  for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
+    const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
+    const bool on = row < q.rows;
+    const int rc = min(row, q.rows - 1);
+    // a row sees the positions up to its own; the tile's last row sees the most
+    const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
+    auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
+    const int limit = on ? seen(row) : 0, most = seen(last), least = seen(first);
+    const int steps = (most + kStep - 1) / kStep, per = (steps + nsplit - 1) / nsplit;
+    const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+
+    RowState<HD> st;
+    st.ref = kNoRef;
+    st.sum = st.lift = 0.f;
+    bool huge = false;
+#pragma unroll
+    for (int u = 0; u < HD / 16; ++u) st.o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    if (s0 < s1) {
+      half8_t qf[NT][HD / 32];
+      float unit;
+      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane,
+                           qf, unit);
+      unit *= a.scale * kLog2e;
+      for (int s = s0 + wave; s < s1; s += 4) {
+        Step<HD> x;
+        load_step<HD>(x, c, q, h, s * kStep, lane);
+        const bool whole = (s + 1) * kStep <= least && x.there[0] && x.there[1] &&
+                           16 * tile + 15 < q.rows * G;
+        if (whole) attend_step<HD, NT, false>(st, huge, x, qf, unit, s * kStep, limit, lane);
+        else attend_step<HD, NT, true>(st, huge, x, qf, unit, s * kStep, limit, lane);
+      }
+    }
+    if (huge) {
+      const float up = __builtin_amdgcn_exp2f(st.lift);
+#pragma unroll
+      for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[u][i] *= up;
+    }
+    // join the wavefronts
+    st.sum += __shfl_xor(st.sum, 16);
+    st.sum += __shfl_xor(st.sum, 32);
+    if (g == 0) {
+      s_ref[wave][r16] = st.ref;
+      s_sum[wave][r16] = st.sum;
+    }
+#pragma unroll
+    for (int hh = 0; hh < HD / 64; ++hh)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(&s_o[wave][r16][64 * hh + 16 * g + 4 * i]) =
+            make_float4(st.o[4 * hh][i], st.o[4 * hh + 1][i], st.o[4 * hh + 2][i],
+                        st.o[4 * hh + 3][i]);
+    __syncthreads();
+    for (int x = threadIdx.x; x < 16 * HD / 4; x += 256) {
+      const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
+      if (tr >= q.rows * G) continue;
+      float ref = s_ref[0][rr];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
+      float sum = 0.f, o[4] = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
+        sum += f * s_sum[w][rr];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += f * s_o[w][rr][d + i];
+      }
+      const int orow = q.row0 + tr / G, ohead = h * G + tr % G;
+      if (nsplit == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= inv;
+        put_out(a, orow, ohead, d, o);
+      } else {
+        const size_t at = ((size_t)orow * a.n_q + ohead) * nsplit + split;
+        *reinterpret_cast<float4*>(part_o + at * HD + d) = make_float4(o[0], o[1], o[2], o[3]);
+        if (d == 0) {
+          part_ml[2 * at] = ref;
+          part_ml[2 * at + 1] = sum;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// out = sum_s 2^(ref_s - ref) o_s / sum_s 2^(ref_s - ref) sum_s over the splits of one row
+// and head: HD / 4 lanes of four dimensions each, every split read once.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit) {
+  constexpr int L = HD / 4, UPB = 256 / L;
+  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / L;
+  const int d = 4 * (threadIdx.x % L);
+  if (u >= (int64_t)r.n_rows * a.n_q) return;
+  const int row = (int)(u / a.n_q), head = (int)(u - (int64_t)row * a.n_q);
+  if (r.kind == KV8_ARRAYS && r.row_start &&
+      (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
+    return;  // a row of no sequence
+  const float* ml = a.work + (size_t)u * nsplit * 2;
+  const float* po = a.work + ((size_t)r.n_rows * a.n_q * 2 + (size_t)u * HD) * nsplit + d;
+  float ref = kNoRef;
+  for (int s = 0; s < nsplit; ++s) ref = fmaxf(ref, ml[2 * s]);
+  float sum = 0.f, o[4] = {};
+  for (int s = 0; s < nsplit; ++s) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - ref);
+    sum += f * ml[2 * s + 1];
+    const float4 v = *reinterpret_cast<const float4*>(po + (size_t)s * HD);
+    o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] *= inv;
+  put_out(a, row, head, d, o);
+}
+
+// ------------------------------------------------------------------- launcher
+namespace {
+struct Plan {
+  int ntile, nsplit;
+};
+Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_length) {
+  const int G = n_q / n_kv;
+  Plan p;
+  p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
+  const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
+  const int64_t want = (1024 + blocks - 1) / blocks;
+  const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
+  return p;
+}
+}  // namespace
+
+size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
+                       int max_length) {
+  const Plan p = plan(n_q, n_kv, n_seqs, n_rows, max_rows, max_length);
+  return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
+}
+
+template <int HD>
+static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st) {
+  const Plan p = plan(a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
+  const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
+  if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)gx, r.n_seqs);
+  const int edge = p.nsplit == 1 ? kOnly : kFirst;
+  if (a.q.bf16 && a.out.p && a.out.bf16)
+    launch_k(k_kv8_attn_split<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
+  else
+    launch_k(k_kv8_attn_split<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
+  if (p.nsplit > 1) {
+    const int64_t per = 256 / (HD / 4), mg = ((int64_t)r.n_rows * a.n_q + per - 1) / per;
+    if (mg > 0x7fffffff) return hipErrorInvalidValue;
+    launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, kLast, c, r, a, p.nsplit);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st) {
+  if (a.hd == 128) return attn<128>(c, r, a, st);
+  if (a.hd == 64) return attn<64>(c, r, a, st);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace wici
