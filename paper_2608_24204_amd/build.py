@@ -32,11 +32,11 @@ FLAGS = [
 ]
 
 
-# Per-source flags.  attention.hip: matrix-core results in ordinary vector
-# registers (not the accumulation registers), so the flash-attention loop's
-# rescaled output rows are not copied between the two register files on every
-# key block.
-EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# Per-source flags.  The attention sources: matrix-core results in ordinary vector
+# registers (not the accumulation registers), so the output rows that the softmax
+# rescales are not copied between the two register files on every key block.
+_VGPR_RESULTS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+EXTRA = {"attention.hip": _VGPR_RESULTS, "kv8_attn.hip": _VGPR_RESULTS}
 
 
 def _run(cmd, verbose):

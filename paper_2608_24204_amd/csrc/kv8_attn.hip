@@ -63,47 +63,96 @@ struct RowState {
   floatx4_t o[HD / 16];     // tile 4 h + t, element i: dimension 64 h + 16 (l / 16) + 4 i + t
 };
 
-// The codes and scales of 32 positions, as one lane holds them.
+// Values that are the same in every lane, as scalars: what is read through memory is not
+// known to be, and a buffer or a branch that depends on it would run lane by lane.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <typename T>
+__device__ __forceinline__ T* uniform(T* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)v), hi = (uint32_t)uniform((int)(v >> 32));
+  return reinterpret_cast<T*>((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ Kv8Seq uniform(const Kv8Seq& s) {
+  return Kv8Seq{uniform(s.base), uniform(s.table), uniform(s.row0), uniform(s.rows), uniform(s.len)};
+}
+
+// A thread's index that the compiler does not know to be the same each time around a loop:
+// addresses made from it are not kept in registers through the loop.
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// The codes and scales of 32 positions (two tiles of 16), as one lane holds them.
 template <int HD>
-struct Step {
+struct Keys {
   uint4 k[2][HD / 64];      // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
+};
+template <int HD>
+struct Values {
   uint4 v[2][HD / 64];      // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
-  float4 ks[2], vs[2];      // scales of positions 4 (l / 16) .. + 3
-  bool there[2];            // the tile's page exists
+  float4 ks[2], vs[2];      // key and value scales of positions 4 (l / 16) .. + 3
 };
 
+// The pages of a step's two tiles (-1: none).
+struct Pages {
+  int phys[2];
+};
+__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int j0) {
+  Pages p;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    p.phys[t] = uniform(
+        kv8_page(q.table, (j0 + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
+  return p;
+}
+
+// Addresses are a scalar block base and offset plus a lane's own offset in 32 bits, the same
+// for every step.
+__device__ __forceinline__ uint4 fetch(__amdgpu_buffer_rsrc_t r, int lane_at, int at) {
+  const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 template <int HD>
-__device__ __forceinline__ void load_step(Step<HD>& s, const Kv8& c, const Kv8Seq& q, int h, int j0,
-                                          int lane) {
-  const int r16 = lane & 15, g = lane >> 4, page = 1 << c.page_shift;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rsrc(const Kv8& c, const Kv8Seq& q, int phys,
+                                                             int which, int h) {
+  const int page = 1 << c.page_shift;
+  return rsrc(q.base + kv8_block_at(max(phys, 0), which, h, c.n_kv, page, HD),
+              kv8_block_bytes(page, HD));
+}
+template <int HD>
+__device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const Kv8Seq& q,
+                                          const Pages& p, int h, int j0, int lane) {
+  const int page = 1 << c.page_shift, mine = kv8_key_at(lane & 15, (lane >> 4) * (HD / 4), HD);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int j = j0 + 16 * t, slot = j & (page - 1);
-    const int phys = kv8_page(q.table, j >> c.page_shift, c.max_pages, c.n_pages);
-    s.there[t] = phys >= 0;
-    const char* kb = q.base + kv8_block_at(max(phys, 0), 0, h, c.n_kv, page, HD);
-    const char* vb = kb + c.n_kv * kv8_block_bytes(page, HD);
-    const char* kp = kb + kv8_key_at(slot + r16, g * (HD / 4), HD);
-    const char* vp = vb + kv8_value_at(slot + 4 * g, 4 * r16, HD);
+    const int slot = (j0 + 16 * t) & (page - 1);
+    const __amdgpu_buffer_rsrc_t b = block_rsrc<HD>(c, q, p.phys[t], 0, h);
 #pragma unroll
-    for (int i = 0; i < HD / 64; ++i) {
-      s.k[t][i] = reinterpret_cast<const uint4*>(kp)[i];
-      s.v[t][i] = *reinterpret_cast<const uint4*>(vp + 256 * i);
-    }
-    s.ks[t] = *reinterpret_cast<const float4*>(kb + kv8_scale_at(slot + 4 * g, page, HD));
-    s.vs[t] = *reinterpret_cast<const float4*>(vb + kv8_scale_at(slot + 4 * g, page, HD));
+    for (int i = 0; i < HD / 64; ++i) s.k[t][i] = fetch(b, mine + 16 * i, kv8_key_at(slot, 0, HD));
+  }
+}
+template <int HD>
+__device__ __forceinline__ void load_values(Values<HD>& s, const Kv8& c, const Kv8Seq& q,
+                                            const Pages& p, int h, int j0, int lane) {
+  const int page = 1 << c.page_shift, g = lane >> 4, mine = kv8_value_at(4 * g, 4 * (lane & 15), HD);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int slot = (j0 + 16 * t) & (page - 1);
+    const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, p.phys[t], 0, h);
+    const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, p.phys[t], 1, h);
+    s.ks[t] = __builtin_bit_cast(float4, fetch(kb, 16 * g, kv8_scale_at(slot, page, HD)));
+    s.vs[t] = __builtin_bit_cast(float4, fetch(vb, 16 * g, kv8_scale_at(slot, page, HD)));
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i)
+      s.v[t][i] = fetch(vb, mine + 256 * i, kv8_value_at(slot, 0, HD));
   }
 }
 
-// One step: positions j0 .. j0 + 31 for the 16 query rows qf (NT terms, scaled so that a
-// score is dot * key scale * q_unit); row l % 16 sees positions below `limit`.  MASKED:
-// some row does not see all of them (or a page is missing).
-template <int HD, int NT, bool MASKED>
-__device__ __forceinline__ void attend_step(RowState<HD>& st, bool& huge, const Step<HD>& s,
-                                            const half8_t (&qf)[NT][HD / 32], float q_unit, int j0,
-                                            int limit, int lane) {
-  const int g = lane >> 4;
-  floatx4_t sc[2];
+// S^T of one step: sc[t][i] is the product of position 16 t + 4 (l / 16) + i with row l % 16.
+template <int HD, int NT>
+__device__ __forceinline__ void scores(floatx4_t (&sc)[2], const Keys<HD>& s,
+                                       const half8_t (&qf)[NT][HD / 32]) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const unsigned* w = reinterpret_cast<const unsigned*>(&s.k[t][0]);
@@ -116,76 +165,91 @@ __device__ __forceinline__ void attend_step(RowState<HD>& st, bool& huge, const 
         sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, qf[n][d], sc[t], 0, 0, 0);
     }
   }
-  float y[8], vs[8], e[8], w[8];
-  bool on[8];
-  float most = 0.f;
+}
+
+// The weights of one step from its products (a score is product * key scale * q_unit), as
+// NT fp16 terms.  MASKED: some row does not see every position: row l % 16 sees the step's
+// positions below `seen`, of the tiles that are there.  Returns whether a row's reference
+// moved: the output so far is then to be multiplied by `corr`.
+template <int HD, int NT, bool MASKED>
+__device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, bool& huge,
+                                        const floatx4_t (&sc)[2], const Values<HD>& s,
+                                        const Pages& p, float q_unit, int seen, int lane,
+                                        float& corr) {
+  const int left = seen - 4 * (lane >> 4);
+  auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
+  auto score = [&](int t, int i) { return sc[t][i] * ((&s.ks[t].x)[i] * q_unit); };
+  float sum, most;
+  // f(t, i) is a score less the reference
+  auto weigh = [&](float down, auto f) {
+    sum = most = 0.f;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int x = 4 * t + i;
-      on[x] = !MASKED || (s.there[t] && j0 + 16 * t + 4 * g + i < limit);
-      const float unit = (&s.ks[t].x)[i] * q_unit;
-      y[x] = on[x] ? sc[t][i] * unit : -INFINITY;
-      vs[x] = (&s.vs[t].x)[i];
-      e[x] = __builtin_amdgcn_exp2f(on[x] ? __builtin_fmaf(sc[t][i], unit, -st.ref) : -INFINITY);
-      w[x] = on[x] ? e[x] * vs[x] : 0.f;
-      most = fmaxf(most, w[x]);
-    }
-  // weights from the rounded scores, which huge scores of a tie share
-  auto weigh = [&]() {
-    const float down = __builtin_amdgcn_exp2f(-st.lift);
-    most = 0.f;
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(on(t, i) ? f(t, i) : -INFINITY);
+        float w = on(t, i) ? e * (&s.vs[t].x)[i] * down : 0.f;
+        // a product rounded once: joined with the conversion below, and not with the
+        // difference, the first term is now and then not the one the second completes
+        if (NT > 1) asm volatile("" : "+v"(w));
+        sum += e;
+        most = fmaxf(most, w);
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      e[x] = __builtin_amdgcn_exp2f(y[x] - st.ref);
-      w[x] = on[x] ? e[x] * vs[x] * down : 0.f;
-      most = fmaxf(most, w[x]);
-    }
+        for (int n = 0; n < NT; ++n) {
+          wf[n][4 * t + i] = (_Float16)w;
+          w -= (float)wf[n][4 * t + i];
+        }
+      }
   };
-  if (huge) weigh();
-  if (__any(most > kMaxWeight)) {  // move the reference, rare after a row's first step
+  auto plain = [&]() {
+    weigh(1.f, [&](int t, int i) {
+      return __builtin_fmaf(sc[t][i], (&s.ks[t].x)[i] * q_unit, -st.ref);
+    });
+  };
+  // with the rounded scores, which the huge scores of a tie share
+  auto lifted = [&]() {
+    weigh(__builtin_amdgcn_exp2f(-st.lift), [&](int t, int i) { return score(t, i) - st.ref; });
+  };
+  if (huge) lifted();
+  else plain();
+  const bool move = __any(most > kMaxWeight);
+  if (move) {  // rare after a row's first step
     // the largest of f over this row's positions
     auto largest = [&](auto f) {
       float z = -INFINITY;
 #pragma unroll
-      for (int x = 0; x < 8; ++x)
-        if (on[x]) z = fmaxf(z, f(x));
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (on(t, i)) z = fmaxf(z, f(t, i));
       z = fmaxf(z, __shfl_xor(z, 16));
       return fmaxf(z, __shfl_xor(z, 32));
     };
-    const float z = largest([&](int x) { return y[x] + __builtin_amdgcn_logf(vs[x]); });
+    auto lv = [&](int t, int i) { return __builtin_amdgcn_logf((&s.vs[t].x)[i]); };
+    const float z = largest([&](int t, int i) { return score(t, i) + lv(t, i); });
     huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
     float ref = fmaxf(st.ref, z - kTopWeight), lift = 0.f;
     if (huge) {
-      ref = fmaxf(st.ref, largest([&](int x) { return y[x]; }));
+      ref = fmaxf(st.ref, largest([&](int t, int i) { return score(t, i); }));
       lift = fmaxf(st.lift + (st.ref - ref),
-                   largest([&](int x) { return y[x] - ref + __builtin_amdgcn_logf(vs[x]); }) -
-                       kTopWeight);
+                   largest([&](int t, int i) { return score(t, i) - ref + lv(t, i); }) - kTopWeight);
       lift = lift > -1e30f ? lift : 0.f;  // a row that sees nothing yet
     }
-    const float corr = __builtin_amdgcn_exp2f(st.ref - ref);
-    const float corr_o = __builtin_amdgcn_exp2f(st.ref - ref + (st.lift - lift));
+    st.sum *= __builtin_amdgcn_exp2f(st.ref - ref);
+    corr = __builtin_amdgcn_exp2f(st.ref - ref + (st.lift - lift));
     st.ref = ref;
     st.lift = lift;
-    st.sum *= corr;
-#pragma unroll
-    for (int u = 0; u < HD / 16; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st.o[u][i] *= corr_o;
-    weigh();
+    if (huge) lifted();
+    else plain();
   }
-  half8_t wf[NT];
-#pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    st.sum += e[x];
-    float rest = w[x];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      wf[n][x] = (_Float16)rest;
-      rest -= (float)wf[n][x];
-    }
-  }
+  st.sum += sum;
+  return move;
+}
+
+// O^T += C^T W^T of one step.
+template <int HD, int NT>
+__device__ __forceinline__ void add_values(RowState<HD>& st, const Values<HD>& s,
+                                           const half8_t (&wf)[NT]) {
 #pragma unroll
   for (int h = 0; h < HD / 64; ++h) {
     const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[0][h]);
@@ -267,15 +331,16 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
 // follows from the sequence's own length, so one launch serves any length.  With one
 // split the output is written here, otherwise (ref, sum, output) to `part` for the merge.
 template <int HD, int NT>
-__global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                         int ntile) {
   __shared__ float s_o[4][16][HD + 4];
   __shared__ float s_ref[4][16], s_sum[4][16];
   const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
   const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r16 = lane & 15, g = lane >> 4, G = a.n_q / c.n_kv;
-  const Kv8Seq q = kv8_seq(c, r, b);
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, G = a.n_q / c.n_kv;
+  const Kv8Seq q = uniform(kv8_seq(c, r, b));
   const int64_t cap = (int64_t)c.max_pages << c.page_shift;
   float* part_ml = a.work;
   float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
@@ -290,6 +355,8 @@ __global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Att
     const int limit = on ? seen(row) : 0, most = seen(last), least = seen(first);
     const int steps = (most + kStep - 1) / kStep, per = (steps + nsplit - 1) / nsplit;
     const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+    // steps that all 16 rows see whole
+    const int whole = 16 * tile + 15 < q.rows * G ? least / kStep : 0;
 
     RowState<HD> st;
     st.ref = kNoRef;
@@ -303,13 +370,40 @@ __global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Att
       load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane,
                            qf, unit);
       unit *= a.scale * kLog2e;
-      for (int s = s0 + wave; s < s1; s += 4) {
-        Step<HD> x;
-        load_step<HD>(x, c, q, h, s * kStep, lane);
-        const bool whole = (s + 1) * kStep <= least && x.there[0] && x.there[1] &&
-                           16 * tile + 15 < q.rows * G;
-        if (whole) attend_step<HD, NT, false>(st, huge, x, qf, unit, s * kStep, limit, lane);
-        else attend_step<HD, NT, true>(st, huge, x, qf, unit, s * kStep, limit, lane);
+      // the next step's keys are requested once this one's are multiplied, its values
+      // likewise, and its pages (which those addresses wait for) a step earlier
+      int s = s0 + wave;
+      if (s < s1) {
+        Keys<HD> k;
+        Values<HD> v;
+        Pages now = find_pages(c, q, s * kStep), next = find_pages(c, q, (s + 4) * kStep);
+        load_keys<HD>(k, c, q, now, h, s * kStep, lane);
+        load_values<HD>(v, c, q, now, h, s * kStep, lane);
+        for (;;) {
+          floatx4_t sc[2];
+          scores<HD, NT>(sc, k, qf);
+          const int then = s + 4;
+          if (then < s1) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
+          half8_t wf[NT];
+          float corr = 1.f;
+          const bool move =
+              s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
+                  ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
+                  : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane,
+                                          corr);
+          if (move) {
+#pragma unroll
+            for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
+          }
+          add_values<HD, NT>(st, v, wf);
+          if (then >= s1) break;
+          load_values<HD>(v, c, q, next, h, then * kStep, lane);
+          now = next;
+          next = find_pages(c, q, (then + 4) * kStep);
+          s = then;
+        }
       }
     }
     if (huge) {
@@ -322,19 +416,20 @@ __global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Att
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);
     st.sum += __shfl_xor(st.sum, 32);
-    if (g == 0) {
-      s_ref[wave][r16] = st.ref;
-      s_sum[wave][r16] = st.sum;
+    const int me = fresh(lane), mr = me & 15, mg = me >> 4;
+    if (mg == 0) {
+      s_ref[wave][mr] = st.ref;
+      s_sum[wave][mr] = st.sum;
     }
 #pragma unroll
     for (int hh = 0; hh < HD / 64; ++hh)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(&s_o[wave][r16][64 * hh + 16 * g + 4 * i]) =
+        *reinterpret_cast<float4*>(&s_o[wave][mr][64 * hh + 16 * mg + 4 * i]) =
             make_float4(st.o[4 * hh][i], st.o[4 * hh + 1][i], st.o[4 * hh + 2][i],
                         st.o[4 * hh + 3][i]);
     __syncthreads();
-    for (int x = threadIdx.x; x < 16 * HD / 4; x += 256) {
+    for (int x = fresh(threadIdx.x); x < 16 * HD / 4; x += 256) {
       const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
       if (tr >= q.rows * G) continue;
       float ref = s_ref[0][rr];
@@ -344,9 +439,9 @@ __global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Att
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
+        const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
         sum += f * s_sum[w][rr];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += f * s_o[w][rr][d + i];
+        o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
       }
       const int orow = q.row0 + tr / G, ohead = h * G + tr % G;
       if (nsplit == 1) {
@@ -368,26 +463,46 @@ __global__ __launch_bounds__(256) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Att
 }
 
 // out = sum_s 2^(ref_s - ref) o_s / sum_s 2^(ref_s - ref) sum_s over the splits of one row
-// and head: HD / 4 lanes of four dimensions each, every split read once.
+// and head.  HD / 4 lanes of four dimensions take every P-th split each, P groups of them a
+// row and head, and are joined: by a group's lanes alone a head's 128 splits took 43 us one
+// after another.
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit) {
-  constexpr int L = HD / 4, UPB = 256 / L;
-  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / L;
-  const int d = 4 * (threadIdx.x % L);
-  if (u >= (int64_t)r.n_rows * a.n_q) return;
+  constexpr int L = HD / 4, P = 256 / L;
+  __shared__ float4 s_o[P][L];
+  __shared__ float2 s_ml[P];
+  const int64_t u = blockIdx.x;
+  const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane;
   const int row = (int)(u / a.n_q), head = (int)(u - (int64_t)row * a.n_q);
   if (r.kind == KV8_ARRAYS && r.row_start &&
       (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
     return;  // a row of no sequence
-  const float* ml = a.work + (size_t)u * nsplit * 2;
+  const float2* ml = reinterpret_cast<const float2*>(a.work) + (size_t)u * nsplit;
   const float* po = a.work + ((size_t)r.n_rows * a.n_q * 2 + (size_t)u * HD) * nsplit + d;
-  float ref = kNoRef;
-  for (int s = 0; s < nsplit; ++s) ref = fmaxf(ref, ml[2 * s]);
-  float sum = 0.f, o[4] = {};
-  for (int s = 0; s < nsplit; ++s) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * s] - ref);
-    sum += f * ml[2 * s + 1];
+  float ref = kNoRef, sum = 0.f, o[4] = {};
+#pragma unroll 4
+  for (int s = p; s < nsplit; s += P) {
+    const float2 m = ml[s];
     const float4 v = *reinterpret_cast<const float4*>(po + (size_t)s * HD);
+    const float now = fmaxf(ref, m.x);
+    const float f = __builtin_amdgcn_exp2f(ref - now), g = __builtin_amdgcn_exp2f(m.x - now);
+    ref = now;
+    sum = sum * f + m.y * g;
+    o[0] = o[0] * f + v.x * g; o[1] = o[1] * f + v.y * g;
+    o[2] = o[2] * f + v.z * g; o[3] = o[3] * f + v.w * g;
+  }
+  s_o[p][lane] = make_float4(o[0], o[1], o[2], o[3]);
+  if (lane == 0) s_ml[p] = make_float2(ref, sum);
+  __syncthreads();
+  if (p) return;
+#pragma unroll
+  for (int w = 0; w < P; ++w) ref = fmaxf(ref, s_ml[w].x);
+  sum = o[0] = o[1] = o[2] = o[3] = 0.f;
+#pragma unroll
+  for (int w = 0; w < P; ++w) {
+    const float f = __builtin_amdgcn_exp2f(s_ml[w].x - ref);
+    const float4 v = s_o[w][lane];
+    sum += f * s_ml[w].y;
     o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -406,7 +521,7 @@ Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_lengt
   Plan p;
   p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
   const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t want = (1024 + blocks - 1) / blocks;
+  const int64_t want = std::max<int64_t>(1, 768 / blocks);
   const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
@@ -431,7 +546,7 @@ static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStre
   else
     launch_k(k_kv8_attn_split<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
   if (p.nsplit > 1) {
-    const int64_t per = 256 / (HD / 4), mg = ((int64_t)r.n_rows * a.n_q + per - 1) / per;
+    const int64_t mg = (int64_t)r.n_rows * a.n_q;
     if (mg > 0x7fffffff) return hipErrorInvalidValue;
     launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, kLast, c, r, a, p.nsplit);
   }

@@ -183,8 +183,8 @@ class KvCache:
 
     ``length`` [n_seqs] (int32) counts each sequence's positions, the call's new rows
     included; without ``row_start`` [n_seqs + 1] (int32) a sequence has one new row, else rows
-    row_start[b] .. row_start[b + 1].  Rows of no sequence are not used, and left as they are
-    in outputs that are given."""
+    row_start[b] .. row_start[b + 1].  Rows of no sequence are not used, and not written in
+    outputs (a new output tensor holds nothing in particular there)."""
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, page: int, head_dim: int):
         device = _on_gpu(pool, "pool")
@@ -266,8 +266,8 @@ class KvCache:
                 length.shape[0]
         with _launch_on(stream, dev, length, row_start, k, v) as raw:
             shape = (n_rows, self.n_kv_heads, d)
-            k = torch.zeros(shape, dtype=dtype, device=dev) if k is None else k
-            v = torch.zeros(shape, dtype=dtype, device=dev) if v is None else v
+            k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
+            v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
             if k.shape[0] != n_rows or v.shape[0] != n_rows:
                 raise ValueError(f"k and v: {k.shape[0]} and {v.shape[0]} rows, expected {n_rows}")
             _check(self.lib.wici_kv8_read(
@@ -293,9 +293,7 @@ class KvCache:
         with _launch_on(stream, dev, q, length, row_start, out, workspace) as raw:
             b = self._batch(n, length, row_start, max_rows, max_length)
             if out is None:
-                # rows of no sequence are left as they are: zeros in a new tensor
-                new = torch.empty if row_start is None else torch.zeros
-                out = new((n, heads, d), dtype=q.dtype, device=dev)
+                out = torch.empty((n, heads, d), dtype=q.dtype, device=dev)
             elif out.shape[0] != n:
                 raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
             need = self._workspace(b, heads)

@@ -306,6 +306,29 @@ def test_prompts(ops, n_kv, G, hd, page, dtype):
         check_attend(bt, q, out, K, V, hd ** -0.5)
 
 
+def test_many_fp32_rows(ops):
+    """20000 rows and heads whose weights are spread over many positions: the two terms of each
+    weight belong together in every one of them (an error of one fp16 step in one weight of
+    some hundred shows)."""
+    n, H, G, hd = 320, 8, 8, 128
+    bt = Batch(ops, [n], [n], n_kv=H, hd=hd, page=64, seed=77)
+    K, V = bt.fill()
+    q = rnd(bt.rng, n, H * G, hd, dtype=F32)
+    out = bt.cache.attend(q, bt.length, row_start=bt.row_start).double()
+    k, v = (torch.from_numpy(x[0]).cuda().transpose(0, 1) for x in (K, V))        # [H, n, hd]
+    x = (q.double().view(n, H, G, hd).permute(1, 2, 0, 3) @ k[:, None].transpose(-1, -2)) * hd ** -0.5
+    x = x.masked_fill(torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1), float("-inf"))
+    p = x.softmax(-1)
+    want, mag = p @ v[:, None], p @ v[:, None].abs()
+    dots = (q.double().abs().view(n, H, G, hd).permute(1, 2, 0, 3) @ k[:, None].abs().transpose(-1, -2)
+            ).amax(-1, keepdim=True) * hd ** -0.5
+    e = (48 * 2.0 ** -24 + 2.0 ** -22) * dots + 2.0 ** -20
+    tol = mag * (2 * e + 2.0 ** -22 + (64 + n / 16) * 2.0 ** -24) + want.abs() * 2.0 ** -24
+    assert want.isfinite().all() and tol.isfinite().all() and out.isfinite().all()
+    err = (out.view(n, H, G, hd).permute(1, 2, 0, 3) - want).abs()
+    assert (err <= tol).all(), float((err / (tol + 1e-30)).max())
+
+
 @pytest.mark.parametrize("rows", [None, [3, 16, 700]])
 def test_long_contexts(ops, rows):
     lens = [5000, 16, 2111] if rows is None else [5000, 16, 2111]
