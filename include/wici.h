@@ -96,7 +96,8 @@ typedef struct {
   double rope_base;       /* > 1 */
   int32_t tied_embeddings;/* 1: the LM head is the embedding matrix */
   int32_t weight_dtype;   /* wici_dtype of every matrix (norm gains are always F32) */
-  int32_t kv_dtype;       /* wici_dtype of the KV cache storage */
+  int32_t kv_dtype;       /* wici_dtype of the KV cache storage: F32, BF16 or KV8 (8-bit
+                             codes, see wici_kv8: about half of BF16's bytes) */
   int32_t max_seq;        /* capacity in positions (prompt + generated); 1..16384 */
   int32_t prefill_chunk;  /* prompt rows processed per pass; 1..8192 */
   int32_t kv_page;        /* positions per KV page: 16, 32, 64 or 128 */
@@ -154,6 +155,44 @@ wici_status wici_memory_requirements(const wici_config* cfg, size_t* weight_byte
 wici_status wici_bind_memory(wici_model* m, void* d_weights, size_t weight_bytes,
                              void* d_kv, size_t kv_bytes, void* d_scratch,
                              size_t scratch_bytes);
+
+typedef enum {
+  WICI_ROPE_HALF = 0, /* pairs (j, j + dim / 2) */
+  WICI_ROPE_PAIRS = 1 /* pairs (2 j, 2 j + 1) */
+} wici_rope_layout;
+
+/* Angle steps f_j of pair j of a rotary embedding of `dim` dimensions, with
+ * b_j = base^(-2 j / dim), s = factor, n = original (the positions trained on): */
+typedef enum {
+  WICI_ROPE_PLAIN = 0,  /* f_j = b_j */
+  WICI_ROPE_LINEAR = 1, /* f_j = b_j / s */
+  WICI_ROPE_BASE = 2,   /* f_j = (base s^(dim / (dim - 2)))^(-2 j / dim) */
+  WICI_ROPE_BANDS = 3,  /* by the turns r_j = n b_j / 2 pi within the trained positions:
+                           k_j = clamp((r_j - low) / (high - low), 0, 1),
+                           f_j = (1 - k_j) b_j / s + k_j b_j */
+  WICI_ROPE_RAMP = 4    /* by dimension: j_lo = floor(D(high)), j_hi = ceil(D(low)), limited
+                           to [0, dim - 1], with D(t) = dim ln(n / 2 pi t) / (2 ln base);
+                           m_j = clamp((j - j_lo) / max(j_hi - j_lo, 0.001), 0, 1),
+                           f_j = m_j b_j / s + (1 - m_j) b_j, and cosines and sines are
+                           multiplied by 1 + 0.1 ln s */
+} wici_rope_scaling;
+
+typedef struct {
+  int32_t dim;     /* rotated dimensions of a head, a multiple of 8, 8..128 */
+  int32_t layout;  /* wici_rope_layout */
+  int32_t scaling; /* wici_rope_scaling; PLAIN ignores the fields below base */
+  double base;     /* > 1 */
+  double factor;   /* s >= 1 */
+  double original; /* n > 0 (BANDS, RAMP) */
+  double low, high;/* 0 < low < high (BANDS, RAMP; both 0: 1 and 4 for BANDS, 1 and 32 for
+                      RAMP) */
+} wici_rope;
+
+/* Rotate by `rope` instead of rope_base alone: part of each head, either layout, tables
+ * scaled for long contexts (wici_config's rope_base is then not used).  Allowed before the
+ * memory is bound.  The weights are given as the layout has them.  Errors: WICI_E_ARG (not a
+ * wici_rope, or dim above head_dim), WICI_E_STATE (memory already bound). */
+wici_status wici_set_rope(wici_model* m, const wici_rope* rope);
 
 /* Upload weight tensors (any subset, any order, any number of calls; a tensor
  * given again overwrites the earlier copy).  The library repacks them into its
@@ -214,7 +253,7 @@ wici_status wici_decode_n(wici_model* m, int32_t token_in, int32_t n, int32_t* t
  * stay alive and must not reload weights while m is used) and its own KV cache
  * and scratch (sizes from wici_memory_requirements of m's configuration).  The
  * configurations must agree on everything the weight region depends on (shapes,
- * weight dtype, rms_eps, rope_base, tied_embeddings, max_seq).  m becomes ready
+ * weight dtype, rms_eps, rope_base and wici_set_rope's, tied_embeddings, max_seq).  m becomes ready
  * at once; wici_load_weights on m is refused (WICI_E_STATE).  Allowed once, in
  * the created state; resets the KV state.  Errors: WICI_E_ARG (NULL or identical
  * models, a differing configuration, NULL/small/misaligned regions),
@@ -254,7 +293,8 @@ wici_status wici_position(const wici_model* m, int32_t* pos);
 
 /* Diagnostic: copy the cached keys and values of one layer for positions
  * [begin, end) into host arrays in logical layout [end-begin, n_kv_heads,
- * head_dim] of the KV storage type (bf16 as uint16 bit patterns).  Synchronous.
+ * head_dim] of the KV storage type (bf16 as uint16 bit patterns; KV8 as the fp32
+ * values that its codes stand for).  Synchronous.
  * Errors: WICI_E_ARG for a bad layer or range (end must not exceed the current
  * position), WICI_E_STATE before bind. */
 wici_status wici_read_kv(wici_model* m, int32_t layer, int32_t begin, int32_t end,
@@ -269,7 +309,8 @@ wici_status wici_read_kv(wici_model* m, int32_t layer, int32_t begin, int32_t en
  * (0 with bf16 weights, whose first QKV GEMV gathers the embedding row itself);
  * per layer: QKV GEMV (with RoPE and the KV append), attention (with a bf16
  * cache and up to 4 query heads of 128 or 8 of 64 per KV head, one launch that
- * also merges the splits; otherwise split pass start to merge end), O GEMV,
+ * also merges the splits; otherwise split pass start to merge end, from the append of the
+ * position on with a KV8 cache), O GEMV,
  * gate/up GEMV, down GEMV; then the LM
  * head GEMV and the final argmax.  Errors as wici_decode_step, plus WICI_E_ARG
  * for NULL outputs or a capacity below 3 + 5 * n_layers. */
@@ -385,38 +426,6 @@ typedef struct {
   int32_t dtype;
   int64_t row_stride, head_stride;
 } wici_head_rows;
-
-typedef enum {
-  WICI_ROPE_HALF = 0, /* pairs (j, j + dim / 2) */
-  WICI_ROPE_PAIRS = 1 /* pairs (2 j, 2 j + 1) */
-} wici_rope_layout;
-
-/* Angle steps f_j of pair j of a rotary embedding of `dim` dimensions, with
- * b_j = base^(-2 j / dim), s = factor, n = original (the positions trained on): */
-typedef enum {
-  WICI_ROPE_PLAIN = 0,  /* f_j = b_j */
-  WICI_ROPE_LINEAR = 1, /* f_j = b_j / s */
-  WICI_ROPE_BASE = 2,   /* f_j = (base s^(dim / (dim - 2)))^(-2 j / dim) */
-  WICI_ROPE_BANDS = 3,  /* by the turns r_j = n b_j / 2 pi within the trained positions:
-                           k_j = clamp((r_j - low) / (high - low), 0, 1),
-                           f_j = (1 - k_j) b_j / s + k_j b_j */
-  WICI_ROPE_RAMP = 4    /* by dimension: j_lo = floor(D(high)), j_hi = ceil(D(low)), limited
-                           to [0, dim - 1], with D(t) = dim ln(n / 2 pi t) / (2 ln base);
-                           m_j = clamp((j - j_lo) / max(j_hi - j_lo, 0.001), 0, 1),
-                           f_j = m_j b_j / s + (1 - m_j) b_j, and cosines and sines are
-                           multiplied by 1 + 0.1 ln s */
-} wici_rope_scaling;
-
-typedef struct {
-  int32_t dim;     /* rotated dimensions of a head, a multiple of 8, 8..128 */
-  int32_t layout;  /* wici_rope_layout */
-  int32_t scaling; /* wici_rope_scaling; PLAIN ignores the fields below base */
-  double base;     /* > 1 */
-  double factor;   /* s >= 1 */
-  double original; /* n > 0 (BANDS, RAMP) */
-  double low, high;/* 0 < low < high (BANDS, RAMP; both 0: 1 and 4 for BANDS, 1 and 32 for
-                      RAMP) */
-} wici_rope;
 
 /* Tables of a rotary embedding: cosines and sines [n_pos][dim / 2], 16-byte aligned.
  * Dimensions from dim on pass through unchanged. */

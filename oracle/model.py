@@ -23,7 +23,8 @@ writes the layer out, so this file takes the standard pre-norm decoder it runs:
   logits = W_lm RMSNorm(x_last; g_final)         W_lm = E when embeddings are tied
   token  = argmax(logits), lowest index on exact ties
 
-Readings where the definition leaves room: no biases, no QK-norm, no RoPE scaling;
+Readings where the definition leaves room: no biases, no QK-norm, no RoPE scaling unless
+the caller names an embedding (``rope``);
 the KV cache holds bf16 values when the workload stores it in bf16 (k after RoPE and
 v are rounded to the nearest bf16, ties to even, at the point they are cached), and
 exact values otherwise (``kv_round``).
@@ -41,6 +42,8 @@ import math
 from typing import Mapping
 
 import numpy as np
+
+from .kv8 import kv8_values, rope_pairs, rope_steps
 
 
 # ---------------------------------------------------------------------------
@@ -140,17 +143,20 @@ class DecoderOracle:
     (names: tok_embeddings, layers.{l}.{attn_norm,wq,wk,wv,wo,ffn_norm,w_gate,w_up,
     w_down}, norm, lm_head).  A mapping that decodes on access keeps memory bounded
     for very large models.
-    kv_round: 'bf16' stores cached k/v rounded to bf16, 'none' keeps them exact;
-    default follows cfg.kv_dtype.
+    kv_round: 'bf16' stores cached k/v rounded to bf16, 'kv8' as 8-bit multiples of a step
+    a row (kv8.py), 'none' keeps them exact; default follows cfg.kv_dtype.
+    rope: None, or the arguments of kv8.rope_steps and a "layout" ("half" or "pairs") as a
+    dict: the embedding used in place of rope_base's.
     """
 
     def __init__(self, cfg, weights: Mapping[str, np.ndarray], kv_round: str | None = None,
-                 max_seq: int | None = None):
+                 max_seq: int | None = None, rope: dict | None = None):
         self.cfg = cfg
         self.w = weights
         if kv_round is None:
-            kv_round = "bf16" if cfg.kv_dtype == "bf16" else "none"
-        assert kv_round in ("bf16", "none")
+            kv_round = cfg.kv_dtype if cfg.kv_dtype in ("bf16", "kv8") else "none"
+        assert kv_round in ("bf16", "kv8", "none")
+        self.rope = rope
         self.kv_round = kv_round
         self.max_seq = max_seq if max_seq is not None else getattr(cfg, "max_seq", 4096)
         self.reset()
@@ -162,7 +168,18 @@ class DecoderOracle:
         self.V = [np.zeros((self.max_seq, c.n_kv_heads, c.head_dim)) for _ in range(c.n_layers)]
 
     def _store(self, a: np.ndarray) -> np.ndarray:
+        if self.kv_round == "kv8":
+            return kv8_values(a)
         return bf16_round(a) if self.kv_round == "bf16" else a
+
+    def _turn(self, z: np.ndarray, positions: np.ndarray) -> np.ndarray:
+        if self.rope is None:
+            return rope_rotate(z, positions, self.cfg.rope_base)
+        spec = dict(self.rope)
+        layout = spec.pop("layout", "half")
+        steps, mult = rope_steps(**spec)
+        ang = np.asarray(positions, np.float64)[:, None] * steps
+        return rope_pairs(z, mult * np.cos(ang), mult * np.sin(ang), layout)
 
     def _lm_name(self) -> str:
         return "tok_embeddings" if self.cfg.tied_embeddings else "lm_head"
@@ -205,8 +222,8 @@ class DecoderOracle:
             q = self._proj(u, pre + "wq").reshape(T, c.n_heads, c.head_dim)
             k = self._proj(u, pre + "wk").reshape(T, c.n_kv_heads, c.head_dim)
             v = self._proj(u, pre + "wv").reshape(T, c.n_kv_heads, c.head_dim)
-            q = rope_rotate(q, positions, c.rope_base)
-            k = rope_rotate(k, positions, c.rope_base)
+            q = self._turn(q, positions)
+            k = self._turn(k, positions)
             self.K[l][p0:p0 + T] = self._store(k)
             self.V[l][p0:p0 + T] = self._store(v)
             n = p0 + T

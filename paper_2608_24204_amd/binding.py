@@ -32,7 +32,7 @@ EXPORTED = ["wici_create", "wici_memory_requirements", "wici_bind_memory", "wici
             "wici_read_kv", "wici_profile_decode_step", "wici_quantize_q8", "wici_md5",
             "wici_load_weights_cached", "wici_bind_memory_shared", "wici_decode_batch",
             "wici_stream_read", "wici_stream_read_noalloc", "wici_last_error", "wici_destroy",
-            "wici_rope_table", "wici_rope_rows", "wici_kv8_bytes", "wici_kv8_append",
+            "wici_set_rope", "wici_rope_table", "wici_rope_rows", "wici_kv8_bytes", "wici_kv8_append",
             "wici_kv8_read", "wici_kv8_attend_workspace", "wici_kv8_attend"]
 
 
@@ -128,6 +128,7 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
                              ctypes.c_int),
         "wici_stream_read_noalloc": ([P, sz, i32, P, ctypes.POINTER(ctypes.c_uint32)],
                                      ctypes.c_int),
+        "wici_set_rope": ([P, ctypes.POINTER(WiciRope)], ctypes.c_int),
         "wici_rope_table": ([ctypes.POINTER(WiciRope), ctypes.c_int64, P, P, P], ctypes.c_int),
         "wici_rope_rows": ([ctypes.POINTER(WiciRopeTab), i32, i32, i32, P, WiciHeadRows,
                             WiciHeadRows, P], ctypes.c_int),
@@ -168,7 +169,7 @@ def make_config(cfg: ModelConfig, prefill_mode: str | None = None, graph: bool =
     c.rms_eps, c.rope_base = cfg.rms_eps, cfg.rope_base
     c.tied_embeddings = int(cfg.tied_embeddings)
     c.weight_dtype = {"bf16": WICI_BF16, "f32": WICI_F32, "q8": WICI_Q8}[cfg.weight_dtype]
-    c.kv_dtype = WICI_BF16 if cfg.kv_dtype == "bf16" else WICI_F32
+    c.kv_dtype = {"bf16": WICI_BF16, "f32": WICI_F32, "kv8": WICI_KV8}[cfg.kv_dtype]
     c.max_seq = cfg.max_seq if max_seq is None else max_seq
     c.prefill_chunk = cfg.prefill_chunk if prefill_chunk is None else prefill_chunk
     c.kv_page = cfg.kv_page if kv_page is None else kv_page
@@ -288,8 +289,9 @@ class WiciModel:
                  max_seq: int | None = None, prefill_chunk: int | None = None,
                  kv_page: int | None = None, device: int = 0,
                  share_weights_of: "WiciModel | None" = None, prefill_planes=None,
-                 fault_drill: bool = False):
-        """share_weights_of: another (loaded) model whose weights this one uses
+                 fault_drill: bool = False, rope: "WiciRope | None" = None):
+        """rope: a rotary embedding other than rope_base's over the whole head
+        (wici_set_rope; see ops.rope_spec).  share_weights_of: another (loaded) model whose weights this one uses
         (wici_bind_memory_shared); only the KV cache and scratch are allocated.
         prefill_planes: see make_config.  fault_drill: WICI_FLAG_FAULT_DRILL
         (tests of the misplaced-split error path)."""
@@ -314,6 +316,8 @@ class WiciModel:
         self._check(self.lib.wici_create(ctypes.byref(self.c), ctypes.c_void_p(self.stream.cuda_stream),
                                          ctypes.byref(h)), "wici_create", handle=None)
         self.h = h
+        if rope is not None:
+            self._check(self.lib.wici_set_rope(self.h, ctypes.byref(rope)), "wici_set_rope")
         if share_weights_of is not None:
             self._check(self.lib.wici_bind_memory_shared(self.h, share_weights_of.h,
                                                          self._kv.data_ptr(), kb,
@@ -417,7 +421,7 @@ class WiciModel:
 
     def read_kv(self, layer: int, begin: int, end: int):
         c = self.cfg
-        dt = np.uint16 if c.kv_dtype == "bf16" else np.float32
+        dt = np.uint16 if c.kv_dtype == "bf16" else np.float32   # (kv8: its values)
         K = np.empty((end - begin, c.n_kv_heads, c.head_dim), dt)
         V = np.empty_like(K)
         self._check(self.lib.wici_read_kv(self.h, layer, begin, end, K.ctypes.data, V.ctypes.data),

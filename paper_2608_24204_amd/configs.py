@@ -30,7 +30,8 @@ class ModelConfig:
     tied_embeddings: bool = False
     weight_dtype: str = "bf16"   # "bf16", "f32", or "q8" (bf16 source weights stored as
                                  # block-scaled 8-bit codes: 34 bytes per 32 weights)
-    kv_dtype: str = "bf16"       # KV cache storage type
+    kv_dtype: str = "bf16"       # KV cache storage type: "bf16", "f32", or "kv8" (8-bit codes,
+                                 # one fp32 scale for each position and head)
     prompt_len: int = 32
     decode_steps: int = 16
     prefill_chunk: int = 2048
@@ -59,7 +60,10 @@ class ModelConfig:
         return {"bf16": 2, "f32": 4, "q8": 34 / 32}[self.weight_dtype]
 
     @property
-    def kvbytes(self) -> int:
+    def kvbytes(self) -> float:
+        """Bytes of one cached value (its share of the row's scale included)."""
+        if self.kv_dtype == "kv8":
+            return (self.head_dim + 4) / self.head_dim
         return 2 if self.kv_dtype == "bf16" else 4
 
     def layer_matrix_params(self) -> int:
@@ -83,7 +87,7 @@ class ModelConfig:
         out: under 0.001% of the total at the benchmarked shapes."""
         w = (self.n_layers * self.layer_matrix_params() + self.vocab * self.d_model) * self.wbytes
         kv_read = n_ctx * self.n_layers * 2 * self.kv_dim * self.kvbytes
-        return int(round(w)) + kv_read
+        return int(round(w)) + int(kv_read)
 
     def prefill_flops(self, n_prompt: int | None = None) -> int:
         """Algorithmic flops of a prefill: projections of every prompt row, causal

@@ -310,7 +310,10 @@ __global__ __launch_bounds__(256) void k_gemv(const WT* __restrict__ W, int N, i
         const float va = which ? a : a * c - b * sn, vb = which ? b : a * sn + b * c;
         const size_t off =
             ((((size_t)phys * 2 + which) * kv.n_kv + h) * kv.page + slot) * kv.hd + j;
-        if (rope.kv_bf16) {
+        if (rope.kv_rows) {
+          y[(size_t)hh * 2 * half + j] = va;
+          y[(size_t)hh * 2 * half + j + half] = vb;
+        } else if (rope.kv_bf16) {
           bf16_t* d = static_cast<bf16_t*>(kv.base) + off;
           d[0] = f32_to_bf16(va);
           d[half] = f32_to_bf16(vb);

@@ -66,6 +66,8 @@ struct QkvRope {
   const void* state;   // DecodeState: the position being appended
   KvLayout kv;         // this layer's cache (kv.hd = head dim, kv.n_kv = KV heads)
   int kv_bf16;         // cache element type: 1 bf16, 0 fp32
+  int kv_rows;         // nonzero: keys and values are stored in y after the query heads
+                       // instead of the cache, whose rows a later launch quantises
   int n_q;             // query heads
   float q_scale;       // 1/sqrt(hd)
   // bf16 embedding [V, K] or nullptr.  Set: the projection's input is the

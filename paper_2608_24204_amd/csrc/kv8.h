@@ -45,6 +45,10 @@ struct HeadRows {
   void* p;  // nullptr: absent
   int bf16;
   int64_t row_stride, head_stride;
+  // inputs of the append only: the rows are the sums, in order, of `n_sum` fp32 arrays
+  // sum_stride elements apart (0 and 1: one array)
+  int n_sum;
+  int64_t sum_stride;
 };
 
 // Rotary tables: cos[pos][dim / 2].  layout 0 rotates (j, j + dim / 2), 1 (2j, 2j + 1);
@@ -70,7 +74,8 @@ hipError_t launch_rope_table(const RopeFreqs& f, int half, int64_t n_pos, float*
 // cache; with q.p, the queries rotated and scaled by q_scale into q_out (which may be q).
 hipError_t launch_kv8_append(int hd, const Kv8& c, const Kv8Rows& r, const RopeTab& rope, int n_q,
                              const HeadRows& q, const HeadRows& q_out, float q_scale,
-                             const HeadRows& k, const HeadRows& v, hipStream_t st);
+                             const HeadRows& k, const HeadRows& v, hipStream_t st,
+                             int edge = 3);
 // The values of the rows' positions: k and v rows written (either may be absent).
 hipError_t launch_kv8_read(int hd, const Kv8& c, const Kv8Rows& r, const HeadRows& k,
                            const HeadRows& v, hipStream_t st);
@@ -88,7 +93,10 @@ struct Kv8Attn {
 };
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length);
-hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st);
+size_t kv8_attn_floats_most(int hd);  // of any launch
+// (edge: which of the timer's events the launches of append and attention record)
+hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st,
+                           int edge = 3);
 
 #ifdef __HIPCC__
 // One sequence of a launch.

@@ -212,6 +212,13 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab ro
   float e[8];
   load4(x, in + run.a, e);
   load4(x, in + run.b, e + 4);
+  for (int s = 1; s < x.n_sum; ++s) {
+    float m[8];
+    load4(x, in + s * x.sum_stride + run.a, m);
+    load4(x, in + s * x.sum_stride + run.b, m + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] += m[i];
+  }
   turn_row(rope, run, lane, w.pos, e);
   if (is_q) {
 #pragma unroll
@@ -307,15 +314,15 @@ hipError_t launch_rope_table(const RopeFreqs& f, int half, int64_t n_pos, float*
 
 hipError_t launch_kv8_append(int hd, const Kv8& c, const Kv8Rows& r, const RopeTab& rope, int n_q,
                              const HeadRows& q, const HeadRows& q_out, float q_scale,
-                             const HeadRows& k, const HeadRows& v, hipStream_t st) {
+                             const HeadRows& k, const HeadRows& v, hipStream_t st, int edge) {
   if (!q.p) n_q = 0;
   const unsigned grid = unit_blocks(hd, (int64_t)r.n_rows * (n_q + 2 * c.n_kv));
   if (!grid) return hipErrorInvalidValue;
   if (hd == 128)
-    launch_k(k_kv8_append<128>, dim3(grid), dim3(256), 0, st, kOnly, c, r, rope, n_q, q, q_out,
+    launch_k(k_kv8_append<128>, dim3(grid), dim3(256), 0, st, edge, c, r, rope, n_q, q, q_out,
              q_scale, k, v);
   else if (hd == 64)
-    launch_k(k_kv8_append<64>, dim3(grid), dim3(256), 0, st, kOnly, c, r, rope, n_q, q, q_out,
+    launch_k(k_kv8_append<64>, dim3(grid), dim3(256), 0, st, edge, c, r, rope, n_q, q, q_out,
              q_scale, k, v);
   else
     return hipErrorInvalidValue;

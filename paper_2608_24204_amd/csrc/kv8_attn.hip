@@ -513,6 +513,7 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 
 // ------------------------------------------------------------------- launcher
 namespace {
+constexpr int kBlocks = 768;  // what the chip holds at once (128 dimensions, bf16 rows)
 struct Plan {
   int ntile, nsplit;
 };
@@ -521,7 +522,7 @@ Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_lengt
   Plan p;
   p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
   const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t want = std::max<int64_t>(1, 768 / blocks);
+  const int64_t want = std::max<int64_t>(1, kBlocks / blocks);
   const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
@@ -534,13 +535,16 @@ size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int ma
   return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
 }
 
+// a split launch has at most kBlocks workgroups of 16 rows x heads
+size_t kv8_attn_floats_most(int hd) { return (size_t)kBlocks * 16 * (hd + 2); }
+
 template <int HD>
-static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st) {
+static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
   const Plan p = plan(a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
   const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
   if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)gx, r.n_seqs);
-  const int edge = p.nsplit == 1 ? kOnly : kFirst;
+  const int edge = p.nsplit == 1 ? last : last & kFirst;
   if (a.q.bf16 && a.out.p && a.out.bf16)
     launch_k(k_kv8_attn_split<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
   else
@@ -548,14 +552,16 @@ static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStre
   if (p.nsplit > 1) {
     const int64_t mg = (int64_t)r.n_rows * a.n_q;
     if (mg > 0x7fffffff) return hipErrorInvalidValue;
-    launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, kLast, c, r, a, p.nsplit);
+    launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, last & kLast, c, r, a,
+             p.nsplit);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st) {
-  if (a.hd == 128) return attn<128>(c, r, a, st);
-  if (a.hd == 64) return attn<64>(c, r, a, st);
+hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st,
+                           int edge) {
+  if (a.hd == 128) return attn<128>(c, r, a, st, edge);
+  if (a.hd == 64) return attn<64>(c, r, a, st, edge);
   return hipErrorInvalidValue;
 }
 

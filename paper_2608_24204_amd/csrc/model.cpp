@@ -17,6 +17,8 @@
 #include "../../include/wici.h"
 #include "common.h"
 #include "kernels.h"
+#include "kv8.h"
+#include "rope.h"
 
 using wici::ArgmaxPart;
 using wici::DecodeState;
@@ -70,7 +72,7 @@ struct Layout {
   size_t kv_layer_stride, kv_bytes;
   // scratch
   size_t x, a, qkv, att, h, kpart, logits, parts, part_o, part_ml, tokens, table, state, hist,
-      seqs, attn_sync, gemm_sync;
+      seqs, attn_sync, gemm_sync, kv8_work;
   size_t scratch_bytes;
   int nsplit;
 };
@@ -96,7 +98,8 @@ bool config_ok(const wici_config* c, std::string* why) {
   if (!(c->rope_base > 1.0) || !std::isfinite(c->rope_base)) return bad("rope_base must be > 1");
   if (c->weight_dtype != WICI_F32 && c->weight_dtype != WICI_BF16 && c->weight_dtype != WICI_Q8)
     return bad("bad weight_dtype");
-  if (c->kv_dtype != WICI_F32 && c->kv_dtype != WICI_BF16) return bad("bad kv_dtype");
+  if (c->kv_dtype != WICI_F32 && c->kv_dtype != WICI_BF16 && c->kv_dtype != WICI_KV8)
+    return bad("bad kv_dtype");
   if (c->max_seq < 1 || c->max_seq > (1 << 20)) return bad("max_seq out of range");
   if (c->prefill_chunk < 1 || c->prefill_chunk > 8192) return bad("prefill_chunk out of range");
   if (c->kv_page != 16 && c->kv_page != 32 && c->kv_page != 64 && c->kv_page != 128)
@@ -150,8 +153,10 @@ Layout make_layout(const wici_config& c) {
   L.weight_bytes = o;
 
   L.n_pages = (c.max_seq + c.kv_page - 1) / c.kv_page;
-  L.kv_layer_stride = align_up((size_t)L.n_pages * 2 * c.n_kv_heads * c.kv_page * c.head_dim *
-                               dsize(c.kv_dtype));
+  const size_t kv_block = c.kv_dtype == WICI_KV8
+                              ? wici::kv8_block_bytes(c.kv_page, c.head_dim)
+                              : (size_t)c.kv_page * c.head_dim * dsize(c.kv_dtype);
+  L.kv_layer_stride = align_up((size_t)L.n_pages * 2 * c.n_kv_heads * kv_block);
   L.kv_bytes = L.kv_layer_stride * c.n_layers;
 
   L.nsplit = wici::attn_decode_splits(c.max_seq);
@@ -178,6 +183,9 @@ Layout make_layout(const wici_config& c) {
   L.attn_sync = o; o = align_up(o + (size_t)wici::attn_fuse_ints(c.n_kv_heads) * 4);
   // counters and XCD records of the batched products' split-K sums
   L.gemm_sync = o; o = align_up(o + (size_t)wici::kGemmRowsSyncInts * 4);
+  // partial results of the attention over an 8-bit cache
+  L.kv8_work = o;
+  if (c.kv_dtype == WICI_KV8) o = align_up(o + wici::kv8_attn_floats_most(c.head_dim) * 4);
   L.scratch_bytes = o;
   return L;
 }
@@ -211,6 +219,8 @@ struct wici_model {
   int32_t pos = 0;
   bool have_token = false;
   bool shared_weights = false;  // weights bound from another model (read-only here)
+  bool own_rope = false;        // wici_set_rope was called
+  wici_rope rope{};             // then: its specification
   DecodeState* h_state = nullptr;         // pinned, device-mapped state mirror (host view)
   DecodeState* d_state_mirror = nullptr;  // the same memory as the kernels address it
   hipGraph_t graph = nullptr;
@@ -241,6 +251,26 @@ struct wici_model {
     k.hd = cfg.head_dim;
     k.max_pos = cfg.max_seq;
     return k;
+  }
+  // layer l of an 8-bit cache
+  wici::Kv8 kv8(int l) const {
+    wici::Kv8 k{};
+    k.base = dkv + (size_t)l * L.kv_layer_stride;
+    k.table = S<int32_t>(L.table);
+    k.n_pages = k.max_pages = L.n_pages;
+    k.page_shift = __builtin_ctz((unsigned)cfg.kv_page);
+    k.n_kv = cfg.n_kv_heads;
+    return k;
+  }
+  // heads [first, ..) of the fp32 projection rows at p, as kernels of the 8-bit cache take
+  // them: the sums of n_sum arrays
+  wici::HeadRows heads(float* p, int first, int n_sum = 1, size_t sum_stride = 0) const {
+    const int64_t hd = cfg.head_dim;
+    return {p + first * hd, 0, (cfg.n_heads + 2 * cfg.n_kv_heads) * hd, hd, n_sum,
+            (int64_t)sum_stride};
+  }
+  wici::RopeTab tables() const {
+    return {W<float>(L.rope_cos), W<float>(L.rope_sin), cfg.max_seq, cfg.head_dim, 0};
   }
 };
 
@@ -295,6 +325,56 @@ void build_specs(wici_model* m) {
 
 bool usable(const wici_model* m) { return m && !m->failed; }
 
+// Dimensions of a head in the order in which the model keeps query and key heads: slots j and
+// j + hd / 2 hold pair j of the rotary embedding (then the dimensions that pass through,
+// turned by nothing), whatever pairs the specification names.  A product of two heads does
+// not depend on that order, so one rotation serves every layout.
+std::vector<int> head_order(const wici_model* m) {
+  const int hd = m->cfg.head_dim, half = hd / 2;
+  std::vector<int> at(hd);
+  for (int j = 0; j < half; ++j) {
+    int a = j, b = j + half;
+    if (m->own_rope) {
+      const int dim = m->rope.dim;
+      const bool turned = j < dim / 2, pairs = m->rope.layout == WICI_ROPE_PAIRS;
+      a = !turned || pairs ? 2 * j : j;
+      b = !turned || pairs ? 2 * j + 1 : j + dim / 2;
+    }
+    at[j] = a;
+    at[j + half] = b;
+  }
+  return at;
+}
+bool in_head_order(const wici_model* m) {
+  const std::vector<int> at = head_order(m);
+  for (size_t i = 0; i < at.size(); ++i)
+    if (at[i] != (int)i) return true;
+  return false;
+}
+
+// Attention of rows over layer l of an 8-bit cache: append first (with RoPE where `rope` is
+// set; q_in are the query rows to rotate), then attend into act.  One timed step.
+hipError_t kv8_attention(const wici_model* m, int l, const wici::Kv8Rows& r, const wici::RopeTab& rope,
+                         const wici::HeadRows& q_in, const wici::HeadRows& q,
+                         const wici::HeadRows& k, const wici::HeadRows& v,
+                         const wici::ActBuf& act, int max_rows) {
+  const wici_config& c = m->cfg;
+  const float q_scale = 1.0f / std::sqrt((float)c.head_dim);
+  if (hipError_t e = wici::launch_kv8_append(c.head_dim, m->kv8(l), r, rope, c.n_heads, q_in, q,
+                                             q_scale, k, v, m->stream, 1))
+    return e;
+  wici::Kv8Attn a{};
+  a.hd = c.head_dim;
+  a.n_q = c.n_heads;
+  a.scale = 1.0f;  // the queries carry it
+  a.q = q;
+  a.act = act;
+  a.max_rows = max_rows;
+  a.max_length = c.max_seq;
+  a.work = m->S<float>(m->L.kv8_work);
+  return wici::launch_kv8_attn(m->kv8(l), r, a, m->stream, 2);
+}
+
 // Enqueue one decode step (position and input token read from device state).
 // With `timers`, every launcher call is timed: a start/stop event pair recorded
 // by the dispatches of its first and last kernel (the profiling entry point uses
@@ -303,7 +383,7 @@ hipError_t enqueue_decode(wici_model* m, std::vector<wici::LaunchTimer>* timers 
   const wici_config& c = m->cfg;
   const Layout& L = m->L;
   const int wb = c.weight_dtype;
-  const bool kb = c.kv_dtype == WICI_BF16;
+  const bool kb = c.kv_dtype == WICI_BF16, k8 = c.kv_dtype == WICI_KV8;
   const int d = c.d_model, F = c.ffn_dim, qd = c.n_heads * c.head_dim;
   const int nqkv = qd + 2 * c.n_kv_heads * c.head_dim;
   float* x = m->S<float>(L.x);
@@ -353,15 +433,29 @@ hipError_t enqueue_decode(wici_model* m, std::vector<wici::LaunchTimer>* timers 
     rope.state = st;
     rope.kv = m->kv(l);
     rope.kv_bf16 = kb ? 1 : 0;
+    rope.kv_rows = k8 ? 1 : 0;
     rope.n_q = c.n_heads;
     rope.q_scale = 1.0f / std::sqrt((float)c.head_dim);
     rope.embed = fold_embed && l == 0 ? m->dw + L.embed : nullptr;
     WICI_STEP(wici::launch_gemv(wb, wici::GEMV_QKV, m->dw + m->layer(l, L.l_wqkv), nqkv, d, x,
                                 m->W<float>(m->layer(l, L.l_anorm)), c.rms_eps, qkv, nullptr,
                                 nullptr, s, &rope));
-    WICI_STEP(wici::launch_attn_decode(kb, qkv, c.n_heads, m->kv(l), st, L.nsplit,
-                                       m->S<float>(L.part_o), m->S<float>(L.part_ml), att,
-                                       kb ? &fuse : nullptr, s));
+    if (k8) {
+      // the projection has rotated the rows (and scaled the queries)
+      wici::Kv8Rows r{};
+      r.kind = wici::KV8_STATE;
+      r.n_seqs = r.n_rows = 1;
+      r.state = st;
+      wici::ActBuf out{};
+      out.f32 = att;
+      WICI_STEP(kv8_attention(m, l, r, wici::RopeTab{}, wici::HeadRows{}, m->heads(qkv, 0),
+                              m->heads(qkv, c.n_heads), m->heads(qkv, c.n_heads + c.n_kv_heads),
+                              out, 1));
+    } else {
+      WICI_STEP(wici::launch_attn_decode(kb, qkv, c.n_heads, m->kv(l), st, L.nsplit,
+                                         m->S<float>(L.part_o), m->S<float>(L.part_ml), att,
+                                         kb ? &fuse : nullptr, s));
+    }
     WICI_STEP(wici::launch_gemv(wb, wici::GEMV_RESID, m->dw + m->layer(l, L.l_wo), d, qd, att,
                                 nullptr, 0.f, x, nullptr, nullptr, s));
     WICI_STEP(wici::launch_gemv(wb, wici::GEMV_SWIGLU, m->dw + m->layer(l, L.l_wgu), 2 * F, d, x,
@@ -386,7 +480,7 @@ hipError_t enqueue_prefill_chunk(wici_model* m, int p0, int T, int tok_off) {
   const wici_config& c = m->cfg;
   const Layout& L = m->L;
   const int wb = c.weight_dtype;
-  const bool kb = c.kv_dtype == WICI_BF16;
+  const bool kb = c.kv_dtype == WICI_BF16, k8 = c.kv_dtype == WICI_KV8;
   const int d = c.d_model, F = c.ffn_dim, qd = c.n_heads * c.head_dim;
   const int nqkv = qd + 2 * c.n_kv_heads * c.head_dim;
   float* x = m->S<float>(L.x);
@@ -465,12 +559,25 @@ hipError_t enqueue_prefill_chunk(wici_model* m, int p0, int T, int tok_off) {
                          nqkv, none, 0))) {
       return e;
     }
-    if ((e = wici::launch_rope_append(kb, qkv, T, p0, c.n_heads, m->W<float>(L.rope_cos),
-                                      m->W<float>(L.rope_sin), m->kv(l), s, s_q > 1 ? P : nullptr,
-                                      s_q, q_split)))
-      return e;
-    if ((e = wici::launch_attn_prefill(kb, qkv, T, p0, c.n_heads, m->kv(l), att, s, pl.attn)))
-      return e;
+    if (k8) {
+      wici::Kv8Rows r{};
+      r.kind = wici::KV8_CHUNK;
+      r.n_seqs = 1;
+      r.n_rows = T;
+      r.fixed_len = p0 + T;
+      float* in = s_q > 1 ? P : qkv;
+      if ((e = kv8_attention(m, l, r, m->tables(), m->heads(in, 0, s_q, q_split),
+                             m->heads(qkv, 0), m->heads(in, c.n_heads, s_q, q_split),
+                             m->heads(in, c.n_heads + c.n_kv_heads, s_q, q_split), att, T)))
+        return e;
+    } else {
+      if ((e = wici::launch_rope_append(kb, qkv, T, p0, c.n_heads, m->W<float>(L.rope_cos),
+                                        m->W<float>(L.rope_sin), m->kv(l), s,
+                                        s_q > 1 ? P : nullptr, s_q, q_split)))
+        return e;
+      if ((e = wici::launch_attn_prefill(kb, qkv, T, p0, c.n_heads, m->kv(l), att, s, pl.attn)))
+        return e;
+    }
     if ((e = resid(rd(att, pl.o), qd, m->layer(l, L.l_wo), s_o))) return e;
     if ((e = norm(m->W<float>(m->layer(l, L.l_fnorm)), s_o, pl.gu))) return e;
     if ((e = prod(wici::GEMV_SWIGLU, rd(a, pl.gu), d, m->layer(l, L.l_wgu), 2 * F, nullptr, 0, h,
@@ -493,7 +600,7 @@ hipError_t enqueue_decode_batch(wici_model* m, int B) {
   const wici_config& c = m->cfg;
   const Layout& L = m->L;
   const int wb = c.weight_dtype;
-  const bool kb = c.kv_dtype == WICI_BF16;
+  const bool kb = c.kv_dtype == WICI_BF16, k8 = c.kv_dtype == WICI_KV8;
   const int d = c.d_model, F = c.ffn_dim, qd = c.n_heads * c.head_dim;
   const int nqkv = qd + 2 * c.n_kv_heads * c.head_dim;
   const size_t C = c.prefill_chunk;
@@ -574,11 +681,23 @@ hipError_t enqueue_decode_batch(wici_model* m, int B) {
     WICI_TRY(norm(m->W<float>(m->layer(l, L.l_anorm)), l ? s_d : 1));
     WICI_TRY(prod(wici::GEMV_STORE, rd(a, pl.qkv), d, m->layer(l, L.l_wqkv), nqkv, qkv, nqkv,
                   none, 0));
-    if (!fuse_rope)
-      WICI_TRY(wici::launch_rope_append_batch(kb, qkv, B, c.n_heads, m->W<float>(L.rope_cos),
-                                              m->W<float>(L.rope_sin), seqs, l, kv, q_scale, s));
-    WICI_TRY(wici::launch_attn_decode_batch(kb, qkv, nqkv, B, c.n_heads, kv, seqs, l, L.nsplit,
-                                            part_o, part_ml, att, s, fuse_rope ? &rope : nullptr));
+    if (k8) {
+      wici::Kv8Rows r{};
+      r.kind = wici::KV8_SEQS;
+      r.n_seqs = r.n_rows = B;
+      r.seqs = seqs;
+      r.layer = l;
+      WICI_TRY(kv8_attention(m, l, r, m->tables(), m->heads(qkv, 0), m->heads(qkv, 0),
+                             m->heads(qkv, c.n_heads), m->heads(qkv, c.n_heads + c.n_kv_heads),
+                             att, 1));
+    } else {
+      if (!fuse_rope)
+        WICI_TRY(wici::launch_rope_append_batch(kb, qkv, B, c.n_heads, m->W<float>(L.rope_cos),
+                                                m->W<float>(L.rope_sin), seqs, l, kv, q_scale, s));
+      WICI_TRY(wici::launch_attn_decode_batch(kb, qkv, nqkv, B, c.n_heads, kv, seqs, l, L.nsplit,
+                                              part_o, part_ml, att, s,
+                                              fuse_rope ? &rope : nullptr));
+    }
     WICI_TRY(resid(rd(att, pl.o), qd, m->layer(l, L.l_wo), s_o));
     WICI_TRY(norm(m->W<float>(m->layer(l, L.l_fnorm)), s_o));
     WICI_TRY(prod(wici::GEMV_SWIGLU, rd(a, pl.gu), d, m->layer(l, L.l_wgu), 2 * F, nullptr, 0, h,
@@ -590,6 +709,15 @@ hipError_t enqueue_decode_batch(wici_model* m, int B) {
   WICI_TRY(wici::launch_argmax_rows(logits, B, c.vocab, seqs, m->d_batch_mirror, s));
 #undef WICI_TRY
   return hipSuccess;
+}
+
+// Whether two models rotate alike (their weight regions hold the same tables, and query
+// and key heads in the same order).
+bool same_rope(const wici_model* a, const wici_model* b) {
+  const wici_rope &x = a->rope, &y = b->rope;
+  return a->own_rope == b->own_rope && x.dim == y.dim && x.layout == y.layout &&
+         x.scaling == y.scaling && x.base == y.base && x.factor == y.factor &&
+         x.original == y.original && x.low == y.low && x.high == y.high;
 }
 
 // Configurations whose weight regions are interchangeable (shapes, storage,
@@ -751,6 +879,18 @@ wici_status wici_create(const wici_config* cfg, void* hip_stream, wici_model** o
   return WICI_OK;
 }
 
+wici_status wici_set_rope(wici_model* m, const wici_rope* rope) {
+  if (!m) return WICI_E_ARG;
+  if (m->failed) return WICI_E_STATE;
+  if (m->bound) return fail(m, WICI_E_STATE, "wici_set_rope must come before the memory is bound");
+  if (!rope || !wici::rope_ok(*rope) || rope->dim > m->cfg.head_dim)
+    return fail(m, WICI_E_ARG, "not a rotary embedding of heads of %d dimensions",
+                m->cfg.head_dim);
+  m->rope = *rope;
+  m->own_rope = true;
+  return WICI_OK;
+}
+
 wici_status wici_bind_memory(wici_model* m, void* d_weights, size_t weight_bytes, void* d_kv,
                              size_t kv_bytes, void* d_scratch, size_t scratch_bytes) {
   if (!m) return WICI_E_ARG;
@@ -766,16 +906,24 @@ wici_status wici_bind_memory(wici_model* m, void* d_weights, size_t weight_bytes
   m->dkv = static_cast<char*>(d_kv);
   m->ds = static_cast<char*>(d_scratch);
   HIP_TRY(m, alloc_state_mirror(m));
-  // RoPE angle table: pos * base^(-2j/hd), evaluated in double, stored as fp32.
+  // RoPE angle table: pos * base^(-2j/hd), or the steps of wici_set_rope (none for the
+  // dimensions that pass through), evaluated in double, stored as fp32.
   const wici_config& c = m->cfg;
   const int half = c.head_dim / 2;
+  wici::RopeFreqs own{};
+  if (m->own_rope) own = wici::rope_freqs(m->rope);
   std::vector<float> cs((size_t)c.max_seq * half), sn((size_t)c.max_seq * half);
   for (int j = 0; j < half; ++j) {
-    const double inv = std::pow(c.rope_base, -2.0 * j / c.head_dim);
+    double inv = std::pow(c.rope_base, -2.0 * j / c.head_dim), mult = 1.0;
+    if (m->own_rope) {
+      const bool turned = j < m->rope.dim / 2;
+      inv = turned ? own.f[j] : 0.0;
+      mult = turned ? own.factor : 1.0;
+    }
     for (int p = 0; p < c.max_seq; ++p) {
       const double ang = (double)p * inv;
-      cs[(size_t)p * half + j] = (float)std::cos(ang);
-      sn[(size_t)p * half + j] = (float)std::sin(ang);
+      cs[(size_t)p * half + j] = (float)(mult * std::cos(ang));
+      sn[(size_t)p * half + j] = (float)(mult * std::sin(ang));
     }
   }
   HIP_TRY(m, hipMemcpy(m->dw + m->L.rope_cos, cs.data(), cs.size() * 4, hipMemcpyHostToDevice));
@@ -823,6 +971,19 @@ wici_status wici_load_weights(wici_model* m, const wici_tensor* tensors, int32_t
   const Layout& L = m->L;
   const size_t ws = dsize(c.weight_dtype), d = c.d_model;
   const size_t qd = (size_t)c.n_heads * c.head_dim, kvd = (size_t)c.n_kv_heads * c.head_dim;
+  // query and key rows go where head_order puts them: one strided copy for each
+  // dimension of a head
+  const std::vector<int> order = head_order(m);
+  const bool reorder = in_head_order(m);
+  auto copy_heads = [&](char* dst, const void* src, size_t row, hipMemcpyKind kind, size_t rows) {
+    const size_t head = (size_t)c.head_dim * row;
+    for (int j = 0; j < c.head_dim; ++j)
+      if (hipError_t e = hipMemcpy2DAsync(dst + j * row, head,
+                                          static_cast<const char*>(src) + order[j] * row, head, row,
+                                          rows / c.head_dim, kind, m->stream))
+        return e;
+    return hipStreamSynchronize(m->stream);
+  };
   if (c.weight_dtype == WICI_Q8) {
     // quantise every matrix first (host), so a bad tensor uploads nothing
     std::vector<std::vector<uint8_t>> codes(n_tensors);
@@ -871,6 +1032,12 @@ wici_status wici_load_weights(wici_model* m, const wici_tensor* tensors, int32_t
       char* dc = m->dw + base;
       char* dsc = dc + wici::q8_scale_offset(rows, K);
       const size_t sb = K / 32 * 2;  // scale bytes per row
+      if (reorder && (sp.kind == T_WQ || sp.kind == T_WK)) {
+        HIP_TRY(m, copy_heads(dc + r0 * K, codes[i].data(), K, hipMemcpyHostToDevice, (size_t)sp.rows));
+        HIP_TRY(m, copy_heads(dsc + r0 * sb, scales[i].data(), sb, hipMemcpyHostToDevice,
+                              (size_t)sp.rows));
+        continue;
+      }
       HIP_TRY(m, hipMemcpy2D(dc + r0 * K, step * K, codes[i].data(), K, K, (size_t)sp.rows,
                              hipMemcpyHostToDevice));
       HIP_TRY(m, hipMemcpy2D(dsc + r0 * sb, step * sb, scales[i].data(), sb, sb, (size_t)sp.rows,
@@ -904,6 +1071,10 @@ wici_status wici_load_weights(wici_model* m, const wici_tensor* tensors, int32_t
         HIP_TRY(m, hipMemcpy2DAsync(base, 2 * rb, t.data, rb, rb, (size_t)sp.rows, kind, m->stream));
         continue;
       }
+    }
+    if (reorder && (sp.kind == T_WQ || sp.kind == T_WK)) {
+      HIP_TRY(m, copy_heads(dst, t.data, (size_t)sp.cols * es, kind, (size_t)sp.rows));
+      continue;
     }
     HIP_TRY(m, hipMemcpyAsync(dst, t.data, bytes, kind, m->stream));
   }
@@ -1059,7 +1230,7 @@ wici_status wici_bind_memory_shared(wici_model* m, const wici_model* src, void* 
   if (m->bound) return fail(m, WICI_E_STATE, "memory already bound");
   if (src->failed || !src->ready())
     return fail(m, WICI_E_STATE, "the source model has no complete weights");
-  if (!same_weights_geometry(m->cfg, src->cfg))
+  if (!same_weights_geometry(m->cfg, src->cfg) || !same_rope(m, src))
     return fail(m, WICI_E_ARG, "configuration differs from the source model's weights");
   if (!d_kv || !d_scratch) return fail(m, WICI_E_ARG, "NULL device pointer");
   if (kv_bytes < m->L.kv_bytes || scratch_bytes < m->L.scratch_bytes)
@@ -1108,7 +1279,7 @@ wici_status wici_decode_batch(wici_model* const* models, int32_t n, const int32_
     for (int j = 0; j < b; ++j)
       if (models[j] == mb) return fail(lead, WICI_E_ARG, "model %d appears twice", b);
     if (mb->failed || !mb->ready()) return fail(lead, WICI_E_STATE, "model %d not ready", b);
-    if (mb->dw != lead->dw || !same_weights_geometry(mb->cfg, c) ||
+    if (mb->dw != lead->dw || !same_weights_geometry(mb->cfg, c) || !same_rope(mb, lead) ||
         mb->cfg.kv_dtype != c.kv_dtype || mb->cfg.kv_page != c.kv_page)
       return fail(lead, WICI_E_ARG, "model %d does not share the lead's weights and config", b);
     const int32_t t = tokens_in ? tokens_in[b] : -1;
@@ -1236,22 +1407,57 @@ wici_status wici_read_kv(wici_model* m, int32_t layer, int32_t begin, int32_t en
   if (layer < 0 || layer >= c.n_layers || begin < 0 || end < begin || end > m->pos || !host_k ||
       !host_v)
     return fail(m, WICI_E_ARG, "bad layer/range/pointer");
-  const size_t es = dsize(c.kv_dtype), hd = c.head_dim, page = c.kv_page, nkv = c.n_kv_heads;
+  const size_t es = c.kv_dtype == WICI_KV8 ? 4 : dsize(c.kv_dtype);
+  const size_t hd = c.head_dim, page = c.kv_page, nkv = c.n_kv_heads;
   std::vector<int32_t> table(m->L.n_pages);
   HIP_TRY(m, hipMemcpyAsync(table.data(), m->ds + m->L.table, table.size() * 4,
                             hipMemcpyDeviceToHost, m->stream));
   HIP_TRY(m, hipStreamSynchronize(m->stream));
   const char* base = m->dkv + (size_t)layer * m->L.kv_layer_stride;
-  for (int p = begin; p < end; ++p) {
-    const size_t phys = table[p / page], slot = p % page;
-    for (int w = 0; w < 2; ++w) {
-      const char* src = base + (((phys * 2 + w) * nkv) * page + slot) * hd * es;
-      char* dst = static_cast<char*>(w ? host_v : host_k) + (size_t)(p - begin) * nkv * hd * es;
-      HIP_TRY(m, hipMemcpy2DAsync(dst, hd * es, src, page * hd * es, hd * es, nkv,
+  if (c.kv_dtype == WICI_KV8) {
+    // whole pages to the host, then the values that their codes stand for
+    const size_t block = wici::kv8_block_bytes(c.kv_page, c.head_dim), bytes = 2 * nkv * block;
+    std::vector<char> buf(bytes);
+    for (int p = begin; p < end; ++p) {
+      if (p == begin || p % page == 0) {
+        HIP_TRY(m, hipMemcpyAsync(buf.data(), base + table[p / page] * bytes, bytes,
                                   hipMemcpyDeviceToHost, m->stream));
+        HIP_TRY(m, hipStreamSynchronize(m->stream));
+      }
+      const int slot = (int)(p % page), h_d = (int)hd;
+      for (size_t w = 0; w < 2; ++w)
+        for (size_t h = 0; h < nkv; ++h) {
+          const char* b = buf.data() + (w * nkv + h) * block;
+          float scale;
+          std::memcpy(&scale, b + wici::kv8_scale_at(slot, c.kv_page, h_d), 4);
+          float* dst = static_cast<float*>(w ? host_v : host_k) + ((p - begin) * nkv + h) * hd;
+          for (int d = 0; d < h_d; ++d) {
+            const int at = w ? wici::kv8_value_at(slot, d, h_d) : wici::kv8_key_at(slot, d, h_d);
+            dst[d] = (float)((int)(unsigned char)b[at] - 128) * scale;
+          }
+        }
+    }
+  } else {
+    for (int p = begin; p < end; ++p) {
+      const size_t phys = table[p / page], slot = p % page;
+      for (int w = 0; w < 2; ++w) {
+        const char* src = base + (((phys * 2 + w) * nkv) * page + slot) * hd * es;
+        char* dst = static_cast<char*>(w ? host_v : host_k) + (size_t)(p - begin) * nkv * hd * es;
+        HIP_TRY(m, hipMemcpy2DAsync(dst, hd * es, src, page * hd * es, hd * es, nkv,
+                                    hipMemcpyDeviceToHost, m->stream));
+      }
+    }
+    HIP_TRY(m, hipStreamSynchronize(m->stream));
+  }
+  if (in_head_order(m)) {  // keys back in the order of the weights' rows
+    const std::vector<int> order = head_order(m);
+    std::vector<char> row(hd * es);
+    for (size_t i = 0; i < (size_t)(end - begin) * nkv; ++i) {
+      char* k = static_cast<char*>(host_k) + i * hd * es;
+      std::memcpy(row.data(), k, hd * es);
+      for (size_t j = 0; j < hd; ++j) std::memcpy(k + order[j] * es, row.data() + j * es, es);
     }
   }
-  HIP_TRY(m, hipStreamSynchronize(m->stream));
   return WICI_OK;
 }
 
