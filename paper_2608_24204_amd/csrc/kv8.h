@@ -93,7 +93,7 @@ struct Kv8Attn {
 };
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length);
-size_t kv8_attn_floats_most(int hd, int n_seqs);  // of any launch of up to n_seqs sequences
+size_t kv8_attn_floats_most(int hd);  // of any launch
 // (edge: which of the timer's events the launches of append and attention record)
 hipError_t launch_kv8_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st,
                            int edge = 3);

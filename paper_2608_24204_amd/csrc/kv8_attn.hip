@@ -324,284 +324,166 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
   }
 }
 
-// ------------------------------------------------------------------- few rows: the stream
-// The work is a list of steps (32 positions of one KV head for a tile of 16 of a sequence's
-// rows x query heads of the group; row r of them: new row r / G, query head r % G), sequence
-// after sequence, and workgroup i takes steps [i per, (i + 1) per) of it, whatever the lengths
-// are: every workgroup reads as much, and the chip is filled once.  (Splits of equal count
-// left 48 sequences of 2000 to 4000 positions at 50 us, the longest waited for.)  A tile's
-// steps within one workgroup write the output, those shared by several leave (ref, sum,
-// output) for the merge.
-struct Stream {
-  int64_t* plan;  // [n_seqs + 2]: the steps before each sequence, all steps, steps a workgroup
-  float* parts;   // two slots a workgroup (its first and its last tile): 16 x (ref, sum),
-                  // then 16 rows of output
-  int per;        // the least steps of a workgroup
-};
-constexpr int kMinSteps = 8;  // two a wavefront
-
-__device__ __forceinline__ int seq_steps(const Kv8Seq& q, int64_t cap) {
-  const int64_t n = q.len < cap ? q.len : cap;
-  return n > kStep ? (int)((n + kStep - 1) / kStep) : 1;  // (one to write zeros for none)
-}
-__device__ __forceinline__ int seq_tiles(const Kv8Seq& q, int G) { return (q.rows * G + 15) / 16; }
-
-// Where a workgroup of 256 threads starts: sequence b, `at` steps into it.
-struct Start {
-  int b;
-  int64_t at, left;
-};
-__device__ __forceinline__ Start find_start(const Kv8& c, const Kv8Rows& r, int G, const Stream& sm) {
-  __shared__ int64_t s_wave[4], s_at;
-  __shared__ int s_b;
-  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  const int tid = threadIdx.x, chunk = (r.n_seqs + 255) / 256;
-  const int b0 = min(tid * chunk, r.n_seqs), b1 = min(b0 + chunk, r.n_seqs);
-  auto work = [&](int b) {
-    const Kv8Seq q = kv8_seq(c, r, b);
-    return (int64_t)seq_steps(q, cap) * seq_tiles(q, G) * c.n_kv;
-  };
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += work(b);
-  int64_t before = mine;  // then: of the threads up to this one
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int64_t v = __shfl_up(before, m);
-    if ((tid & 63) >= m) before += v;
-  }
-  if ((tid & 63) == 63) s_wave[tid >> 6] = before;
-  __syncthreads();
-  int64_t all = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < tid >> 6) before += s_wave[w];
-    all += s_wave[w];
-  }
-  before -= mine;
-  int64_t per = (all + gridDim.x - 1) / gridDim.x;
-  per = max((per + 3) / 4 * 4, (int64_t)sm.per);
-  const int64_t lo = blockIdx.x * per;
-  const bool lead = blockIdx.x == 0;
-  if (lead && tid == 0) {
-    sm.plan[r.n_seqs] = all;
-    sm.plan[r.n_seqs + 1] = per;
-  }
-  if (lead || (before <= lo && lo < before + mine))
-    for (int b = b0; b < b1; ++b) {
-      const int64_t n = work(b);
-      if (lead) sm.plan[b] = before;
-      if (before <= lo && lo < before + n) {
-        s_b = b;
-        s_at = lo - before;
-      }
-      before += n;
-    }
-  __syncthreads();
-  Start st{0, 0, min(min(per, all - lo), (int64_t)1 << 30)};
-  if (st.left > 0) {
-    st.b = s_b;
-    st.at = s_at;
-  }
-  return st;
-}
-
-// One tile's steps [s0, s1) of the sequence's: four wavefronts take them in turn and are
-// joined.  part: nullptr (all steps are here: the output is written) or the slot to leave the
-// tile's state in.
+// ------------------------------------------------------------------- split over positions
+// Workgroup (KV head, sequence, split): four wavefronts take the split's steps of 32
+// positions in turn for a tile of 16 of the sequence's rows x query heads of the group
+// (row r: new row r / G, query head r % G), and are joined at the end.  A split's range
+// follows from the sequence's own length, so one launch serves any length.  With one
+// split the output is written here, otherwise (ref, sum, output) to `part` for the merge.
 template <int HD, int NT>
-__device__ __forceinline__ void attend_tile(const Kv8& c, const Kv8Attn& a, const Kv8Seq& q, int h,
-                                            int tile, int s0, int s1, float* part, int wave,
-                                            int lane) {
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+                                                        int ntile) {
   __shared__ float s_o[4][16][HD + 4];
   __shared__ float s_ref[4][16], s_sum[4][16];
+  const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
+  const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, G = a.n_q / c.n_kv;
+  const Kv8Seq q = uniform(kv8_seq(c, r, b));
   const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  const int G = a.n_q / c.n_kv;
-  const int qr = 16 * tile + (lane & 15), row = qr / G, head = h * G + qr % G;
-  const bool on = row < q.rows;
-  const int rc = min(row, q.rows - 1);
-  // a row sees the positions up to its own; the tile's last row sees the most
-  const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
-  auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-  const int limit = on ? seen(row) : 0;
-  s1 = min(s1, (seen(last) + kStep - 1) / kStep);
-  // steps that all 16 rows see whole
-  const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
+  float* part_ml = a.work;
+  float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
 
-  RowState<HD> st;
-  st.ref = kNoRef;
-  st.sum = st.lift = 0.f;
-  bool huge = false;
+  for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
+    const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
+    const bool on = row < q.rows;
+    const int rc = min(row, q.rows - 1);
+    // a row sees the positions up to its own; the tile's last row sees the most
+    const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
+    auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
+    const int limit = on ? seen(row) : 0, most = seen(last), least = seen(first);
+    const int steps = (most + kStep - 1) / kStep, per = (steps + nsplit - 1) / nsplit;
+    const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+    // steps that all 16 rows see whole
+    const int whole = 16 * tile + 15 < q.rows * G ? least / kStep : 0;
+
+    RowState<HD> st;
+    st.ref = kNoRef;
+    st.sum = st.lift = 0.f;
+    bool huge = false;
 #pragma unroll
-  for (int u = 0; u < HD / 16; ++u) st.o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-  int s = s0 + wave;
-  if (s < s1) {
-    // the next step's keys are requested once this one's are multiplied, its values
-    // likewise, and its pages (which those addresses wait for) a step earlier
-    Keys<HD> k;
-    Values<HD> v;
-    Pages now = find_pages(c, q, s * kStep), next = find_pages(c, q, (s + 4) * kStep);
-    load_keys<HD>(k, c, q, now, h, s * kStep, lane);
-    load_values<HD>(v, c, q, now, h, s * kStep, lane);
-    half8_t qf[NT][HD / 32];
-    float unit;
-    load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf,
-                         unit);
-    unit *= a.scale * kLog2e;
-    for (;;) {
-      floatx4_t sc[2];
-      scores<HD, NT>(sc, k, qf);
-      const int then = s + 4;
-      if (then < s1) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
-      half8_t wf[NT];
-      float corr = 1.f;
-      const bool move =
-          s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
-              ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
-              : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane, corr);
-      if (move) {
+    for (int u = 0; u < HD / 16; ++u) st.o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    if (s0 < s1) {
+      half8_t qf[NT][HD / 32];
+      float unit;
+      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane,
+                           qf, unit);
+      unit *= a.scale * kLog2e;
+      // the next step's keys are requested once this one's are multiplied, its values
+      // likewise, and its pages (which those addresses wait for) a step earlier
+      int s = s0 + wave;
+      if (s < s1) {
+        Keys<HD> k;
+        Values<HD> v;
+        Pages now = find_pages(c, q, s * kStep), next = find_pages(c, q, (s + 4) * kStep);
+        load_keys<HD>(k, c, q, now, h, s * kStep, lane);
+        load_values<HD>(v, c, q, now, h, s * kStep, lane);
+        for (;;) {
+          floatx4_t sc[2];
+          scores<HD, NT>(sc, k, qf);
+          const int then = s + 4;
+          if (then < s1) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
+          half8_t wf[NT];
+          float corr = 1.f;
+          const bool move =
+              s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
+                  ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
+                  : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane,
+                                          corr);
+          if (move) {
 #pragma unroll
-        for (int u = 0; u < HD / 16; ++u)
+            for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
+              for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
+          }
+          add_values<HD, NT>(st, v, wf);
+          if (then >= s1) break;
+          load_values<HD>(v, c, q, next, h, then * kStep, lane);
+          now = next;
+          next = find_pages(c, q, (then + 4) * kStep);
+          s = then;
+        }
       }
-      add_values<HD, NT>(st, v, wf);
-      if (then >= s1) break;
-      load_values<HD>(v, c, q, next, h, then * kStep, lane);
-      now = next;
-      next = find_pages(c, q, (then + 4) * kStep);
-      s = then;
     }
-  }
-  if (huge) {
-    const float up = __builtin_amdgcn_exp2f(st.lift);
+    if (huge) {
+      const float up = __builtin_amdgcn_exp2f(st.lift);
 #pragma unroll
-    for (int u = 0; u < HD / 16; ++u)
+      for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) st.o[u][i] *= up;
-  }
-  // join the wavefronts
-  st.sum += __shfl_xor(st.sum, 16);
-  st.sum += __shfl_xor(st.sum, 32);
-  const int me = fresh(lane), mr = me & 15, mg = me >> 4;
-  if (mg == 0) {
-    s_ref[wave][mr] = st.ref;
-    s_sum[wave][mr] = st.sum;
-  }
-#pragma unroll
-  for (int hh = 0; hh < HD / 64; ++hh)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<float4*>(&s_o[wave][mr][64 * hh + 16 * mg + 4 * i]) = make_float4(
-          st.o[4 * hh][i], st.o[4 * hh + 1][i], st.o[4 * hh + 2][i], st.o[4 * hh + 3][i]);
-  __syncthreads();
-  for (int x = fresh(threadIdx.x); x < 16 * HD / 4; x += 256) {
-    const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
-    if (tr >= q.rows * G) continue;
-    float ref = s_ref[0][rr];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
-    float sum = 0.f, o[4] = {};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
-      const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
-      sum += f * s_sum[w][rr];
-      o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
+        for (int i = 0; i < 4; ++i) st.o[u][i] *= up;
     }
-    if (!part) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+    // join the wavefronts
+    st.sum += __shfl_xor(st.sum, 16);
+    st.sum += __shfl_xor(st.sum, 32);
+    const int me = fresh(lane), mr = me & 15, mg = me >> 4;
+    if (mg == 0) {
+      s_ref[wave][mr] = st.ref;
+      s_sum[wave][mr] = st.sum;
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] *= inv;
-      put_out(a, q.row0 + tr / G, h * G + tr % G, d, o);
-    } else {
-      *reinterpret_cast<float4*>(part + 32 + rr * HD + d) = make_float4(o[0], o[1], o[2], o[3]);
-      if (d == 0) *reinterpret_cast<float2*>(part + 2 * rr) = make_float2(ref, sum);
+    for (int hh = 0; hh < HD / 64; ++hh)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(&s_o[wave][mr][64 * hh + 16 * mg + 4 * i]) =
+            make_float4(st.o[4 * hh][i], st.o[4 * hh + 1][i], st.o[4 * hh + 2][i],
+                        st.o[4 * hh + 3][i]);
+    __syncthreads();
+    for (int x = fresh(threadIdx.x); x < 16 * HD / 4; x += 256) {
+      const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
+      if (tr >= q.rows * G) continue;
+      float ref = s_ref[0][rr];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
+      float sum = 0.f, o[4] = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
+        const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
+        sum += f * s_sum[w][rr];
+        o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
+      }
+      const int orow = q.row0 + tr / G, ohead = h * G + tr % G;
+      if (nsplit == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= inv;
+        put_out(a, orow, ohead, d, o);
+      } else {
+        const size_t at = ((size_t)orow * a.n_q + ohead) * nsplit + split;
+        *reinterpret_cast<float4*>(part_o + at * HD + d) = make_float4(o[0], o[1], o[2], o[3]);
+        if (d == 0) {
+          part_ml[2 * at] = ref;
+          part_ml[2 * at + 1] = sum;
+        }
+      }
     }
-  }
-  __syncthreads();
-}
-
-template <int HD, int NT>
-__global__ __launch_bounds__(256)
-__attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void
-k_kv8_attn_stream(Kv8 c, Kv8Rows r, Kv8Attn a, Stream sm) {
-  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int G = a.n_q / c.n_kv;
-  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  const Start start = find_start(c, r, G, sm);
-  int left = uniform((int)max(start.left, (int64_t)0)), b = uniform(start.b);
-  int64_t at = start.at;
-  bool first = true;
-  while (left > 0 && b < r.n_seqs) {
-    const Kv8Seq q = uniform(kv8_seq(c, r, b));
-    const int tiles = seq_tiles(q, G), steps = seq_steps(q, cap);
-    const int64_t work = (int64_t)steps * tiles * c.n_kv;
-    if (at >= work) {  // the sequence is done (or has no rows)
-      ++b;
-      at = 0;
-      continue;
-    }
-    const int unit = uniform((int)(at / steps)), s0 = uniform((int)(at - (int64_t)unit * steps));
-    const int n = min(left, steps - s0);
-    float* part = n == steps ? nullptr
-                             : sm.parts + (size_t)(2 * blockIdx.x + !first) * 16 * (HD + 2);
-    attend_tile<HD, NT>(c, a, q, unit % c.n_kv, unit / c.n_kv, s0, s0 + n, part, wave, lane);
-    first = false;
-    at += n;
-    left -= n;
+    __syncthreads();
   }
 }
 
-// Short sequences: one workgroup for each KV head, sequence and tile, nothing to merge.
-template <int HD, int NT>
-__global__ __launch_bounds__(256)
-__attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void
-k_kv8_attn_short(Kv8 c, Kv8Rows r, Kv8Attn a, int ntile) {
-  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const Kv8Seq q = uniform(kv8_seq(c, r, blockIdx.y));
-  const int tiles = seq_tiles(q, a.n_q / c.n_kv);
-  for (int tile = blockIdx.x / c.n_kv; tile < tiles; tile += ntile)
-    attend_tile<HD, NT>(c, a, q, blockIdx.x % c.n_kv, tile, 0, 0x7fffffff, nullptr, wave, lane);
-}
-
-// out = sum_i 2^(ref_i - ref) o_i / sum_i 2^(ref_i - ref) sum_i over the workgroups i that
-// share the tile of one row and head (none: it is written).  HD / 4 lanes of four dimensions
-// take every P-th of them, P groups of lanes a row and head, and are joined.
+// out = sum_s 2^(ref_s - ref) o_s / sum_s 2^(ref_s - ref) sum_s over the splits of one row
+// and head.  HD / 4 lanes of four dimensions take every P-th split each, P groups of them a
+// row and head, and are joined: by a group's lanes alone a head's 128 splits took 43 us one
+// after another.
 template <int HD>
-__global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Attn a, Stream sm) {
+__global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit) {
   constexpr int L = HD / 4, P = 256 / L;
   __shared__ float4 s_o[P][L];
   __shared__ float2 s_ml[P];
-  __shared__ int s_n[4];
   const int64_t u = blockIdx.x;
-  const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane, G = a.n_q / c.n_kv;
+  const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane;
   const int row = (int)(u / a.n_q), head = (int)(u - (int64_t)row * a.n_q);
-  int b = r.kind == KV8_CHUNK ? 0 : row;
-  if (r.kind == KV8_ARRAYS && r.row_start) {  // the sequences that start at or before the row
-    int n = 0;
-    for (int j = threadIdx.x; j <= r.n_seqs; j += 256) n += r.row_start[j] <= row;
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m);
-    if ((threadIdx.x & 63) == 0) s_n[threadIdx.x >> 6] = n;
-    __syncthreads();
-    b = s_n[0] + s_n[1] + s_n[2] + s_n[3] - 1;
-  }
-  if (b < 0 || b >= r.n_seqs) return;  // a row of no sequence
-  const Kv8Seq q = kv8_seq(c, r, b);
-  if (row < q.row0 || row >= q.row0 + q.rows) return;
-  const int tr = (row - q.row0) * G + head % G, tile = tr >> 4, rr = tr & 15;
-  const int64_t cap = (int64_t)c.max_pages << c.page_shift, per = sm.plan[r.n_seqs + 1];
-  const int steps = seq_steps(q, cap);
-  const int64_t s0 = sm.plan[b] + ((int64_t)tile * c.n_kv + head / G) * steps;
-  const int64_t i0 = s0 / per, i1 = (s0 + steps - 1) / per;
-  if (i0 == i1) return;
+  if (r.kind == KV8_ARRAYS && r.row_start &&
+      (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
+    return;  // a row of no sequence
+  const float2* ml = reinterpret_cast<const float2*>(a.work) + (size_t)u * nsplit;
+  const float* po = a.work + ((size_t)r.n_rows * a.n_q * 2 + (size_t)u * HD) * nsplit + d;
   float ref = kNoRef, sum = 0.f, o[4] = {};
 #pragma unroll 4
-  for (int64_t i = i0 + p; i <= i1; i += P) {
-    // a workgroup's slots: the tile it starts with, and the one it ends with
-    const float* part = sm.parts + (size_t)(2 * i + (i * per < s0)) * 16 * (HD + 2);
-    const float2 m = *reinterpret_cast<const float2*>(part + 2 * rr);
-    const float4 v = *reinterpret_cast<const float4*>(part + 32 + rr * HD + d);
+  for (int s = p; s < nsplit; s += P) {
+    const float2 m = ml[s];
+    const float4 v = *reinterpret_cast<const float4*>(po + (size_t)s * HD);
     const float now = fmaxf(ref, m.x);
     const float f = __builtin_amdgcn_exp2f(ref - now), g = __builtin_amdgcn_exp2f(m.x - now);
     ref = now;
@@ -631,61 +513,48 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 
 // ------------------------------------------------------------------- launcher
 namespace {
-
-// Workgroups of the stream that the chip holds at once: 4, 3 or 2 wavefronts a SIMD.
-constexpr int kCus = 256;
-int stream_blocks(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
-
+constexpr int kBlocks = 768;  // what the chip holds at once (128 dimensions, bf16 rows)
 struct Plan {
-  bool split;
-  int ntile, blocks;
+  int ntile, nsplit;
 };
-Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
+Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_length) {
   const int G = n_q / n_kv;
-  Plan p{};
+  Plan p;
   p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
-  const int64_t tiles = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t steps = std::max<int64_t>(1, ((int64_t)max_length + kStep - 1) / kStep);
-  p.split = steps > kMinSteps;
-  p.blocks = (int)std::min<int64_t>(stream_blocks(hd, terms),
-                                    (tiles * steps + kMinSteps - 1) / kMinSteps);
+  const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
+  const int64_t want = std::max<int64_t>(1, kBlocks / blocks);
+  const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
 }
-size_t plan_floats(int n_seqs) { return ((size_t)n_seqs + 2 + 1) / 2 * 4; }  // in 16-byte units
-
 }  // namespace
 
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
-  const Plan p = plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
-  return p.split ? plan_floats(n_seqs) + (size_t)p.blocks * 2 * 16 * (hd + 2) : 0;
-}
-size_t kv8_attn_floats_most(int hd, int n_seqs) {
-  return plan_floats(n_seqs) + (size_t)stream_blocks(hd, 1) * 2 * 16 * (hd + 2);
+  const Plan p = plan(n_q, n_kv, n_seqs, n_rows, max_rows, max_length);
+  return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
 }
 
+// a split launch has at most kBlocks workgroups of 16 rows x heads
+size_t kv8_attn_floats_most(int hd) { return (size_t)kBlocks * 16 * (hd + 2); }
+
 template <int HD>
-static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int edge) {
-  // two fp16 terms unless queries and output are bf16
-  const int terms = a.q.bf16 && a.out.p && a.out.bf16 ? 1 : 2;
-  const Plan p = plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
-  const int64_t gx = (int64_t)c.n_kv * p.ntile, mx = (int64_t)r.n_rows * a.n_q;
-  if (gx > 0x7fffffff || mx > 0x7fffffff || r.n_seqs > 65535 || (p.split && !a.work))
-    return hipErrorInvalidValue;
-  if (!p.split) {
-    const dim3 grid((unsigned)gx, r.n_seqs);
-    if (terms == 1)
-      launch_k(k_kv8_attn_short<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.ntile);
-    else
-      launch_k(k_kv8_attn_short<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.ntile);
-    return hipGetLastError();
-  }
-  const Stream sm{reinterpret_cast<int64_t*>(a.work), a.work + plan_floats(r.n_seqs), kMinSteps};
-  if (terms == 1)
-    launch_k(k_kv8_attn_stream<HD, 1>, dim3(p.blocks), dim3(256), 0, st, edge & kFirst, c, r, a, sm);
+static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
+  const Plan p = plan(a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
+  const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
+  if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)gx, r.n_seqs);
+  const int edge = p.nsplit == 1 ? last : last & kFirst;
+  if (a.q.bf16 && a.out.p && a.out.bf16)
+    launch_k(k_kv8_attn_split<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
   else
-    launch_k(k_kv8_attn_stream<HD, 2>, dim3(p.blocks), dim3(256), 0, st, edge & kFirst, c, r, a, sm);
-  launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mx), dim3(256), 0, st, edge & kLast, c, r, a, sm);
+    launch_k(k_kv8_attn_split<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
+  if (p.nsplit > 1) {
+    const int64_t mg = (int64_t)r.n_rows * a.n_q;
+    if (mg > 0x7fffffff) return hipErrorInvalidValue;
+    launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, last & kLast, c, r, a,
+             p.nsplit);
+  }
   return hipGetLastError();
 }
 

@@ -185,7 +185,7 @@ Layout make_layout(const wici_config& c) {
   L.gemm_sync = o; o = align_up(o + (size_t)wici::kGemmRowsSyncInts * 4);
   // partial results of the attention over an 8-bit cache
   L.kv8_work = o;
-  if (c.kv_dtype == WICI_KV8) o = align_up(o + wici::kv8_attn_floats_most(c.head_dim, kMaxBatch) * 4);
+  if (c.kv_dtype == WICI_KV8) o = align_up(o + wici::kv8_attn_floats_most(c.head_dim) * 4);
   L.scratch_bytes = o;
   return L;
 }
