@@ -98,12 +98,12 @@ struct Values {
 struct Pages {
   int phys[2];
 };
-__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int j0) {
+__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
   Pages p;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
     p.phys[t] = uniform(
-        kv8_page(q.table, (j0 + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
+        kv8_page(q.table, (step * kStep + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
   return p;
 }
 
@@ -327,8 +327,8 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
 // ------------------------------------------------------------------- split over positions
 // Workgroup (KV head, sequence, split): four wavefronts take the split's steps of 32
 // positions in turn for a tile of 16 of the sequence's rows x query heads of the group
-// (row r: new row r / G, query head r % G), and are joined at the end.  A split's range
-// follows from the sequence's own length, so one launch serves any length.  With one
+// (row r: new row r / G, query head r % G), and are joined at the end.  Splits take
+// groups of four steps in turn, so one launch serves any length evenly.  With one
 // split the output is written here, otherwise (ref, sum, output) to `part` for the merge.
 template <int HD, int NT>
 __global__ __launch_bounds__(256)
@@ -344,19 +344,26 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   const int64_t cap = (int64_t)c.max_pages << c.page_shift;
   float* part_ml = a.work;
   float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
+  // the wavefront's first steps do not depend on the length, so that their pages are
+  // looked up beside it
+  const int s0 = 4 * split + wave;
+  const Pages p0 = find_pages(c, q, s0), p1 = find_pages(c, q, s0 + 4 * nsplit);
 
   for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
     const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
     const bool on = row < q.rows;
     const int rc = min(row, q.rows - 1);
+    half8_t qf[NT][HD / 32];
+    float unit;
+    load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf,
+                         unit);
+    unit *= a.scale * kLog2e;
     // a row sees the positions up to its own; the tile's last row sees the most
     const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-    const int limit = on ? seen(row) : 0, most = seen(last), least = seen(first);
-    const int steps = (most + kStep - 1) / kStep, per = (steps + nsplit - 1) / nsplit;
-    const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep - 1) / kStep;
     // steps that all 16 rows see whole
-    const int whole = 16 * tile + 15 < q.rows * G ? least / kStep : 0;
+    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
 
     RowState<HD> st;
     st.ref = kNoRef;
@@ -364,46 +371,40 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     bool huge = false;
 #pragma unroll
     for (int u = 0; u < HD / 16; ++u) st.o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    if (s0 < s1) {
-      half8_t qf[NT][HD / 32];
-      float unit;
-      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane,
-                           qf, unit);
-      unit *= a.scale * kLog2e;
-      // the next step's keys are requested once this one's are multiplied, its values
-      // likewise, and its pages (which those addresses wait for) a step earlier
-      int s = s0 + wave;
-      if (s < s1) {
-        Keys<HD> k;
-        Values<HD> v;
-        Pages now = find_pages(c, q, s * kStep), next = find_pages(c, q, (s + 4) * kStep);
-        load_keys<HD>(k, c, q, now, h, s * kStep, lane);
-        load_values<HD>(v, c, q, now, h, s * kStep, lane);
-        for (;;) {
-          floatx4_t sc[2];
-          scores<HD, NT>(sc, k, qf);
-          const int then = s + 4;
-          if (then < s1) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
-          half8_t wf[NT];
-          float corr = 1.f;
-          const bool move =
-              s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
-                  ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
-                  : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane,
-                                          corr);
-          if (move) {
+    // the next step's keys are requested once this one's are multiplied, its values
+    // likewise, and its pages (which those addresses wait for) a step earlier
+    const int stride = 4 * nsplit;
+    int s = s0;
+    if (s < steps) {
+      Keys<HD> k;
+      Values<HD> v;
+      Pages now = p0, next = p1;
+      load_keys<HD>(k, c, q, now, h, s * kStep, lane);
+      load_values<HD>(v, c, q, now, h, s * kStep, lane);
+      for (;;) {
+        floatx4_t sc[2];
+        scores<HD, NT>(sc, k, qf);
+        const int then = s + stride;
+        if (then < steps) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
+        half8_t wf[NT];
+        float corr = 1.f;
+        const bool move =
+            s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
+                ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
+                : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane,
+                                        corr);
+        if (move) {
 #pragma unroll
-            for (int u = 0; u < HD / 16; ++u)
+          for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
-          }
-          add_values<HD, NT>(st, v, wf);
-          if (then >= s1) break;
-          load_values<HD>(v, c, q, next, h, then * kStep, lane);
-          now = next;
-          next = find_pages(c, q, (then + 4) * kStep);
-          s = then;
+            for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
         }
+        add_values<HD, NT>(st, v, wf);
+        if (then >= steps) break;
+        load_values<HD>(v, c, q, next, h, then * kStep, lane);
+        now = next;
+        next = find_pages(c, q, then + stride);
+        s = then;
       }
     }
     if (huge) {
@@ -513,16 +514,18 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 
 // ------------------------------------------------------------------- launcher
 namespace {
-constexpr int kBlocks = 768;  // what the chip holds at once (128 dimensions, bf16 rows)
+// Workgroups that the chip holds at once: 4, 3 or 2 wavefronts a SIMD.
+constexpr int kCus = 256;
+int resident(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
 struct Plan {
   int ntile, nsplit;
 };
-Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_length) {
+Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_length) {
   const int G = n_q / n_kv;
   Plan p;
   p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
   const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t want = std::max<int64_t>(1, kBlocks / blocks);
+  const int64_t want = std::max<int64_t>(1, resident(hd, terms) / blocks);
   const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
@@ -531,21 +534,23 @@ Plan plan(int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_lengt
 
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
-  const Plan p = plan(n_q, n_kv, n_seqs, n_rows, max_rows, max_length);
+  const Plan p = plan(hd, 1, n_q, n_kv, n_seqs, n_rows, max_rows, max_length);
   return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
 }
 
-// a split launch has at most kBlocks workgroups of 16 rows x heads
-size_t kv8_attn_floats_most(int hd) { return (size_t)kBlocks * 16 * (hd + 2); }
+// a split launch has at most resident() workgroups of 16 rows x heads
+size_t kv8_attn_floats_most(int hd) { return (size_t)resident(hd, 1) * 16 * (hd + 2); }
 
 template <int HD>
 static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
-  const Plan p = plan(a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
+  // two fp16 terms unless queries and output are bf16
+  const int terms = a.q.bf16 && a.out.p && a.out.bf16 ? 1 : 2;
+  const Plan p = plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
   const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
   if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)gx, r.n_seqs);
   const int edge = p.nsplit == 1 ? last : last & kFirst;
-  if (a.q.bf16 && a.out.p && a.out.bf16)
+  if (terms == 1)
     launch_k(k_kv8_attn_split<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
   else
     launch_k(k_kv8_attn_split<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
