@@ -37,7 +37,6 @@ constexpr float kNoRef = -3e38f;    // ref before the first weight
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
 constexpr float kHugeScore = 16777216.f;
-constexpr int kStep = 32;           // positions a wavefront takes at a time: two tiles of 16
 
 // Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
 // Both steps are exact.
@@ -83,27 +82,41 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
-// The codes and scales of 32 positions (two tiles of 16), as one lane holds them.
+// Tiles of 16 positions that a wavefront takes at a time, a step.
+template <int HD>
+constexpr int kTiles = 2;
+template <int HD>
+constexpr int kStep = 16 * kTiles<HD>;
+
+// The codes and scales of a step, as one lane holds them.
 template <int HD>
 struct Keys {
-  uint4 k[2][HD / 64];      // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
+  uint4 k[kTiles<HD>][HD / 64];  // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
 };
 template <int HD>
 struct Values {
-  uint4 v[2][HD / 64];      // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
-  float4 ks[2], vs[2];      // key and value scales of positions 4 (l / 16) .. + 3
+  uint4 v[kTiles<HD>][HD / 64];  // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
+  float4 ks[kTiles<HD>], vs[kTiles<HD>];  // key and value scales of positions 4 (l / 16) .. + 3
 };
 
-// The pages of a step's two tiles (-1: none).
+// The pages of a step's tiles (-1: none).
+template <int HD>
 struct Pages {
-  int phys[2];
-};
-__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
-  Pages p;
+  int phys[kTiles<HD>];
+  __device__ __forceinline__ bool all() const {
+    int m = 0;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < kTiles<HD>; ++t) m |= phys[t];
+    return m >= 0;
+  }
+};
+template <int HD>
+__device__ __forceinline__ Pages<HD> find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
+  Pages<HD> p;
+#pragma unroll
+  for (int t = 0; t < kTiles<HD>; ++t)
     p.phys[t] = uniform(
-        kv8_page(q.table, (step * kStep + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
+        kv8_page(q.table, (step * kStep<HD> + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
   return p;
 }
 
@@ -122,11 +135,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rsrc(const Kv8& c, const
 }
 template <int HD>
 __device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const Kv8Seq& q,
-                                          const Pages& p, int h, int j0, int lane) {
+                                          const Pages<HD>& p, int h, int step, int lane) {
   const int page = 1 << c.page_shift, mine = kv8_key_at(lane & 15, (lane >> 4) * (HD / 4), HD);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int slot = (j0 + 16 * t) & (page - 1);
+  for (int t = 0; t < kTiles<HD>; ++t) {
+    const int slot = (step * kStep<HD> + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = block_rsrc<HD>(c, q, p.phys[t], 0, h);
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i) s.k[t][i] = fetch(b, mine + 16 * i, kv8_key_at(slot, 0, HD));
@@ -134,11 +147,11 @@ __device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const Kv8Se
 }
 template <int HD>
 __device__ __forceinline__ void load_values(Values<HD>& s, const Kv8& c, const Kv8Seq& q,
-                                            const Pages& p, int h, int j0, int lane) {
+                                            const Pages<HD>& p, int h, int step, int lane) {
   const int page = 1 << c.page_shift, g = lane >> 4, mine = kv8_value_at(4 * g, 4 * (lane & 15), HD);
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int slot = (j0 + 16 * t) & (page - 1);
+  for (int t = 0; t < kTiles<HD>; ++t) {
+    const int slot = (step * kStep<HD> + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, p.phys[t], 0, h);
     const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, p.phys[t], 1, h);
     s.ks[t] = __builtin_bit_cast(float4, fetch(kb, 16 * g, kv8_scale_at(slot, page, HD)));
@@ -151,10 +164,10 @@ __device__ __forceinline__ void load_values(Values<HD>& s, const Kv8& c, const K
 
 // S^T of one step: sc[t][i] is the product of position 16 t + 4 (l / 16) + i with row l % 16.
 template <int HD, int NT>
-__device__ __forceinline__ void scores(floatx4_t (&sc)[2], const Keys<HD>& s,
+__device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles<HD>], const Keys<HD>& s,
                                        const half8_t (&qf)[NT][HD / 32]) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < kTiles<HD>; ++t) {
     const unsigned* w = reinterpret_cast<const unsigned*>(&s.k[t][0]);
     sc[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -172,9 +185,9 @@ __device__ __forceinline__ void scores(floatx4_t (&sc)[2], const Keys<HD>& s,
 // positions below `seen`, of the tiles that are there.  Returns whether a row's reference
 // moved: the output so far is then to be multiplied by `corr`.
 template <int HD, int NT, bool MASKED>
-__device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, bool& huge,
-                                        const floatx4_t (&sc)[2], const Values<HD>& s,
-                                        const Pages& p, float q_unit, int seen, int lane,
+__device__ __forceinline__ bool weights(half8_t (&wf)[kTiles<HD> / 2][NT], RowState<HD>& st,
+                                        bool& huge, const floatx4_t (&sc)[kTiles<HD>],
+                                        const Values<HD>& s, const Pages<HD>& p, float q_unit, int seen, int lane,
                                         float& corr) {
   const int left = seen - 4 * (lane >> 4);
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
@@ -184,7 +197,7 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, boo
   auto weigh = [&](float down, auto f) {
     sum = most = 0.f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < kTiles<HD>; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float e = __builtin_amdgcn_exp2f(on(t, i) ? f(t, i) : -INFINITY);
@@ -196,8 +209,9 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, boo
         most = fmaxf(most, w);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          wf[n][4 * t + i] = (_Float16)w;
-          w -= (float)wf[n][4 * t + i];
+          const _Float16 term = (_Float16)w;
+          wf[t / 2][n][4 * (t & 1) + i] = term;
+          w -= (float)term;
         }
       }
   };
@@ -218,7 +232,7 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, boo
     auto largest = [&](auto f) {
       float z = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < kTiles<HD>; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (on(t, i)) z = fmaxf(z, f(t, i));
@@ -246,23 +260,25 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState<HD>& st, boo
   return move;
 }
 
-// O^T += C^T W^T of one step.
+// O^T += C^T W^T of one step, two tiles (32 positions) a product.
 template <int HD, int NT>
 __device__ __forceinline__ void add_values(RowState<HD>& st, const Values<HD>& s,
-                                           const half8_t (&wf)[NT]) {
+                                           const half8_t (&wf)[kTiles<HD> / 2][NT]) {
 #pragma unroll
-  for (int h = 0; h < HD / 64; ++h) {
-    const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[0][h]);
-    const unsigned* v1 = reinterpret_cast<const unsigned*>(&s.v[1][h]);
+  for (int p = 0; p < kTiles<HD> / 2; ++p)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const half8_t a = codes8(v0[t], v1[t]);
+    for (int h = 0; h < HD / 64; ++h) {
+      const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[2 * p][h]);
+      const unsigned* v1 = reinterpret_cast<const unsigned*>(&s.v[2 * p + 1][h]);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        st.o[4 * h + t] =
-            __builtin_amdgcn_mfma_f32_16x16x32_f16(a, wf[n], st.o[4 * h + t], 0, 0, 0);
+      for (int t = 0; t < 4; ++t) {
+        const half8_t a = codes8(v0[t], v1[t]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          st.o[4 * h + t] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(a, wf[p][n], st.o[4 * h + t], 0, 0, 0);
+      }
     }
-  }
 }
 
 // Eight elements of a row from element offset `at` (a multiple of 8).
@@ -347,7 +363,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   // the wavefront's first steps do not depend on the length, so that their pages are
   // looked up beside it
   const int s0 = 4 * split + wave;
-  const Pages p0 = find_pages(c, q, s0), p1 = find_pages(c, q, s0 + 4 * nsplit);
+  const Pages<HD> p0 = find_pages<HD>(c, q, s0), p1 = find_pages<HD>(c, q, s0 + 4 * nsplit);
 
   for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
     const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
@@ -361,9 +377,9 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // a row sees the positions up to its own; the tile's last row sees the most
     const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep - 1) / kStep;
+    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep<HD> - 1) / kStep<HD>;
     // steps that all 16 rows see whole
-    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
+    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep<HD> : 0;
 
     RowState<HD> st;
     st.ref = kNoRef;
@@ -378,20 +394,20 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     if (s < steps) {
       Keys<HD> k;
       Values<HD> v;
-      Pages now = p0, next = p1;
-      load_keys<HD>(k, c, q, now, h, s * kStep, lane);
-      load_values<HD>(v, c, q, now, h, s * kStep, lane);
+      Pages<HD> now = p0, next = p1;
+      load_keys<HD>(k, c, q, now, h, s, lane);
+      load_values<HD>(v, c, q, now, h, s, lane);
       for (;;) {
-        floatx4_t sc[2];
+        floatx4_t sc[kTiles<HD>];
         scores<HD, NT>(sc, k, qf);
         const int then = s + stride;
-        if (then < steps) load_keys<HD>(k, c, q, next, h, then * kStep, lane);
-        half8_t wf[NT];
+        if (then < steps) load_keys<HD>(k, c, q, next, h, then, lane);
+        half8_t wf[kTiles<HD> / 2][NT];
         float corr = 1.f;
         const bool move =
-            s < whole && now.phys[0] >= 0 && now.phys[1] >= 0
+            s < whole && now.all()
                 ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
-                : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep, lane,
+                : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep<HD>, lane,
                                         corr);
         if (move) {
 #pragma unroll
@@ -401,9 +417,9 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         }
         add_values<HD, NT>(st, v, wf);
         if (then >= steps) break;
-        load_values<HD>(v, c, q, next, h, then * kStep, lane);
+        load_values<HD>(v, c, q, next, h, then, lane);
         now = next;
-        next = find_pages(c, q, then + stride);
+        next = find_pages<HD>(c, q, then + stride);
         s = then;
       }
     }
@@ -526,7 +542,8 @@ Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int n_rows, int max_
   p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
   const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
   const int64_t want = std::max<int64_t>(1, resident(hd, terms) / blocks);
-  const int64_t most = std::max<int64_t>(1, (max_length + 4 * kStep - 1) / (4 * kStep));
+  const int64_t least = hd == 64 ? 4 * kStep<64> : 4 * kStep<128>;  // a step a wavefront
+  const int64_t most = std::max<int64_t>(1, (max_length + least - 1) / least);
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
 }

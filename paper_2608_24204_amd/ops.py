@@ -31,6 +31,12 @@ HeadRows = binding.WiciHeadRows
 _NO_ROWS = HeadRows()
 
 
+# The current stream of a GPU as the library takes it.  Of a small call's time on the host
+# torch.cuda.current_stream is 2 us, its raw form 0.2.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _check(st: int, what: str) -> None:
     if st != WICI_OK:
         raise WiciError(st, what)
@@ -39,9 +45,11 @@ def _check(st: int, what: str) -> None:
 def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> HeadRows:
     """x [rows, heads, head_dim] as the library takes it (strides of its own, dimensions
     side by side)."""
-    if x.dtype not in _DTYPES:
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
         raise TypeError(f"{name}: dtype {x.dtype} (float32 or bfloat16)")
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected [rows, {heads}, {head_dim}]")
     if x.device != device:
         raise ValueError(f"{name}: on {x.device}, expected {device}")
@@ -50,9 +58,9 @@ def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> Head
         raise ValueError(f"{name}: the dimensions of a head must lie side by side")
     if heads == 1:
         h = head_dim
-    if x.shape[0] <= 1:
+    if shape[0] <= 1:
         r = heads * max(h, head_dim)
-    return HeadRows(x.data_ptr(), _DTYPES[x.dtype], r, h)
+    return HeadRows(x.data_ptr(), dtype, r, h)
 
 
 def _ints(x: torch.Tensor, shape, name: str, device) -> int:
@@ -63,37 +71,50 @@ def _ints(x: torch.Tensor, shape, name: str, device) -> int:
     return x.data_ptr()
 
 
+def _like(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _on_gpu(x: torch.Tensor, name: str):
     if not x.is_cuda:
         raise ValueError(f"{name}: on {x.device}, expected a HIP GPU")
     return x.device
 
 
-@contextlib.contextmanager
-def _other_stream(stream, device, tensors):
-    with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield stream.cuda_stream
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+class _Here:
+    """The raw current stream, where the tensors' GPU is current."""
+
+    def __init__(self, raw):
+        self.raw = raw
+
+    def __enter__(self):
+        return self.raw
+
+    def __exit__(self, *exc):
+        return False
 
 
 @contextlib.contextmanager
-def _other_device(device):
+def _elsewhere(stream, device, tensors):
     with torch.cuda.device(device):
-        yield torch.cuda.current_stream(device).cuda_stream
+        if stream is None:
+            yield _raw_stream(device.index)
+            return
+        with torch.cuda.stream(stream):
+            yield stream.cuda_stream
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
 
 
 def _launch_on(stream, device, *tensors):
     """Context giving the raw stream, with the tensors' GPU current and allocations made
     for that stream."""
-    if stream is not None and stream != torch.cuda.current_stream(device):
-        if stream.device != device:
-            raise ValueError(f"stream: on {stream.device}, expected {device}")
-        return _other_stream(stream, device, tensors)
-    if device.index == torch.cuda.current_device():
-        return contextlib.nullcontext(torch.cuda.current_stream(device).cuda_stream)
-    return _other_device(device)
+    if stream is None and device.index == torch.cuda.current_device():
+        return _Here(_raw_stream(device.index))
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, expected {device}")
+    return _elsewhere(stream, device, tensors)
 
 
 class RopeTable:
@@ -163,16 +184,16 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     lib = binding.load_library()
     with _launch_on(stream, device, x, positions, out) as raw:
         if out is None:
-            out = torch.empty((n, h, d), dtype=x.dtype, device=device)
+            out = _like(x)
         elif out.shape[0] != n:
             raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
         if n == 0:
             return out
-        _check(lib.wici_rope_rows(ctypes.byref(table._c), d, n, h,
-                                  _ints(positions, (n,), "positions", device),
-                                  _rows(x, h, d, "x", device), _rows(out, h, d, "out", device), raw),
-               f"rope: {h} heads of {d}, {table.dim} rotated (strides multiples of 8, 16-byte "
-               "aligned rows)")
+        st = lib.wici_rope_rows(table._c, d, n, h, _ints(positions, (n,), "positions", device),
+                                _rows(x, h, d, "x", device), _rows(out, h, d, "out", device), raw)
+        if st:
+            _check(st, f"rope: {h} heads of {d}, {table.dim} rotated (strides multiples of 8, "
+                   "16-byte aligned rows)")
     return out
 
 
@@ -243,7 +264,7 @@ class KvCache:
             if q is not None:
                 heads = q.shape[1]
                 if q_out is None:
-                    q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                    q_out = _like(q)
                 elif q_out.shape[0] != n:
                     raise ValueError(f"q_out: {q_out.shape[0]} rows, expected {n}")
                 qr, qo = _rows(q, heads, d, "q", dev), _rows(q_out, heads, d, "q_out", dev)
@@ -293,7 +314,7 @@ class KvCache:
         with _launch_on(stream, dev, q, length, row_start, out, workspace) as raw:
             b = self._batch(n, length, row_start, max_rows, max_length)
             if out is None:
-                out = torch.empty((n, heads, d), dtype=q.dtype, device=dev)
+                out = _like(q)
             elif out.shape[0] != n:
                 raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
             need = self._workspace(b, heads)
@@ -302,18 +323,20 @@ class KvCache:
             elif workspace.device != dev or not workspace.is_contiguous():
                 raise ValueError(f"workspace: contiguous on {dev} expected")
             size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-            _check(self.lib.wici_kv8_attend(
+            st = self.lib.wici_kv8_attend(
                 self._c, b, heads, d ** -0.5 if scale is None else scale,
                 _rows(q, heads, d, "q", dev), _rows(out, heads, d, "out", dev),
-                None if workspace is None else workspace.data_ptr(), size, raw),
-                f"attend: {heads} query heads on {self.n_kv_heads}, {need} workspace bytes (strides "
-                "multiples of 8, 16-byte aligned rows)")
+                None if workspace is None else workspace.data_ptr(), size, raw)
+            if st:
+                _check(st, f"attend: {heads} query heads on {self.n_kv_heads}, {need} workspace "
+                       "bytes (strides multiples of 8, 16-byte aligned rows)")
         return out
 
     def _workspace(self, batch, heads: int) -> int:
         size = ctypes.c_size_t()
-        _check(self.lib.wici_kv8_attend_workspace(self._c, batch, heads, ctypes.byref(size)),
-               f"attend: {heads} query heads on {self.n_kv_heads}")
+        st = self.lib.wici_kv8_attend_workspace(self._c, batch, heads, size)
+        if st:
+            _check(st, f"attend: {heads} query heads on {self.n_kv_heads}")
         return size.value
 
     def attend_workspace(self, n_rows: int, heads: int, n_seqs: int, *, row_start: bool = False,
