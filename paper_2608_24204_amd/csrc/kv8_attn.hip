@@ -37,6 +37,8 @@ constexpr float kNoRef = -3e38f;    // ref before the first weight
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
 constexpr float kHugeScore = 16777216.f;
+constexpr int kTiles = 2;           // tiles of 16 positions that a wavefront takes at a time
+constexpr int kStep = 16 * kTiles;
 
 // Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
 // Both steps are exact.
@@ -55,12 +57,13 @@ __device__ __forceinline__ half8_t codes8(unsigned a, unsigned b) {
 }
 
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
-template <int HD>
 struct RowState {
-  float ref, sum;           // sum over this lane's positions
-  float lift;               // o holds 2^-lift of its sum (0 until a score passes kHugeScore)
-  floatx4_t o[HD / 16];     // tile 4 h + t, element i: dimension 64 h + 16 (l / 16) + 4 i + t
+  float ref = kNoRef, sum = 0.f;  // sum over this lane's positions
+  float lift = 0.f;  // the output holds 2^-lift of its sum (0 until a score passes kHugeScore)
 };
+// Output of 16 rows: tile 4 h + t, element i: dimension 64 h + 16 (l / 16) + 4 i + t.
+template <int HD>
+using RowOut = floatx4_t[HD / 16];
 
 // Values that are the same in every lane, as scalars: what is read through memory is not
 // known to be, and a buffer or a branch that depends on it would run lane by lane.
@@ -82,41 +85,30 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
-// Tiles of 16 positions that a wavefront takes at a time, a step.
-template <int HD>
-constexpr int kTiles = 2;
-template <int HD>
-constexpr int kStep = 16 * kTiles<HD>;
-
 // The codes and scales of a step, as one lane holds them.
 template <int HD>
 struct Keys {
-  uint4 k[kTiles<HD>][HD / 64];  // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
+  uint4 k[kTiles][HD / 64];  // tile t: position l % 16, dimensions (HD / 4) (l / 16) ..
 };
 template <int HD>
 struct Values {
-  uint4 v[kTiles<HD>][HD / 64];  // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
-  float4 ks[kTiles<HD>], vs[kTiles<HD>];  // key and value scales of positions 4 (l / 16) .. + 3
+  uint4 v[kTiles][HD / 64];  // positions 4 (l / 16) .. + 3, dimensions 64 h + 4 (l % 16) .. + 3
+};
+struct Scales {
+  float4 k[kTiles], v[kTiles];  // of the keys and values of positions 4 (l / 16) .. + 3
 };
 
 // The pages of a step's tiles (-1: none).
-template <int HD>
 struct Pages {
-  int phys[kTiles<HD>];
-  __device__ __forceinline__ bool all() const {
-    int m = 0;
-#pragma unroll
-    for (int t = 0; t < kTiles<HD>; ++t) m |= phys[t];
-    return m >= 0;
-  }
+  int phys[kTiles];
+  __device__ __forceinline__ bool all() const { return (phys[0] | phys[1]) >= 0; }
 };
-template <int HD>
-__device__ __forceinline__ Pages<HD> find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
-  Pages<HD> p;
+__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
+  Pages p;
 #pragma unroll
-  for (int t = 0; t < kTiles<HD>; ++t)
+  for (int t = 0; t < kTiles; ++t)
     p.phys[t] = uniform(
-        kv8_page(q.table, (step * kStep<HD> + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
+        kv8_page(q.table, (step * kStep + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
   return p;
 }
 
@@ -135,27 +127,27 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rsrc(const Kv8& c, const
 }
 template <int HD>
 __device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const Kv8Seq& q,
-                                          const Pages<HD>& p, int h, int step, int lane) {
+                                          const Pages& p, int h, int step, int lane) {
   const int page = 1 << c.page_shift, mine = kv8_key_at(lane & 15, (lane >> 4) * (HD / 4), HD);
 #pragma unroll
-  for (int t = 0; t < kTiles<HD>; ++t) {
-    const int slot = (step * kStep<HD> + 16 * t) & (page - 1);
+  for (int t = 0; t < kTiles; ++t) {
+    const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = block_rsrc<HD>(c, q, p.phys[t], 0, h);
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i) s.k[t][i] = fetch(b, mine + 16 * i, kv8_key_at(slot, 0, HD));
   }
 }
 template <int HD>
-__device__ __forceinline__ void load_values(Values<HD>& s, const Kv8& c, const Kv8Seq& q,
-                                            const Pages<HD>& p, int h, int step, int lane) {
+__device__ __forceinline__ void load_values(Values<HD>& s, Scales& sl, const Kv8& c, const Kv8Seq& q,
+                                            const Pages& p, int h, int step, int lane) {
   const int page = 1 << c.page_shift, g = lane >> 4, mine = kv8_value_at(4 * g, 4 * (lane & 15), HD);
 #pragma unroll
-  for (int t = 0; t < kTiles<HD>; ++t) {
-    const int slot = (step * kStep<HD> + 16 * t) & (page - 1);
+  for (int t = 0; t < kTiles; ++t) {
+    const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, p.phys[t], 0, h);
     const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, p.phys[t], 1, h);
-    s.ks[t] = __builtin_bit_cast(float4, fetch(kb, 16 * g, kv8_scale_at(slot, page, HD)));
-    s.vs[t] = __builtin_bit_cast(float4, fetch(vb, 16 * g, kv8_scale_at(slot, page, HD)));
+    sl.k[t] = __builtin_bit_cast(float4, fetch(kb, 16 * g, kv8_scale_at(slot, page, HD)));
+    sl.v[t] = __builtin_bit_cast(float4, fetch(vb, 16 * g, kv8_scale_at(slot, page, HD)));
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i)
       s.v[t][i] = fetch(vb, mine + 256 * i, kv8_value_at(slot, 0, HD));
@@ -164,10 +156,10 @@ __device__ __forceinline__ void load_values(Values<HD>& s, const Kv8& c, const K
 
 // S^T of one step: sc[t][i] is the product of position 16 t + 4 (l / 16) + i with row l % 16.
 template <int HD, int NT>
-__device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles<HD>], const Keys<HD>& s,
+__device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles], const Keys<HD>& s,
                                        const half8_t (&qf)[NT][HD / 32]) {
 #pragma unroll
-  for (int t = 0; t < kTiles<HD>; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     const unsigned* w = reinterpret_cast<const unsigned*>(&s.k[t][0]);
     sc[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -184,24 +176,24 @@ __device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles<HD>], const Keys<H
 // NT fp16 terms.  MASKED: some row does not see every position: row l % 16 sees the step's
 // positions below `seen`, of the tiles that are there.  Returns whether a row's reference
 // moved: the output so far is then to be multiplied by `corr`.
-template <int HD, int NT, bool MASKED>
-__device__ __forceinline__ bool weights(half8_t (&wf)[kTiles<HD> / 2][NT], RowState<HD>& st,
-                                        bool& huge, const floatx4_t (&sc)[kTiles<HD>],
-                                        const Values<HD>& s, const Pages<HD>& p, float q_unit, int seen, int lane,
+template <int NT, bool MASKED>
+__device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& huge,
+                                        const floatx4_t (&sc)[kTiles], const Scales& s,
+                                        const Pages& p, float q_unit, int seen, int lane,
                                         float& corr) {
   const int left = seen - 4 * (lane >> 4);
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
-  auto score = [&](int t, int i) { return sc[t][i] * ((&s.ks[t].x)[i] * q_unit); };
+  auto score = [&](int t, int i) { return sc[t][i] * ((&s.k[t].x)[i] * q_unit); };
   float sum, most;
   // f(t, i) is a score less the reference
   auto weigh = [&](float down, auto f) {
     sum = most = 0.f;
 #pragma unroll
-    for (int t = 0; t < kTiles<HD>; ++t)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float e = __builtin_amdgcn_exp2f(on(t, i) ? f(t, i) : -INFINITY);
-        float w = on(t, i) ? e * (&s.vs[t].x)[i] * down : 0.f;
+        float w = on(t, i) ? e * (&s.v[t].x)[i] * down : 0.f;
         // a product rounded once: joined with the conversion below, and not with the
         // difference, the first term is now and then not the one the second completes
         if (NT > 1) asm volatile("" : "+v"(w));
@@ -210,14 +202,14 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[kTiles<HD> / 2][NT], RowSt
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const _Float16 term = (_Float16)w;
-          wf[t / 2][n][4 * (t & 1) + i] = term;
+          wf[n][4 * t + i] = term;
           w -= (float)term;
         }
       }
   };
   auto plain = [&]() {
     weigh(1.f, [&](int t, int i) {
-      return __builtin_fmaf(sc[t][i], (&s.ks[t].x)[i] * q_unit, -st.ref);
+      return __builtin_fmaf(sc[t][i], (&s.k[t].x)[i] * q_unit, -st.ref);
     });
   };
   // with the rounded scores, which the huge scores of a tie share
@@ -232,14 +224,14 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[kTiles<HD> / 2][NT], RowSt
     auto largest = [&](auto f) {
       float z = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < kTiles<HD>; ++t)
+      for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (on(t, i)) z = fmaxf(z, f(t, i));
       z = fmaxf(z, __shfl_xor(z, 16));
       return fmaxf(z, __shfl_xor(z, 32));
     };
-    auto lv = [&](int t, int i) { return __builtin_amdgcn_logf((&s.vs[t].x)[i]); };
+    auto lv = [&](int t, int i) { return __builtin_amdgcn_logf((&s.v[t].x)[i]); };
     const float z = largest([&](int t, int i) { return score(t, i) + lv(t, i); });
     huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
     float ref = fmaxf(st.ref, z - kTopWeight), lift = 0.f;
@@ -260,25 +252,30 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[kTiles<HD> / 2][NT], RowSt
   return move;
 }
 
-// O^T += C^T W^T of one step, two tiles (32 positions) a product.
+// O^T += C^T W^T of one step.
 template <int HD, int NT>
-__device__ __forceinline__ void add_values(RowState<HD>& st, const Values<HD>& s,
-                                           const half8_t (&wf)[kTiles<HD> / 2][NT]) {
+__device__ __forceinline__ void add_values(RowOut<HD>& o, const Values<HD>& s,
+                                           const half8_t (&wf)[NT]) {
 #pragma unroll
-  for (int p = 0; p < kTiles<HD> / 2; ++p)
+  for (int h = 0; h < HD / 64; ++h) {
+    const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[0][h]);
+    const unsigned* v1 = reinterpret_cast<const unsigned*>(&s.v[1][h]);
 #pragma unroll
-    for (int h = 0; h < HD / 64; ++h) {
-      const unsigned* v0 = reinterpret_cast<const unsigned*>(&s.v[2 * p][h]);
-      const unsigned* v1 = reinterpret_cast<const unsigned*>(&s.v[2 * p + 1][h]);
+    for (int t = 0; t < 4; ++t) {
+      const half8_t a = codes8(v0[t], v1[t]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const half8_t a = codes8(v0[t], v1[t]);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-          st.o[4 * h + t] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(a, wf[p][n], st.o[4 * h + t], 0, 0, 0);
-      }
+      for (int n = 0; n < NT; ++n)
+        o[4 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, wf[n], o[4 * h + t], 0, 0, 0);
     }
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void rescale(RowOut<HD>& o, float f) {
+#pragma unroll
+  for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[u][i] *= f;
 }
 
 // Eight elements of a row from element offset `at` (a multiple of 8).
@@ -340,6 +337,23 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
   }
 }
 
+// Four dimensions of a row of one split: the output where it is the only one, else
+// (ref, sum, output) for the merge.
+__device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, float* part_ml,
+                                      float* part_o, int row, int head, int d, float ref, float sum,
+                                      float (&o)[4]) {
+  if (nsplit == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] *= inv;
+    put_out(a, row, head, d, o);
+  } else {
+    const size_t at = ((size_t)row * a.n_q + head) * nsplit + split;
+    *reinterpret_cast<float4*>(part_o + at * a.hd + d) = make_float4(o[0], o[1], o[2], o[3]);
+    if (d == 0) *reinterpret_cast<float2*>(part_ml + 2 * at) = make_float2(ref, sum);
+  }
+}
+
 // ------------------------------------------------------------------- split over positions
 // Workgroup (KV head, sequence, split): four wavefronts take the split's steps of 32
 // positions in turn for a tile of 16 of the sequence's rows x query heads of the group
@@ -363,7 +377,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   // the wavefront's first steps do not depend on the length, so that their pages are
   // looked up beside it
   const int s0 = 4 * split + wave;
-  const Pages<HD> p0 = find_pages<HD>(c, q, s0), p1 = find_pages<HD>(c, q, s0 + 4 * nsplit);
+  const Pages p0 = find_pages(c, q, s0), p1 = find_pages(c, q, s0 + 4 * nsplit);
 
   for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
     const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
@@ -377,16 +391,15 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // a row sees the positions up to its own; the tile's last row sees the most
     const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep<HD> - 1) / kStep<HD>;
+    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep - 1) / kStep;
     // steps that all 16 rows see whole
-    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep<HD> : 0;
+    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
 
-    RowState<HD> st;
-    st.ref = kNoRef;
-    st.sum = st.lift = 0.f;
+    RowState st;
+    RowOut<HD> o;
     bool huge = false;
 #pragma unroll
-    for (int u = 0; u < HD / 16; ++u) st.o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     // the next step's keys are requested once this one's are multiplied, its values
     // likewise, and its pages (which those addresses wait for) a step earlier
     const int stride = 4 * nsplit;
@@ -394,42 +407,31 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     if (s < steps) {
       Keys<HD> k;
       Values<HD> v;
-      Pages<HD> now = p0, next = p1;
+      Scales sl;
+      Pages now = p0, next = p1;
       load_keys<HD>(k, c, q, now, h, s, lane);
-      load_values<HD>(v, c, q, now, h, s, lane);
+      load_values<HD>(v, sl, c, q, now, h, s, lane);
       for (;;) {
-        floatx4_t sc[kTiles<HD>];
+        floatx4_t sc[kTiles];
         scores<HD, NT>(sc, k, qf);
         const int then = s + stride;
         if (then < steps) load_keys<HD>(k, c, q, next, h, then, lane);
-        half8_t wf[kTiles<HD> / 2][NT];
+        half8_t wf[NT];
         float corr = 1.f;
         const bool move =
             s < whole && now.all()
-                ? weights<HD, NT, false>(wf, st, huge, sc, v, now, unit, 0, lane, corr)
-                : weights<HD, NT, true>(wf, st, huge, sc, v, now, unit, limit - s * kStep<HD>, lane,
-                                        corr);
-        if (move) {
-#pragma unroll
-          for (int u = 0; u < HD / 16; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st.o[u][i] *= corr;
-        }
-        add_values<HD, NT>(st, v, wf);
+                ? weights<NT, false>(wf, st, huge, sc, sl, now, unit, 0, lane, corr)
+                : weights<NT, true>(wf, st, huge, sc, sl, now, unit, limit - s * kStep, lane, corr);
+        if (move) rescale<HD>(o, corr);
+        add_values<HD, NT>(o, v, wf);
         if (then >= steps) break;
-        load_values<HD>(v, c, q, next, h, then, lane);
+        load_values<HD>(v, sl, c, q, next, h, then, lane);
         now = next;
-        next = find_pages<HD>(c, q, then + stride);
+        next = find_pages(c, q, then + stride);
         s = then;
       }
     }
-    if (huge) {
-      const float up = __builtin_amdgcn_exp2f(st.lift);
-#pragma unroll
-      for (int u = 0; u < HD / 16; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.o[u][i] *= up;
-    }
+    if (huge) rescale<HD>(o, __builtin_amdgcn_exp2f(st.lift));
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);
     st.sum += __shfl_xor(st.sum, 32);
@@ -443,8 +445,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<float4*>(&s_o[wave][mr][64 * hh + 16 * mg + 4 * i]) =
-            make_float4(st.o[4 * hh][i], st.o[4 * hh + 1][i], st.o[4 * hh + 2][i],
-                        st.o[4 * hh + 3][i]);
+            make_float4(o[4 * hh][i], o[4 * hh + 1][i], o[4 * hh + 2][i], o[4 * hh + 3][i]);
     __syncthreads();
     for (int x = fresh(threadIdx.x); x < 16 * HD / 4; x += 256) {
       const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
@@ -452,30 +453,214 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
       float ref = s_ref[0][rr];
 #pragma unroll
       for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
-      float sum = 0.f, o[4] = {};
+      float sum = 0.f, all[4] = {};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
         const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
         sum += f * s_sum[w][rr];
-        o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
+        all[0] += f * v.x; all[1] += f * v.y; all[2] += f * v.z; all[3] += f * v.w;
       }
-      const int orow = q.row0 + tr / G, ohead = h * G + tr % G;
-      if (nsplit == 1) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+      leave(a, nsplit, split, part_ml, part_o, q.row0 + tr / G, h * G + tr % G, d, ref, sum, all);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------- prompts: row tiles
+// Workgroup (KV head, tile of 128 rows x query heads, split, sequence): each of four
+// wavefronts holds 32 rows and takes every chunk of 64 positions of the split.  The codes of
+// a chunk become fp16 operands once for all four, in LDS, lane by lane as the products read
+// them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers: the
+// next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
+// parts a buffer's readers from its next writers.  Bound by the softmax's vector work
+// (about eight issue slots a score, four of them the exponential, beside two matrix
+// products).  Tiles are taken from the last one back: it sees the most positions.
+constexpr int kRowTiles = 2;                  // tiles of 16 rows a wavefront
+constexpr int kRows = 4 * 16 * kRowTiles;     // of a workgroup
+constexpr int kChunkTiles = 4;                // tiles of 16 positions a chunk
+constexpr int kChunkPos = 16 * kChunkTiles;
+
+template <int HD, int NT>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+                                                            int ntile) {
+  constexpr int DS = HD / 32, DT = HD / 16;
+  __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
+  __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
+  __shared__ float s_scale[2][2][kChunkPos];         // of keys, of values
+  const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
+  const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, g = lane >> 4, G = a.n_q / c.n_kv;
+  const Kv8Seq q = uniform(kv8_seq(c, r, b));
+  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+  const int page = 1 << c.page_shift;
+  float* part_ml = a.work;
+  float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
+  const int total = q.rows * G, tiles = (total + kRows - 1) / kRows;
+
+  for (int back = tile0; back < tiles; back += ntile) {
+    const int row0 = kRows * (tiles - 1 - back), mine = row0 + 16 * kRowTiles * wave;
+    auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
+    // this wavefront's rows: positions each sees, and the most and least any does
+    half8_t qf[kRowTiles][NT][DS];
+    float unit[kRowTiles];
+    int limit[kRowTiles], at_row[kRowTiles], at_head[kRowTiles];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] *= inv;
-        put_out(a, orow, ohead, d, o);
-      } else {
-        const size_t at = ((size_t)orow * a.n_q + ohead) * nsplit + split;
-        *reinterpret_cast<float4*>(part_o + at * HD + d) = make_float4(o[0], o[1], o[2], o[3]);
-        if (d == 0) {
-          part_ml[2 * at] = ref;
-          part_ml[2 * at + 1] = sum;
+    for (int x = 0; x < kRowTiles; ++x) {
+      const int qr = mine + 16 * x + r16, row = qr / G, rc = min(row, q.rows - 1);
+      const bool on = qr < total;
+      at_row[x] = on ? q.row0 + row : -1;
+      at_head[x] = h * G + qr % G;
+      limit[x] = on ? seen(row) : 0;
+      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + at_head[x] * a.q.head_stride, on,
+                           lane, qf[x], unit[x]);
+      unit[x] *= a.scale * kLog2e;
+    }
+    const int most = mine < total ? seen(min((mine + 16 * kRowTiles - 1) / G, q.rows - 1)) : 0;
+    const int least = mine + 16 * kRowTiles <= total ? seen(mine / G) : 0;
+    const int all = seen(min((row0 + kRows - 1) / G, q.rows - 1));  // of the workgroup's rows
+    const int chunks = (all + kChunkPos - 1) / kChunkPos, per = (chunks + nsplit - 1) / nsplit;
+    const int c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
+
+    RowState st[kRowTiles];
+    RowOut<HD> o[kRowTiles];
+    bool huge = false;
+#pragma unroll
+    for (int x = 0; x < kRowTiles; ++x)
+#pragma unroll
+      for (int u = 0; u < DT; ++u) o[x][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+
+    // what this wavefront brings of a chunk: the keys of tile `wave`; of the pair of tiles
+    // wave / 2 the values of half the dimensions (64 dimensions: of half of each word's four);
+    // the scales of the keys (wavefront 0) or values (1)
+    uint4 kc[HD / 64], vc[2];
+    float sc = 0.f;
+    int phys[kChunkTiles], later[kChunkTiles];
+    const int pair = wave >> 1, half = HD == 128 ? wave & 1 : 0;
+    auto find = [&](int (&p)[kChunkTiles], int chunk) {
+#pragma unroll
+      for (int t = 0; t < kChunkTiles; ++t)
+        p[t] = uniform(kv8_page(q.table, ((int64_t)chunk * kChunkPos + 16 * t) >> c.page_shift,
+                                c.max_pages, c.n_pages));
+    };
+    auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
+      const int j0 = chunk * kChunkPos;
+      auto pick = [&](int t) { return t == 0 ? p[0] : t == 1 ? p[1] : t == 2 ? p[2] : p[3]; };
+      const int ks = (j0 + 16 * wave) & (page - 1);
+      const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, uniform(pick(wave)), 0, h);
+#pragma unroll
+      for (int i = 0; i < HD / 64; ++i)
+        kc[i] = fetch(kb, kv8_key_at(r16, g * (HD / 4), HD) + 16 * i, kv8_key_at(ks, 0, HD));
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int vs = (j0 + 32 * pair + 16 * t) & (page - 1);
+        const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, uniform(pick(2 * pair + t)), 1, h);
+        vc[t] = fetch(vb, kv8_value_at(4 * g, 4 * r16, HD) + 256 * half, kv8_value_at(vs, 0, HD));
+      }
+      if (wave < 2) {
+        const int at = max(pick(g), 0), slot = (j0 + lane) & (page - 1);
+        sc = *reinterpret_cast<const float*>(q.base + kv8_block_at(at, wave, h, c.n_kv, page, HD) +
+                                             kv8_scale_at(slot, page, HD));
+      }
+    };
+    auto convert = [&](int buf) {
+      const unsigned* w = reinterpret_cast<const unsigned*>(kc);
+#pragma unroll
+      for (int d = 0; d < DS; ++d)
+        s_k[buf][wave][d][lane] = __builtin_bit_cast(uint4, codes8(w[2 * d], w[2 * d + 1]));
+      const unsigned* v0 = reinterpret_cast<const unsigned*>(&vc[0]);
+      const unsigned* v1 = reinterpret_cast<const unsigned*>(&vc[1]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (HD == 128 || (t >> 1) == (wave & 1))
+          s_v[buf][pair][4 * half + t][lane] = __builtin_bit_cast(uint4, codes8(v0[t], v1[t]));
+      if (wave < 2) s_scale[buf][wave][lane] = sc;
+    };
+
+    if (c0 < c1) {
+      find(phys, c0);
+      bring(phys, c0);
+      find(later, c0 + 1);
+    }
+    for (int ch = c0; ch < c1; ++ch) {
+      const int buf = (ch - c0) & 1;
+      convert(buf);
+      int now[kChunkTiles];
+#pragma unroll
+      for (int t = 0; t < kChunkTiles; ++t) {
+        now[t] = phys[t];
+        phys[t] = later[t];
+      }
+      if (ch + 1 < c1) {
+        bring(phys, ch + 1);
+        find(later, ch + 2);
+      }
+      __syncthreads();
+      if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
+#pragma unroll
+      for (int p = 0; p < kChunkTiles / 2; ++p) {
+        const int j0 = ch * kChunkPos + 32 * p;
+        Pages pg;
+        Scales sl;
+        floatx4_t x[kRowTiles][kTiles];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          pg.phys[t] = now[2 * p + t];
+          sl.k[t] = *reinterpret_cast<const float4*>(&s_scale[buf][0][32 * p + 16 * t + 4 * g]);
+          sl.v[t] = *reinterpret_cast<const float4*>(&s_scale[buf][1][32 * p + 16 * t + 4 * g]);
+#pragma unroll
+          for (int y = 0; y < kRowTiles; ++y) x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int d = 0; d < DS; ++d) {
+            const half8_t k = __builtin_bit_cast(half8_t, s_k[buf][2 * p + t][d][lane]);
+#pragma unroll
+            for (int y = 0; y < kRowTiles; ++y)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[y][n][d], x[y][t], 0, 0, 0);
+          }
+        }
+        const bool whole = j0 + kStep <= least && pg.all();
+        half8_t wf[kRowTiles][NT];
+#pragma unroll
+        for (int y = 0; y < kRowTiles; ++y) {
+          float corr = 1.f;
+          const bool move =
+              whole ? weights<NT, false>(wf[y], st[y], huge, x[y], sl, pg, unit[y], 0, lane, corr)
+                    : weights<NT, true>(wf[y], st[y], huge, x[y], sl, pg, unit[y], limit[y] - j0,
+                                        lane, corr);
+          if (move) rescale<HD>(o[y], corr);
+        }
+#pragma unroll
+        for (int u = 0; u < DT; ++u) {
+          const half8_t v = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
+#pragma unroll
+          for (int y = 0; y < kRowTiles; ++y)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, wf[y][n], o[y][u], 0, 0, 0);
         }
       }
     }
-    __syncthreads();
+    __syncthreads();  // the buffers are free for the next tile
+#pragma unroll
+    for (int y = 0; y < kRowTiles; ++y) {
+      if (huge) rescale<HD>(o[y], __builtin_amdgcn_exp2f(st[y].lift));
+      st[y].sum += __shfl_xor(st[y].sum, 16);
+      st[y].sum += __shfl_xor(st[y].sum, 32);
+      if (at_row[y] < 0) continue;
+#pragma unroll
+      for (int hh = 0; hh < HD / 64; ++hh)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v[4] = {o[y][4 * hh][i], o[y][4 * hh + 1][i], o[y][4 * hh + 2][i],
+                        o[y][4 * hh + 3][i]};
+          leave(a, nsplit, split, part_ml, part_o, at_row[y], at_head[y], 64 * hh + 16 * g + 4 * i,
+                st[y].ref, st[y].sum, v);
+        }
+    }
   }
 }
 
@@ -534,16 +719,21 @@ namespace {
 constexpr int kCus = 256;
 int resident(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
 struct Plan {
+  bool tile;  // row tiles (prompts), else a split of few rows
   int ntile, nsplit;
 };
-Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows, int max_length) {
-  const int G = n_q / n_kv;
+// Rows x heads of a KV head from which the row tiles are taken.
+constexpr int kTileRows = 64;
+Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
+  const int64_t rows = (int64_t)max_rows * (n_q / n_kv);
   Plan p;
-  p.ntile = std::max(1, (int)(((int64_t)max_rows * G + 15) / 16));
+  p.tile = rows >= kTileRows;
+  const int64_t per = p.tile ? kRows : 16;
+  p.ntile = std::max(1, (int)((rows + per - 1) / per));
   const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t want = std::max<int64_t>(1, resident(hd, terms) / blocks);
-  const int64_t least = hd == 64 ? 4 * kStep<64> : 4 * kStep<128>;  // a step a wavefront
-  const int64_t most = std::max<int64_t>(1, (max_length + least - 1) / least);
+  const int64_t want = (p.tile ? 2 * kCus : resident(hd, terms)) / blocks;
+  const int64_t least = p.tile ? 2 * kChunkPos : 4 * kStep;  // positions worth a split
+  const int64_t most = (max_length + least - 1) / least;
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
   return p;
 }
@@ -551,26 +741,34 @@ Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int n_rows, int max_
 
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
-  const Plan p = plan(hd, 1, n_q, n_kv, n_seqs, n_rows, max_rows, max_length);
+  const Plan p = plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
   return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
 }
 
-// a split launch has at most resident() workgroups of 16 rows x heads
-size_t kv8_attn_floats_most(int hd) { return (size_t)resident(hd, 1) * 16 * (hd + 2); }
+// (launches that split have at most resident() workgroups of 16 rows x heads, or 2 kCus of kRows)
+size_t kv8_attn_floats_most(int hd) {
+  return (size_t)std::max(resident(hd, 1) * 16, 2 * kCus * kRows) * (hd + 2);
+}
 
 template <int HD>
 static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
   // two fp16 terms unless queries and output are bf16
   const int terms = a.q.bf16 && a.out.p && a.out.bf16 ? 1 : 2;
-  const Plan p = plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, r.n_rows, a.max_rows, a.max_length);
+  const Plan p = plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
   const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
   if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)gx, r.n_seqs);
   const int edge = p.nsplit == 1 ? last : last & kFirst;
-  if (terms == 1)
-    launch_k(k_kv8_attn_split<HD, 1>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
-  else
-    launch_k(k_kv8_attn_split<HD, 2>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile);
+#define WICI_ATTN(kernel, nt) \
+  launch_k(kernel<HD, nt>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
+  if (p.tile) {
+    if (terms == 1) WICI_ATTN(k_kv8_attn_tile, 1);
+    else WICI_ATTN(k_kv8_attn_tile, 2);
+  } else {
+    if (terms == 1) WICI_ATTN(k_kv8_attn_split, 1);
+    else WICI_ATTN(k_kv8_attn_split, 2);
+  }
+#undef WICI_ATTN
   if (p.nsplit > 1) {
     const int64_t mg = (int64_t)r.n_rows * a.n_q;
     if (mg > 0x7fffffff) return hipErrorInvalidValue;
