@@ -25,6 +25,7 @@
 
 #include <algorithm>
 
+#include "kv8_plan.h"
 #include "launch.h"
 
 namespace wici {
@@ -37,8 +38,6 @@ constexpr float kNoRef = -3e38f;    // ref before the first weight
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
 constexpr float kHugeScore = 16777216.f;
-constexpr int kTiles = 2;           // tiles of 16 positions that a wavefront takes at a time
-constexpr int kStep = 16 * kTiles;
 
 // Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
 // Both steps are exact.
@@ -468,24 +467,21 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 }
 
 // ------------------------------------------------------------------- prompts: row tiles
-// Workgroup (KV head, tile of 128 rows x query heads, split, sequence): each of four
-// wavefronts holds 32 rows and takes every chunk of 64 positions of the split.  The codes of
+// Workgroup (KV head, tile of 128 (or 64) rows x query heads, split, sequence): each of
+// four wavefronts holds a quarter of the rows and takes every chunk of 64 positions of the split.  The codes of
 // a chunk become fp16 operands once for all four, in LDS, lane by lane as the products read
 // them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers: the
 // next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
 // parts a buffer's readers from its next writers.  Bound by the softmax's vector work
 // (about eight issue slots a score, four of them the exponential, beside two matrix
-// products).  Tiles are taken from the last one back: it sees the most positions.
-constexpr int kRowTiles = 2;                  // tiles of 16 rows a wavefront
-constexpr int kRows = 4 * 16 * kRowTiles;     // of a workgroup
-constexpr int kChunkTiles = 4;                // tiles of 16 positions a chunk
-constexpr int kChunkPos = 16 * kChunkTiles;
+// products).
 
-template <int HD, int NT>
+template <int HD, int NT, int kRowTiles>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                             int ntile) {
-  constexpr int DS = HD / 32, DT = HD / 16;
+  constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles;
+  constexpr bool kHold = kRowTiles * NT <= 2;  // a chunk's operands fit the registers
   __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
   __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
   __shared__ float s_scale[2][2][kChunkPos];         // of keys, of values
@@ -499,23 +495,26 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
   float* part_ml = a.work;
   float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
   const int total = q.rows * G, tiles = (total + kRows - 1) / kRows;
+  const bool two_a_cu = gridDim.x > kCus && gridDim.x * gridDim.y <= 2 * kCus && tiles <= ntile;
 
   for (int back = tile0; back < tiles; back += ntile) {
-    const int row0 = kRows * (tiles - 1 - back), mine = row0 + 16 * kRowTiles * wave;
+    // From the last tile back; with two workgroups a CU, the second half from the first tile
+    // on, so that a CU's two see about as many positions together as any other's.
+    const int first = (tiles + 1) / 2;
+    const int tile = two_a_cu && back >= first ? back - first : tiles - 1 - back;
+    const int row0 = kRows * tile, mine = row0 + 16 * kRowTiles * wave;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
     // this wavefront's rows: positions each sees, and the most and least any does
     half8_t qf[kRowTiles][NT][DS];
     float unit[kRowTiles];
-    int limit[kRowTiles], at_row[kRowTiles], at_head[kRowTiles];
+    int limit[kRowTiles];
 #pragma unroll
     for (int x = 0; x < kRowTiles; ++x) {
       const int qr = mine + 16 * x + r16, row = qr / G, rc = min(row, q.rows - 1);
       const bool on = qr < total;
-      at_row[x] = on ? q.row0 + row : -1;
-      at_head[x] = h * G + qr % G;
       limit[x] = on ? seen(row) : 0;
-      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + at_head[x] * a.q.head_stride, on,
-                           lane, qf[x], unit[x]);
+      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + (h * G + qr % G) * a.q.head_stride,
+                           on, lane, qf[x], unit[x]);
       unit[x] *= a.scale * kLog2e;
     }
     const int most = mine < total ? seen(min((mine + 16 * kRowTiles - 1) / G, q.rows - 1)) : 0;
@@ -604,61 +603,85 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
         const int j0 = ch * kChunkPos + 32 * p;
         Pages pg;
         Scales sl;
-        floatx4_t x[kRowTiles][kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
           pg.phys[t] = now[2 * p + t];
           sl.k[t] = *reinterpret_cast<const float4*>(&s_scale[buf][0][32 * p + 16 * t + 4 * g]);
           sl.v[t] = *reinterpret_cast<const float4*>(&s_scale[buf][1][32 * p + 16 * t + 4 * g]);
+        }
+        // Row tile after row tile: the matrix cores work on one's products while the vector
+        // units turn the other's scores into weights.
+        floatx4_t x[kRowTiles][kTiles];
+        half8_t op[DT];
 #pragma unroll
-          for (int y = 0; y < kRowTiles; ++y) x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int d = 0; d < DS; ++d) {
-            const half8_t k = __builtin_bit_cast(half8_t, s_k[buf][2 * p + t][d][lane]);
+            op[t * DS + d] = __builtin_bit_cast(half8_t, s_k[buf][2 * p + t][d][lane]);
+            if constexpr (!kHold) {
 #pragma unroll
-            for (int y = 0; y < kRowTiles; ++y)
+              for (int y = 0; y < kRowTiles; ++y) {
+                if (d == 0) x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
-                x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[y][n][d], x[y][t], 0, 0, 0);
+                for (int n = 0; n < NT; ++n)
+                  x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[t * DS + d], qf[y][n][d],
+                                                                   x[y][t], 0, 0, 0);
+              }
+            }
           }
-        }
-        const bool whole = j0 + kStep <= least && pg.all();
-        half8_t wf[kRowTiles][NT];
-#pragma unroll
-        for (int y = 0; y < kRowTiles; ++y) {
-          float corr = 1.f;
-          const bool move =
-              whole ? weights<NT, false>(wf[y], st[y], huge, x[y], sl, pg, unit[y], 0, lane, corr)
-                    : weights<NT, true>(wf[y], st[y], huge, x[y], sl, pg, unit[y], limit[y] - j0,
-                                        lane, corr);
-          if (move) rescale<HD>(o[y], corr);
-        }
-#pragma unroll
-        for (int u = 0; u < DT; ++u) {
-          const half8_t v = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
+        if constexpr (kHold) {
 #pragma unroll
           for (int y = 0; y < kRowTiles; ++y)
 #pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+              x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int d = 0; d < DS; ++d)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                  x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[t * DS + d], qf[y][n][d],
+                                                                   x[y][t], 0, 0, 0);
+            }
+#pragma unroll
+          for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
+        }
+        const bool whole = j0 + kStep <= least && pg.all();
+#pragma unroll
+        for (int y = 0; y < kRowTiles; ++y) {
+          float corr = 1.f;
+          half8_t wf[NT];
+          const bool move =
+              whole ? weights<NT, false>(wf, st[y], huge, x[y], sl, pg, unit[y], 0, lane, corr)
+                    : weights<NT, true>(wf, st[y], huge, x[y], sl, pg, unit[y], limit[y] - j0, lane,
+                                        corr);
+          if (move) rescale<HD>(o[y], corr);
+#pragma unroll
+          for (int u = 0; u < DT; ++u) {
+            if (!kHold) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
+#pragma unroll
             for (int n = 0; n < NT; ++n)
-              o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, wf[y][n], o[y][u], 0, 0, 0);
+              o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[u], wf[n], o[y][u], 0, 0, 0);
+          }
         }
       }
     }
     __syncthreads();  // the buffers are free for the next tile
+    const int me = fresh(lane), mg = me >> 4;
 #pragma unroll
     for (int y = 0; y < kRowTiles; ++y) {
       if (huge) rescale<HD>(o[y], __builtin_amdgcn_exp2f(st[y].lift));
       st[y].sum += __shfl_xor(st[y].sum, 16);
       st[y].sum += __shfl_xor(st[y].sum, 32);
-      if (at_row[y] < 0) continue;
+      const int qr = mine + 16 * y + (me & 15);
+      if (qr >= total) continue;
 #pragma unroll
       for (int hh = 0; hh < HD / 64; ++hh)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float v[4] = {o[y][4 * hh][i], o[y][4 * hh + 1][i], o[y][4 * hh + 2][i],
                         o[y][4 * hh + 3][i]};
-          leave(a, nsplit, split, part_ml, part_o, at_row[y], at_head[y], 64 * hh + 16 * g + 4 * i,
-                st[y].ref, st[y].sum, v);
+          leave(a, nsplit, split, part_ml, part_o, q.row0 + qr / G, h * G + qr % G,
+                64 * hh + 16 * mg + 4 * i, st[y].ref, st[y].sum, v);
         }
     }
   }
@@ -714,59 +737,37 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 }
 
 // ------------------------------------------------------------------- launcher
-namespace {
-// Workgroups that the chip holds at once: 4, 3 or 2 wavefronts a SIMD.
-constexpr int kCus = 256;
-int resident(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
-struct Plan {
-  bool tile;  // row tiles (prompts), else a split of few rows
-  int ntile, nsplit;
-};
-// Rows x heads of a KV head from which the row tiles are taken.
-constexpr int kTileRows = 64;
-Plan plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
-  const int64_t rows = (int64_t)max_rows * (n_q / n_kv);
-  Plan p;
-  p.tile = rows >= kTileRows;
-  const int64_t per = p.tile ? kRows : 16;
-  p.ntile = std::max(1, (int)((rows + per - 1) / per));
-  const int64_t blocks = (int64_t)n_seqs * n_kv * p.ntile;
-  const int64_t want = (p.tile ? 2 * kCus : resident(hd, terms)) / blocks;
-  const int64_t least = p.tile ? 2 * kChunkPos : 4 * kStep;  // positions worth a split
-  const int64_t most = (max_length + least - 1) / least;
-  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
-  return p;
-}
-}  // namespace
-
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
-  const Plan p = plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
+  const Kv8Plan p = kv8_plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
   return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
 }
 
-// (launches that split have at most resident() workgroups of 16 rows x heads, or 2 kCus of kRows)
+// (launches that split have at most resident() workgroups of 16 rows x heads, or 2 kCus of 128)
 size_t kv8_attn_floats_most(int hd) {
-  return (size_t)std::max(resident(hd, 1) * 16, 2 * kCus * kRows) * (hd + 2);
+  return (size_t)std::max(resident(hd, 1) * 16, 2 * kCus * 128) * (hd + 2);
 }
 
 template <int HD>
 static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
   // two fp16 terms unless queries and output are bf16
   const int terms = a.q.bf16 && a.out.p && a.out.bf16 ? 1 : 2;
-  const Plan p = plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
+  const Kv8Plan p = kv8_plan(HD, terms, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
   const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
   if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)gx, r.n_seqs);
   const int edge = p.nsplit == 1 ? last : last & kFirst;
-#define WICI_ATTN(kernel, nt) \
-  launch_k(kernel<HD, nt>, grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
-  if (p.tile) {
-    if (terms == 1) WICI_ATTN(k_kv8_attn_tile, 1);
-    else WICI_ATTN(k_kv8_attn_tile, 2);
+#define WICI_ATTN(...) \
+  launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
+  if (p.row_tiles == 2) {
+    if (terms == 1) WICI_ATTN(k_kv8_attn_tile<HD, 1, 2>);
+    else WICI_ATTN(k_kv8_attn_tile<HD, 2, 2>);
+  } else if (p.row_tiles == 1) {
+    if (terms == 1) WICI_ATTN(k_kv8_attn_tile<HD, 1, 1>);
+    else WICI_ATTN(k_kv8_attn_tile<HD, 2, 1>);
   } else {
-    if (terms == 1) WICI_ATTN(k_kv8_attn_split, 1);
-    else WICI_ATTN(k_kv8_attn_split, 2);
+    if (terms == 1) WICI_ATTN(k_kv8_attn_split<HD, 1>);
+    else WICI_ATTN(k_kv8_attn_split<HD, 2>);
   }
 #undef WICI_ATTN
   if (p.nsplit > 1) {

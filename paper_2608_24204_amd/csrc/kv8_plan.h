@@ -1,0 +1,53 @@
+// Which kernel attends over the 8-bit cache, in which grid.  Host code alone (no HIP), so that
+// a test can evaluate the rules.
+#pragma once
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+namespace wici {
+
+constexpr int kCus = 256;         // compute units of the chip
+constexpr int kTiles = 2;         // tiles of 16 positions that a wavefront takes at a time
+constexpr int kStep = 16 * kTiles;
+constexpr int kChunkTiles = 4;    // tiles of 16 positions a chunk of the row tiles
+constexpr int kChunkPos = 16 * kChunkTiles;
+
+// Workgroups that the chip holds at once: 4, 3 or 2 wavefronts a SIMD.
+inline int resident(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
+struct Kv8Plan {
+  int row_tiles;  // prompts: tiles of 16 rows a wavefront; 0: a split of few rows
+  int ntile, nsplit;
+};
+// Which kernel, from the rows x heads of a KV head, the workgroups of 128 of them and the
+// 16 rows x 32 positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us,
+// split / 64 rows / 128 rows):
+//  - below 128 rows the split: 16 new rows of each of 8 sequences of 2000: 25 / 32 / 32;
+//  - where 128 rows fill the chip, or have long contexts to split: 2048 of 8192 positions:
+//    668 / 580 / 379; 16 x 100 of 1000: 100 / 96 / 67; 128 of 8000: 63 / 63 / 54;
+//  - a chip half full: 64 rows: 1024 of 1024: 49 / 44 / 63; 32 x 32 of 300: 36 / 25 / 50;
+//  - few workgroups and little to do: the split: 333 of 333: 14 / 30 / 32.
+constexpr int kTileRows = 128, kFull = 400, kHalf = 200;
+constexpr int64_t kMuch = 60000;
+inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
+  const int64_t rows = (int64_t)max_rows * (n_q / n_kv), heads = (int64_t)n_seqs * n_kv;
+  const int64_t tiles = heads * ((rows + 127) / 128);
+  const int64_t work = heads * ((rows + 15) / 16) * ((max_length + kStep - 1) / kStep);
+  Kv8Plan p;
+  p.row_tiles = rows < kTileRows ? 0
+                : tiles >= kFull || work >= 2 * kMuch ? 2
+                : tiles >= kHalf ? 1
+                : work >= kMuch ? 2 : 0;
+  const int64_t per = p.row_tiles ? 64 * p.row_tiles : 16;
+  p.ntile = std::max(1, (int)((rows + per - 1) / per));
+  const int64_t blocks = heads * p.ntile;
+  const int64_t want = (p.row_tiles ? 2 * kCus : resident(hd, terms)) / blocks;
+  // positions worth a split: a step a wavefront; eight chunks of a tile's, whose 128 rows'
+  // partial results are the larger traffic
+  const int64_t least = p.row_tiles ? 8 * kChunkPos : 4 * kStep;
+  const int64_t most = (max_length + least - 1) / least;
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
+  return p;
+}
+
+}  // namespace wici

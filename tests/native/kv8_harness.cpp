@@ -5,14 +5,15 @@
 #include <vector>
 
 #include "kv8_layout.h"
+#include "kv8_plan.h"
 
 using namespace wici;
 
 int main() {
   char what[16];
-  long long a[6];
+  long long a[7];
   while (std::scanf("%15s", what) == 1) {
-    for (int i = 0; i < 6; ++i)
+    for (int i = 0; i < 7; ++i)
       if (std::scanf("%lld", &a[i]) != 1) return 1;
     if (!std::strcmp(what, "block")) {  // page, hd: byte of every code, key then value, then scale
       const int page = (int)a[0], hd = (int)a[1];
@@ -35,6 +36,9 @@ int main() {
       std::printf("%d %d\n", row0, rows);
     } else if (!std::strcmp(what, "seen")) {  // len, rows, i, cap
       std::printf("%d\n", kv8_seen((int)a[0], (int)a[1], (int)a[2], a[3]));
+    } else if (!std::strcmp(what, "plan")) {  // hd, terms, heads, KV heads, sequences, rows, length
+      const Kv8Plan p = kv8_plan((int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)a[4], (int)a[5], (int)a[6]);
+      std::printf("%d %d %d\n", p.row_tiles, p.ntile, p.nsplit);
     } else {
       return 2;
     }

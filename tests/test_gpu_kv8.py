@@ -306,6 +306,51 @@ def test_prompts(ops, n_kv, G, hd, page, dtype):
         check_attend(bt, q, out, K, V, hd ** -0.5)
 
 
+# Calls that between them meet every kernel of the attention (which one a call takes is
+# read off the launch rules in test_kv8_host.py): sequences, new rows and positions of each, KV
+# heads, query heads a KV head, head size, page-table entries, page.
+PLAN_CASES = [
+    (1, 37, 90, 2, 2, 128, 8, 16), (1, 37, 90, 2, 2, 64, 8, 16),              # split, one
+    (2, 5, 700, 2, 2, 128, 50, 16), (2, 5, 700, 2, 2, 64, 50, 16),            # split, several
+    (26, 8, 40, 8, 16, 128, 4, 16), (26, 8, 40, 8, 16, 64, 4, 16),            # 64 rows
+    (1, 390, 400, 25, 4, 128, 26, 16), (1, 390, 400, 25, 4, 64, 26, 16),
+    (52, 8, 70, 8, 16, 128, 6, 16), (52, 8, 70, 8, 16, 64, 6, 16),            # 128 rows, one
+    (2, 700, 730, 8, 5, 128, 6, 128), (2, 700, 730, 8, 5, 64, 6, 128),
+    (1, 130, 200, 4, 5, 128, 2100, 128), (1, 130, 200, 4, 5, 64, 2100, 128),  # 128 rows, several
+]
+
+
+@pytest.mark.parametrize("n_seqs,rows,length,n_kv,G,hd,entries,page", PLAN_CASES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_kernel(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dtype):
+    """Against float64 on the GPU, all rows; some sequences shorter and with fewer rows, one
+    without any."""
+    lens = [max(rows, length - 7 * b) for b in range(n_seqs)]
+    new = [max(0, rows - b % 4) if b != 1 else 0 for b in range(n_seqs)]
+    need = -(-max(lens) // page)
+    bt = Batch(ops, lens, new, n_kv=n_kv, hd=hd, page=page, seed=rows + n_seqs, extra_pages=entries - need)
+    K, V = bt.fill(dtype=BF16)
+    q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype, scale=1.5)
+    out = bt.cache.attend(q, bt.length, row_start=bt.row_start, max_rows=rows)
+    single = dtype == BF16
+    for b, (n, r) in enumerate(zip(lens, new)):
+        if not r:
+            continue
+        at = slice(bt.start[b], bt.start[b] + r)
+        k, v = (torch.from_numpy(x).cuda().transpose(0, 1)[:, None].contiguous() for x in (K[b], V[b]))
+        qq = q[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3).contiguous()
+        x = qq @ k.transpose(-1, -2).contiguous() * hd ** -0.5
+        late = torch.arange(n, device="cuda")[None] > torch.arange(n - r, n, device="cuda")[:, None]
+        p = x.masked_fill(late, float("-inf")).softmax(-1)
+        want, mag = p @ v, p @ v.abs()
+        dots = (qq.abs() @ k.abs().transpose(-1, -2).contiguous()).amax(-1, keepdim=True) * hd ** -0.5
+        e = (48 * 2.0 ** -24 + (0 if single else 2.0 ** -22)) * dots + 2.0 ** -20
+        rel = 2 * e + (2.0 ** -11 if single else 2.0 ** -22) + (64 + n / 16) * 2.0 ** -24
+        tol = mag * rel + want.abs() * torch.finfo(dtype).eps / 2 + 1e-30
+        err = (out[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3) - want).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
 def test_many_fp32_rows(ops):
     """20000 rows and heads whose weights are spread over many positions: the two terms of each
     weight belong together in every one of them (an error of one fp16 step in one weight of

@@ -14,6 +14,7 @@ import pytest
 
 import oracle
 from paper_2608_24204_amd import binding
+from tests.test_gpu_kv8 import PLAN_CASES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 GXX = shutil.which("g++")
@@ -31,7 +32,7 @@ def ask(tmp_path_factory):
                     os.path.join(ROOT, "tests", "native", "kv8_harness.cpp"), "-o", exe], check=True)
 
     def run(questions):
-        text = "".join(" ".join(map(str, (list(q) + [0] * 7)[:7])) + "\n" for q in questions)
+        text = "".join(" ".join(map(str, (list(q) + [0] * 8)[:8])) + "\n" for q in questions)
         r = subprocess.run([exe], input=text, capture_output=True, text=True, timeout=60)
         assert r.returncode == 0, r.stderr[-2000:]
         out = [tuple(map(int, l.split())) for l in r.stdout.splitlines()]
@@ -100,6 +101,38 @@ def test_the_oracle_rounds_codes_exactly():
     assert not n.any() and step[0] == np.float32(2.0 ** -60 / 127)
     assert np.isnan(oracle.kv8_values(np.array([[1.0, np.inf] * 4]))).all()
     assert np.isnan(oracle.kv8_values(np.array([[1.0, np.nan] * 4]))).all()
+
+
+def test_the_gpu_tests_meet_every_kernel(ask):
+    """The attention's kernels (a split of few rows, tiles of 64 and of 128 rows), with and
+    without partial results to merge, for both head sizes and one and two terms."""
+    seen = set()
+    for n_seqs, rows, length, n_kv, G, hd, entries, page in PLAN_CASES:
+        for terms in (1, 2):
+            (kind, _, nsplit), = ask([("plan", hd, terms, n_kv * G, n_kv, n_seqs, rows,
+                                       entries * page)])
+            seen.add((hd, terms, kind, nsplit > 1))
+    # (tiles of 64 rows are taken where the chip is half full: nothing is left to split)
+    assert seen == {(hd, t, k, s) for hd in (64, 128) for t in (1, 2)
+                    for k, s in ((0, False), (0, True), (1, False), (2, False), (2, True))}
+
+
+def test_launch_sizes(ask):
+    """Grids within their limits, splits and row tiles that cover the rows, over the range of
+    the operator."""
+    rng = np.random.default_rng(0)
+    q = []
+    for _ in range(2000):
+        n_kv = int(rng.choice([1, 2, 8, 64]))
+        q.append(("plan", int(rng.choice([64, 128])), int(rng.choice([1, 2])),
+                  n_kv * int(rng.integers(1, 17)), n_kv, int(2 ** rng.uniform(0, 12)),
+                  int(2 ** rng.uniform(0, 16)), int(2 ** rng.uniform(0, 24))))
+    for (_, hd, terms, hq, n_kv, n_seqs, rows, length), (kind, ntile, nsplit) in zip(q, ask(q)):
+        per = 64 * kind if kind else 16
+        assert kind in (0, 1, 2) and ntile * per >= rows * (hq // n_kv) > (ntile - 1) * per
+        assert 1 <= nsplit <= 128
+        most = 2 * 256 if kind else 256 * (4 if hd == 64 else 3 if terms == 1 else 2)
+        assert nsplit == 1 or (kind != 1 and nsplit * ntile * n_kv * n_seqs <= most)
 
 
 # ------------------------------------------------------------------ refusals
