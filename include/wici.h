@@ -416,7 +416,9 @@ wici_status wici_stream_read_noalloc(const void* d_buf, size_t bytes, int32_t gr
  *  - arguments are checked before anything is enqueued.  Errors: WICI_E_ARG, WICI_E_HIP
  *    (the launch failed);
  *  - what lies in device memory (lengths, rows, page tables, positions) is not seen by
- *    those checks.  The kernels bound it: no value there makes them leave their tensors. */
+ *    those checks.  The kernels bound it: no value there makes them leave their tensors;
+ *  - a call takes fewer than 2^28 head rows (rows times all heads it is given), an attention
+ *    at most 2^24 (rows times query heads), and at most 65535 sequences. */
 
 /* Head rows: element (row, head, d) at data[row * row_stride + head * head_stride + d].
  * dtype WICI_F32 or WICI_BF16; data 16-byte aligned, strides (in elements, positive) multiples
@@ -498,7 +500,7 @@ typedef struct {
  * their positions first (in fp32, as by wici_rope_rows, with no rounding before the
  * quantisation), and with q.data set the n_heads query heads too, into q_out (which may be
  * q): the work between a layer's projection and its attention in one launch.  q.data needs
- * rope; rope.dim at most head_dim.  At most 65535 sequences. */
+ * rope; rope.dim at most head_dim. */
 wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
                             const wici_rope_tab* rope, int32_t n_heads, wici_head_rows q,
                             wici_head_rows q_out, wici_head_rows k, wici_head_rows v,

@@ -87,10 +87,10 @@ __global__ __launch_bounds__(256) void k_rope_rows(HeadRows x, HeadRows y, int n
                                                    const int32_t* __restrict__ positions,
                                                    RopeTab rope) {
   constexpr int LPU = HD / 8, UPB = 256 / LPU;
-  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
+  const unsigned u = blockIdx.x * UPB + threadIdx.x / LPU;  // below 2^28
   const int c = threadIdx.x % LPU;
-  if (u >= (int64_t)n_rows * n_heads) return;
-  const int row = (int)(u / n_heads), h = (int)(u - (int64_t)row * n_heads);
+  const int row = (int)(u / n_heads), h = (int)(u % n_heads);
+  if (row >= n_rows) return;
   const int pos = positions[row];
   if (pos < 0) return;  // padding: left as it is
   const Runs r = runs(rope, c);
@@ -165,6 +165,7 @@ struct RowAt {
   char* base;
   const int32_t* table;
   int pos;
+  int end;  // the row after the sequence's last
 };
 template <int LPU>
 __device__ __forceinline__ RowAt row_at(const Kv8& c, const Kv8Rows& r, int t, int lane) {
@@ -178,115 +179,189 @@ __device__ __forceinline__ RowAt row_at(const Kv8& c, const Kv8Rows& r, int t, i
   } else if (r.kind == KV8_CHUNK) {
     b = 0;
   }
-  if (b < 0 || b >= r.n_seqs) return RowAt{false, nullptr, nullptr, 0};
+  if (b < 0 || b >= r.n_seqs) return RowAt{false, nullptr, nullptr, 0, 0};
   const Kv8Seq s = kv8_seq(c, r, b);
   const int pos = s.len - s.rows + (t - s.row0);
-  return RowAt{t < s.row0 + s.rows && pos >= 0, s.base, s.table, pos};
+  return RowAt{t < s.row0 + s.rows && pos >= 0, s.base, s.table, pos, s.row0 + s.rows};
+}
+// The places of R neighbouring rows from t on: found once for those of one sequence.
+template <int LPU, int R>
+__device__ __forceinline__ void rows_at(RowAt (&w)[R], const Kv8& c, const Kv8Rows& r, int t,
+                                        int lane) {
+  w[0] = row_at<LPU>(c, r, t, lane);
+#pragma unroll
+  for (int i = 1; i < R; ++i) {
+    if (w[i - 1].there && t + i < w[i - 1].end) {
+      w[i] = w[i - 1];
+      w[i].pos += 1;
+    } else {
+      w[i] = t + i < r.n_rows ? row_at<LPU>(c, r, t + i, lane)
+                              : RowAt{false, nullptr, nullptr, 0, 0};
+    }
+  }
 }
 // The block of a position's page, or nullptr when no page holds it.
 template <int HD>
 __device__ __forceinline__ char* block_of(const Kv8& c, const RowAt& w, int which, int h) {
+  if (!w.there) return nullptr;
   const int phys = kv8_page(w.table, w.pos >> c.page_shift, c.max_pages, c.n_pages);
   return phys < 0 ? nullptr
                   : w.base + kv8_block_at(phys, which, h, c.n_kv, 1 << c.page_shift, HD);
 }
+// Whether R rows are the R positions of one word of value codes (in a page that exists).
+template <int R>
+__device__ __forceinline__ bool one_word(const RowAt (&w)[R], char* const (&blk)[R]) {
+  return R == 4 && blk[0] && (w[0].pos & 3) == 0 && w[R - 1].there && w[R - 1].end == w[0].end &&
+         w[R - 1].table == w[0].table && w[R - 1].pos == w[0].pos + R - 1;
+}
 
-template <int HD>
+// A unit takes R neighbouring rows of one head.  The rows do not wait for their places, so
+// they are requested first.  With four rows (prompts) a value word of four positions is
+// written whole where the rows are those four: single bytes took 14.7 us for 2048 rows of 8
+// heads of 128, whose bytes take 6.
+template <int HD, int R>
 __global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab rope, int n_q,
                                                     HeadRows q, HeadRows q_out, float q_scale,
                                                     HeadRows k, HeadRows v) {
   constexpr int LPU = HD / 8, UPB = 256 / LPU;
   const int lane = threadIdx.x % LPU, per = n_q + 2 * c.n_kv;
-  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
-  if (u >= (int64_t)r.n_rows * per) return;  // whole units leave together
-  const int t = (int)(u / per), item = (int)(u - (int64_t)t * per);
-  const RowAt w = row_at<LPU>(c, r, t, lane);
-  if (!w.there) return;
+  const unsigned u = blockIdx.x * UPB + threadIdx.x / LPU;  // below 2^28
+  const int t = R * (int)(u / per), item = (int)(u % per);
+  if (t >= r.n_rows) return;  // whole units leave together
   const bool is_q = item < n_q, is_v = item >= n_q + c.n_kv;
   const int h = is_q ? item : is_v ? item - n_q - c.n_kv : item - n_q;
   const HeadRows& x = is_q ? q : is_v ? v : k;
   RopeTab none = rope;
   none.cos = nullptr;
   const Runs run = runs(is_v ? none : rope, lane);
-  const int64_t in = t * x.row_stride + h * x.head_stride;
-  float e[8];
-  load4(x, in + run.a, e);
-  load4(x, in + run.b, e + 4);
-  for (int s = 1; s < x.n_sum; ++s) {
-    float m[8];
-    load4(x, in + s * x.sum_stride + run.a, m);
-    load4(x, in + s * x.sum_stride + run.b, m + 4);
+  float e[R][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] += m[i];
+  for (int i = 0; i < R; ++i) {
+    const int64_t in = min(t + i, r.n_rows - 1) * x.row_stride + h * x.head_stride;
+    load4(x, in + run.a, e[i]);
+    load4(x, in + run.b, e[i] + 4);
+    for (int s = 1; s < x.n_sum; ++s) {
+      float m[8];
+      load4(x, in + s * x.sum_stride + run.a, m);
+      load4(x, in + s * x.sum_stride + run.b, m + 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[i][j] += m[j];
+    }
   }
-  turn_row(rope, run, lane, w.pos, e);
+  RowAt w[R];
+  rows_at<LPU>(w, c, r, t, lane);
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (w[i].there) turn_row(rope, run, lane, w[i].pos, e[i]);
   if (is_q) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] *= q_scale;
-    const int64_t out = t * q_out.row_stride + h * q_out.head_stride;
-    put4(q_out, out + run.a, e);
-    put4(q_out, out + run.b, e + 4);
+    for (int i = 0; i < R; ++i) {
+      if (!w[i].there) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[i][j] *= q_scale;
+      const int64_t out = (t + i) * q_out.row_stride + h * q_out.head_stride;
+      put4(q_out, out + run.a, e[i]);
+      put4(q_out, out + run.b, e[i] + 4);
+    }
     return;
   }
-  const int page = 1 << c.page_shift, slot = w.pos & (page - 1);
-  char* blk = block_of<HD>(c, w, is_v, h);
-  unsigned code[2];
-  const float scale = quantise<LPU>(e, code);
-  if (!blk) return;
-  if (is_v) {
-    char* d = blk + kv8_value_at(slot, 8 * lane, HD);
+  const int page = 1 << c.page_shift;
+  char* blk[R];
+  unsigned code[R][2];
+  float scale[R];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d[4 * i] = (char)(code[i >> 2] >> (8 * (i & 3)));
-  } else {
-    *reinterpret_cast<unsigned*>(blk + kv8_key_at(slot, run.a, HD)) = code[0];
-    *reinterpret_cast<unsigned*>(blk + kv8_key_at(slot, run.b, HD)) = code[1];
+  for (int i = 0; i < R; ++i) {
+    blk[i] = block_of<HD>(c, w[i], is_v, h);
+    scale[i] = quantise<LPU>(e[i], code[i]);
   }
-  if (lane == 0) *reinterpret_cast<float*>(blk + kv8_scale_at(slot, page, HD)) = scale;
+  const int slot = w[0].pos & (page - 1);
+  const bool word = one_word(w, blk);
+  if (is_v && word) {
+    unsigned d[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      d[j] = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) d[j] |= (code[i][j >> 2] >> (8 * (j & 3)) & 0xffu) << (8 * (i & 3));
+    }
+    uint4* to = reinterpret_cast<uint4*>(blk[0] + kv8_value_at(slot, 8 * lane, HD));
+    to[0] = make_uint4(d[0], d[1], d[2], d[3]);
+    to[1] = make_uint4(d[4], d[5], d[6], d[7]);
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (!blk[i]) continue;
+    const int at = w[i].pos & (page - 1);
+    if (!is_v) {
+      *reinterpret_cast<unsigned*>(blk[i] + kv8_key_at(at, run.a, HD)) = code[i][0];
+      *reinterpret_cast<unsigned*>(blk[i] + kv8_key_at(at, run.b, HD)) = code[i][1];
+    } else if (!word) {
+      char* d = blk[i] + kv8_value_at(at, 8 * lane, HD);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[4 * j] = (char)(code[i][j >> 2] >> (8 * (j & 3)));
+    }
+    if (lane == 0) *reinterpret_cast<float*>(blk[i] + kv8_scale_at(at, page, HD)) = scale[i];
+  }
 }
 
-template <int HD>
+template <int HD, int R>
 __global__ __launch_bounds__(256) void k_kv8_read(Kv8 c, Kv8Rows r, HeadRows k, HeadRows v) {
   constexpr int LPU = HD / 8, UPB = 256 / LPU;
   const int lane = threadIdx.x % LPU, per = 2 * c.n_kv;
-  const int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / LPU;
-  if (u >= (int64_t)r.n_rows * per) return;
-  const int t = (int)(u / per), item = (int)(u - (int64_t)t * per);
-  const RowAt w = row_at<LPU>(c, r, t, lane);
+  const unsigned u = blockIdx.x * UPB + threadIdx.x / LPU;  // below 2^28
+  const int t = R * (int)(u / per), item = (int)(u % per);
+  if (t >= r.n_rows) return;
+  RowAt w[R];
+  rows_at<LPU>(w, c, r, t, lane);
   const bool is_v = item >= c.n_kv;
   const int h = is_v ? item - c.n_kv : item;
   const HeadRows& y = is_v ? v : k;
-  if (!w.there || !y.p) return;
-  const int page = 1 << c.page_shift, slot = w.pos & (page - 1);
-  const char* blk = block_of<HD>(c, w, is_v, h);
-  float e[8] = {};  // a position without a page reads as zero
-  if (blk) {
-    const float scale = *reinterpret_cast<const float*>(blk + kv8_scale_at(slot, page, HD));
-    unsigned code[8];
-    if (is_v) {
-      const uint4* s =
-          reinterpret_cast<const uint4*>(blk + kv8_value_at(slot & ~3, 8 * lane, HD));
-      const uint4 a = s[0], b = s[1];
-      const unsigned words[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (!y.p) return;
+  const int page = 1 << c.page_shift;
+  char* blk[R];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) code[i] = words[i] >> (8 * (slot & 3)) & 0xffu;
-    } else {
-      const uint2 a = *reinterpret_cast<const uint2*>(blk + kv8_key_at(slot, 8 * lane, HD));
+  for (int i = 0; i < R; ++i) blk[i] = block_of<HD>(c, w[i], is_v, h);
+  unsigned word[8];
+  const bool one = is_v && one_word(w, blk);
+  auto words = [&](const char* b, int at) {  // the value words of slot `at`
+    const uint4* s = reinterpret_cast<const uint4*>(b + kv8_value_at(at & ~3, 8 * lane, HD));
+    const uint4 x = s[0], z = s[1];
+    word[0] = x.x; word[1] = x.y; word[2] = x.z; word[3] = x.w;
+    word[4] = z.x; word[5] = z.y; word[6] = z.z; word[7] = z.w;
+  };
+  if (one) words(blk[0], w[0].pos & (page - 1));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) code[i] = (i < 4 ? a.x : a.y) >> (8 * (i & 3)) & 0xffu;
+  for (int i = 0; i < R; ++i) {
+    if (!w[i].there) continue;
+    float e[8] = {};  // a position without a page reads as zero
+    if (blk[i]) {
+      const int at = w[i].pos & (page - 1);
+      const float scale = *reinterpret_cast<const float*>(blk[i] + kv8_scale_at(at, page, HD));
+      unsigned code[8];
+      if (is_v) {
+        if (!one) words(blk[i], at);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) code[j] = word[j] >> (8 * (at & 3)) & 0xffu;
+      } else {
+        const uint2 a = *reinterpret_cast<const uint2*>(blk[i] + kv8_key_at(at, 8 * lane, HD));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) code[j] = (j < 4 ? a.x : a.y) >> (8 * (j & 3)) & 0xffu;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = (float)((int)code[j] - 128) * scale;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = (float)((int)code[i] - 128) * scale;
+    const int64_t out = (t + i) * y.row_stride + h * y.head_stride + 8 * lane;
+    put4(y, out, e);
+    put4(y, out + 4, e + 4);
   }
-  const int64_t out = t * y.row_stride + h * y.head_stride + 8 * lane;
-  put4(y, out, e);
-  put4(y, out + 4, e + 4);
 }
 
 // ------------------------------------------------------------------- launchers
-// Workgroups of `units` head rows, or 0 when there are none or more than a grid holds.
+// Workgroups of `units` units, or 0 when there are none or 2^28 and more (16 threads each, of
+// 2^32 in a grid).
 static unsigned unit_blocks(int hd, int64_t units) {
   const int64_t per = 256 / (hd / 8), n = (units + per - 1) / per;
-  return n < 1 || n > 0x7fffffff ? 0 : (unsigned)n;
+  return units < 1 || units >= (int64_t)1 << 28 ? 0 : (unsigned)n;
 }
 
 hipError_t launch_rope_rows(int hd, const HeadRows& x, const HeadRows& y, int n_rows, int n_heads,
@@ -312,33 +387,41 @@ hipError_t launch_rope_table(const RopeFreqs& f, int half, int64_t n_pos, float*
   return hipGetLastError();
 }
 
+// Rows a unit takes: four of a prompt, one where rows are few or belong to as many sequences.
+static int rows_of_unit(const Kv8Rows& r) { return r.n_rows >= 64 && r.n_rows >= 4 * r.n_seqs ? 4 : 1; }
+
 hipError_t launch_kv8_append(int hd, const Kv8& c, const Kv8Rows& r, const RopeTab& rope, int n_q,
                              const HeadRows& q, const HeadRows& q_out, float q_scale,
                              const HeadRows& k, const HeadRows& v, hipStream_t st, int edge) {
   if (!q.p) n_q = 0;
-  const unsigned grid = unit_blocks(hd, (int64_t)r.n_rows * (n_q + 2 * c.n_kv));
+  const int R = rows_of_unit(r);
+  const unsigned grid = unit_blocks(hd, ((int64_t)r.n_rows + R - 1) / R * (n_q + 2 * c.n_kv));
   if (!grid) return hipErrorInvalidValue;
-  if (hd == 128)
-    launch_k(k_kv8_append<128>, dim3(grid), dim3(256), 0, st, edge, c, r, rope, n_q, q, q_out,
-             q_scale, k, v);
-  else if (hd == 64)
-    launch_k(k_kv8_append<64>, dim3(grid), dim3(256), 0, st, edge, c, r, rope, n_q, q, q_out,
-             q_scale, k, v);
-  else
-    return hipErrorInvalidValue;
+#define WICI_APPEND(HD, R)                                                                       \
+  launch_k(k_kv8_append<HD, R>, dim3(grid), dim3(256), 0, st, edge, c, r, rope, n_q, q, q_out, \
+           q_scale, k, v)
+  if (hd == 128 && R == 4) WICI_APPEND(128, 4);
+  else if (hd == 128) WICI_APPEND(128, 1);
+  else if (hd == 64 && R == 4) WICI_APPEND(64, 4);
+  else if (hd == 64) WICI_APPEND(64, 1);
+  else return hipErrorInvalidValue;
+#undef WICI_APPEND
   return hipGetLastError();
 }
 
 hipError_t launch_kv8_read(int hd, const Kv8& c, const Kv8Rows& r, const HeadRows& k,
                            const HeadRows& v, hipStream_t st) {
-  const unsigned grid = unit_blocks(hd, (int64_t)r.n_rows * 2 * c.n_kv);
+  const int R = rows_of_unit(r);
+  const unsigned grid = unit_blocks(hd, ((int64_t)r.n_rows + R - 1) / R * 2 * c.n_kv);
   if (!grid) return hipErrorInvalidValue;
-  if (hd == 128)
-    launch_k(k_kv8_read<128>, dim3(grid), dim3(256), 0, st, kOnly, c, r, k, v);
-  else if (hd == 64)
-    launch_k(k_kv8_read<64>, dim3(grid), dim3(256), 0, st, kOnly, c, r, k, v);
-  else
-    return hipErrorInvalidValue;
+#define WICI_READ(HD, R) \
+  launch_k(k_kv8_read<HD, R>, dim3(grid), dim3(256), 0, st, kOnly, c, r, k, v)
+  if (hd == 128 && R == 4) WICI_READ(128, 4);
+  else if (hd == 128) WICI_READ(128, 1);
+  else if (hd == 64 && R == 4) WICI_READ(64, 4);
+  else if (hd == 64) WICI_READ(64, 1);
+  else return hipErrorInvalidValue;
+#undef WICI_READ
   return hipGetLastError();
 }
 

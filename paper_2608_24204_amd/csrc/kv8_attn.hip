@@ -696,9 +696,9 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
   constexpr int L = HD / 4, P = 256 / L;
   __shared__ float4 s_o[P][L];
   __shared__ float2 s_ml[P];
-  const int64_t u = blockIdx.x;
+  const unsigned u = blockIdx.x;
   const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane;
-  const int row = (int)(u / a.n_q), head = (int)(u - (int64_t)row * a.n_q);
+  const int row = (int)(u / a.n_q), head = (int)(u % a.n_q);
   if (r.kind == KV8_ARRAYS && r.row_start &&
       (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
     return;  // a row of no sequence

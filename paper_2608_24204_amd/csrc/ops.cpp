@@ -41,6 +41,11 @@ class OnDeviceOf {
   int back_ = -1;
 };
 
+// Head rows a grid of one launch takes: 16 threads each, 2^32 in all; and of the attention,
+// whose partial results are joined by a workgroup a row and head.
+constexpr int64_t kMostAttended = 1 << 24;
+bool units_ok(int64_t rows, int64_t heads) { return rows * heads < (int64_t)1 << 28; }
+
 bool aligned(const void* p) { return p && (uintptr_t)p % 16 == 0; }
 
 bool rows_ok(const wici_head_rows& x, int64_t heads, int64_t head_dim) {
@@ -131,7 +136,7 @@ wici_status wici_rope_rows(const wici_rope_tab* rope, int32_t head_dim, int32_t 
                            int32_t n_heads, const int32_t* positions, wici_head_rows x,
                            wici_head_rows y, void* hip_stream) {
   if ((head_dim != 64 && head_dim != 128) || !tab_ok(rope, head_dim) || n_rows < 0 ||
-      n_rows > (1 << 24) || n_heads < 1 || n_heads > 1024)
+      n_heads < 1 || n_heads > 1024 || !units_ok(n_rows, n_heads))
     return WICI_E_ARG;
   if (n_rows == 0) return WICI_OK;
   if (!positions || !rows_ok(x, n_heads, head_dim) || !rows_ok(y, n_heads, head_dim))
@@ -156,6 +161,7 @@ wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
   if (!call_ok(cache, batch) || (rope && !tab_ok(rope, cache->head_dim))) return WICI_E_ARG;
   const int hd = cache->head_dim;
   if (q.data && (!rope || n_heads < 1 || n_heads > 1024)) return WICI_E_ARG;
+  if (!units_ok(batch->n_rows, (q.data ? n_heads : 0) + 2 * cache->n_kv_heads)) return WICI_E_ARG;
   if (empty(batch)) return WICI_OK;
   if (!rows_ok(k, cache->n_kv_heads, hd) || !rows_ok(v, cache->n_kv_heads, hd) ||
       (q.data && (!rows_ok(q, n_heads, hd) || !rows_ok(q_out, n_heads, hd))))
@@ -169,7 +175,9 @@ wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
 
 wici_status wici_kv8_read(const wici_kv8* cache, const wici_kv8_batch* batch, wici_head_rows k,
                           wici_head_rows v, void* hip_stream) {
-  if (!call_ok(cache, batch) || (!k.data && !v.data)) return WICI_E_ARG;
+  if (!call_ok(cache, batch) || (!k.data && !v.data) ||
+      !units_ok(batch->n_rows, 2 * cache->n_kv_heads))
+    return WICI_E_ARG;
   if (empty(batch)) return WICI_OK;
   if ((k.data && !rows_ok(k, cache->n_kv_heads, cache->head_dim)) ||
       (v.data && !rows_ok(v, cache->n_kv_heads, cache->head_dim)))
@@ -184,7 +192,7 @@ wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batc
                                       int32_t n_heads, size_t* bytes) {
   if (!bytes || !geometry_ok(cache) || !batch_shape_ok(cache, batch) || n_heads < 1 ||
       n_heads > 1024 || n_heads % cache->n_kv_heads ||
-      (int64_t)batch->n_rows * n_heads > 0x7fffffff)
+      (int64_t)batch->n_rows * n_heads > kMostAttended)
     return WICI_E_ARG;
   *bytes = empty(batch) ? 0
                         : 4 * wici::kv8_attn_floats(cache->head_dim, n_heads, cache->n_kv_heads,
