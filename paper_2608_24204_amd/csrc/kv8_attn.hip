@@ -102,12 +102,14 @@ struct Pages {
   int phys[kTiles];
   __device__ __forceinline__ bool all() const { return (phys[0] | phys[1]) >= 0; }
 };
-__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int64_t step) {
+__device__ __forceinline__ int find_page(const Kv8& c, const Kv8Seq& q, uint32_t pos) {
+  return uniform(kv8_page_of(q.table, pos >> c.page_shift, c.max_pages, c.n_pages));
+}
+// (steps end below 2^31 positions; one looked up past them is still below 2^32)
+__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int step) {
   Pages p;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-    p.phys[t] = uniform(
-        kv8_page(q.table, (step * kStep + 16 * t) >> c.page_shift, c.max_pages, c.n_pages));
+  p.phys[0] = find_page(c, q, (uint32_t)step * kStep);
+  p.phys[1] = c.page_shift >= 5 ? p.phys[0] : find_page(c, q, (uint32_t)step * kStep + 16);
   return p;
 }
 
@@ -117,34 +119,45 @@ __device__ __forceinline__ uint4 fetch(__amdgpu_buffer_rsrc_t r, int lane_at, in
   const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
+// One KV head of a pool: its key block in page 0, and the bytes from page to page and from a
+// key block to its value block.
 template <int HD>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rsrc(const Kv8& c, const Kv8Seq& q, int phys,
-                                                             int which, int h) {
-  const int page = 1 << c.page_shift;
-  return rsrc(q.base + kv8_block_at(max(phys, 0), which, h, c.n_kv, page, HD),
-              kv8_block_bytes(page, HD));
-}
+struct HeadAt {
+  const char* base;
+  uint32_t page, values;
+  __device__ __forceinline__ HeadAt(const Kv8& c, const Kv8Seq& q, int h)
+      : base(q.base + kv8_block_at(0, 0, h, c.n_kv, 1 << c.page_shift, HD)),
+        page(2 * c.n_kv * (uint32_t)kv8_block_bytes(1 << c.page_shift, HD)),
+        values(page / 2) {}
+  __device__ __forceinline__ const char* block(int phys, int which) const {
+    return base + (uint64_t)(uint32_t)max(phys, 0) * page + (which ? values : 0);
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const Kv8& c, int phys, int which) const {
+    return rsrc(block(phys, which), kv8_block_bytes(1 << c.page_shift, HD));
+  }
+};
 template <int HD>
-__device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const Kv8Seq& q,
-                                          const Pages& p, int h, int step, int lane) {
+__device__ __forceinline__ void load_keys(Keys<HD>& s, const Kv8& c, const HeadAt<HD>& at,
+                                          const Pages& p, int step, int lane) {
   const int page = 1 << c.page_shift, mine = kv8_key_at(lane & 15, (lane >> 4) * (HD / 4), HD);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
-    const __amdgpu_buffer_rsrc_t b = block_rsrc<HD>(c, q, p.phys[t], 0, h);
+    const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0);
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i) s.k[t][i] = fetch(b, mine + 16 * i, kv8_key_at(slot, 0, HD));
   }
 }
 template <int HD>
-__device__ __forceinline__ void load_values(Values<HD>& s, Scales& sl, const Kv8& c, const Kv8Seq& q,
-                                            const Pages& p, int h, int step, int lane) {
+__device__ __forceinline__ void load_values(Values<HD>& s, Scales& sl, const Kv8& c,
+                                            const HeadAt<HD>& at, const Pages& p, int step,
+                                            int lane) {
   const int page = 1 << c.page_shift, g = lane >> 4, mine = kv8_value_at(4 * g, 4 * (lane & 15), HD);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
-    const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, p.phys[t], 0, h);
-    const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, p.phys[t], 1, h);
+    const __amdgpu_buffer_rsrc_t kb = at.buffer(c, p.phys[t], 0);
+    const __amdgpu_buffer_rsrc_t vb = at.buffer(c, p.phys[t], 1);
     sl.k[t] = __builtin_bit_cast(float4, fetch(kb, 16 * g, kv8_scale_at(slot, page, HD)));
     sl.v[t] = __builtin_bit_cast(float4, fetch(vb, 16 * g, kv8_scale_at(slot, page, HD)));
 #pragma unroll
@@ -375,6 +388,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
   // the wavefront's first steps do not depend on the length, so that their pages are
   // looked up beside it
+  const HeadAt<HD> kv(c, q, h);
   const int s0 = 4 * split + wave;
   const Pages p0 = find_pages(c, q, s0), p1 = find_pages(c, q, s0 + 4 * nsplit);
 
@@ -408,13 +422,13 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
       Values<HD> v;
       Scales sl;
       Pages now = p0, next = p1;
-      load_keys<HD>(k, c, q, now, h, s, lane);
-      load_values<HD>(v, sl, c, q, now, h, s, lane);
+      load_keys<HD>(k, c, kv, now, s, lane);
+      load_values<HD>(v, sl, c, kv, now, s, lane);
       for (;;) {
         floatx4_t sc[kTiles];
         scores<HD, NT>(sc, k, qf);
         const int then = s + stride;
-        if (then < steps) load_keys<HD>(k, c, q, next, h, then, lane);
+        if (then < steps) load_keys<HD>(k, c, kv, next, then, lane);
         half8_t wf[NT];
         float corr = 1.f;
         const bool move =
@@ -424,7 +438,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         if (move) rescale<HD>(o, corr);
         add_values<HD, NT>(o, v, wf);
         if (then >= steps) break;
-        load_values<HD>(v, sl, c, q, next, h, then, lane);
+        load_values<HD>(v, sl, c, kv, next, then, lane);
         now = next;
         next = find_pages(c, q, then + stride);
         s = then;
@@ -495,6 +509,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
   float* part_ml = a.work;
   float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
   const int total = q.rows * G, tiles = (total + kRows - 1) / kRows;
+  const HeadAt<HD> kv(c, q, h);
   const bool two_a_cu = gridDim.x > kCus && gridDim.x * gridDim.y <= 2 * kCus && tiles <= ntile;
 
   for (int back = tile0; back < tiles; back += ntile) {
@@ -539,30 +554,28 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     int phys[kChunkTiles], later[kChunkTiles];
     const int pair = wave >> 1, half = HD == 128 ? wave & 1 : 0;
     auto find = [&](int (&p)[kChunkTiles], int chunk) {
+      p[0] = find_page(c, q, (uint32_t)chunk * kChunkPos);
 #pragma unroll
-      for (int t = 0; t < kChunkTiles; ++t)
-        p[t] = uniform(kv8_page(q.table, ((int64_t)chunk * kChunkPos + 16 * t) >> c.page_shift,
-                                c.max_pages, c.n_pages));
+      for (int t = 1; t < kChunkTiles; ++t)
+        p[t] = c.page_shift >= 6 ? p[0] : find_page(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
     };
     auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
       const int j0 = chunk * kChunkPos;
       auto pick = [&](int t) { return t == 0 ? p[0] : t == 1 ? p[1] : t == 2 ? p[2] : p[3]; };
       const int ks = (j0 + 16 * wave) & (page - 1);
-      const __amdgpu_buffer_rsrc_t kb = block_rsrc<HD>(c, q, uniform(pick(wave)), 0, h);
+      const __amdgpu_buffer_rsrc_t kb = kv.buffer(c, uniform(pick(wave)), 0);
 #pragma unroll
       for (int i = 0; i < HD / 64; ++i)
         kc[i] = fetch(kb, kv8_key_at(r16, g * (HD / 4), HD) + 16 * i, kv8_key_at(ks, 0, HD));
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int vs = (j0 + 32 * pair + 16 * t) & (page - 1);
-        const __amdgpu_buffer_rsrc_t vb = block_rsrc<HD>(c, q, uniform(pick(2 * pair + t)), 1, h);
+        const __amdgpu_buffer_rsrc_t vb = kv.buffer(c, uniform(pick(2 * pair + t)), 1);
         vc[t] = fetch(vb, kv8_value_at(4 * g, 4 * r16, HD) + 256 * half, kv8_value_at(vs, 0, HD));
       }
-      if (wave < 2) {
-        const int at = max(pick(g), 0), slot = (j0 + lane) & (page - 1);
-        sc = *reinterpret_cast<const float*>(q.base + kv8_block_at(at, wave, h, c.n_kv, page, HD) +
-                                             kv8_scale_at(slot, page, HD));
-      }
+      if (wave < 2)
+        sc = *reinterpret_cast<const float*>(
+            kv.block(pick(g), wave) + kv8_scale_at((j0 + lane) & (page - 1), page, HD));
     };
     auto convert = [&](int buf) {
       const unsigned* w = reinterpret_cast<const unsigned*>(kc);

@@ -36,6 +36,12 @@ WICI_HD int kv8_page(const int32_t* table, int64_t p, int max_pages, int n_pages
   return phys < 0 || phys >= n_pages ? -1 : phys;
 }
 
+// The same with no branch around the look-up (p below 2^32, max_pages at least 1).
+WICI_HD int kv8_page_of(const int32_t* table, uint32_t p, int max_pages, int n_pages) {
+  const int phys = table[p < (uint32_t)max_pages ? p : (uint32_t)max_pages - 1];
+  return p < (uint32_t)max_pages && (uint32_t)phys < (uint32_t)n_pages ? phys : -1;
+}
+
 // The rows a sequence has when row_start says [from, to): a range inside [0, n_rows].
 WICI_HD void kv8_range(int from, int to, int n_rows, int& row0, int& rows) {
   row0 = from < 0 ? 0 : from > n_rows ? n_rows : from;

@@ -29,7 +29,9 @@ int main() {
     } else if (!std::strcmp(what, "page")) {  // logical page, max_pages, n_pages, table's entry
       // a table of exactly max_pages entries: an access past it is the sanitizer's to find
       std::vector<int32_t> table((size_t)a[1], (int32_t)a[3]);
-      std::printf("%d\n", kv8_page(table.data(), a[0], (int)a[1], (int)a[2]));
+      const int got = kv8_page(table.data(), a[0], (int)a[1], (int)a[2]);
+      if (a[0] >= 0 && kv8_page_of(table.data(), (uint32_t)a[0], (int)a[1], (int)a[2]) != got) return 3;
+      std::printf("%d\n", got);
     } else if (!std::strcmp(what, "range")) {  // from, to, n_rows
       int row0, rows;
       kv8_range((int)a[0], (int)a[1], (int)a[2], row0, rows);
