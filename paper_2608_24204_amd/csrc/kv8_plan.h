@@ -28,11 +28,12 @@ struct Kv8Plan {
 //  - a chip half full: 64 rows: 1024 of 1024: 49 / 44 / 63; 32 x 32 of 300: 36 / 25 / 50;
 //  - few workgroups and little to do: the split: 333 of 333: 14 / 30 / 32.
 constexpr int kTileRows = 128, kFull = 400, kHalf = 200;
-constexpr int64_t kMuch = 60000;
+constexpr double kMuch = 60000;
 inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
   const int64_t rows = (int64_t)max_rows * (n_q / n_kv), heads = (int64_t)n_seqs * n_kv;
   const int64_t tiles = heads * ((rows + 127) / 128);
-  const int64_t work = heads * ((rows + 15) / 16) * ((max_length + kStep - 1) / kStep);
+  // (a double: 65535 sequences of the longest contexts pass 2^63)
+  const double work = (double)heads * ((rows + 15) / 16) * (((int64_t)max_length + kStep - 1) / kStep);
   Kv8Plan p;
   p.row_tiles = rows < kTileRows ? 0
                 : tiles >= kFull || work >= 2 * kMuch ? 2

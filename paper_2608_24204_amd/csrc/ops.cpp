@@ -81,7 +81,7 @@ bool batch_shape_ok(const wici_kv8* c, const wici_kv8_batch* b) {
 }
 bool empty(const wici_kv8_batch* b) { return b->n_rows == 0 || b->n_seqs == 0; }
 bool call_ok(const wici_kv8* c, const wici_kv8_batch* b) {
-  return geometry_ok(c) && batch_shape_ok(c, b) && aligned(c->pool) && c->table &&
+  return geometry_ok(c) && batch_shape_ok(c, b) && aligned(c->pool) && (c->table || empty(b)) &&
          (b->n_seqs <= 1 || c->table_stride >= c->max_pages) && c->table_stride >= 0 &&
          (b->length || empty(b));
 }
@@ -175,11 +175,9 @@ wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
 
 wici_status wici_kv8_read(const wici_kv8* cache, const wici_kv8_batch* batch, wici_head_rows k,
                           wici_head_rows v, void* hip_stream) {
-  if (!call_ok(cache, batch) || (!k.data && !v.data) ||
-      !units_ok(batch->n_rows, 2 * cache->n_kv_heads))
-    return WICI_E_ARG;
+  if (!call_ok(cache, batch) || !units_ok(batch->n_rows, 2 * cache->n_kv_heads)) return WICI_E_ARG;
   if (empty(batch)) return WICI_OK;
-  if ((k.data && !rows_ok(k, cache->n_kv_heads, cache->head_dim)) ||
+  if ((!k.data && !v.data) || (k.data && !rows_ok(k, cache->n_kv_heads, cache->head_dim)) ||
       (v.data && !rows_ok(v, cache->n_kv_heads, cache->head_dim)))
     return WICI_E_ARG;
   OnDeviceOf dev(hip_stream);

@@ -182,7 +182,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     if table.device != device:
         raise ValueError(f"table: on {table.device}, expected {device}")
     lib = binding.load_library()
-    with _launch_on(stream, device, x, positions, out) as raw:
+    with _launch_on(stream, device, x, positions, out, table.cos, table.sin) as raw:
         if out is None:
             out = _like(x)
         elif out.shape[0] != n:
@@ -235,6 +235,9 @@ class KvCache:
                            device=_on_gpu(table, "table"))
         return cls(pool, table, page=page, head_dim=head_dim)
 
+    def _on(self, stream, *tensors):
+        return _launch_on(stream, self.device, self.pool, self.table, *tensors)
+
     def _batch(self, n_rows, length, row_start, max_rows=0, max_length=0):
         n = length.shape[0]
         if n > self.table.shape[0]:
@@ -259,7 +262,8 @@ class KvCache:
             raise ValueError("q is only rotated: it needs rope")
         if rope is not None and rope.device != dev:
             raise ValueError(f"rope: on {rope.device}, expected {dev}")
-        with _launch_on(stream, dev, k, v, length, row_start, q, q_out) as raw:
+        with self._on(stream, k, v, length, row_start, q, q_out, rope and rope.cos,
+                      rope and rope.sin) as raw:
             qr, qo, heads = _NO_ROWS, _NO_ROWS, 0
             if q is not None:
                 heads = q.shape[1]
@@ -285,7 +289,7 @@ class KvCache:
         if n_rows is None:
             n_rows = k.shape[0] if k is not None else v.shape[0] if v is not None else \
                 length.shape[0]
-        with _launch_on(stream, dev, length, row_start, k, v) as raw:
+        with self._on(stream, length, row_start, k, v) as raw:
             shape = (n_rows, self.n_kv_heads, d)
             k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
             v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
@@ -311,7 +315,7 @@ class KvCache:
         if q.dim() != 3:
             raise ValueError(f"q: shape {tuple(q.shape)}, expected [rows, heads, {d}]")
         n, heads = q.shape[0], q.shape[1]
-        with _launch_on(stream, dev, q, length, row_start, out, workspace) as raw:
+        with self._on(stream, q, length, row_start, out, workspace) as raw:
             b = self._batch(n, length, row_start, max_rows, max_length)
             if out is None:
                 out = _like(q)

@@ -127,6 +127,7 @@ def test_launch_sizes(ask):
         q.append(("plan", int(rng.choice([64, 128])), int(rng.choice([1, 2])),
                   n_kv * int(rng.integers(1, 17)), n_kv, int(2 ** rng.uniform(0, 12)),
                   int(2 ** rng.uniform(0, 16)), int(2 ** rng.uniform(0, 24))))
+    q += [("plan", hd, 1, 8, 8, n, 2 ** 24, 2 ** 31 - 1) for hd in (64, 128) for n in (1, 65535)]
     for (_, hd, terms, hq, n_kv, n_seqs, rows, length), (kind, ntile, nsplit) in zip(q, ask(q)):
         per = 64 * kind if kind else 16
         assert kind in (0, 1, 2) and ntile * per >= rows * (hq // n_kv) > (ntile - 1) * per
@@ -221,6 +222,16 @@ def test_refusals_of_single_calls():
         a = dict(head_dim=128, n_rows=3, n_heads=2, positions=FAKE) | kw
         assert lib.wici_rope_rows(_tab(), a["head_dim"], a["n_rows"], a["n_heads"], a["positions"],
                                   _rows(), _rows(), None) == E
+    # more rows than a call takes
+    big = _batch(n_seqs=1, n_rows=1 << 24, row_start=FAKE)
+    for heads in (2, 4):
+        assert lib.wici_kv8_attend_workspace(c, big, heads, size) == E
+        assert lib.wici_kv8_attend(c, big, heads, 0.1, _rows(heads), _rows(heads), FAKE, 1 << 60, None) == E
+    wide = _cache(n_kv_heads=8)
+    assert lib.wici_kv8_append(wide, big, None, 0, no, no, _rows(8), _rows(8), None) == E
+    assert lib.wici_kv8_append(c, big, _tab(), 12, _rows(12), _rows(12), _rows(), _rows(), None) == E
+    assert lib.wici_kv8_read(wide, big, _rows(8), no, None) == E
+    assert lib.wici_rope_rows(_tab(), 128, 1 << 24, 16, FAKE, _rows(16), _rows(16), None) == E
     for bad in BAD_ROWS:
         assert lib.wici_rope_rows(_tab(), 128, 3, 2, FAKE, _rows(**bad), _rows(), None) == E
         assert lib.wici_rope_rows(_tab(), 128, 3, 2, FAKE, _rows(), _rows(**bad), None) == E
@@ -252,6 +263,10 @@ def test_nothing_to_do_is_no_error_and_no_gpu_call():
         assert lib.wici_kv8_read(_cache(), b, _rows(), no, None) == 0
         assert lib.wici_kv8_attend_workspace(_cache(), b, 4, size) == 0 and size.value == 0
         assert lib.wici_kv8_attend(_cache(), b, 4, 0.1, no, no, None, 0, None) == 0
+    b = _batch(n_seqs=0, n_rows=0, length=None)          # a table of no sequences has no address
+    assert lib.wici_kv8_append(_cache(table=None), b, None, 0, no, no, no, no, None) == 0
+    assert lib.wici_kv8_read(_cache(table=None), b, _rows(), no, None) == 0
+    assert lib.wici_kv8_attend(_cache(table=None), b, 4, 0.1, no, no, None, 0, None) == 0
     assert lib.wici_rope_rows(_tab(), 128, 0, 2, None, no, no, None) == 0
     r = binding.WiciRope(64, 0, 0, 10000.0, 0.0, 0.0, 0.0, 0.0)
     assert lib.wici_rope_table(ctypes.byref(r), 0, None, None, None) == 0
