@@ -465,7 +465,8 @@ wici_status wici_rope_rows(const wici_rope_tab* rope, int32_t head_dim, int32_t 
  * dimensions) or 132 (128) bytes for each position, head, key or value.
  * table[seq * table_stride + i] names the page of the sequence's positions page * i ..; an
  * entry outside [0, n_pages) names none: those positions are not attended, appending to them
- * does nothing, and they read as zero.  So do positions past max_pages pages. */
+ * does nothing, and they read as zero.  So do positions past max_pages pages.  Sequences may
+ * share pages that are only read; the places that one append writes are to be different ones. */
 typedef struct {
   void* pool;           /* device, 16-byte aligned, wici_kv8_bytes bytes */
   int32_t n_pages;
@@ -521,8 +522,9 @@ wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batc
  * (append first),
  *   out = sum_j e^(scale q . k_j) v_j / sum_j e^(scale q . k_j),
  * with scores, weights and sums in fp32; q and the weights enter the matrix products as one
- * fp16 term where q and out are bf16 (exact for q; within 2^-11 of a weight), else two (2^-22).  A row
- * that sees nothing gives zeros.  q and out are n_heads heads, of any of the two types each;
+ * fp16 term where q and out are bf16 (exact for q; within 2^-11 of a weight), else two (2^-22),
+ * and within 2^-31 of the row's largest where they are 2^-20 and less of that.  A row that sees
+ * nothing gives zeros.  q and out are n_heads heads, of any of the two types each;
  * out may be q only if they are the same rows exactly.  workspace: device, 16-byte aligned,
  * undefined before and after. */
 wici_status wici_kv8_attend(const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,

@@ -10,9 +10,11 @@
 // the values' scales are, and one factor 2^-ref cancels in the quotient.  It moves only
 // when a weight would pass 2^15 (it is set 2^6 below the largest), so most steps rescale
 // nothing.  (Where scores pass 2^24 a reference cannot hold log2 t_j beside them: such a
-// row goes on with the largest score and a power of two of its own, `lift`.)  Scores, weights, sums and the output are fp32; q and w enter the products as
-// NT fp16 terms: one for bf16 rows (q is exact in it, a weight within 2^-11, an eighth of
-// the output's own rounding), two where queries or output are fp32 (2^-22).
+// row goes on with the largest score and a power of two of its own, `lift`.)  Scores,
+// weights, sums and the output are fp32; q and w enter the products as NT fp16 terms: one
+// for bf16 rows (q is exact in it, a weight within 2^-11, an eighth of the output's own
+// rounding), two where queries or output are fp32 (2^-22); a weight 2^-20 and more below
+// the largest, within 2^-31 of that.
 //
 // Layout.  S^T = A Q^T and O^T = C^T W^T on v_mfma_f32_16x16x32_f16: lane l holds query
 // row l % 16 in both results, so maximum, sum and rescaling of a row are that lane's own
@@ -37,6 +39,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoRef = -3e38f;    // ref before the first weight
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
+constexpr float kLeastLog = -100.f;  // below log2 of every scale that is stored
 constexpr float kHugeScore = 16777216.f;
 
 // Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
@@ -210,7 +213,7 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
         // difference, the first term is now and then not the one the second completes
         if (NT > 1) asm volatile("" : "+v"(w));
         sum += e;
-        most = fmaxf(most, w);
+        most = __builtin_elementwise_maximum(most, w);  // NaN if one is
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const _Float16 term = (_Float16)w;
@@ -230,7 +233,8 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
   };
   if (huge) lifted();
   else plain();
-  const bool move = __any(most > kMaxWeight);
+  // (NaN: values of scale zero, in memory never appended to, before there is a reference)
+  const bool move = __any(!(most <= kMaxWeight));
   if (move) {  // rare after a row's first step
     // the largest of f over this row's positions
     auto largest = [&](auto f) {
@@ -243,7 +247,9 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
       z = fmaxf(z, __shfl_xor(z, 16));
       return fmaxf(z, __shfl_xor(z, 32));
     };
-    auto lv = [&](int t, int i) { return __builtin_amdgcn_logf((&s.v[t].x)[i]); };
+    auto lv = [&](int t, int i) {
+      return fmaxf(__builtin_amdgcn_logf((&s.v[t].x)[i]), kLeastLog);
+    };
     const float z = largest([&](int t, int i) { return score(t, i) + lv(t, i); });
     huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
     float ref = fmaxf(st.ref, z - kTopWeight), lift = 0.f;
@@ -296,9 +302,10 @@ __device__ __forceinline__ void load_row8(const HeadRows& x, int64_t at, float* 
   else load8(static_cast<const float*>(x.p) + at, o);
 }
 
-// 16 query rows (row l % 16 of the tile, zero where `on` is false) as NT fp16 terms,
-// scaled by a power of two that brings the largest finite magnitude of the 16 into
-// [2^6, 2^7); `unit` undoes it.  Infinities and NaN stay in their own rows.
+// 16 query rows (row l % 16 of the tile, zero where `on` is false) as NT fp16 terms, each
+// row scaled by a power of two that brings its largest finite magnitude into [2^6, 2^7);
+// `unit` undoes it.  An element 2^23 below its row's largest is the first that fp16 rounds
+// (bf16 rows) or leaves to 2^-31 of that largest.  Infinities and NaN stay in their rows.
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(const HeadRows& q, int64_t at, bool on, int lane,
                                              half8_t (&qf)[NT][HD / 32], float& unit) {
@@ -314,8 +321,9 @@ __device__ __forceinline__ void load_queries(const HeadRows& q, int64_t at, bool
       most = a < INFINITY ? fmaxf(most, a) : most;
     }
   }
-  most = wave_max(most);
-  const int ex = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 100);
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const int ex = max((int)(__float_as_uint(most) >> 23) - 127, -120);
   const float up = __uint_as_float((unsigned)(127 + 6 - ex) << 23);
   unit = __uint_as_float((unsigned)(127 - 6 + ex) << 23);
 #pragma unroll

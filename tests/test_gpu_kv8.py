@@ -6,7 +6,7 @@ equality (a bf16 result with the rounding of that answer).  Attention: with S th
 sum |q_d k_d| scale of a row and A the output with |v| in place of v, a score is off by at
 most e = (48 2^-24 + [fp32 rows: 2^-22]) S + 2^-20 (a sum of 128 products in fp32, two fp16
 terms of the query, the exponential's argument and result), which moves a weight and the sum
-by e each; a weight is rounded by 2^-12 (one fp16 term, bf16 rows) or 2^-23 (two) of itself;
+by e each; a weight is off by at most 2^-11 (one fp16 term, bf16 rows) or 2^-22 (two) of itself;
 the sums over n positions add at most (64 + n / 16) roundings of 2^-24 A; and the result is
 rounded once, by eps / 2 of itself."""
 
@@ -89,8 +89,13 @@ class Batch:
         return self.cache.pool[int(self.table[b, p])].cpu().numpy()
 
 
-def check_attend(bt, q, out, K, V, scale, seen=None, rows=None):
-    """out [n_rows, heads, hd] of q against the definition, for every row of the batch."""
+def check_attend(bt, q, out, K, V, scale, seen=None, far=False):
+    """out [n_rows, heads, hd] of q against the definition, for every row of the batch.
+
+    far: with weights 2^-20 and more below the largest W of a row, which fp16 holds only to the
+    half of its least step, 2^-25, where W is 2^6 or more: to 2^-31 W.  W is p_j t_j of some
+    position j, of which a code is 127 in some dimension, so that 127 W <= max_d A_d; codes
+    are at most 127, so n such errors add at most n 2^-31 max_d A_d to a dimension."""
     qn, on = f64(q), f64(out)
     for b, (n, r) in enumerate(zip(bt.lens, bt.rows)):
         at = slice(bt.start[b], bt.start[b] + r)
@@ -103,6 +108,8 @@ def check_attend(bt, q, out, K, V, scale, seen=None, rows=None):
         e = (48 * 2.0 ** -24 + (0 if single else 2.0 ** -22)) * dots + 2.0 ** -20
         rel = 2 * e + (2.0 ** -11 if single else 2.0 ** -22) + (64 + n / 16) * 2.0 ** -24
         tol = mag * rel[..., None] + np.abs(want) * torch.finfo(out.dtype).eps / 2 + 1e-30
+        if far:
+            tol += n * 2.0 ** -31 * mag.max(-1, keepdims=True)
         err = np.abs(on[at] - want)
         assert np.all(err <= tol), (b, float(np.max(err / tol)))
 
@@ -416,6 +423,47 @@ def test_values_of_any_magnitude(ops):
             check_attend(bt, q, bt.cache.attend(q, bt.length), K, V, 128 ** -0.5)
 
 
+def test_queries_of_any_magnitude_in_one_tile(ops):
+    """Rows and heads from 1e-9 to 1e9 (and one of 1e38 on keys of 1e-38) beside each other, in
+    every order, for single tokens and for prompts: each row's precision is its own."""
+    for rows in (None, [40, 9]):
+        bt = Batch(ops, [150, 90], rows, n_kv=2, hd=64, page=32, seed=5)
+        K, V = bt.fill()
+        for dtype in (BF16, F32):
+            q = rnd(bt.rng, bt.n_rows, 6, 64, dtype=F32)
+            size = 10.0 ** bt.rng.uniform(-9, 9, (bt.n_rows, 6, 1))
+            size[bt.rng.random(size.shape) < 0.4] = 1.0
+            q = (q * torch.from_numpy(size).float().cuda()).to(dtype)
+            check_attend(bt, q, bt.cache.attend(q, bt.length, row_start=bt.row_start), K, V, 0.125,
+                         far=True)
+    bt = Batch(ops, [60], [20], n_kv=1, hd=128, page=16, seed=6)
+    k, v = (rnd(bt.rng, 60, 1, 128, dtype=F32) for _ in "kv")
+    k *= 1e-18
+    bt.cache.append(k, v, bt.length, row_start=ints([0, 60]))
+    K, V = ([oracle.kv8_values(f64(x))] for x in (k, v))
+    for dtype in (BF16, F32):
+        q = rnd(bt.rng, 20, 4, 128, dtype=F32).clamp(-3, 3)
+        q[::3] *= 1e38
+        q[1::3] *= 1e18
+        q = q.to(dtype)
+        check_attend(bt, q, bt.cache.attend(q, bt.length, row_start=bt.row_start, scale=1e-20), K, V,
+                     1e-20, far=True)
+
+
+def test_hints_that_are_wrong(ops):
+    """max_rows and max_length below what the batch holds (a plan captured for a small batch), or
+    far above: the same rows, beyond the order of sums; a scale of zero weighs all alike."""
+    bt = Batch(ops, [900, 5, 300], [130, 5, 17], n_kv=2, hd=128, page=16)
+    K, V = bt.fill()
+    q = rnd(bt.rng, bt.n_rows, 8, 128, dtype=F32)
+    for hints in (dict(max_rows=1), dict(max_rows=1, max_length=1), dict(max_length=33),
+                  dict(max_rows=2 ** 31 - 1, max_length=2 ** 31 - 1), dict(max_rows=40, max_length=20000)):
+        check_attend(bt, q, bt.cache.attend(q, bt.length, row_start=bt.row_start, **hints), K, V,
+                     128 ** -0.5)
+    for scale in (0.0, -128 ** -0.5):
+        check_attend(bt, q, bt.cache.attend(q, bt.length, row_start=bt.row_start, scale=scale), K, V, scale)
+
+
 def test_rows_that_see_nothing(ops):
     """Length zero, every page absent, more rows than positions: zeros, where garbage lies in
     the pages; and rows of no sequence are left."""
@@ -582,6 +630,124 @@ def test_prompt_then_tokens_is_one_long_prompt(ops):
         assert torch.equal(x, y)
     # both within the bound of check_attend; rows of unit scale: 2^-17 covers twice that
     assert (torch.cat(parts) - full).abs().max() <= 2.0 ** -17 * 4
+
+
+def test_prompts_in_a_graph(ops):
+    """A packed batch of prompts (its rows padded) captured once for each way of launching it, and
+    replayed as rows, lengths and pages change in place, against eager calls."""
+    rng = np.random.default_rng(12)
+    H, G, hd, page = 4, 8, 128, 16
+    for hints in (dict(max_rows=400, max_length=500), dict(max_rows=4, max_length=500),
+                  dict(max_rows=400, max_length=30000)):
+        table = ints(rng.permutation(96).reshape(2, 48).tolist())
+        cache = ops.KvCache.empty(96, H, hd, table, page=page)
+        cache.pool.zero_()
+        t = ops.rope_table(800, hd)
+        q, k, v = (rnd(rng, 440, n, hd) for n in (H * G, H, H))
+        length, start = ints([400, 40]), ints([0, 400, 440])
+        qq, out = torch.empty_like(q), torch.empty_like(q)
+
+        def step():
+            cache.append(k, v, length, row_start=start, rope=t, q=q, q_out=qq)
+            cache.attend(qq, length, row_start=start, out=out, **hints)
+
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            step()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step()
+        for lens, rows in (((400, 40), (400, 40)), ((640, 200), (240, 160)), ((641, 768), (1, 436)),
+                           ((641, 768), (0, 0)), ((700, 3), (59, 3))):
+            length.copy_(ints(lens))
+            start.copy_(ints([1, 1 + rows[0], 1 + sum(rows)]))
+            for x in (q, k, v):
+                x.copy_(rnd(rng, *x.shape))
+            kept = cache.pool.clone()
+            out.fill_(3), qq.fill_(3)
+            step()
+            want, pool = out.clone(), cache.pool.clone()
+            cache.pool.copy_(kept)
+            out.fill_(3), qq.fill_(3)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(cache.pool, pool)
+            assert (out[0] == 3).all() and (out[1 + sum(rows):] == 3).all()
+
+
+def test_shared_pages_and_two_streams(ops):
+    """Sequences that begin with the same pages (and one page twice in a sequence) attend over
+    them at once on two streams, each call with a workspace of its own."""
+    bt = Batch(ops, [640], [640], n_kv=2, hd=128, page=16)
+    K, V = bt.fill()
+    own = bt.table[0, :40]
+    shared = torch.stack([own, own.flip(0), own[:1].expand(40)]).contiguous()
+    cache = ops.KvCache(bt.cache.pool, shared, page=16, head_dim=128)
+    lens = [640, 631, 100]
+    where = [np.arange(640), (39 - np.arange(640) // 16) * 16 + np.arange(640) % 16, np.arange(640) % 16]
+    sub = Batch.__new__(Batch)
+    sub.lens, sub.rows, sub.start = lens, [1, 1, 1], np.arange(4)
+    KK, VV = ([x[0][w[:n]] for w, n in zip(where, lens)] for x in (K, V))
+    q = [rnd(bt.rng, 3, 8, 128, dtype=F32) for _ in "ab"]
+    length = ints(lens)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in "ab"]
+    outs = [[cache.attend(x, length, stream=s) for s, x in zip(streams, q)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for got in outs:
+        for x, first, out in zip(q, outs[0], got):
+            assert torch.equal(out, first)
+            check_attend(sub, x, out, KK, VV, 128 ** -0.5)
+    for x, first in zip(q, outs[0]):
+        y = x.clone()
+        assert cache.attend(y, length, out=y) is y and torch.equal(y, first)   # out may be q
+
+
+def test_memory_in_use_on_another_stream_is_not_handed_out(ops):
+    """A cache or a table dropped while a call on another stream still waits stays allocated
+    until that call is done."""
+    side = torch.cuda.Stream()
+    x = torch.zeros(1, 2, 64, device="cuda")
+    one = ints([1])
+
+    def calls():
+        cache = ops.KvCache.empty(64, 2, 64, ints([[0]]), page=64)
+        table = ops.rope_table(50000, 64)
+        kept = [t.data_ptr() for t in (cache.pool, table.cos, table.sin)]
+        yield lambda: cache.append(x, x, one, rope=table, stream=side), kept
+        cache = ops.KvCache.empty(64, 2, 64, ints([[0]]), page=64)
+        yield lambda: cache.read(one, stream=side), [cache.pool.data_ptr()]
+        cache = ops.KvCache.empty(64, 2, 64, ints([[0]]), page=64)
+        yield lambda: cache.attend(x, one, stream=side), [cache.pool.data_ptr()]
+        table = ops.rope_table(50000, 64)
+        yield lambda: ops.rope(x, one, table, stream=side), [table.cos.data_ptr(), table.sin.data_ptr()]
+
+    for i in range(4):
+        it = calls()
+        for _ in range(i + 1):
+            call, kept = next(it)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(200_000_000)
+        call()
+        it.close()
+        del it, call
+        new = [torch.empty(n, dtype=torch.uint8, device="cuda")
+               for n in (64 * 2 * 2 * 64 * 68, 50000 * 32 * 4, 50000 * 32 * 4)]
+        busy = not side.query()
+        assert busy and not set(kept) & {t.data_ptr() for t in new}, i
+        torch.cuda.synchronize()
+
+
+def test_no_sequences(ops):
+    """A cache whose table has no sequence takes calls that have no rows."""
+    cache = ops.KvCache.empty(2, 2, 64, torch.zeros(0, 3, dtype=torch.int32, device="cuda"), page=16)
+    none, x = ints([]).view(0), torch.zeros(0, 2, 64, device="cuda")
+    assert cache.append(x, x, none) is None
+    assert cache.attend(x, none).shape == (0, 2, 64) and cache.read(none)[0].shape == (0, 2, 64)
 
 
 def test_workspace_given_and_refused(ops):
