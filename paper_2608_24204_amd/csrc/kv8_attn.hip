@@ -105,14 +105,26 @@ struct Pages {
   int phys[kTiles];
   __device__ __forceinline__ bool all() const { return (phys[0] | phys[1]) >= 0; }
 };
-__device__ __forceinline__ int find_page(const Kv8& c, const Kv8Seq& q, uint32_t pos) {
-  return uniform(kv8_page_of(q.table, pos >> c.page_shift, c.max_pages, c.n_pages));
+// A sequence's table entries are read by scalar loads, a chunk or step before they are looked
+// at: loads of the vector path would first wait for every row requested since.
+__device__ __forceinline__ int entry(const Kv8& c, const Kv8Seq& q, uint32_t pos) {
+  typedef const __attribute__((address_space(4))) int32_t* Table;
+  return ((Table)(uintptr_t)q.table)[kv8_entry(pos >> c.page_shift, c.max_pages)];
 }
-// (steps end below 2^31 positions; one looked up past them is still below 2^32)
-__device__ __forceinline__ Pages find_pages(const Kv8& c, const Kv8Seq& q, int step) {
+// The entries of a step (steps end below 2^31 positions; one past them is still below 2^32).
+struct Entries {
+  int e[kTiles];
+};
+__device__ __forceinline__ Entries find(const Kv8& c, const Kv8Seq& q, int step) {
+  Entries f;
+  f.e[0] = entry(c, q, (uint32_t)step * kStep);
+  f.e[1] = c.page_shift >= 5 ? f.e[0] : entry(c, q, (uint32_t)step * kStep + 16);
+  return f;
+}
+__device__ __forceinline__ Pages named(const Kv8& c, const Entries& f) {
   Pages p;
-  p.phys[0] = find_page(c, q, (uint32_t)step * kStep);
-  p.phys[1] = c.page_shift >= 5 ? p.phys[0] : find_page(c, q, (uint32_t)step * kStep + 16);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) p.phys[t] = kv8_named(f.e[t], c.n_pages);
   return p;
 }
 
@@ -198,7 +210,15 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
                                         float& corr) {
   const int left = seen - 4 * (lane >> 4);
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
-  auto score = [&](int t, int i) { return sc[t][i] * ((&s.k[t].x)[i] * q_unit); };
+  // a score rounded by itself, never joined with what follows: of two that are equal and huge
+  // the difference is zero
+  auto score = [&](int t, int i) {
+    float y = sc[t][i];
+    asm volatile("" : "+v"(y));  // (and not for every step, ahead of the rare branches)
+    y *= (&s.k[t].x)[i] * q_unit;
+    asm volatile("" : "+v"(y));
+    return y;
+  };
   float sum, most;
   // f(t, i) is a score less the reference
   auto weigh = [&](float down, auto f) {
@@ -227,7 +247,6 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
       return __builtin_fmaf(sc[t][i], (&s.k[t].x)[i] * q_unit, -st.ref);
     });
   };
-  // with the rounded scores, which the huge scores of a tie share
   auto lifted = [&]() {
     weigh(__builtin_amdgcn_exp2f(-st.lift), [&](int t, int i) { return score(t, i) - st.ref; });
   };
@@ -247,8 +266,10 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
       z = fmaxf(z, __shfl_xor(z, 16));
       return fmaxf(z, __shfl_xor(z, 32));
     };
-    auto lv = [&](int t, int i) {
-      return fmaxf(__builtin_amdgcn_logf((&s.v[t].x)[i]), kLeastLog);
+    auto lv = [&](int t, int i) {  // (taken here: not for every step, ahead of the branch)
+      float x = (&s.v[t].x)[i];
+      asm volatile("" : "+v"(x));
+      return fmaxf(__builtin_amdgcn_logf(x), kLeastLog);
     };
     const float z = largest([&](int t, int i) { return score(t, i) + lv(t, i); });
     huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
@@ -398,7 +419,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   // looked up beside it
   const HeadAt<HD> kv(c, q, h);
   const int s0 = 4 * split + wave;
-  const Pages p0 = find_pages(c, q, s0), p1 = find_pages(c, q, s0 + 4 * nsplit);
+  const Entries e0 = find(c, q, s0), e1 = find(c, q, s0 + 4 * nsplit);
 
   for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
     const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
@@ -429,13 +450,15 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
       Keys<HD> k;
       Values<HD> v;
       Scales sl;
-      Pages now = p0, next = p1;
+      Pages now = named(c, e0);
+      Entries later = e1;
       load_keys<HD>(k, c, kv, now, s, lane);
       load_values<HD>(v, sl, c, kv, now, s, lane);
       for (;;) {
         floatx4_t sc[kTiles];
         scores<HD, NT>(sc, k, qf);
         const int then = s + stride;
+        const Pages next = named(c, later);
         if (then < steps) load_keys<HD>(k, c, kv, next, then, lane);
         half8_t wf[NT];
         float corr = 1.f;
@@ -448,7 +471,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         if (then >= steps) break;
         load_values<HD>(v, sl, c, kv, next, then, lane);
         now = next;
-        next = find_pages(c, q, then + stride);
+        later = find(c, q, then + stride);
         s = then;
       }
     }
@@ -561,15 +584,22 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     float sc = 0.f;
     int phys[kChunkTiles], later[kChunkTiles];
     const int pair = wave >> 1, half = HD == 128 ? wave & 1 : 0;
-    auto find = [&](int (&p)[kChunkTiles], int chunk) {
-      p[0] = find_page(c, q, (uint32_t)chunk * kChunkPos);
+    auto find = [&](int chunk) {
 #pragma unroll
-      for (int t = 1; t < kChunkTiles; ++t)
-        p[t] = c.page_shift >= 6 ? p[0] : find_page(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
+      for (int t = 0; t < kChunkTiles; ++t)
+        later[t] = entry(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
+    };
+    auto look = [&]() {
+#pragma unroll
+      for (int t = 0; t < kChunkTiles; ++t) phys[t] = kv8_named(later[t], c.n_pages);
     };
     auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
       const int j0 = chunk * kChunkPos;
-      auto pick = [&](int t) { return t == 0 ? p[0] : t == 1 ? p[1] : t == 2 ? p[2] : p[3]; };
+      // p[t], with bits: a choice between the elements would put them into memory
+      auto pick = [&](int t) {
+        const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
+        return lo ^ ((lo ^ hi) & -(t >> 1));
+      };
       const int ks = (j0 + 16 * wave) & (page - 1);
       const __amdgpu_buffer_rsrc_t kb = kv.buffer(c, uniform(pick(wave)), 0);
 #pragma unroll
@@ -582,7 +612,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
         vc[t] = fetch(vb, kv8_value_at(4 * g, 4 * r16, HD) + 256 * half, kv8_value_at(vs, 0, HD));
       }
       if (wave < 2)
-        sc = *reinterpret_cast<const float*>(
+        sc = *(const __attribute__((address_space(1))) float*)(uintptr_t)(
             kv.block(pick(g), wave) + kv8_scale_at((j0 + lane) & (page - 1), page, HD));
     };
     auto convert = [&](int buf) {
@@ -600,23 +630,20 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     };
 
     if (c0 < c1) {
-      find(phys, c0);
+      find(c0);
+      look();
       bring(phys, c0);
-      find(later, c0 + 1);
+      find(c0 + 1);
     }
     for (int ch = c0; ch < c1; ++ch) {
       const int buf = (ch - c0) & 1;
-      convert(buf);
       int now[kChunkTiles];
 #pragma unroll
-      for (int t = 0; t < kChunkTiles; ++t) {
-        now[t] = phys[t];
-        phys[t] = later[t];
-      }
-      if (ch + 1 < c1) {
-        bring(phys, ch + 1);
-        find(later, ch + 2);
-      }
+      for (int t = 0; t < kChunkTiles; ++t) now[t] = phys[t];
+      look();
+      find(ch + 2);
+      convert(buf);
+      if (ch + 1 < c1) bring(phys, ch + 1);
       __syncthreads();
       if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
 #pragma unroll

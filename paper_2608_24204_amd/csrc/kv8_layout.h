@@ -36,10 +36,14 @@ WICI_HD int kv8_page(const int32_t* table, int64_t p, int max_pages, int n_pages
   return phys < 0 || phys >= n_pages ? -1 : phys;
 }
 
-// The same with no branch around the look-up (p below 2^32, max_pages at least 1).
-WICI_HD int kv8_page_of(const int32_t* table, uint32_t p, int max_pages, int n_pages) {
-  const int phys = table[p < (uint32_t)max_pages ? p : (uint32_t)max_pages - 1];
-  return p < (uint32_t)max_pages && (uint32_t)phys < (uint32_t)n_pages ? phys : -1;
+// The same in two parts, for a look-up whose answer is wanted later: the entry to read (p below
+// 2^32, max_pages at least 1; past the table the last one, whose page then stands for positions
+// that no row sees), and the page it names or -1.
+WICI_HD uint32_t kv8_entry(uint32_t p, int max_pages) {
+  return p < (uint32_t)max_pages ? p : (uint32_t)max_pages - 1;
+}
+WICI_HD int kv8_named(int entry, int n_pages) {
+  return (uint32_t)entry < (uint32_t)n_pages ? entry : -1;
 }
 
 // The rows a sequence has when row_start says [from, to): a range inside [0, n_rows].

@@ -30,7 +30,11 @@ int main() {
       // a table of exactly max_pages entries: an access past it is the sanitizer's to find
       std::vector<int32_t> table((size_t)a[1], (int32_t)a[3]);
       const int got = kv8_page(table.data(), a[0], (int)a[1], (int)a[2]);
-      if (a[0] >= 0 && kv8_page_of(table.data(), (uint32_t)a[0], (int)a[1], (int)a[2]) != got) return 3;
+      if (a[0] >= 0) {  // the look-up in two parts, of entries inside the table
+        const uint32_t at = kv8_entry((uint32_t)a[0], (int)a[1]);
+        const int two = kv8_named(table[at], (int)a[2]);
+        if (a[0] < a[1] ? two != got : at != (uint32_t)a[1] - 1 || two >= (int)a[2]) return 3;
+      }
       std::printf("%d\n", got);
     } else if (!std::strcmp(what, "range")) {  // from, to, n_rows
       int row0, rows;
