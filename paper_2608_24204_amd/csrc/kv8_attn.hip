@@ -584,14 +584,19 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     float sc = 0.f;
     int phys[kChunkTiles], later[kChunkTiles];
     const int pair = wave >> 1, half = HD == 128 ? wave & 1 : 0;
+    const bool whole_chunk = c.page_shift >= 6;  // one page holds a chunk
     auto find = [&](int chunk) {
+      later[0] = entry(c, q, (uint32_t)chunk * kChunkPos);
+      if (!whole_chunk)
 #pragma unroll
-      for (int t = 0; t < kChunkTiles; ++t)
-        later[t] = entry(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
+        for (int t = 1; t < kChunkTiles; ++t)
+          later[t] = entry(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
     };
     auto look = [&]() {
+      phys[0] = kv8_named(later[0], c.n_pages);
 #pragma unroll
-      for (int t = 0; t < kChunkTiles; ++t) phys[t] = kv8_named(later[t], c.n_pages);
+      for (int t = 1; t < kChunkTiles; ++t)
+        phys[t] = whole_chunk ? phys[0] : kv8_named(later[t], c.n_pages);
     };
     auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
       const int j0 = chunk * kChunkPos;
@@ -600,20 +605,32 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
         const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
         return lo ^ ((lo ^ hi) & -(t >> 1));
       };
-      const int ks = (j0 + 16 * wave) & (page - 1);
-      const __amdgpu_buffer_rsrc_t kb = kv.buffer(c, uniform(pick(wave)), 0);
+      auto keys = [&](__amdgpu_buffer_rsrc_t b, int slot) {
 #pragma unroll
-      for (int i = 0; i < HD / 64; ++i)
-        kc[i] = fetch(kb, kv8_key_at(r16, g * (HD / 4), HD) + 16 * i, kv8_key_at(ks, 0, HD));
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int vs = (j0 + 32 * pair + 16 * t) & (page - 1);
-        const __amdgpu_buffer_rsrc_t vb = kv.buffer(c, uniform(pick(2 * pair + t)), 1);
-        vc[t] = fetch(vb, kv8_value_at(4 * g, 4 * r16, HD) + 256 * half, kv8_value_at(vs, 0, HD));
-      }
-      if (wave < 2)
+        for (int i = 0; i < HD / 64; ++i)
+          kc[i] = fetch(b, kv8_key_at(r16, g * (HD / 4), HD) + 16 * i, kv8_key_at(slot, 0, HD));
+      };
+      auto values = [&](int t, __amdgpu_buffer_rsrc_t b, int slot) {
+        vc[t] = fetch(b, kv8_value_at(4 * g, 4 * r16, HD) + 256 * half, kv8_value_at(slot, 0, HD));
+      };
+      auto scales = [&](const char* block) {
         sc = *(const __attribute__((address_space(1))) float*)(uintptr_t)(
-            kv.block(pick(g), wave) + kv8_scale_at((j0 + lane) & (page - 1), page, HD));
+            block + kv8_scale_at((j0 + lane) & (page - 1), page, HD));
+      };
+      if (whole_chunk) {
+        const int slot = j0 & (page - 1);
+        keys(kv.buffer(c, p[0], 0), slot + 16 * wave);
+        const __amdgpu_buffer_rsrc_t b = kv.buffer(c, p[0], 1);
+        values(0, b, slot + 32 * pair);
+        values(1, b, slot + 32 * pair + 16);
+        if (wave < 2) scales(kv.block(p[0], wave));
+      } else {
+        keys(kv.buffer(c, pick(wave), 0), (j0 + 16 * wave) & (page - 1));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          values(t, kv.buffer(c, pick(2 * pair + t), 1), (j0 + 32 * pair + 16 * t) & (page - 1));
+        if (wave < 2) scales(kv.block(pick(g), wave));
+      }
     };
     auto convert = [&](int buf) {
       const unsigned* w = reinterpret_cast<const unsigned*>(kc);
