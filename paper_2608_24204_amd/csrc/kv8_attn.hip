@@ -106,7 +106,8 @@ struct Pages {
   __device__ __forceinline__ bool all() const { return (phys[0] | phys[1]) >= 0; }
 };
 // A sequence's table entries are read by scalar loads, a chunk or step before they are looked
-// at: loads of the vector path would first wait for every row requested since.
+// at: loads of the vector path would first wait for every row requested before them (2048
+// rows of 8192: 344 us, so 313).
 __device__ __forceinline__ int entry(const Kv8& c, const Kv8Seq& q, uint32_t pos) {
   typedef const __attribute__((address_space(4))) int32_t* Table;
   return ((Table)(uintptr_t)q.table)[kv8_entry(pos >> c.page_shift, c.max_pages)];
@@ -401,6 +402,14 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, f
 // (row r: new row r / G, query head r % G), and are joined at the end.  Splits take
 // groups of four steps in turn, so one launch serves any length evenly.  With one
 // split the output is written here, otherwise (ref, sum, output) to `part` for the merge.
+//
+// Bound by the cache's bytes, each read once: 32 tokens at 16384 (40 query on 8 KV heads of
+// 128, bf16) 188 us for 1.11 GB, 5.9 TB/s where a large copy moves 5.2; its loads with
+// nothing behind them take as long.  Where there is less to read the start, the first loads'
+// latency and the join show: 48 tokens at up to 4000 (heads of 64) 37 us for 173 MB, one at
+// 16384 (fp32) 14 us for 35 MB.  Three wavefronts a SIMD for heads of 128 (two with two fp16
+// terms), four for heads of 64; 256 / 512 / 768 / 1024 workgroups: 289 / 203 / 195 / 231 us
+// of the first case, which is why a launch splits no further than fills the chip once.
 template <int HD, int NT>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
@@ -513,14 +522,18 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 
 // ------------------------------------------------------------------- prompts: row tiles
 // Workgroup (KV head, tile of 128 (or 64) rows x query heads, split, sequence): each of
-// four wavefronts holds a quarter of the rows and takes every chunk of 64 positions of the split.  The codes of
-// a chunk become fp16 operands once for all four, in LDS, lane by lane as the products read
-// them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers: the
-// next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
-// parts a buffer's readers from its next writers.  Bound by the softmax's vector work
-// (about eight issue slots a score, four of them the exponential, beside two matrix
-// products).
-
+// four wavefronts holds a quarter of the rows and takes every chunk of 64 positions of the
+// split.  The codes of a chunk become fp16 operands once for all four, in LDS, lane by lane as
+// the products read them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.
+// Two buffers: the next chunk's codes are on their way while this one is multiplied, and one
+// barrier a chunk parts a buffer's readers from its next writers.
+//
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 299 us in bf16, 804 TFLOP/s
+// of products where a large fp16 product reaches 1300; 477 us with two fp16 terms.  No unit is
+// full: the vector units are busy 53% of the time, the matrix cores 32%, and a wavefront waits
+// for operands, products or the other one (the registers allow two a SIMD).  Eight vector
+// instructions fewer for 512 scores, and priorities of the products or the weights, changed
+// nothing; the next products ahead of the weights need more registers than there are.
 template <int HD, int NT, int kRowTiles>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,

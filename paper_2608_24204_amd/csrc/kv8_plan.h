@@ -22,11 +22,15 @@ struct Kv8Plan {
 // Which kernel, from the rows x heads of a KV head, the workgroups of 128 of them and the
 // 16 rows x 32 positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us,
 // split / 64 rows / 128 rows):
-//  - below 128 rows the split: 16 new rows of each of 8 sequences of 2000: 25 / 32 / 32;
+//  - below 128 rows the split: 16 new rows of each of 8 sequences of 2000: 24 / 25 / 33;
+//    16 of 8000 positions: 20 / 23 / 29;
 //  - where 128 rows fill the chip, or have long contexts to split: 2048 of 8192 positions:
-//    668 / 580 / 379; 16 x 100 of 1000: 100 / 96 / 67; 128 of 8000: 63 / 63 / 54;
-//  - a chip half full: 64 rows: 1024 of 1024: 49 / 44 / 63; 32 x 32 of 300: 36 / 25 / 50;
-//  - few workgroups and little to do: the split: 333 of 333: 14 / 30 / 32.
+//    634 / 392 / 300; 16 x 100 of 1000: 64 / 54 / 52; 128 of 8000: 57 / 49 / 49;
+//  - a chip half full: 64 rows: 1024 of 1024: 41 / 32 / 58; 32 x 32 of 300: 30 / 19 / 22;
+//  - few workgroups and little to do: the split: 333 of 333: 12 / 16 / 23; 256 of 512:
+//    12 / 18 / 25.
+// (The farthest from the best of 24 such: 32 of 4000 in 4 sequences, 36 for 32; fp32, 512 of
+// 2048, 65 for 59.)
 constexpr int kTileRows = 128, kFull = 400, kHalf = 200;
 constexpr double kMuch = 60000;
 inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {

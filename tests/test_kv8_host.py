@@ -14,6 +14,7 @@ import pytest
 
 import oracle
 from paper_2608_24204_amd import binding
+from tests.helpers import small_cfg
 from tests.test_gpu_kv8 import PLAN_CASES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -277,3 +278,49 @@ def test_pool_size():
     lib, size = binding.load_library(), ctypes.c_size_t()
     assert lib.wici_kv8_bytes(_cache(n_pages=100000, n_kv_heads=8), size) == 0
     assert size.value == 100000 * 2 * 8 * 64 * 132
+
+
+# ------------------------------------------------------------------ the model's side of it
+def _model_cfg(**kw):
+    return binding.make_config(small_cfg(**(dict(n_layers=2, d_model=512, n_heads=4, n_kv_heads=2,
+                                                 head_dim=128, ffn_dim=512, vocab=1000,
+                                                 kv_dtype="kv8") | kw)), max_seq=1000)
+
+
+@lib_built
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+def test_a_models_cache_has_the_pools_bytes(hd, page):
+    c = _model_cfg(head_dim=hd)
+    c.kv_page = page
+    pages = -(-1000 // page)
+    size = ctypes.c_size_t()
+    lib = binding.load_library()
+    assert lib.wici_kv8_bytes(_cache(n_pages=pages, page=page, n_kv_heads=2, head_dim=hd), size) == 0
+    kv = binding.memory_requirements(c)[1]
+    assert 2 * size.value <= kv <= 2 * size.value + 4096
+    other = _model_cfg(head_dim=hd, kv_dtype="bf16")
+    other.kv_page = page
+    assert abs(kv / binding.memory_requirements(other)[1] - (hd + 4) / (2 * hd)) < 0.01
+
+
+@lib_built
+def test_set_rope_before_memory_is_bound():
+    lib, h = binding.load_library(), ctypes.c_void_p()
+    spec = lambda **kw: binding.WiciRope(*(dict(dim=64, layout=1, scaling=3, base=10000.0, factor=2.0,
+                                                original=2048.0, low=0.0, high=0.0) | kw).values())
+    for kv in ("kv8", "bf16", "f32"):
+        c = _model_cfg(head_dim=64, kv_dtype=kv)
+        assert lib.wici_create(ctypes.byref(c), None, ctypes.byref(h)) == binding.WICI_OK
+        try:
+            sizes = binding.memory_requirements(c)
+            for bad in (dict(dim=72), dict(dim=128), dict(dim=0), dict(layout=2), dict(scaling=9),
+                        dict(base=1.0), dict(factor=0.5), dict(original=-1.0)):
+                assert lib.wici_set_rope(h, ctypes.byref(spec(**bad))) == binding.WICI_E_ARG, bad
+            assert lib.wici_set_rope(h, None) == binding.WICI_E_ARG
+            assert lib.wici_set_rope(None, ctypes.byref(spec())) == binding.WICI_E_ARG
+            for good in (dict(), dict(dim=8, layout=0), dict(scaling=0, factor=0.0, original=0.0)):
+                assert lib.wici_set_rope(h, ctypes.byref(spec(**good))) == binding.WICI_OK
+            assert binding.memory_requirements(c) == sizes
+        finally:
+            lib.wici_destroy(h)
