@@ -406,7 +406,7 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, f
 // Bound by the cache's bytes, each read once: 32 tokens at 16384 (40 query on 8 KV heads of
 // 128, bf16) 188 us for 1.11 GB, 5.9 TB/s where a large copy moves 5.2; its loads with
 // nothing behind them take as long.  Where there is less to read the start, the first loads'
-// latency and the join show: 48 tokens at up to 4000 (heads of 64) 37 us for 173 MB, one at
+// latency and the join show: 48 tokens at up to 4000 (heads of 64) 37 us for 162 MB, one at
 // 16384 (fp32) 14 us for 35 MB.  Three wavefronts a SIMD for heads of 128 (two with two fp16
 // terms), four for heads of 64; 256 / 512 / 768 / 1024 workgroups: 289 / 203 / 195 / 231 us
 // of the first case, which is why a launch splits no further than fills the chip once.

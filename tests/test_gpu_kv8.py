@@ -742,6 +742,72 @@ def test_memory_in_use_on_another_stream_is_not_handed_out(ops):
         torch.cuda.synchronize()
 
 
+def test_many_sequences_in_a_part_of_a_wider_table(ops):
+    """3000 sequences of none to three new rows each: every row finds its own, in a table whose
+    rows are longer than the cache's part of them."""
+    rng = np.random.default_rng(31)
+    n, H, G, hd, page = 3000, 1, 4, 64, 16
+    new = rng.integers(0, 4, n)
+    new[:5], new[-3:] = 0, 0
+    lens = new + rng.integers(0, 20, n)
+    wide = ints(rng.integers(-9, 0, (n, 9)).tolist())
+    wide[:, 4:6] = ints(rng.permutation(2 * n).reshape(n, 2).tolist())
+    cache = ops.KvCache.empty(2 * n, H, hd, wide[:, 4:6], page=page)
+    length = ints(lens.tolist())
+    whole = np.concatenate([[0], np.cumsum(lens)])
+    k, v = (rnd(rng, int(whole[-1]), H, hd) for _ in "kv")
+    cache.append(k, v, length, row_start=ints(whole.tolist()))
+    K, V = oracle.kv8_values(f64(k)), oracle.kv8_values(f64(v))
+    rk, rv = cache.read(length, row_start=ints(whole.tolist()), n_rows=int(whole[-1]), dtype=F32)
+    assert np.array_equal(f64(rk), K.astype(np.float32)) and np.array_equal(f64(rv), V.astype(np.float32))
+    bt = Batch.__new__(Batch)
+    bt.lens, bt.rows, bt.start = lens.tolist(), new.tolist(), np.concatenate([[0], np.cumsum(new)])
+    for dtype in (BF16, F32):
+        q = rnd(rng, int(bt.start[-1]), H * G, hd, dtype=dtype)
+        out = cache.attend(q, length, row_start=ints(bt.start.tolist()))
+        check_attend(bt, q, out, [K[a:b] for a, b in zip(whole, whole[1:])],
+                     [V[a:b] for a, b in zip(whole, whole[1:])], 0.125)
+
+
+def test_keys_past_the_rotary_tables_are_kept_as_nan(ops):
+    bt = Batch(ops, [30], [30], n_kv=1, hd=64, page=16)
+    t = ops.rope_table(20, 32, layout="pairs")
+    k, v = (rnd(bt.rng, 30, 1, 64) for _ in "kv")
+    q = bt.cache.append(k, v, bt.length, row_start=bt.row_start, rope=t, q=k.repeat(1, 2, 1))
+    rk, rv = bt.cache.read(bt.length, row_start=bt.row_start, n_rows=30, dtype=F32)
+    assert not rk[:20].isnan().any() and rk[20:].isnan().all() and not rv.isnan().any()
+    assert not q[:20].isnan().any() and q[20:, :, :32].isnan().all() and not q[20:, :, 32:].isnan().any()
+    out = bt.cache.attend(k.repeat(1, 2, 1), bt.length, row_start=bt.row_start)
+    assert not out[:20].isnan().any() and out[20:].isnan().all()
+
+
+def test_calls_that_name_the_captured_stream(ops):
+    """Capture of calls that name their stream, on the stream that is captured."""
+    bt = Batch(ops, [300, 40], n_kv=2, hd=64, page=16)
+    bt.fill()
+    q, k, v = (rnd(bt.rng, 2, h, 64) for h in (8, 2, 2))
+    t = ops.rope_table(400, 64)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def step():
+        qq = bt.cache.append(k, v, bt.length, rope=t, q=q, stream=s)
+        return bt.cache.attend(qq, bt.length, stream=s)
+
+    with torch.cuda.stream(s):
+        want = step().clone()
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = step()
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
 def test_no_sequences(ops):
     """A cache whose table has no sequence takes calls that have no rows."""
     cache = ops.KvCache.empty(2, 2, 64, torch.zeros(0, 3, dtype=torch.int32, device="cuda"), page=16)
