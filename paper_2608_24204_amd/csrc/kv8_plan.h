@@ -46,12 +46,23 @@ inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int ma
   const int64_t per = p.row_tiles ? 64 * p.row_tiles : 16;
   p.ntile = std::max(1, (int)((rows + per - 1) / per));
   const int64_t blocks = heads * p.ntile;
-  const int64_t want = (p.row_tiles ? 2 * kCus : resident(hd, terms)) / blocks;
-  // positions worth a split: a step a wavefront; eight chunks of a tile's, whose 128 rows'
-  // partial results are the larger traffic
-  const int64_t least = p.row_tiles ? 8 * kChunkPos : 4 * kStep;
-  const int64_t most = (max_length + least - 1) / least;
-  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 128));
+  const int64_t want =
+      std::min<int64_t>((p.row_tiles ? 2 * kCus : resident(hd, terms)) / blocks, 128);
+  if (want <= 1) {
+    p.nsplit = 1;
+  } else if (p.row_tiles) {
+    // eight chunks a split at least: partial results of 128 rows are the larger traffic
+    const int64_t most = ((int64_t)max_length + 8 * kChunkPos - 1) / (8 * kChunkPos);
+    p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
+  } else {
+    // Each wavefront as many steps: one at 16384 positions 16.4 us with 64 splits of two
+    // steps a wavefront, 17.6 with the 96 that the chip holds.  Up to 512 positions, four
+    // steps, no split: 256 7.7 us (one split) for 9.1 (two, and the merge), 512 9.5 for 9.1,
+    // and a call's host work 3 us less; 700 would be 11.0 for 9.1.
+    const int64_t steps = ((int64_t)max_length + kStep - 1) / kStep;
+    const int64_t each = steps <= 16 ? 4 : (steps + 4 * want - 1) / (4 * want);
+    p.nsplit = (int)std::max<int64_t>(1, (steps + 4 * each - 1) / (4 * each));
+  }
   return p;
 }
 
