@@ -529,7 +529,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 // barrier a chunk parts a buffer's readers from its next writers.
 //
 // 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 299 us in bf16, 804 TFLOP/s
-// of products where a large fp16 product reaches 1300; 477 us with two fp16 terms.  No unit is
+// of products where a large fp16 product reaches 1300; 493 us with two fp16 terms.  No unit is
 // full: the vector units are busy 53% of the time, the matrix cores 32%, and a wavefront waits
 // for operands, products or the other one (the registers allow two a SIMD).  Eight vector
 // instructions fewer for 512 scores, and priorities of the products or the weights, changed
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                             int ntile) {
   constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles;
-  constexpr bool kHold = kRowTiles * NT <= 2;  // a chunk's operands fit the registers
+  static_assert(kRowTiles * NT <= 2, "a step's operands are held in registers");
   __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
   __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
   __shared__ float s_scale[2][2][kChunkPos];         // of keys, of values
@@ -694,35 +694,22 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-          for (int d = 0; d < DS; ++d) {
+          for (int d = 0; d < DS; ++d)
             op[t * DS + d] = __builtin_bit_cast(half8_t, s_k[buf][2 * p + t][d][lane]);
-            if constexpr (!kHold) {
 #pragma unroll
-              for (int y = 0; y < kRowTiles; ++y) {
-                if (d == 0) x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        for (int y = 0; y < kRowTiles; ++y)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                  x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[t * DS + d], qf[y][n][d],
-                                                                   x[y][t], 0, 0, 0);
-              }
-            }
+          for (int t = 0; t < kTiles; ++t) {
+            x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < DS; ++d)
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[t * DS + d], qf[y][n][d],
+                                                                 x[y][t], 0, 0, 0);
           }
-        if constexpr (kHold) {
 #pragma unroll
-          for (int y = 0; y < kRowTiles; ++y)
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-              x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int d = 0; d < DS; ++d)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                  x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[t * DS + d], qf[y][n][d],
-                                                                   x[y][t], 0, 0, 0);
-            }
-#pragma unroll
-          for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
-        }
+        for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
         const bool whole = j0 + kStep <= least && pg.all();
 #pragma unroll
         for (int y = 0; y < kRowTiles; ++y) {
@@ -734,12 +721,10 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
                                         corr);
           if (move) rescale<HD>(o[y], corr);
 #pragma unroll
-          for (int u = 0; u < DT; ++u) {
-            if (!kHold) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
+          for (int u = 0; u < DT; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
               o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[u], wf[n], o[y][u], 0, 0, 0);
-          }
         }
       }
     }
@@ -838,8 +823,7 @@ static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStre
 #define WICI_ATTN(...) \
   launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
   if (p.row_tiles == 2) {
-    if (terms == 1) WICI_ATTN(k_kv8_attn_tile<HD, 1, 2>);
-    else WICI_ATTN(k_kv8_attn_tile<HD, 2, 2>);
+    WICI_ATTN(k_kv8_attn_tile<HD, 1, 2>);
   } else if (p.row_tiles == 1) {
     if (terms == 1) WICI_ATTN(k_kv8_attn_tile<HD, 1, 1>);
     else WICI_ATTN(k_kv8_attn_tile<HD, 2, 1>);

@@ -29,8 +29,10 @@ struct Kv8Plan {
 //  - a chip half full: 64 rows: 1024 of 1024: 41 / 32 / 58; 32 x 32 of 300: 30 / 19 / 22;
 //  - few workgroups and little to do: the split: 333 of 333: 12 / 16 / 23; 256 of 512:
 //    12 / 18 / 25.
-// (The farthest from the best of 24 such: 32 of 4000 in 4 sequences, 36 for 32; fp32, 512 of
-// 2048, 65 for 59.)
+// With two terms 128 rows' operands and results leave no registers to hold a chunk's operands
+// in: 64 rows in their place (64 / 128 rows: 2048 of 2048: 93 / 125; 8 x 500 of 1000: 105 / 127;
+// 128 of 8000: 56 / 62; 2048 of 8192: 493 / 477, of 16384: 1038 / 997).
+// (The farthest from the best of 24 such: 32 of 4000 in 4 sequences, 36 for 32.)
 constexpr int kTileRows = 128, kFull = 400, kHalf = 200;
 constexpr double kMuch = 60000;
 inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
@@ -43,6 +45,7 @@ inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int ma
                 : tiles >= kFull || work >= 2 * kMuch ? 2
                 : tiles >= kHalf ? 1
                 : work >= kMuch ? 2 : 0;
+  if (terms == 2) p.row_tiles = std::min(p.row_tiles, 1);
   const int64_t per = p.row_tiles ? 64 * p.row_tiles : 16;
   p.ntile = std::max(1, (int)((rows + per - 1) / per));
   const int64_t blocks = heads * p.ntile;

@@ -113,9 +113,11 @@ def test_the_gpu_tests_meet_every_kernel(ask):
             (kind, _, nsplit), = ask([("plan", hd, terms, n_kv * G, n_kv, n_seqs, rows,
                                        entries * page)])
             seen.add((hd, terms, kind, nsplit > 1))
-    # (tiles of 64 rows are taken where the chip is half full: nothing is left to split)
-    assert seen == {(hd, t, k, s) for hd in (64, 128) for t in (1, 2)
-                    for k, s in ((0, False), (0, True), (1, False), (2, False), (2, True))}
+    # (one term: tiles of 64 rows are taken where the chip is half full: nothing is left to
+    # split; two terms: never tiles of 128)
+    assert seen == {(hd, t, k, s) for hd in (64, 128) for t, k, s in (
+        (1, 0, False), (1, 0, True), (1, 1, False), (1, 2, False), (1, 2, True),
+        (2, 0, False), (2, 0, True), (2, 1, False), (2, 1, True))}
 
 
 def test_launch_sizes(ask):
@@ -134,7 +136,13 @@ def test_launch_sizes(ask):
         assert kind in (0, 1, 2) and ntile * per >= rows * (hq // n_kv) > (ntile - 1) * per
         assert 1 <= nsplit <= 128
         most = 2 * 256 if kind else 256 * (4 if hd == 64 else 3 if terms == 1 else 2)
-        assert nsplit == 1 or (kind != 1 and nsplit * ntile * n_kv * n_seqs <= most)
+        assert nsplit == 1 or nsplit * ntile * n_kv * n_seqs <= most
+        assert kind < 2 or terms == 1
+    # workspaces are sized for one term's plan: two terms never split further
+    for (one,), (two,) in zip(*[[ask([("plan", hd, t, 32, 8, n, r, m)]) for hd in (64, 128)
+                                 for n in (1, 3, 20) for r in (1, 40, 333, 2048)
+                                 for m in (100, 513, 700, 2000, 9000, 2 ** 31 - 1)] for t in (1, 2)]):
+        assert two[2] <= one[2]
 
 
 # ------------------------------------------------------------------ refusals
@@ -216,9 +224,11 @@ def test_refusals_of_single_calls():
     for scale in (float("nan"), float("inf")):
         assert lib.wici_kv8_attend(c, b, 4, scale, _rows(4), _rows(4), FAKE, 1 << 40, None) == E
     # a workspace that is too small, missing or misaligned
-    assert lib.wici_kv8_attend_workspace(c, b, 4, size) == 0 and size.value > 0
+    assert lib.wici_kv8_attend_workspace(c, b, 4, size) == 0 and size.value == 0   # short: no split
+    long = _cache(max_pages=50, table_stride=50)
+    assert lib.wici_kv8_attend_workspace(long, b, 4, size) == 0 and size.value > 0
     for ws, n in ((FAKE, size.value - 1), (None, size.value), (FAKE + 4, size.value)):
-        assert lib.wici_kv8_attend(c, b, 4, 0.1, _rows(4), _rows(4), ws, n, None) == E
+        assert lib.wici_kv8_attend(long, b, 4, 0.1, _rows(4), _rows(4), ws, n, None) == E
     for kw in (dict(head_dim=96), dict(n_rows=-1), dict(n_heads=0), dict(positions=None)):
         a = dict(head_dim=128, n_rows=3, n_heads=2, positions=FAKE) | kw
         assert lib.wici_rope_rows(_tab(), a["head_dim"], a["n_rows"], a["n_heads"], a["positions"],
