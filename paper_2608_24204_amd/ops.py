@@ -75,6 +75,12 @@ def _like(x: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
+def _new_rows(x: torch.Tensor) -> HeadRows:
+    """A tensor made here (so contiguous, of a type and on a GPU already checked)."""
+    _, h, d = x.shape
+    return HeadRows(x.data_ptr(), _DTYPES[x.dtype], h * d, d)
+
+
 def _on_gpu(x: torch.Tensor, name: str):
     if not x.is_cuda:
         raise ValueError(f"{name}: on {x.device}, expected a HIP GPU")
@@ -183,14 +189,18 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
         raise ValueError(f"table: on {table.device}, expected {device}")
     lib = binding.load_library()
     with _launch_on(stream, device, x, positions, out, table.cos, table.sin) as raw:
+        xr = _rows(x, h, d, "x", device)
         if out is None:
             out = _like(x)
+            outr = _new_rows(out)
         elif out.shape[0] != n:
             raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+        else:
+            outr = _rows(out, h, d, "out", device)
         if n == 0:
             return out
-        st = lib.wici_rope_rows(table._c, d, n, h, _ints(positions, (n,), "positions", device),
-                                _rows(x, h, d, "x", device), _rows(out, h, d, "out", device), raw)
+        st = lib.wici_rope_rows(table._c, d, n, h, _ints(positions, (n,), "positions", device), xr,
+                                outr, raw)
         if st:
             _check(st, f"rope: {h} heads of {d}, {table.dim} rotated (strides multiples of 8, "
                    "16-byte aligned rows)")
@@ -267,11 +277,14 @@ class KvCache:
             qr, qo, heads = _NO_ROWS, _NO_ROWS, 0
             if q is not None:
                 heads = q.shape[1]
+                qr = _rows(q, heads, d, "q", dev)
                 if q_out is None:
                     q_out = _like(q)
+                    qo = _new_rows(q_out)
                 elif q_out.shape[0] != n:
                     raise ValueError(f"q_out: {q_out.shape[0]} rows, expected {n}")
-                qr, qo = _rows(q, heads, d, "q", dev), _rows(q_out, heads, d, "q_out", dev)
+                else:
+                    qo = _rows(q_out, heads, d, "q_out", dev)
             kr, vr = _rows(k, self.n_kv_heads, d, "k", dev), _rows(v, self.n_kv_heads, d, "v", dev)
             _check(self.lib.wici_kv8_append(
                 self._c, self._batch(n, length, row_start), None if rope is None else rope._c, heads,
@@ -290,15 +303,21 @@ class KvCache:
             n_rows = k.shape[0] if k is not None else v.shape[0] if v is not None else \
                 length.shape[0]
         with self._on(stream, length, row_start, k, v) as raw:
-            shape = (n_rows, self.n_kv_heads, d)
-            k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
-            v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
-            if k.shape[0] != n_rows or v.shape[0] != n_rows:
-                raise ValueError(f"k and v: {k.shape[0]} and {v.shape[0]} rows, expected {n_rows}")
-            _check(self.lib.wici_kv8_read(
-                self._c, self._batch(n_rows, length, row_start),
-                _rows(k, self.n_kv_heads, d, "k", dev), _rows(v, self.n_kv_heads, d, "v", dev), raw),
-                "read (strides multiples of 8, 16-byte aligned rows)")
+            if dtype not in _DTYPES:
+                raise TypeError(f"dtype {dtype} (float32 or bfloat16)")
+            rows = []
+            for name, x in (("k", k), ("v", v)):
+                if x is None:
+                    x = torch.empty((n_rows, self.n_kv_heads, d), dtype=dtype, device=dev)
+                    rows += [x, _new_rows(x)]
+                elif x.shape[0] != n_rows:
+                    raise ValueError(f"{name}: {x.shape[0]} rows, expected {n_rows}")
+                else:
+                    rows += [x, _rows(x, self.n_kv_heads, d, name, dev)]
+            k, kr, v, vr = rows
+            _check(self.lib.wici_kv8_read(self._c, self._batch(n_rows, length, row_start), kr, vr,
+                                          raw),
+                   "read (strides multiples of 8, 16-byte aligned rows)")
         return k, v
 
     def attend(self, q: torch.Tensor, length: torch.Tensor, *,
@@ -317,10 +336,14 @@ class KvCache:
         n, heads = q.shape[0], q.shape[1]
         with self._on(stream, q, length, row_start, out, workspace) as raw:
             b = self._batch(n, length, row_start, max_rows, max_length)
+            qr = _rows(q, heads, d, "q", dev)
             if out is None:
                 out = _like(q)
+                outr = _new_rows(out)
             elif out.shape[0] != n:
                 raise ValueError(f"out: {out.shape[0]} rows, expected {n}")
+            else:
+                outr = _rows(out, heads, d, "out", dev)
             need = self._workspace(b, heads)
             if workspace is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
@@ -328,8 +351,7 @@ class KvCache:
                 raise ValueError(f"workspace: contiguous on {dev} expected")
             size = 0 if workspace is None else workspace.numel() * workspace.element_size()
             st = self.lib.wici_kv8_attend(
-                self._c, b, heads, d ** -0.5 if scale is None else scale,
-                _rows(q, heads, d, "q", dev), _rows(out, heads, d, "out", dev),
+                self._c, b, heads, d ** -0.5 if scale is None else scale, qr, outr,
                 None if workspace is None else workspace.data_ptr(), size, raw)
             if st:
                 _check(st, f"attend: {heads} query heads on {self.n_kv_heads}, {need} workspace "
