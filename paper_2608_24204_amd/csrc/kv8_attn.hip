@@ -318,12 +318,6 @@ __device__ __forceinline__ void rescale(RowOut<HD>& o, float f) {
     for (int i = 0; i < 4; ++i) o[u][i] *= f;
 }
 
-// Eight elements of a row from element offset `at` (a multiple of 8).
-__device__ __forceinline__ void load_row8(const HeadRows& x, int64_t at, float* o) {
-  if (x.bf16) load8(static_cast<const bf16_t*>(x.p) + at, o);
-  else load8(static_cast<const float*>(x.p) + at, o);
-}
-
 // 16 query rows (row l % 16 of the tile, zero where `on` is false) as NT fp16 terms, each
 // row scaled by a power of two that brings its largest finite magnitude into [2^6, 2^7);
 // `unit` undoes it.  An element 2^23 below its row's largest is the first that fp16 rounds
@@ -331,11 +325,34 @@ __device__ __forceinline__ void load_row8(const HeadRows& x, int64_t at, float* 
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(const HeadRows& q, int64_t at, bool on, int lane,
                                              half8_t (&qf)[NT][HD / 32], float& unit) {
-  const int g = lane >> 4;
   float v[HD / 32][8], most = 0.f;
+  at += (lane >> 4) * (HD / 4);
+  // (all requested, then all used: one wait)
+  if (NT == 1 || q.bf16) {
+    uint4 raw[HD / 32];
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+      raw[d] = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(q.p) + at + 8 * d);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = (&raw[d].x)[i];
+        v[d][2 * i] = __uint_as_float(w << 16);
+        v[d][2 * i + 1] = __uint_as_float(w & 0xffff0000u);
+      }
+  } else {
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 x =
+            *reinterpret_cast<const float4*>(static_cast<const float*>(q.p) + at + 8 * d + 4 * i);
+        v[d][4 * i] = x.x; v[d][4 * i + 1] = x.y; v[d][4 * i + 2] = x.z; v[d][4 * i + 3] = x.w;
+      }
+  }
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) {
-    load_row8(q, at + g * (HD / 4) + 8 * d, v[d]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       v[d][i] = on ? v[d][i] : 0.f;
@@ -434,11 +451,6 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
     const bool on = row < q.rows;
     const int rc = min(row, q.rows - 1);
-    half8_t qf[NT][HD / 32];
-    float unit;
-    load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf,
-                         unit);
-    unit *= a.scale * kLog2e;
     // a row sees the positions up to its own; the tile's last row sees the most
     const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
@@ -446,23 +458,31 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // steps that all 16 rows see whole
     const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
 
+    // the first step is requested before the queries; then the next one's keys once this
+    // one's are multiplied, its values likewise, and its pages (which those addresses wait
+    // for) a step earlier
+    const int stride = 4 * nsplit;
+    int s = s0;
+    Keys<HD> k;
+    Values<HD> v;
+    Scales sl;
+    Pages now = named(c, e0);
+    Entries later = e1;
+    if (s < steps) {
+      load_keys<HD>(k, c, kv, now, s, lane);
+      load_values<HD>(v, sl, c, kv, now, s, lane);
+    }
+    half8_t qf[NT][HD / 32];
+    float unit;
+    load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf,
+                         unit);
+    unit *= a.scale * kLog2e;
     RowState st;
     RowOut<HD> o;
     bool huge = false;
 #pragma unroll
     for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    // the next step's keys are requested once this one's are multiplied, its values
-    // likewise, and its pages (which those addresses wait for) a step earlier
-    const int stride = 4 * nsplit;
-    int s = s0;
     if (s < steps) {
-      Keys<HD> k;
-      Values<HD> v;
-      Scales sl;
-      Pages now = named(c, e0);
-      Entries later = e1;
-      load_keys<HD>(k, c, kv, now, s, lane);
-      load_values<HD>(v, sl, c, kv, now, s, lane);
       for (;;) {
         floatx4_t sc[kTiles];
         scores<HD, NT>(sc, k, qf);
@@ -563,19 +583,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     const int tile = two_a_cu && back >= first ? back - first : tiles - 1 - back;
     const int row0 = kRows * tile, mine = row0 + 16 * kRowTiles * wave;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-    // this wavefront's rows: positions each sees, and the most and least any does
-    half8_t qf[kRowTiles][NT][DS];
-    float unit[kRowTiles];
-    int limit[kRowTiles];
-#pragma unroll
-    for (int x = 0; x < kRowTiles; ++x) {
-      const int qr = mine + 16 * x + r16, row = qr / G, rc = min(row, q.rows - 1);
-      const bool on = qr < total;
-      limit[x] = on ? seen(row) : 0;
-      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + (h * G + qr % G) * a.q.head_stride,
-                           on, lane, qf[x], unit[x]);
-      unit[x] *= a.scale * kLog2e;
-    }
+    // positions this wavefront's rows see at most and at least
     const int most = mine < total ? seen(min((mine + 16 * kRowTiles - 1) / G, q.rows - 1)) : 0;
     const int least = mine + 16 * kRowTiles <= total ? seen(mine / G) : 0;
     const int all = seen(min((row0 + kRows - 1) / G, q.rows - 1));  // of the workgroup's rows
@@ -664,6 +672,18 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
       look();
       bring(phys, c0);
       find(c0 + 1);
+    }
+    half8_t qf[kRowTiles][NT][DS];
+    float unit[kRowTiles];
+    int limit[kRowTiles];  // positions each row sees
+#pragma unroll
+    for (int x = 0; x < kRowTiles; ++x) {
+      const int qr = mine + 16 * x + r16, row = qr / G, rc = min(row, q.rows - 1);
+      const bool on = qr < total;
+      limit[x] = on ? seen(row) : 0;
+      load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + (h * G + qr % G) * a.q.head_stride,
+                           on, lane, qf[x], unit[x]);
+      unit[x] *= a.scale * kLog2e;
     }
     for (int ch = c0; ch < c1; ++ch) {
       const int buf = (ch - c0) & 1;
