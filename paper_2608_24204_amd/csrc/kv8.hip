@@ -219,7 +219,7 @@ __device__ __forceinline__ bool one_word(const RowAt (&w)[R], char* const (&blk)
 // A unit takes R neighbouring rows of one head.  The rows do not wait for their places, so
 // they are requested first.  With four rows (prompts) a value word of four positions is
 // written whole where the rows are those four: single bytes took 14.7 us for 2048 rows of 8
-// heads of 128, now 10.6: 8.4 MB in and 4.3 out, of which a call of 48 rows already takes the
+// heads of 128, now 11: 8.4 MB in and 4.3 out, of which a call of 48 rows already takes the
 // first 4.7 (a row's place is three loads, one after another).  Bound by neither bytes nor
 // arithmetic: half the vector instructions, or one load less in the chain, changed nothing.
 // 12 prompts of up to 500 rows whose positions start anywhere in a word (fp32, heads of 64)
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab ro
 }
 
 // Bound by memory where there is much to read: 16384 rows of 8 heads of 128 (to bf16) 22 us for
-// 102 MB, 4.5 TB/s; 2048 rows 8.8 us.
+// 102 MB, 4.5 TB/s; 2048 rows 9 us.
 template <int HD, int R>
 __global__ __launch_bounds__(256) void k_kv8_read(Kv8 c, Kv8Rows r, HeadRows k, HeadRows v) {
   constexpr int LPU = HD / 8, UPB = 256 / LPU;

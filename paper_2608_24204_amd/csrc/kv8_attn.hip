@@ -458,20 +458,10 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // steps that all 16 rows see whole
     const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
 
-    // the first step is requested before the queries; then the next one's keys once this
-    // one's are multiplied, its values likewise, and its pages (which those addresses wait
-    // for) a step earlier
+    // the next step's keys are requested once this one's are multiplied, its values
+    // likewise, and its pages (which those addresses wait for) a step earlier
     const int stride = 4 * nsplit;
     int s = s0;
-    Keys<HD> k;
-    Values<HD> v;
-    Scales sl;
-    Pages now = named(c, e0);
-    Entries later = e1;
-    if (s < steps) {
-      load_keys<HD>(k, c, kv, now, s, lane);
-      load_values<HD>(v, sl, c, kv, now, s, lane);
-    }
     half8_t qf[NT][HD / 32];
     float unit;
     load_queries<HD, NT>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf,
@@ -483,6 +473,13 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 #pragma unroll
     for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     if (s < steps) {
+      Keys<HD> k;
+      Values<HD> v;
+      Scales sl;
+      Pages now = named(c, e0);
+      Entries later = e1;
+      load_keys<HD>(k, c, kv, now, s, lane);
+      load_values<HD>(v, sl, c, kv, now, s, lane);
       for (;;) {
         floatx4_t sc[kTiles];
         scores<HD, NT>(sc, k, qf);
@@ -548,8 +545,8 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 // Two buffers: the next chunk's codes are on their way while this one is multiplied, and one
 // barrier a chunk parts a buffer's readers from its next writers.
 //
-// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 299 us in bf16, 804 TFLOP/s
-// of products where a large fp16 product reaches 1300; 493 us with two fp16 terms.  No unit is
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 298 us in bf16, 807 TFLOP/s
+// of products where a large fp16 product reaches 1300; 495 us with two fp16 terms.  No unit is
 // full: the vector units are busy 53% of the time, the matrix cores 32%, and a wavefront waits
 // for operands, products or the other one (the registers allow two a SIMD).  Eight vector
 // instructions fewer for 512 scores, and priorities of the products or the weights, changed
