@@ -30,6 +30,29 @@ __device__ __forceinline__ void put4(const HeadRows& x, int64_t at, const float*
   }
 }
 
+// Eight: runs a and b of four, as one where they are consecutive.
+__device__ __forceinline__ void load44(const HeadRows& x, int64_t at, int a, int b, float (&o)[8]) {
+  if (x.bf16 && b == a + 4) {
+    load8(static_cast<const bf16_t*>(x.p) + at + a, o);
+  } else {
+    load4(x, at + a, o);
+    load4(x, at + b, o + 4);
+  }
+}
+__device__ __forceinline__ void put44(const HeadRows& x, int64_t at, int a, int b,
+                                      const float (&v)[8]) {
+  if (x.bf16 && b == a + 4) {
+    uint4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      (&w.x)[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(x.p) + at + a) = w;
+  } else {
+    put4(x, at + a, v);
+    put4(x, at + b, v + 4);
+  }
+}
+
 // The eight dimensions of lane c of a unit, as two runs of four: consecutive, or (a
 // rotated run of the half layout) the first members of four pairs and the second.
 struct Runs {
@@ -81,8 +104,8 @@ __device__ __forceinline__ void turn_row(const RopeTab& rope, const Runs& r, int
 
 // ------------------------------------------------------------------- rotary positions
 // The table is read where another head of the row has read it before; a row's heads are
-// neighbouring units.  Bound by memory: 8192 rows of 32 heads of 128 (bf16) 26 us for 134 MB,
-// the rate of a large copy (5.2 TB/s); 32 rows 3.2 us.
+// neighbouring units.  Bound by memory: 8192 rows of 32 heads of 128 (bf16, pairs) 24 us for 134
+// MB, 5.6 TB/s where a large copy moves 5.2 (8 bytes a lane at a time: 26); 32 rows 3.2 us.
 template <int HD>
 __global__ __launch_bounds__(256) void k_rope_rows(HeadRows x, HeadRows y, int n_rows, int n_heads,
                                                    const int32_t* __restrict__ positions,
@@ -97,12 +120,57 @@ __global__ __launch_bounds__(256) void k_rope_rows(HeadRows x, HeadRows y, int n
   const Runs r = runs(rope, c);
   float v[8];
   const int64_t in = row * x.row_stride + h * x.head_stride;
-  load4(x, in + r.a, v);
-  load4(x, in + r.b, v + 4);
+  load44(x, in, r.a, r.b, v);
   turn_row(rope, r, c, pos, v);
+  put44(y, row * y.row_stride + h * y.head_stride, r.a, r.b, v);
+}
+
+// bf16 rows of the half layout, 16 dimensions of it at a time turned: two runs of eight a
+// lane, so that they too are read and written 16 bytes a lane (calls of the same 8192 rows, all turned,
+// take 28 us, with runs of four 34).
+template <int HD>
+__global__ __launch_bounds__(256) void k_rope_halves(HeadRows x, HeadRows y, int n_rows, int n_heads,
+                                                     const int32_t* __restrict__ positions,
+                                                     RopeTab rope) {
+  constexpr int LPU = HD / 16, UPB = 256 / LPU;
+  const unsigned u = blockIdx.x * UPB + threadIdx.x / LPU;  // below 2^28
+  const int c = threadIdx.x % LPU;
+  const int row = (int)(u / n_heads), h = (int)(u % n_heads);
+  if (row >= n_rows) return;
+  const int pos = positions[row];
+  if (pos < 0) return;  // padding: left as it is
+  const bool turn = 16 * c < rope.dim;
+  const int a = turn ? 8 * c : 16 * c, b = turn ? rope.dim / 2 + 8 * c : 16 * c + 8;
+  const bf16_t* from = static_cast<const bf16_t*>(x.p) + row * x.row_stride + h * x.head_stride;
+  float v[16];
+  load8(from + a, v);
+  load8(from + b, v + 8);
+  if (turn) {
+    // four pairs at a time, as turn_row takes them
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        p[j] = v[4 * i + j];
+        p[4 + j] = v[8 + 4 * i + j];
+      }
+      turn_row(rope, Runs{0, 0, true}, 2 * c + i, pos, p);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[4 * i + j] = p[j];
+        v[8 + 4 * i + j] = p[4 + j];
+      }
+    }
+  }
   const int64_t out = row * y.row_stride + h * y.head_stride;
-  put4(y, out + r.a, v);
-  put4(y, out + r.b, v + 4);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = v[8 * i + j];
+    put44(y, out, i ? b : a, (i ? b : a) + 4, p);
+  }
 }
 
 __global__ __launch_bounds__(256) void k_rope_table(RopeFreqs f, int half, int64_t n,
@@ -243,8 +311,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab ro
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int64_t in = min(t + i, r.n_rows - 1) * x.row_stride + h * x.head_stride;
-    load4(x, in + run.a, e[i]);
-    load4(x, in + run.b, e[i] + 4);
+    load44(x, in, run.a, run.b, e[i]);
     for (int s = 1; s < x.n_sum; ++s) {
       float m[8];
       load4(x, in + s * x.sum_stride + run.a, m);
@@ -264,9 +331,7 @@ __global__ __launch_bounds__(256) void k_kv8_append(Kv8 c, Kv8Rows r, RopeTab ro
       if (!w[i].there) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[i][j] *= q_scale;
-      const int64_t out = (t + i) * q_out.row_stride + h * q_out.head_stride;
-      put4(q_out, out + run.a, e[i]);
-      put4(q_out, out + run.b, e[i] + 4);
+      put44(q_out, (t + i) * q_out.row_stride + h * q_out.head_stride, run.a, run.b, e[i]);
     }
     return;
   }
@@ -357,9 +422,7 @@ __global__ __launch_bounds__(256) void k_kv8_read(Kv8 c, Kv8Rows r, HeadRows k, 
 #pragma unroll
       for (int j = 0; j < 8; ++j) e[j] = (float)((int)code[j] - 128) * scale;
     }
-    const int64_t out = (t + i) * y.row_stride + h * y.head_stride + 8 * lane;
-    put4(y, out, e);
-    put4(y, out + 4, e + 4);
+    put44(y, (t + i) * y.row_stride + h * y.head_stride, 8 * lane, 8 * lane + 4, e);
   }
 }
 
@@ -373,16 +436,18 @@ static unsigned unit_blocks(int hd, int64_t units) {
 
 hipError_t launch_rope_rows(int hd, const HeadRows& x, const HeadRows& y, int n_rows, int n_heads,
                             const int32_t* positions, const RopeTab& rope, hipStream_t st) {
-  const unsigned grid = unit_blocks(hd, (int64_t)n_rows * n_heads);
-  if (!grid) return hipErrorInvalidValue;
-  if (hd == 128)
-    launch_k(k_rope_rows<128>, dim3(grid), dim3(256), 0, st, kOnly, x, y, n_rows, n_heads,
-             positions, rope);
-  else if (hd == 64)
-    launch_k(k_rope_rows<64>, dim3(grid), dim3(256), 0, st, kOnly, x, y, n_rows, n_heads,
-             positions, rope);
-  else
-    return hipErrorInvalidValue;
+  const bool halves = rope.layout == 0 && rope.dim % 16 == 0 && x.bf16 && y.bf16;
+  // (the second, of half as many lanes a unit, in as many fewer workgroups)
+  const unsigned full = unit_blocks(hd, (int64_t)n_rows * n_heads), grid = halves ? (full + 1) / 2 : full;
+  if (!full) return hipErrorInvalidValue;
+#define WICI_ROPE(K)                                                                          \
+  launch_k(K, dim3(grid), dim3(256), 0, st, kOnly, x, y, n_rows, n_heads, positions, rope)
+  if (hd == 128 && halves) WICI_ROPE(k_rope_halves<128>);
+  else if (hd == 128) WICI_ROPE(k_rope_rows<128>);
+  else if (hd == 64 && halves) WICI_ROPE(k_rope_halves<64>);
+  else if (hd == 64) WICI_ROPE(k_rope_rows<64>);
+  else return hipErrorInvalidValue;
+#undef WICI_ROPE
   return hipGetLastError();
 }
 
