@@ -159,6 +159,22 @@ def test_rope_rows(ops, layout, hd, dim, dtype):
     assert not wide[:, 0].any() and not wide[:, -1].any()
 
 
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("hd,dim", [(128, 16), (128, 48), (128, 112), (128, 120), (64, 16), (64, 48), (64, 56)])
+@pytest.mark.parametrize("xt,ot", [(BF16, BF16), (BF16, F32), (F32, BF16)])
+def test_rope_rows_of_other_widths_and_types(ops, layout, hd, dim, xt, ot):
+    rng = np.random.default_rng(dim + 1)
+    n, heads = 301, 5
+    t = ops.rope_table(400, dim, layout=layout, base=10000.0)
+    pos = rng.integers(0, 400, n)
+    x = rnd(rng, n, heads, hd, dtype=xt)
+    out = torch.full((n, heads, hd), 7.0, dtype=ot, device="cuda")
+    ops.rope(x, ints(pos.tolist()), t, out=out)
+    want = oracle.rope_pairs(x.float().cpu().numpy(), t.cos.cpu().numpy()[pos], t.sin.cpu().numpy()[pos],
+                             layout)
+    assert torch.equal(out.cpu(), torch.from_numpy(want).to(ot))
+
+
 def test_rope_rows_outside_the_table(ops):
     t = ops.rope_table(10, 64)
     x = rnd(np.random.default_rng(1), 5, 2, 128)
