@@ -397,10 +397,9 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
 }
 
 // Four dimensions of a row of one split: the output where it is the only one, else
-// (ref, sum, output) for the merge.
-__device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, float* part_ml,
-                                      float* part_o, int row, int head, int d, float ref, float sum,
-                                      float (&o)[4]) {
+// (ref, sum, output) for the merge.  parts: of the launch.
+__device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, size_t parts, int row,
+                                      int head, int d, float ref, float sum, float (&o)[4]) {
   if (nsplit == 1) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
 #pragma unroll
@@ -408,8 +407,10 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, f
     put_out(a, row, head, d, o);
   } else {
     const size_t at = ((size_t)row * a.n_q + head) * nsplit + split;
-    *reinterpret_cast<float4*>(part_o + at * a.hd + d) = make_float4(o[0], o[1], o[2], o[3]);
-    if (d == 0) *reinterpret_cast<float2*>(part_ml + 2 * at) = make_float2(ref, sum);
+    *reinterpret_cast<float4*>(a.work + kv8_part_out(at, a.hd) + d) =
+        make_float4(o[0], o[1], o[2], o[3]);
+    if (d == 0)
+      *reinterpret_cast<float2*>(a.work + kv8_part_state(at, parts, a.hd)) = make_float2(ref, sum);
   }
 }
 
@@ -439,8 +440,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
   const int r16 = lane & 15, G = a.n_q / c.n_kv;
   const Kv8Seq q = uniform(kv8_seq(c, r, b));
   const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  float* part_ml = a.work;
-  float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
+  const size_t parts = (size_t)r.n_rows * a.n_q * nsplit;
   // the wavefront's first steps do not depend on the length, so that their pages are
   // looked up beside it
   const HeadAt<HD> kv(c, q, h);
@@ -531,7 +531,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         sum += f * s_sum[w][rr];
         all[0] += f * v.x; all[1] += f * v.y; all[2] += f * v.z; all[3] += f * v.w;
       }
-      leave(a, nsplit, split, part_ml, part_o, q.row0 + tr / G, h * G + tr % G, d, ref, sum, all);
+      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, sum, all);
     }
     __syncthreads();
   }
@@ -567,8 +567,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
   const Kv8Seq q = uniform(kv8_seq(c, r, b));
   const int64_t cap = (int64_t)c.max_pages << c.page_shift;
   const int page = 1 << c.page_shift;
-  float* part_ml = a.work;
-  float* part_o = a.work + (size_t)r.n_rows * a.n_q * nsplit * 2;
+  const size_t parts = (size_t)r.n_rows * a.n_q * nsplit;
   const int total = q.rows * G, tiles = (total + kRows - 1) / kRows;
   const HeadAt<HD> kv(c, q, h);
   const bool two_a_cu = gridDim.x > kCus && gridDim.x * gridDim.y <= 2 * kCus && tiles <= ntile;
@@ -760,7 +759,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
         for (int i = 0; i < 4; ++i) {
           float v[4] = {o[y][4 * hh][i], o[y][4 * hh + 1][i], o[y][4 * hh + 2][i],
                         o[y][4 * hh + 3][i]};
-          leave(a, nsplit, split, part_ml, part_o, q.row0 + qr / G, h * G + qr % G,
+          leave(a, nsplit, split, parts, q.row0 + qr / G, h * G + qr % G,
                 64 * hh + 16 * mg + 4 * i, st[y].ref, st[y].sum, v);
         }
     }
@@ -782,8 +781,9 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
   if (r.kind == KV8_ARRAYS && r.row_start &&
       (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
     return;  // a row of no sequence
-  const float2* ml = reinterpret_cast<const float2*>(a.work) + (size_t)u * nsplit;
-  const float* po = a.work + ((size_t)r.n_rows * a.n_q * 2 + (size_t)u * HD) * nsplit + d;
+  const size_t first = (size_t)u * nsplit, parts = (size_t)r.n_rows * a.n_q * nsplit;
+  const float2* ml = reinterpret_cast<const float2*>(a.work + kv8_part_state(first, parts, HD));
+  const float* po = a.work + kv8_part_out(first, HD) + d;
   float ref = kNoRef, sum = 0.f, o[4] = {};
 #pragma unroll 4
   for (int s = p; s < nsplit; s += P) {
@@ -820,12 +820,12 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 size_t kv8_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
   const Kv8Plan p = kv8_plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
-  return p.nsplit == 1 ? 0 : (size_t)n_rows * n_q * p.nsplit * (hd + 2);
+  return p.nsplit == 1 ? 0 : kv8_part_floats((size_t)n_rows * n_q * p.nsplit, hd);
 }
 
 // (launches that split have at most resident() workgroups of 16 rows x heads, or 2 kCus of 128)
 size_t kv8_attn_floats_most(int hd) {
-  return (size_t)std::max(resident(hd, 1) * 16, 2 * kCus * 128) * (hd + 2);
+  return kv8_part_floats(std::max(resident(hd, 1) * 16, 2 * kCus * 128), hd);
 }
 
 template <int HD>

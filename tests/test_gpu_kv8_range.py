@@ -1,0 +1,80 @@
+"""Attention over the 8-bit key-value cache at the ends of its range, against float64
+(the stored rows by oracle/kv8.py) within the bound that tests/test_gpu_kv8.py derives."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import oracle
+from tests.test_gpu_kv8 import BF16, F32, Batch, f64, ints, ops, rnd, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# Calls of every kernel: lengths, new rows (None: one each), KV heads, query heads a KV head,
+# page-table entries beyond the contexts' (which shape the launch), page.
+KERNELS = {
+    "split_one": ([400, 33, 129], None, 2, 4, 0, 64),
+    "split_several": ([1500, 700, 33], None, 1, 4, 90, 16),
+    "split_rows": ([200, 90], [16, 7], 2, 2, 0, 16),
+    "tile_64": ([70] * 26, [8] * 26, 8, 16, 0, 16),
+    "tile_128": ([70] * 52, [8] * 52, 8, 16, 0, 16),
+    "tile_several": ([700], [130], 4, 5, 2000, 128),
+}
+
+
+def store(bt, k, v):
+    """Whole contexts k, v [sum of the lengths, n_kv, hd] appended; what they stand for, by sequence."""
+    start = np.concatenate([[0], np.cumsum(bt.lens)])
+    bt.cache.append(k, v, bt.length, row_start=ints(start.tolist()))
+    return ([oracle.kv8_values(f64(x))[a:b] for a, b in zip(start, start[1:])] for x in (k, v))
+
+
+def batch(ops, name, hd, seed):
+    lens, rows, n_kv, G, extra, page = KERNELS[name]
+    bt = Batch(ops, lens, rows, n_kv=n_kv, hd=hd, page=page, extra_pages=extra, seed=seed)
+    return bt, n_kv * G
+
+
+def attend(bt, q, **kw):
+    return bt.cache.attend(q, bt.length, row_start=bt.row_start, max_rows=max(bt.rows), **kw)
+
+
+def check(bt, q, out, K, V, scale, seen=None):
+    """check_attend's bound (with `far`) on the GPU."""
+    n_kv, hd = bt.n_kv, bt.hd
+    G = q.shape[1] // n_kv
+    single = q.dtype == BF16 and out.dtype == BF16
+    for b, (n, r) in enumerate(zip(bt.lens, bt.rows)):
+        at = slice(bt.start[b], bt.start[b] + r)
+        k, v = (torch.from_numpy(x[b]).cuda().transpose(0, 1)[:, None].contiguous() for x in (K, V))
+        qq = q[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3).contiguous()
+        x = qq @ k.transpose(-1, -2).contiguous() * scale
+        pos = torch.arange(n, device="cuda")
+        off = pos[None] > torch.arange(n - r, n, device="cuda")[:, None]
+        if seen is not None:
+            off = off | ~seen(pos)[None]
+        p = x.masked_fill(off, float("-inf")).softmax(-1)
+        want, mag = p @ v, p @ v.abs()
+        dots = (qq.abs() @ k.abs().transpose(-1, -2).contiguous()).amax(-1, keepdim=True) * abs(scale)
+        e = (48 * 2.0 ** -24 + (0 if single else 2.0 ** -22)) * dots + 2.0 ** -20
+        rel = 2 * e + (2.0 ** -11 if single else 2.0 ** -22) + (64 + n / 16) * 2.0 ** -24
+        tol = mag * rel + want.abs() * torch.finfo(out.dtype).eps / 2 + 1e-30 + \
+            n * 2.0 ** -31 * mag.amax(-1, keepdim=True)
+        err = (out[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3) - want).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("length,entries", [(500, 34), (1090, 69), (40, 34)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_an_odd_number_of_partial_results(ops, hd, length, entries):
+    """One row, one head, five or nine splits: five or nine outputs and states in the workspace."""
+    bt = Batch(ops, [length], n_kv=1, hd=hd, page=16, extra_pages=entries - -(-length // 16))
+    K, V = bt.fill()
+    for dtype in (BF16, F32):
+        q = rnd(bt.rng, 1, 1, hd, dtype=dtype)
+        need = bt.cache.attend_workspace(1, 1, 1)
+        assert need // 4 // hd % 2 == 1
+        space = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+        check(bt, q, attend(bt, q, workspace=space[:need]), K, V, hd ** -0.5)
+        assert (space[need:] == 255).all()
