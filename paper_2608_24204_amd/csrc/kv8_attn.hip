@@ -6,11 +6,15 @@
 // The codes are small integers, exact in fp16, so both products run on the fp16 matrix
 // cores with the scales outside them: the keys' on the scores, the values' on the
 // weights w_j = 2^(y_j - ref) t_j.  `ref` runs with the largest y_j + log2 t_j (an online
-// softmax on the weights themselves), so the weights stay inside fp16's range whatever
-// the values' scales are, and one factor 2^-ref cancels in the quotient.  It moves only
-// when a weight would pass 2^15 (it is set 2^6 below the largest), so most steps rescale
-// nothing.  (Where scores pass 2^24 a reference cannot hold log2 t_j beside them: such a
-// row goes on with the largest score and a power of two of its own, `lift`.)  Scores,
+// softmax on the weights themselves), so the weights stay inside fp16's range, and one
+// factor 2^-ref cancels in the quotient.  It moves only when a weight would pass 2^15 (it is
+// set 2^6 below the largest), so most steps rescale nothing.  That one reference serves the
+// sum too while it is near the largest score: values' scales are 2^-67 (a row of zeros) and
+// more, and up to scales of 2^20 a sum of 2^(y_j - ref) is between 2^-14 and 2^83 of a term
+// at the largest score, so that neither it nor the factors between two references leave
+// fp32.  Where a scale is larger, or a score passes 2^24 (a reference then cannot hold log2 t_j
+// beside it), rows go on with the largest score as `ref` and a power of two of the outputs'
+// own, `lift`: they hold 2^-lift of their sum (`apart` below).  Scores,
 // weights, sums and the output are fp32; q and w enter the products as NT fp16 terms: one
 // for bf16 rows (q is exact in it, a weight within 2^-11, an eighth of the output's own
 // rounding), two where queries or output are fp32 (2^-22); a weight 2^-20 and more below
@@ -39,8 +43,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNoRef = -3e38f;    // ref before the first weight
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
-constexpr float kLeastLog = -100.f;  // below log2 of every scale that is stored
+constexpr float kLeastLog = -68.f;  // below log2 of every scale that is stored
+constexpr float kMostScale = 0x1p20f;  // of the values, up to which one reference serves
 constexpr float kHugeScore = 16777216.f;
+constexpr float kFarBelow = -64.f, kFarStep = 96.f;
 
 // Four codes (bytes b + 128) as fp16 values b: 0x6400 | byte is 1024 + byte, less 1152.
 // Both steps are exact.
@@ -61,7 +67,8 @@ __device__ __forceinline__ half8_t codes8(unsigned a, unsigned b) {
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
 struct RowState {
   float ref = kNoRef, sum = 0.f;  // sum over this lane's positions
-  float lift = 0.f;  // the output holds 2^-lift of its sum (0 until a score passes kHugeScore)
+  float lift = 0.f;  // the output holds 2^-lift of its sum (whole; 0 while ref serves both)
+  bool apart = false;  // the same in all lanes of a row: other rows' values change nothing
 };
 // Output of 16 rows: tile 4 h + t, element i: dimension 64 h + 16 (l / 16) + 4 i + t.
 template <int HD>
@@ -202,10 +209,13 @@ __device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles], const Keys<HD>& 
 
 // The weights of one step from its products (a score is product * key scale * q_unit), as
 // NT fp16 terms.  MASKED: some row does not see every position: row l % 16 sees the step's
-// positions below `seen`, of the tiles that are there.  Returns whether a row's reference
-// moved: the output so far is then to be multiplied by `corr`.
-template <int NT, bool MASKED>
-__device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& huge,
+// positions below `seen`, of the tiles that are there.  `lifts`: some row of the wavefront is
+// apart.  Returns whether a row's reference moved: the output so far is then to be multiplied by
+// `corr`.  HINT: the compiler is told that moves are rare.  That places the row tiles' code well
+// (heads of 64, 2048 rows of 8192: 220 us for 235; 16 x 100 of 1000: 41 for 43), the split's not
+// (48 tokens at 4000, fp32: 45.9 for 44.5).
+template <int NT, bool MASKED, bool HINT>
+__device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& lifts,
                                         const floatx4_t (&sc)[kTiles], const Scales& s,
                                         const Pages& p, float q_unit, int seen, int lane,
                                         float& corr) {
@@ -221,15 +231,15 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
     return y;
   };
   float sum, most;
-  // f(t, i) is a score less the reference
-  auto weigh = [&](float down, auto f) {
+  // f(t, i): the exponent of the sum's term; g(t, i, term): the weight (and the term, if another)
+  auto weigh = [&](auto f, auto g) {
     sum = most = 0.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(on(t, i) ? f(t, i) : -INFINITY);
-        float w = on(t, i) ? e * (&s.v[t].x)[i] * down : 0.f;
+        float e = __builtin_amdgcn_exp2f(on(t, i) ? f(t, i) : -INFINITY);
+        float w = on(t, i) ? g(t, i, e) : 0.f;
         // a product rounded once: joined with the conversion below, and not with the
         // difference, the first term is now and then not the one the second completes
         if (NT > 1) asm volatile("" : "+v"(w));
@@ -243,19 +253,43 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
         }
       }
   };
+  auto ahead = [&](int t, int i) {  // a score less the reference
+    return __builtin_fmaf(sc[t][i], (&s.k[t].x)[i] * q_unit, -st.ref);
+  };
   auto plain = [&]() {
-    weigh(1.f, [&](int t, int i) {
-      return __builtin_fmaf(sc[t][i], (&s.k[t].x)[i] * q_unit, -st.ref);
-    });
+    weigh(ahead, [&](int t, int i, float& e) { return e * (&s.v[t].x)[i]; });
   };
+  // The same where some row (`lifts`) has its output's power of two: the weight
+  // 2^(y - ref - lift) t, also where 2^(y - ref) alone is below fp32's least: the largest values
+  // then outweigh what their softmax weights lack.  Such a term is nothing to the sum.  Rows
+  // that are not apart come out as above.
   auto lifted = [&]() {
-    weigh(__builtin_amdgcn_exp2f(-st.lift), [&](int t, int i) { return score(t, i) - st.ref; });
+    bool far = false;
+    weigh(
+        [&](int t, int i) {
+          const float d = st.apart ? score(t, i) - st.ref : ahead(t, i);
+          far = st.apart && d < kFarBelow;
+          return far ? d + kFarStep : d;
+        },
+        [&](int t, int i, float& e) {
+          const float v = (&s.v[t].x)[i];
+          // (one scaling by all the powers of two: no two of them need be within fp32 together)
+          const float w = __builtin_amdgcn_ldexpf(
+              e * __builtin_amdgcn_frexp_mantf(v),
+              __builtin_amdgcn_frexp_expf(v) - (int)st.lift - (far ? (int)kFarStep : 0));
+          if (far) e = 0.f;
+          __builtin_amdgcn_sched_barrier(0);  // (one after another: registers)
+          return w;
+        });
   };
-  if (huge) lifted();
-  else plain();
-  // (NaN: values of scale zero, in memory never appended to, before there is a reference)
-  const bool move = __any(!(most <= kMaxWeight));
-  if (move) {  // rare after a row's first step
+  // (rows with lifts move at every step: rare, and one copy less of their code)
+  bool move = lifts;
+  if (HINT ? __builtin_expect(!move, true) : !move) {
+    plain();
+    // (NaN: values of scale zero, in memory never appended to, before there is a reference)
+    move = __any(!(most <= kMaxWeight));
+  }
+  if (HINT ? __builtin_expect(move, false) : move) {  // rare after a row's first step
     // the largest of f over this row's positions
     auto largest = [&](auto f) {
       float z = -INFINITY;
@@ -273,19 +307,27 @@ __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& h
       return fmaxf(__builtin_amdgcn_logf(x), kLeastLog);
     };
     const float z = largest([&](int t, int i) { return score(t, i) + lv(t, i); });
-    huge |= __any(z != -INFINITY && fabsf(z) > kHugeScore);
+    bool large = z != -INFINITY && fabsf(z) > kHugeScore;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) large |= on(t, i) && (&s.v[t].x)[i] > kMostScale;
+    const uint64_t lanes = __ballot(large);  // lanes l, l + 16, .. : row l
+    const uint32_t two = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+    st.apart |= (two | two >> 16) >> (lane & 15) & 1;
+    lifts |= __any(st.apart);
     float ref = fmaxf(st.ref, z - kTopWeight), lift = 0.f;
-    if (huge) {
+    if (st.apart) {  // (a row's lanes together, so that they still exchange)
       ref = fmaxf(st.ref, largest([&](int t, int i) { return score(t, i); }));
       lift = fmaxf(st.lift + (st.ref - ref),
                    largest([&](int t, int i) { return score(t, i) - ref + lv(t, i); }) - kTopWeight);
-      lift = lift > -1e30f ? lift : 0.f;  // a row that sees nothing yet
+      lift = lift > -1e30f ? floorf(lift) : 0.f;  // (0: a row that sees nothing yet)
     }
     st.sum *= __builtin_amdgcn_exp2f(st.ref - ref);
     corr = __builtin_amdgcn_exp2f(st.ref - ref + (st.lift - lift));
     st.ref = ref;
     st.lift = lift;
-    if (huge) lifted();
+    if (HINT ? __builtin_expect(lifts, false) : lifts) lifted();
     else plain();
   }
   st.sum += sum;
@@ -396,21 +438,29 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
   }
 }
 
-// Four dimensions of a row of one split: the output where it is the only one, else
-// (ref, sum, output) for the merge.  parts: of the launch.
-__device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, size_t parts, int row,
-                                      int head, int d, float ref, float sum, float (&o)[4]) {
-  if (nsplit == 1) {
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+// The joined output of outputs that hold 2^-lift of their sum.
+__device__ __forceinline__ void quotient(float (&o)[4], float lift, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+  const float up = __builtin_amdgcn_exp2f(lift);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= inv;
+  for (int i = 0; i < 4; ++i) o[i] = o[i] * inv * up;
+}
+
+// Four dimensions of a row of one split: the output where it is the only one, else
+// (ref, lift, sum, output) for the merge.  parts: of the launch.
+__device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, size_t parts, int row,
+                                      int head, int d, float ref, float lift, float sum,
+                                      float (&o)[4]) {
+  if (nsplit == 1) {
+    quotient(o, lift, sum);
     put_out(a, row, head, d, o);
   } else {
     const size_t at = ((size_t)row * a.n_q + head) * nsplit + split;
     *reinterpret_cast<float4*>(a.work + kv8_part_out(at, a.hd) + d) =
         make_float4(o[0], o[1], o[2], o[3]);
     if (d == 0)
-      *reinterpret_cast<float2*>(a.work + kv8_part_state(at, parts, a.hd)) = make_float2(ref, sum);
+      *reinterpret_cast<float4*>(a.work + kv8_part_state(at, parts, a.hd)) =
+          make_float4(ref, lift, sum, 0.f);
   }
 }
 
@@ -433,7 +483,7 @@ __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                         int ntile) {
   __shared__ float s_o[4][16][HD + 4];
-  __shared__ float s_ref[4][16], s_sum[4][16];
+  __shared__ float s_ref[4][16], s_lift[4][16], s_sum[4][16];
   const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
   const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -469,7 +519,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     unit *= a.scale * kLog2e;
     RowState st;
     RowOut<HD> o;
-    bool huge = false;
+    bool lifts = false;
 #pragma unroll
     for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     if (s < steps) {
@@ -490,8 +540,8 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         float corr = 1.f;
         const bool move =
             s < whole && now.all()
-                ? weights<NT, false>(wf, st, huge, sc, sl, now, unit, 0, lane, corr)
-                : weights<NT, true>(wf, st, huge, sc, sl, now, unit, limit - s * kStep, lane, corr);
+                ? weights<NT, false, false>(wf, st, lifts, sc, sl, now, unit, 0, lane, corr)
+                : weights<NT, true, false>(wf, st, lifts, sc, sl, now, unit, limit - s * kStep, lane, corr);
         if (move) rescale<HD>(o, corr);
         add_values<HD, NT>(o, v, wf);
         if (then >= steps) break;
@@ -501,13 +551,13 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
         s = then;
       }
     }
-    if (huge) rescale<HD>(o, __builtin_amdgcn_exp2f(st.lift));
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);
     st.sum += __shfl_xor(st.sum, 32);
     const int me = fresh(lane), mr = me & 15, mg = me >> 4;
     if (mg == 0) {
       s_ref[wave][mr] = st.ref;
+      s_lift[wave][mr] = st.lift;
       s_sum[wave][mr] = st.sum;
     }
 #pragma unroll
@@ -523,15 +573,30 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
       float ref = s_ref[0][rr];
 #pragma unroll
       for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
-      float sum = 0.f, all[4] = {};
+      float sum = 0.f, lift = 0.f, all[4] = {};
+      bool any = false;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
+        any |= s_lift[w][rr] != 0.f;
         const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
         const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
         sum += f * s_sum[w][rr];
         all[0] += f * v.x; all[1] += f * v.y; all[2] += f * v.z; all[3] += f * v.w;
       }
-      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, sum, all);
+      if (__builtin_expect(any, false)) {  // the outputs again, each with its power of two
+        lift = -INFINITY;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) lift = fmaxf(lift, s_lift[w][rr] + (s_ref[w][rr] - ref));
+        lift = floorf(lift);
+        all[0] = all[1] = all[2] = all[3] = 0.f;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+          const float g = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref + (s_lift[w][rr] - lift));
+          const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
+          all[0] += g * v.x; all[1] += g * v.y; all[2] += g * v.z; all[3] += g * v.w;
+        }
+      }
+      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, lift, sum, all);
     }
     __syncthreads();
   }
@@ -588,7 +653,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
 
     RowState st[kRowTiles];
     RowOut<HD> o[kRowTiles];
-    bool huge = false;
+    bool lifts = false;
 #pragma unroll
     for (int x = 0; x < kRowTiles; ++x)
 #pragma unroll
@@ -732,8 +797,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
           float corr = 1.f;
           half8_t wf[NT];
           const bool move =
-              whole ? weights<NT, false>(wf, st[y], huge, x[y], sl, pg, unit[y], 0, lane, corr)
-                    : weights<NT, true>(wf, st[y], huge, x[y], sl, pg, unit[y], limit[y] - j0, lane,
+              whole ? weights<NT, false, true>(wf, st[y], lifts, x[y], sl, pg, unit[y], 0, lane, corr)
+                    : weights<NT, true, true>(wf, st[y], lifts, x[y], sl, pg, unit[y], limit[y] - j0, lane,
                                         corr);
           if (move) rescale<HD>(o[y], corr);
 #pragma unroll
@@ -748,7 +813,6 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     const int me = fresh(lane), mg = me >> 4;
 #pragma unroll
     for (int y = 0; y < kRowTiles; ++y) {
-      if (huge) rescale<HD>(o[y], __builtin_amdgcn_exp2f(st[y].lift));
       st[y].sum += __shfl_xor(st[y].sum, 16);
       st[y].sum += __shfl_xor(st[y].sum, 32);
       const int qr = mine + 16 * y + (me & 15);
@@ -760,21 +824,21 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
           float v[4] = {o[y][4 * hh][i], o[y][4 * hh + 1][i], o[y][4 * hh + 2][i],
                         o[y][4 * hh + 3][i]};
           leave(a, nsplit, split, parts, q.row0 + qr / G, h * G + qr % G,
-                64 * hh + 16 * mg + 4 * i, st[y].ref, st[y].sum, v);
+                64 * hh + 16 * mg + 4 * i, st[y].ref, st[y].lift, st[y].sum, v);
         }
     }
   }
 }
 
-// out = sum_s 2^(ref_s - ref) o_s / sum_s 2^(ref_s - ref) sum_s over the splits of one row
-// and head.  HD / 4 lanes of four dimensions take every P-th split each, P groups of them a
+// out = sum_s 2^(ref_s + lift_s - ref) o_s / sum_s 2^(ref_s - ref) sum_s over the splits of one
+// row and head.  HD / 4 lanes of four dimensions take every P-th split each, P groups of them a
 // row and head, and are joined: by a group's lanes alone a head's 128 splits took 43 us one
 // after another.
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit) {
   constexpr int L = HD / 4, P = 256 / L;
   __shared__ float4 s_o[P][L];
-  __shared__ float2 s_ml[P];
+  __shared__ float4 s_state[P];
   const unsigned u = blockIdx.x;
   const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane;
   const int row = (int)(u / a.n_q), head = (int)(u % a.n_q);
@@ -782,37 +846,52 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
       (row < r.row_start[0] || row >= r.row_start[r.n_seqs]))
     return;  // a row of no sequence
   const size_t first = (size_t)u * nsplit, parts = (size_t)r.n_rows * a.n_q * nsplit;
-  const float2* ml = reinterpret_cast<const float2*>(a.work + kv8_part_state(first, parts, HD));
+  const float4* states = reinterpret_cast<const float4*>(a.work + kv8_part_state(first, parts, HD));
   const float* po = a.work + kv8_part_out(first, HD) + d;
-  float ref = kNoRef, sum = 0.f, o[4] = {};
-#pragma unroll 4
-  for (int s = p; s < nsplit; s += P) {
-    const float2 m = ml[s];
-    const float4 v = *reinterpret_cast<const float4*>(po + (size_t)s * HD);
-    const float now = fmaxf(ref, m.x);
-    const float f = __builtin_amdgcn_exp2f(ref - now), g = __builtin_amdgcn_exp2f(m.x - now);
+  float ref = kNoRef, lift = 0.f, sum = 0.f, o[4] = {};
+  // joins a state and its output to those so far; the lifts where there are any
+  bool lifts = false;
+  auto join = [&](const float4& m, const float4& v, bool all) {
+    const float now = fmaxf(ref, m.x), e = ref - now, g = m.x - now;
+    float x = __builtin_amdgcn_exp2f(e), y = __builtin_amdgcn_exp2f(g);
+    sum = sum * x + m.z * y;
+    if (all) {
+      const float up = floorf(fmaxf(lift + e, m.y + g));
+      x = __builtin_amdgcn_exp2f(e + (lift - up));
+      y = __builtin_amdgcn_exp2f(g + (m.y - up));
+      lift = up;
+    }
+    o[0] = o[0] * x + v.x * y; o[1] = o[1] * x + v.y * y;
+    o[2] = o[2] * x + v.z * y; o[3] = o[3] * x + v.w * y;
     ref = now;
-    sum = sum * f + m.y * g;
-    o[0] = o[0] * f + v.x * g; o[1] = o[1] * f + v.y * g;
-    o[2] = o[2] * f + v.z * g; o[3] = o[3] * f + v.w * g;
+    lifts |= m.y != 0.f;
+  };
+  auto restart = [&]() {
+    ref = kNoRef;
+    lift = sum = o[0] = o[1] = o[2] = o[3] = 0.f;
+  };
+#pragma unroll 4
+  for (int s = p; s < nsplit; s += P)
+    join(states[s], *reinterpret_cast<const float4*>(po + (size_t)s * HD), false);
+  if (lifts) {
+    restart();
+#pragma unroll 1
+    for (int s = p; s < nsplit; s += P)
+      join(states[s], *reinterpret_cast<const float4*>(po + (size_t)s * HD), true);
   }
   s_o[p][lane] = make_float4(o[0], o[1], o[2], o[3]);
-  if (lane == 0) s_ml[p] = make_float2(ref, sum);
+  if (lane == 0) s_state[p] = make_float4(ref, lift, sum, 0.f);
   __syncthreads();
   if (p) return;
+  lifts = lift != 0.f;
 #pragma unroll
-  for (int w = 0; w < P; ++w) ref = fmaxf(ref, s_ml[w].x);
-  sum = o[0] = o[1] = o[2] = o[3] = 0.f;
-#pragma unroll
-  for (int w = 0; w < P; ++w) {
-    const float f = __builtin_amdgcn_exp2f(s_ml[w].x - ref);
-    const float4 v = s_o[w][lane];
-    sum += f * s_ml[w].y;
-    o[0] += f * v.x; o[1] += f * v.y; o[2] += f * v.z; o[3] += f * v.w;
+  for (int w = 1; w < P; ++w) join(s_state[w], s_o[w][lane], false);
+  if (lifts) {
+    restart();
+#pragma unroll 1
+    for (int w = 0; w < P; ++w) join(s_state[w], s_o[w][lane], true);
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] *= inv;
+  quotient(o, lift, sum);
   put_out(a, row, head, d, o);
 }
 

@@ -60,10 +60,10 @@ WICI_HD int kv8_seen(int len, int rows, int i, int64_t cap) {
 }
 
 // Floats of the partial results of a launch that splits its positions (parts: rows x heads x
-// splits): their outputs, hd floats each, and behind all outputs their (ref, sum) pairs.  The
-// outputs come first, so that each is as aligned as the workspace, for any number of parts.
+// splits): their outputs, hd floats each, and behind all outputs their states (ref, lift, sum and
+// one float that is not used): each is as aligned as the workspace, for any number of parts.
 WICI_HD size_t kv8_part_out(size_t part, int hd) { return part * hd; }
-WICI_HD size_t kv8_part_state(size_t part, size_t parts, int hd) { return parts * hd + 2 * part; }
-WICI_HD size_t kv8_part_floats(size_t parts, int hd) { return parts * (hd + 2); }
+WICI_HD size_t kv8_part_state(size_t part, size_t parts, int hd) { return parts * hd + 4 * part; }
+WICI_HD size_t kv8_part_floats(size_t parts, int hd) { return parts * (hd + 4); }
 
 }  // namespace wici

@@ -41,7 +41,8 @@ def attend(bt, q, **kw):
 
 
 def check(bt, q, out, K, V, scale, seen=None):
-    """check_attend's bound (with `far`) on the GPU."""
+    """check_attend's bound (with `far`) on the GPU.  A row of zeros has no code of 127, but the
+    scale of a largest value of 2^-60: where its weight is the largest, W <= 2^-60 / 127."""
     n_kv, hd = bt.n_kv, bt.hd
     G = q.shape[1] // n_kv
     single = q.dtype == BF16 and out.dtype == BF16
@@ -54,13 +55,15 @@ def check(bt, q, out, K, V, scale, seen=None):
         off = pos[None] > torch.arange(n - r, n, device="cuda")[:, None]
         if seen is not None:
             off = off | ~seen(pos)[None]
-        p = x.masked_fill(off, float("-inf")).softmax(-1)
+        x = x.masked_fill(off, float("-inf"))
+        p = (x - x.amax(-1, keepdim=True)).exp()    # (softmax() drops what is below fp32's range)
+        p /= p.sum(-1, keepdim=True)
         want, mag = p @ v, p @ v.abs()
         dots = (qq.abs() @ k.abs().transpose(-1, -2).contiguous()).amax(-1, keepdim=True) * abs(scale)
         e = (48 * 2.0 ** -24 + (0 if single else 2.0 ** -22)) * dots + 2.0 ** -20
         rel = 2 * e + (2.0 ** -11 if single else 2.0 ** -22) + (64 + n / 16) * 2.0 ** -24
         tol = mag * rel + want.abs() * torch.finfo(out.dtype).eps / 2 + 1e-30 + \
-            n * 2.0 ** -31 * mag.amax(-1, keepdim=True)
+            n * 2.0 ** -31 * mag.amax(-1, keepdim=True).clamp(min=2.0 ** -60)
         err = (out[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3) - want).abs()
         assert (err <= tol).all(), (b, float((err / tol).max()))
 
@@ -78,3 +81,70 @@ def test_an_odd_number_of_partial_results(ops, hd, length, entries):
         space = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
         check(bt, q, attend(bt, q, workspace=space[:need]), K, V, hd ** -0.5)
         assert (space[need:] == 255).all()
+
+
+# ------------------------------------------------------------------ values' scales
+@pytest.mark.parametrize("order", ["small_first", "large_first", "in_turn", "shuffled"])
+@pytest.mark.parametrize("size", [1e4, 1e20, 1e30, 1e38])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("name", ["split_one", "split_several", "split_rows", "tile_several"])
+def test_rows_of_zeros_beside_large_values(ops, name, hd, size, order):
+    """Half the value rows zero (their scale is 2^-67), half about `size`, all of similar weight: the
+    zero rows count in the softmax's sum whatever the scales and wherever they are."""
+    bt, heads = batch(ops, name, hd, seed=11)
+    n = sum(bt.lens)
+    k, v = (rnd(bt.rng, n, bt.n_kv, hd, dtype=F32).clamp(-2.5, 2.5) for _ in "kv")
+    at = np.concatenate([np.arange(m) for m in bt.lens])
+    of = np.concatenate([np.full(m, m) for m in bt.lens])
+    big = {"small_first": at >= of // 2, "large_first": at < of // 2, "in_turn": at // 32 % 2 == 1,
+           "shuffled": bt.rng.random(n) < 0.5}[order]
+    v *= torch.from_numpy(np.where(big, size, 0.0)).float().cuda()[:, None, None]
+    K, V = store(bt, k, v)
+    for dtype in (BF16, F32):
+        q = rnd(bt.rng, bt.n_rows, heads, hd, dtype=dtype, scale=0.3)
+        out = attend(bt, q)
+        assert out.isfinite().all()
+        check(bt, q, out, K, V, hd ** -0.5)
+
+
+@pytest.mark.parametrize("size", [1e9, 1e34, 3e38])
+@pytest.mark.parametrize("name", ["split_several", "tile_several"])
+def test_many_small_weights_beside_a_large_one(ops, name, size):
+    """One position of score s, all others of s - 8.5 (a weight of 2^-12 each, most of the sum
+    together), with values of any size: none is lost from the sum or the output."""
+    hd = 128
+    bt, heads = batch(ops, name, hd, seed=12)
+    n = sum(bt.lens)
+    k = torch.zeros(n, bt.n_kv, hd, device="cuda")
+    k[:, :, 0] = -8.5
+    start = np.concatenate([[0], np.cumsum(bt.lens)])
+    k[torch.from_numpy(start[:-1] + np.array(bt.lens) // 3).cuda(), :, 0] = 8.5
+    v = rnd(bt.rng, n, bt.n_kv, hd, dtype=F32).clamp(-1, 1) * size
+    K, V = store(bt, k, v)
+    for dtype in (BF16, F32):
+        q = torch.zeros(bt.n_rows, heads, hd, dtype=dtype, device="cuda")
+        q[:, :, 0] = 0.5
+        check(bt, q, attend(bt, q, scale=1.0), K, V, 1.0)
+
+
+@pytest.mark.parametrize("name", list(KERNELS))
+def test_scales_over_the_whole_range(ops, name):
+    """Value rows from 2^-60 to 2^127 in any order, scores over some tens: weights, sums and
+    output keep their precision where the largest values have the least weights and elsewhere."""
+    for seed in range(4):
+        bt, heads = batch(ops, name, 64, seed=20 + seed)
+        n = sum(bt.lens)
+        k, v = (rnd(bt.rng, n, bt.n_kv, 64, dtype=F32).clamp(-3, 3) for _ in "kv")
+        size = 2.0 ** bt.rng.uniform(-60, 125, n)
+        size[bt.rng.random(n) < 0.2] = 0.0
+        v *= torch.from_numpy(size).float().cuda()[:, None, None]
+        k *= [1.0, 6.0, 1.0, 40.0][seed]
+        if seed == 2:    # the larger the value the lower the score
+            k[:, :, 5] = torch.from_numpy(-np.log(np.maximum(size, 2.0 ** -60)) / 3).float().cuda()[:, None]
+        K, V = store(bt, k, v)
+        for dtype in (BF16, F32):
+            q = rnd(bt.rng, bt.n_rows, heads, 64, dtype=dtype)
+            if seed == 2:
+                q[:, :, 5] = 24.0      # (its eighth, the scale's, times a third of the logarithm)
+            out = attend(bt, q)
+            check(bt, q, out, K, V, 0.125)
