@@ -524,9 +524,9 @@ wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batc
  * with scores, weights and sums in fp32; q and the weights enter the matrix products as one
  * fp16 term where q and out are bf16 (exact for q; within 2^-11 of a weight), else two (2^-22),
  * and within 2^-31 of the row's largest where they are 2^-20 and less of that.  A row that sees
- * nothing gives zeros.  q and out are n_heads heads, of any of the two types each;
- * out may be q only if they are the same rows exactly.  workspace: device, 16-byte aligned,
- * undefined before and after. */
+ * nothing gives zeros; one whose scores are all minus infinity, NaN.  q and out are n_heads
+ * heads, of any of the two types each; out may be q only if they are the same rows exactly.
+ * workspace: device, 16-byte aligned, undefined before and after. */
 wici_status wici_kv8_attend(const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream);

@@ -40,7 +40,8 @@ typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNoRef = -3e38f;    // ref before the first weight
+constexpr float kNoRef = -3e38f;    // ref before the first weight,
+constexpr float kNoWeight = -2.99e38f;  // and of rows that see positions, all of weight zero
 constexpr float kTopWeight = 6.f;   // log2 of the largest weight when ref is set
 constexpr float kMaxWeight = 32768.f;
 constexpr float kLeastLog = -68.f;  // below log2 of every scale that is stored
@@ -438,9 +439,18 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
   }
 }
 
+// `ref` of a row whose weights sum up to nothing: whether any of its n positions (1 or more) is
+// there.  Rare: its scores are all minus infinity, or its pages absent.
+__device__ __forceinline__ float no_weight(const Kv8& c, const Kv8Seq& q, int n) {
+  for (int p = 0; p <= (n - 1) >> c.page_shift; ++p)
+    if (kv8_page(q.table, p, c.max_pages, c.n_pages) >= 0) return kNoWeight;
+  return kNoRef;
+}
+
 // The joined output of outputs that hold 2^-lift of their sum.
-__device__ __forceinline__ void quotient(float (&o)[4], float lift, float sum) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no position: zeros
+__device__ __forceinline__ void quotient(float (&o)[4], float ref, float lift, float sum) {
+  // no position: zeros; only scores of minus infinity: the quotient of two zeros
+  const float inv = sum != 0.f ? 1.f / sum : ref == kNoRef ? 0.f : __uint_as_float(0x7fc00000u);
   const float up = __builtin_amdgcn_exp2f(lift);
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = o[i] * inv * up;
@@ -452,7 +462,7 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, s
                                       int head, int d, float ref, float lift, float sum,
                                       float (&o)[4]) {
   if (nsplit == 1) {
-    quotient(o, lift, sum);
+    quotient(o, ref, lift, sum);
     put_out(a, row, head, d, o);
   } else {
     const size_t at = ((size_t)row * a.n_q + head) * nsplit + split;
@@ -554,6 +564,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);
     st.sum += __shfl_xor(st.sum, 32);
+    if (st.sum == 0.f && limit > s0 * kStep) st.ref = no_weight(c, q, limit);
     const int me = fresh(lane), mr = me & 15, mg = me >> 4;
     if (mg == 0) {
       s_ref[wave][mr] = st.ref;
@@ -815,6 +826,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     for (int y = 0; y < kRowTiles; ++y) {
       st[y].sum += __shfl_xor(st[y].sum, 16);
       st[y].sum += __shfl_xor(st[y].sum, 32);
+      if (st[y].sum == 0.f && (uint32_t)limit[y] > (uint32_t)c0 * kChunkPos)
+        st[y].ref = no_weight(c, q, limit[y]);
       const int qr = mine + 16 * y + (me & 15);
       if (qr >= total) continue;
 #pragma unroll
@@ -891,7 +904,7 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
 #pragma unroll 1
     for (int w = 0; w < P; ++w) join(s_state[w], s_o[w][lane], true);
   }
-  quotient(o, lift, sum);
+  quotient(o, ref, lift, sum);
   put_out(a, row, head, d, o);
 }
 

@@ -148,3 +148,49 @@ def test_scales_over_the_whole_range(ops, name):
                 q[:, :, 5] = 24.0      # (its eighth, the scale's, times a third of the logarithm)
             out = attend(bt, q)
             check(bt, q, out, K, V, 0.125)
+
+
+# ------------------------------------------------------------------ scores of minus infinity
+@pytest.mark.parametrize("name", list(KERNELS))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_whose_every_score_is_minus_infinity(ops, name, dtype):
+    """An infinite query over keys of the opposite sign, and finite queries whose scores pass the
+    largest fp32: the quotient of two zeros, NaN; where nothing is seen zeros all the same, and
+    finite scores beside such ones are attended alone."""
+    hd = 64
+    bt, heads = batch(ops, name, hd, seed=30)
+    n = sum(bt.lens)
+    k = torch.zeros(n, bt.n_kv, hd, device="cuda")
+    v = rnd(bt.rng, n, bt.n_kv, hd, dtype=F32)
+    q = torch.zeros(bt.n_rows, heads, hd, dtype=dtype, device="cuda")
+    for value, size in ((float("inf"), 1.0), (1e30, 1e30)):
+        for sign in (1.0, -1.0):
+            k[:, :, 7] = -sign * size
+            store(bt, k, v)
+            q[:, :, 7] = sign * value
+            out = attend(bt, q)
+            assert out.isnan().all(), (value, sign)
+            # the other sign: plus infinity less itself
+            q[:, :, 7] = -sign * value
+            assert attend(bt, q).isnan().all()
+    # a sequence without positions or pages, beside others
+    length, table = bt.length.clone(), bt.cache.table.clone()
+    bt.length[-1] = 0
+    if len(bt.lens) > 1:
+        bt.cache.table[0] = -1
+    q[:, :, 7] = 1e30
+    k[:, :, 7] = -1e30
+    start = np.concatenate([[0], np.cumsum(bt.lens)])
+    bt.cache.append(k, v, length, row_start=ints(start.tolist()))
+    out = attend(bt, q)
+    for b in range(len(bt.lens)):
+        got = out[bt.start[b]:bt.start[b + 1]]
+        assert not got.any() if b == len(bt.lens) - 1 or b == 0 else got.isnan().all(), b
+    bt.length.copy_(length), bt.cache.table.copy_(table)
+    # every fifth position finite (a score of zero), the first of them position 0
+    finite = np.concatenate([np.arange(m) % 5 == 0 for m in bt.lens])
+    k[:, :, 7] = torch.from_numpy(np.where(finite, 0.0, -1e30)).float().cuda()[:, None]
+    K, V = store(bt, k, v)
+    out = attend(bt, q)
+    check(bt, torch.zeros_like(q), out, [x * 0 for x in K], V, 0.125,
+                 seen=lambda j: j % 5 == 0)
