@@ -514,7 +514,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // a row sees the positions up to its own; the tile's last row sees the most
     const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
     auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
-    const int limit = on ? seen(row) : 0, steps = (seen(last) + kStep - 1) / kStep;
+    const int limit = on ? seen(row) : 0, steps = kv8_steps(seen(last), kStep);
     // steps that all 16 rows see whole
     const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
 
@@ -659,7 +659,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     const int most = mine < total ? seen(min((mine + 16 * kRowTiles - 1) / G, q.rows - 1)) : 0;
     const int least = mine + 16 * kRowTiles <= total ? seen(mine / G) : 0;
     const int all = seen(min((row0 + kRows - 1) / G, q.rows - 1));  // of the workgroup's rows
-    const int chunks = (all + kChunkPos - 1) / kChunkPos, per = (chunks + nsplit - 1) / nsplit;
+    const int chunks = kv8_steps(all, kChunkPos), per = (chunks + nsplit - 1) / nsplit;
     const int c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
 
     RowState st[kRowTiles];
@@ -802,7 +802,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
           }
 #pragma unroll
         for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(half8_t, s_v[buf][p][u][lane]);
-        const bool whole = j0 + kStep <= least && pg.all();
+        const bool whole = least - j0 >= kStep && pg.all();
 #pragma unroll
         for (int y = 0; y < kRowTiles; ++y) {
           float corr = 1.f;

@@ -59,6 +59,11 @@ WICI_HD int kv8_seen(int len, int rows, int i, int64_t cap) {
   return (int)(n < 0 ? 0 : n > cap ? cap : n);
 }
 
+// Steps of `step` positions that hold n (0 .. 2^31 - 1).
+WICI_HD int kv8_steps(int n, int step) {
+  return (int)(((uint32_t)n + (uint32_t)step - 1) / (uint32_t)step);
+}
+
 // Floats of the partial results of a launch that splits its positions (parts: rows x heads x
 // splits): their outputs, hd floats each, and behind all outputs their states (ref, lift, sum and
 // one float that is not used): each is as aligned as the workspace, for any number of parts.

@@ -19,6 +19,8 @@ int main() {
       std::printf("%zu %zu %zu\n", kv8_part_out((size_t)a[0], (int)a[2]),
                   kv8_part_state((size_t)a[0], (size_t)a[1], (int)a[2]),
                   kv8_part_floats((size_t)a[1], (int)a[2]));
+    } else if (!std::strcmp(what, "steps")) {  // n, step
+      std::printf("%d\n", kv8_steps((int)a[0], (int)a[1]));
     } else {
       return 2;
     }

@@ -194,3 +194,40 @@ def test_rows_whose_every_score_is_minus_infinity(ops, name, dtype):
     out = attend(bt, q)
     check(bt, torch.zeros_like(q), out, [x * 0 for x in K], V, 0.125,
                  seen=lambda j: j % 5 == 0)
+
+
+# ------------------------------------------------------------------ the longest contexts
+@pytest.mark.parametrize("rows", [None, 200])
+def test_contexts_of_all_positions_that_32_bits_count(ops, rows):
+    """2^31 - 1 positions (one page named 2^24 - 1 times, then another): the last page's positions
+    have all but 2^31 e^-40 of the weight, and the slot past the end, of more, has none."""
+    hd, page, n = 64, 128, 2 ** 31 - 1
+    table = torch.zeros(1, 2 ** 24, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    cache = ops.KvCache.empty(2, 1, hd, table, page=page)
+    rng = np.random.default_rng(40)
+    v = rnd(rng, 256, 1, hd, dtype=F32)
+    k = torch.zeros_like(v)
+    k[128:255, 0, 0], k[255, 0, 0] = 40.0, 45.0
+    v[255] = 1000.0
+    ops.KvCache(cache.pool, ints([[0, 1]]), page=page, head_dim=hd).append(
+        k, v, ints([256]), row_start=ints([0, 256]))
+    V = oracle.kv8_values(f64(v))[:, 0]
+    r = rows or 1
+    q = torch.zeros(r, 1, hd, device="cuda")
+    q[:, 0, 0] = 1.0
+    kw = {} if rows is None else dict(row_start=ints([0, rows]), max_rows=rows)
+    out = f64(cache.attend(q, ints([n]), scale=1.0, **kw))[:, 0]
+    for i in {0, r // 2, r - 5, r - 1} & set(range(r)):
+        seen = V[128:256 - (r - i)] if r - i < 128 else None
+        if seen is None:
+            continue
+        # the others: at most 2^31 e^-40 / len(seen) of the weight, each way; two fp16 terms, and
+        # the sum of the last page's 127 weights
+        tol = 2.0 ** 31 * np.exp(-40.0) * np.abs(V).max() * 2 + 2.0 ** -17 * np.abs(seen).mean(0)
+        assert np.all(np.abs(out[i] - seen.mean(0)) <= tol), i
+    if rows:
+        # rows that do not see the last page: the plain mean of the first.  A lane's sum of 2^19
+        # steps is off by at most 2^19 / 2 roundings of 2^-24 of it, a product's by twice that.
+        first = V[:128].mean(0)
+        assert np.all(np.abs(out[0] - first) <= 2.0 ** -4 * np.abs(V[:128]).mean(0))

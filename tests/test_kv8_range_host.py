@@ -49,3 +49,9 @@ def test_partial_results_are_aligned_and_apart(ask, hd):
             assert state + 2 <= floats
         states = [g[1] for g in got]
         assert all(b - a >= 2 for a, b in zip(states, states[1:]))
+
+
+def test_steps_of_the_longest_contexts(ask):
+    q = [(n, step) for step in (32, 64) for n in (0, 1, 31, 32, 33, 64, 65, 2 ** 30, BIG - 64, BIG - 63,
+                                                  BIG - 32, BIG - 1, BIG)]
+    assert [g[0] for g in ask([("steps", *x) for x in q])] == [-(-n // step) for n, step in q]
