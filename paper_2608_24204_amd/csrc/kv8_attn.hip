@@ -852,7 +852,8 @@ __global__ __launch_bounds__(256) void k_kv8_attn_merge(Kv8 c, Kv8Rows r, Kv8Att
   constexpr int L = HD / 4, P = 256 / L;
   __shared__ float4 s_o[P][L];
   __shared__ float4 s_state[P];
-  const unsigned u = blockIdx.x;
+  const unsigned u = blockIdx.y * gridDim.x + blockIdx.x;  // (see kv8_merge_grid)
+  if (u >= (unsigned)(r.n_rows * a.n_q)) return;
   const int lane = threadIdx.x % L, p = threadIdx.x / L, d = 4 * lane;
   const int row = (int)(u / a.n_q), head = (int)(u % a.n_q);
   if (r.kind == KV8_ARRAYS && r.row_start &&
@@ -944,7 +945,8 @@ static hipError_t attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStre
   if (p.nsplit > 1) {
     const int64_t mg = (int64_t)r.n_rows * a.n_q;
     if (mg > 0x7fffffff) return hipErrorInvalidValue;
-    launch_k(k_kv8_attn_merge<HD>, dim3((unsigned)mg), dim3(256), 0, st, last & kLast, c, r, a,
+    const Kv8Merge m = kv8_merge_grid((int)mg);
+    launch_k(k_kv8_attn_merge<HD>, dim3(m.x, m.y), dim3(256), 0, st, last & kLast, c, r, a,
              p.nsplit);
   }
   return hipGetLastError();

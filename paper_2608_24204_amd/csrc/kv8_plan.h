@@ -69,4 +69,15 @@ inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int ma
   return p;
 }
 
+// Workgroups of the merge, one of 256 work-items for each of n rows x heads (1 or more), in two
+// dimensions: along one there may be no more than 2^32 - 1 work-items, and n may be 2^24.  The
+// last of y may pass n.
+struct Kv8Merge {
+  unsigned x, y;
+};
+inline Kv8Merge kv8_merge_grid(int n) {
+  const unsigned x = std::min(n, 1 << 20);
+  return {x, ((unsigned)n + x - 1) / x};
+}
+
 }  // namespace wici

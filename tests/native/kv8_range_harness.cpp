@@ -21,6 +21,9 @@ int main() {
                   kv8_part_floats((size_t)a[1], (int)a[2]));
     } else if (!std::strcmp(what, "steps")) {  // n, step
       std::printf("%d\n", kv8_steps((int)a[0], (int)a[1]));
+    } else if (!std::strcmp(what, "merge")) {  // rows x heads
+      const Kv8Merge m = kv8_merge_grid((int)a[0]);
+      std::printf("%u %u\n", m.x, m.y);
     } else {
       return 2;
     }

@@ -231,3 +231,28 @@ def test_contexts_of_all_positions_that_32_bits_count(ops, rows):
         # steps is off by at most 2^19 / 2 roundings of 2^-24 of it, a product's by twice that.
         first = V[:128].mean(0)
         assert np.all(np.abs(out[0] - first) <= 2.0 ** -4 * np.abs(V[:128]).mean(0))
+
+
+# ------------------------------------------------------------------ the most rows
+def test_as_many_rows_and_heads_as_a_call_takes(ops):
+    """2^24 rows of one head, 2^15 in each of 512 sequences that share their pages: the last 600
+    see their positions, the others nothing; split in two (hints of one row and 544
+    positions), so that every row is merged."""
+    n_seqs, r, n, hd = 512, 2 ** 15, 600, 64
+    bt = Batch(ops, [n], [n], n_kv=1, hd=hd, page=16, seed=50)
+    K, V = bt.fill()
+    cache = ops.KvCache(bt.cache.pool, bt.table.expand(n_seqs, -1).contiguous(), page=16, head_dim=hd)
+    start = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda") * r
+    one = rnd(bt.rng, r, 1, hd)
+    q = one.repeat(n_seqs, 1, 1)
+    out = torch.full_like(q, 7.0)
+    hints = dict(max_rows=1, max_length=544)
+    assert cache.attend_workspace(n_seqs * r, 1, n_seqs, row_start=True, **hints) // (4 * n_seqs * r) \
+        == 2 * (hd + 4)
+    cache.attend(q, torch.full((n_seqs,), n, dtype=torch.int32, device="cuda"), row_start=start, out=out,
+                 **hints)
+    first = out[:r].clone()
+    assert not first[:r - n].any()
+    check(bt, one[r - n:], first[r - n:], K, V, hd ** -0.5)
+    for b in range(n_seqs):
+        assert torch.equal(out[b * r:(b + 1) * r], first), b

@@ -55,3 +55,13 @@ def test_steps_of_the_longest_contexts(ask):
     q = [(n, step) for step in (32, 64) for n in (0, 1, 31, 32, 33, 64, 65, 2 ** 30, BIG - 64, BIG - 63,
                                                   BIG - 32, BIG - 1, BIG)]
     assert [g[0] for g in ask([("steps", *x) for x in q])] == [-(-n // step) for n, step in q]
+
+
+def test_the_merge_of_as_many_rows_as_a_call_takes(ask):
+    """2^24 rows x heads, the most of a call, and any fewer: a grid that covers them, of fewer than
+    2^32 work-items (256 a workgroup) along each dimension."""
+    n = [1, 2, 40, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1, 5 * 10 ** 6, 2 ** 24 - 1, 2 ** 24]
+    for rows, (x, y) in zip(n, ask([("merge", r) for r in n])):
+        assert 256 * x < 2 ** 32 and 1 <= y <= 65535
+        assert x * y >= rows > x * (y - 1)
+        assert y == 1 or rows > 2 ** 20
