@@ -354,10 +354,12 @@ bool in_head_order(const wici_model* m) {
 
 // Attention of rows over layer l of an 8-bit cache: append first (with RoPE where `rope` is
 // set; q_in are the query rows to rotate), then attend into act.  One timed step.
+// max_length: the most positions of a sequence, max_seq where a captured launch reads them on
+// the device; a prompt's are known, and planned for.
 hipError_t kv8_attention(const wici_model* m, int l, const wici::Kv8Rows& r, const wici::RopeTab& rope,
                          const wici::HeadRows& q_in, const wici::HeadRows& q,
                          const wici::HeadRows& k, const wici::HeadRows& v,
-                         const wici::ActBuf& act, int max_rows) {
+                         const wici::ActBuf& act, int max_rows, int max_length) {
   const wici_config& c = m->cfg;
   const float q_scale = 1.0f / std::sqrt((float)c.head_dim);
   if (hipError_t e = wici::launch_kv8_append(c.head_dim, m->kv8(l), r, rope, c.n_heads, q_in, q,
@@ -370,7 +372,7 @@ hipError_t kv8_attention(const wici_model* m, int l, const wici::Kv8Rows& r, con
   a.q = q;
   a.act = act;
   a.max_rows = max_rows;
-  a.max_length = c.max_seq;
+  a.max_length = max_length;
   a.work = m->S<float>(m->L.kv8_work);
   return wici::launch_kv8_attn(m->kv8(l), r, a, m->stream, 2);
 }
@@ -450,7 +452,7 @@ hipError_t enqueue_decode(wici_model* m, std::vector<wici::LaunchTimer>* timers 
       out.f32 = att;
       WICI_STEP(kv8_attention(m, l, r, wici::RopeTab{}, wici::HeadRows{}, m->heads(qkv, 0),
                               m->heads(qkv, c.n_heads), m->heads(qkv, c.n_heads + c.n_kv_heads),
-                              out, 1));
+                              out, 1, c.max_seq));
     } else {
       WICI_STEP(wici::launch_attn_decode(kb, qkv, c.n_heads, m->kv(l), st, L.nsplit,
                                          m->S<float>(L.part_o), m->S<float>(L.part_ml), att,
@@ -568,7 +570,8 @@ hipError_t enqueue_prefill_chunk(wici_model* m, int p0, int T, int tok_off) {
       float* in = s_q > 1 ? P : qkv;
       if ((e = kv8_attention(m, l, r, m->tables(), m->heads(in, 0, s_q, q_split),
                              m->heads(qkv, 0), m->heads(in, c.n_heads, s_q, q_split),
-                             m->heads(in, c.n_heads + c.n_kv_heads, s_q, q_split), att, T)))
+                             m->heads(in, c.n_heads + c.n_kv_heads, s_q, q_split), att, T,
+                             p0 + T)))
         return e;
     } else {
       if ((e = wici::launch_rope_append(kb, qkv, T, p0, c.n_heads, m->W<float>(L.rope_cos),
@@ -689,7 +692,7 @@ hipError_t enqueue_decode_batch(wici_model* m, int B) {
       r.layer = l;
       WICI_TRY(kv8_attention(m, l, r, m->tables(), m->heads(qkv, 0), m->heads(qkv, 0),
                              m->heads(qkv, c.n_heads), m->heads(qkv, c.n_heads + c.n_kv_heads),
-                             att, 1));
+                             att, 1, c.max_seq));
     } else {
       if (!fuse_rope)
         WICI_TRY(wici::launch_rope_append_batch(kb, qkv, B, c.n_heads, m->W<float>(L.rope_cos),
