@@ -253,11 +253,12 @@ wici_status wici_decode_n(wici_model* m, int32_t token_in, int32_t n, int32_t* t
  * stay alive and must not reload weights while m is used) and its own KV cache
  * and scratch (sizes from wici_memory_requirements of m's configuration).  The
  * configurations must agree on everything the weight region depends on (shapes,
- * weight dtype, rms_eps, rope_base and wici_set_rope's, tied_embeddings, max_seq).  m becomes ready
- * at once; wici_load_weights on m is refused (WICI_E_STATE).  Allowed once, in
- * the created state; resets the KV state.  Errors: WICI_E_ARG (NULL or identical
- * models, a differing configuration, NULL/small/misaligned regions),
- * WICI_E_STATE (m already bound, src without complete weights). */
+ * weight dtype, rms_eps, rope_base and the rotation by it or wici_set_rope,
+ * tied_embeddings, max_seq).  m becomes ready at once; wici_load_weights on m is
+ * refused (WICI_E_STATE).  Allowed once, in the created state; resets the KV state.
+ * Errors: WICI_E_ARG (NULL or identical models, a differing configuration,
+ * NULL/small/misaligned regions), WICI_E_STATE (m already bound, src without complete
+ * weights). */
 wici_status wici_bind_memory_shared(wici_model* m, const wici_model* src, void* d_kv,
                                     size_t kv_bytes, void* d_scratch, size_t scratch_bytes);
 

@@ -352,6 +352,27 @@ bool in_head_order(const wici_model* m) {
   return false;
 }
 
+// Angle step of each slot pair, and the factor on its cosines and sines: pos * base^(-2j/hd), or
+// the steps of wici_set_rope (none for the dimensions that pass through).
+struct SlotSteps {
+  double step[64], mult[64];
+};
+SlotSteps slot_steps(const wici_model* m) {
+  SlotSteps s{};
+  wici::RopeFreqs own{};
+  if (m->own_rope) own = wici::rope_freqs(m->rope);
+  for (int j = 0; j < m->cfg.head_dim / 2; ++j) {
+    s.step[j] = std::pow(m->cfg.rope_base, -2.0 * j / m->cfg.head_dim);
+    s.mult[j] = 1.0;
+    if (m->own_rope) {
+      const bool turned = j < m->rope.dim / 2;
+      s.step[j] = turned ? own.f[j] : 0.0;
+      s.mult[j] = turned ? own.factor : 1.0;
+    }
+  }
+  return s;
+}
+
 // Attention of rows over layer l of an 8-bit cache: append first (with RoPE where `rope` is
 // set; q_in are the query rows to rotate), then attend into act.  One timed step.
 // max_length: the most positions of a sequence, max_seq where a captured launch reads them on
@@ -714,13 +735,14 @@ hipError_t enqueue_decode_batch(wici_model* m, int B) {
   return hipSuccess;
 }
 
-// Whether two models rotate alike (their weight regions hold the same tables, and query
-// and key heads in the same order).
+// Whether two models of one head size rotate alike: their weight regions hold the same tables,
+// and query and key heads in the same order.  (Not the specifications' fields: a scaling
+// ignores some of them.)
 bool same_rope(const wici_model* a, const wici_model* b) {
-  const wici_rope &x = a->rope, &y = b->rope;
-  return a->own_rope == b->own_rope && x.dim == y.dim && x.layout == y.layout &&
-         x.scaling == y.scaling && x.base == y.base && x.factor == y.factor &&
-         x.original == y.original && x.low == y.low && x.high == y.high;
+  const SlotSteps x = slot_steps(a), y = slot_steps(b);
+  return std::equal(std::begin(x.step), std::end(x.step), std::begin(y.step)) &&
+         std::equal(std::begin(x.mult), std::end(x.mult), std::begin(y.mult)) &&
+         head_order(a) == head_order(b);
 }
 
 // Configurations whose weight regions are interchangeable (shapes, storage,
@@ -909,20 +931,13 @@ wici_status wici_bind_memory(wici_model* m, void* d_weights, size_t weight_bytes
   m->dkv = static_cast<char*>(d_kv);
   m->ds = static_cast<char*>(d_scratch);
   HIP_TRY(m, alloc_state_mirror(m));
-  // RoPE angle table: pos * base^(-2j/hd), or the steps of wici_set_rope (none for the
-  // dimensions that pass through), evaluated in double, stored as fp32.
+  // RoPE angle table, evaluated in double, stored as fp32.
   const wici_config& c = m->cfg;
   const int half = c.head_dim / 2;
-  wici::RopeFreqs own{};
-  if (m->own_rope) own = wici::rope_freqs(m->rope);
+  const SlotSteps slots = slot_steps(m);
   std::vector<float> cs((size_t)c.max_seq * half), sn((size_t)c.max_seq * half);
   for (int j = 0; j < half; ++j) {
-    double inv = std::pow(c.rope_base, -2.0 * j / c.head_dim), mult = 1.0;
-    if (m->own_rope) {
-      const bool turned = j < m->rope.dim / 2;
-      inv = turned ? own.f[j] : 0.0;
-      mult = turned ? own.factor : 1.0;
-    }
+    const double inv = slots.step[j], mult = slots.mult[j];
     for (int p = 0; p < c.max_seq; ++p) {
       const double ang = (double)p * inv;
       cs[(size_t)p * half + j] = (float)(mult * std::cos(ang));
