@@ -5,7 +5,8 @@ Argument marshalling only: every operator is a HIP kernel of libwici.so.  Tensor
 one HIP GPU; a call enqueues on ``stream`` (default: the current stream of the tensors' GPU)
 and returns without waiting.  On a stream other than the current one the caller orders the
 inputs' producers before the call, as for any torch operation; results are allocated on
-that stream.  Every call may be captured into a HIP graph.
+that stream.  Every call may be captured into a HIP graph.  The operators have no gradients: a
+tensor that requires one is refused where gradients are recorded.
 
     table = ops.rope_table(n_pos, dim, base=500000.0, scaling="bands", factor=8, original=8192)
     cache = ops.KvCache.empty(n_pages, n_kv_heads, head_dim, page_table)
@@ -42,12 +43,19 @@ def _check(st: int, what: str) -> None:
         raise WiciError(st, what)
 
 
+def _no_gradient(x: torch.Tensor, name: str) -> None:
+    if x.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError(f"{name}: requires a gradient, which these operators do not have (call "
+                           "them under torch.no_grad(), or detach)")
+
+
 def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> HeadRows:
     """x [rows, heads, head_dim] as the library takes it (strides of its own, dimensions
     side by side)."""
     dtype = _DTYPES.get(x.dtype)
     if dtype is None:
         raise TypeError(f"{name}: dtype {x.dtype} (float32 or bfloat16)")
+    _no_gradient(x, name)
     shape = x.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected [rows, {heads}, {head_dim}]")
@@ -187,6 +195,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     n, h, d = x.shape
     if table.device != device:
         raise ValueError(f"table: on {table.device}, expected {device}")
+    _no_gradient(table.cos, "table.cos"), _no_gradient(table.sin, "table.sin")
     lib = binding.load_library()
     with _launch_on(stream, device, x, positions, out, table.cos, table.sin) as raw:
         xr = _rows(x, h, d, "x", device)
@@ -272,6 +281,8 @@ class KvCache:
             raise ValueError("q is only rotated: it needs rope")
         if rope is not None and rope.device != dev:
             raise ValueError(f"rope: on {rope.device}, expected {dev}")
+        if rope is not None:
+            _no_gradient(rope.cos, "rope.cos"), _no_gradient(rope.sin, "rope.sin")
         with self._on(stream, k, v, length, row_start, q, q_out, rope and rope.cos,
                       rope and rope.sin) as raw:
             qr, qo, heads = _NO_ROWS, _NO_ROWS, 0
