@@ -48,8 +48,9 @@ def _check(st: int, what: str) -> None:
         raise WiciError(st, what)
 
 
-def _no_gradient(x: torch.Tensor, name: str) -> None:
-    if x.requires_grad and torch.is_grad_enabled():
+def _no_gradient(name: str) -> None:
+    """For a tensor that requires a gradient."""
+    if torch.is_grad_enabled():
         raise RuntimeError(f"{name}: requires a gradient, which these operators do not have (call "
                            "them under torch.no_grad(), or detach)")
 
@@ -60,7 +61,8 @@ def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> Head
     dtype = _DTYPES.get(x.dtype)
     if dtype is None:
         raise TypeError(f"{name}: dtype {x.dtype} (float32 or bfloat16)")
-    _no_gradient(x, name)
+    if x.requires_grad:
+        _no_gradient(name)
     shape = x.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected [rows, {heads}, {head_dim}]")
@@ -200,7 +202,8 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     n, h, d = x.shape
     if table.device != device:
         raise ValueError(f"table: on {table.device}, expected {device}")
-    _no_gradient(table.cos, "table.cos"), _no_gradient(table.sin, "table.sin")
+    if table.cos.requires_grad or table.sin.requires_grad:
+        _no_gradient("table")
     lib = binding.load_library()
     with _launch_on(stream, device, x, positions, out, table.cos, table.sin) as raw:
         xr = _rows(x, h, d, "x", device)
@@ -289,8 +292,8 @@ class KvCache:
             raise ValueError("q is only rotated: it needs rope")
         if rope is not None and rope.device != dev:
             raise ValueError(f"rope: on {rope.device}, expected {dev}")
-        if rope is not None:
-            _no_gradient(rope.cos, "rope.cos"), _no_gradient(rope.sin, "rope.sin")
+        if rope is not None and (rope.cos.requires_grad or rope.sin.requires_grad):
+            _no_gradient("rope")
         with self._on(stream, k, v, length, row_start, q, q_out, rope and rope.cos,
                       rope and rope.sin) as raw:
             qr, qo, heads, given = _NO_ROWS, _NO_ROWS, 0, q is not None and q_out is not None
