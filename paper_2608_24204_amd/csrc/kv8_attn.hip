@@ -439,12 +439,22 @@ __device__ __forceinline__ void put_out(const Kv8Attn& a, int row, int head, int
   }
 }
 
-// `ref` of a row whose weights sum up to nothing: whether any of its n positions (1 or more) is
-// there.  Rare: its scores are all minus infinity, or its pages absent.
-__device__ __forceinline__ float no_weight(const Kv8& c, const Kv8Seq& q, int n) {
-  for (int p = 0; p <= (n - 1) >> c.page_shift; ++p)
-    if (kv8_page(q.table, p, c.max_pages, c.n_pages) >= 0) return kNoWeight;
-  return kNoRef;
+// Rows whose weights sum up to nothing though they have positions (`limit` of them, past the
+// first that this wavefront takes; `most` the largest limit): where one of those is there, `ref`
+// says so.  Rare: their scores are all minus infinity, or their pages absent.  The wavefront
+// looks for the sequence's first page together, 64 entries at a time.
+__device__ __forceinline__ void note_no_weight(RowState& st, const Kv8& c, const Kv8Seq& q, int limit,
+                                               uint32_t past, int most, int lane) {
+  const bool none = st.sum == 0.f && (uint32_t)limit > past;
+  if (!__any(none)) return;
+  const int pages = kv8_steps(most, 1 << c.page_shift);
+  for (int p = 0; p < pages; p += 64) {
+    const uint64_t there =
+        __ballot(p + lane < pages && kv8_page(q.table, p + lane, c.max_pages, c.n_pages) >= 0);
+    if (there == 0) continue;
+    if (none && (p + __builtin_ctzll(there)) << c.page_shift < limit) st.ref = kNoWeight;
+    return;
+  }
 }
 
 // The joined output of outputs that hold 2^-lift of their sum.
@@ -564,7 +574,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);
     st.sum += __shfl_xor(st.sum, 32);
-    if (st.sum == 0.f && limit > s0 * kStep) st.ref = no_weight(c, q, limit);
+    note_no_weight(st, c, q, limit, s0 * kStep, seen(last), lane);
     const int me = fresh(lane), mr = me & 15, mg = me >> 4;
     if (mg == 0) {
       s_ref[wave][mr] = st.ref;
@@ -826,8 +836,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv8_attn_tile(Kv8 c, Kv8Rows r, K
     for (int y = 0; y < kRowTiles; ++y) {
       st[y].sum += __shfl_xor(st[y].sum, 16);
       st[y].sum += __shfl_xor(st[y].sum, 32);
-      if (st[y].sum == 0.f && (uint32_t)limit[y] > (uint32_t)c0 * kChunkPos)
-        st[y].ref = no_weight(c, q, limit[y]);
+      note_no_weight(st[y], c, q, limit[y], (uint32_t)c0 * kChunkPos, most, lane);
       const int qr = mine + 16 * y + (me & 15);
       if (qr >= total) continue;
 #pragma unroll
