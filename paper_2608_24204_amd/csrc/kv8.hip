@@ -105,7 +105,8 @@ __device__ __forceinline__ void turn_row(const RopeTab& rope, const Runs& r, int
 // ------------------------------------------------------------------- rotary positions
 // The table is read where another head of the row has read it before; a row's heads are
 // neighbouring units.  Bound by memory: 8192 rows of 32 heads of 128 (bf16, pairs) 24 us for 134
-// MB, 5.6 TB/s where a large copy moves 5.2 (8 bytes a lane at a time: 26); 32 rows 3.2 us.
+// MB, 5.6 TB/s where a large copy moves 5.2 (8 bytes a lane at a time: 26), on inputs partly in
+// the memory-side cache; in calls whose inputs change 28.7 us, 4.7 TB/s.  32 rows 3.2 us.
 template <int HD>
 __global__ __launch_bounds__(256) void k_rope_rows(HeadRows x, HeadRows y, int n_rows, int n_heads,
                                                    const int32_t* __restrict__ positions,
@@ -288,8 +289,9 @@ __device__ __forceinline__ bool one_word(const RowAt (&w)[R], char* const (&blk)
 // they are requested first.  With four rows (prompts) a value word of four positions is
 // written whole where the rows are those four: single bytes took 14.7 us for 2048 rows of 8
 // heads of 128, now 11: 8.4 MB in and 4.3 out, of which a call of 48 rows already takes the
-// first 4.7 (a row's place is three loads, one after another).  Bound by neither bytes nor
-// arithmetic: half the vector instructions, or one load less in the chain, changed nothing.
+// first 4.7 (a row's place is three loads, one after another).  What bounds it is not known:
+// neither bytes (2.4 us) nor arithmetic nor that chain, since half the vector instructions, or one
+// load less in the chain, changed nothing.
 // 12 prompts of up to 500 rows whose positions start anywhere in a word (fp32, heads of 64)
 // take 15 us, their values written byte by byte.
 template <int HD, int R>

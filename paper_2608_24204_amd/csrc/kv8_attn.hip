@@ -213,8 +213,8 @@ __device__ __forceinline__ void scores(floatx4_t (&sc)[kTiles], const Keys<HD>& 
 // positions below `seen`, of the tiles that are there.  `lifts`: some row of the wavefront is
 // apart.  Returns whether a row's reference moved: the output so far is then to be multiplied by
 // `corr`.  HINT: the compiler is told that moves are rare.  That places the row tiles' code well
-// (heads of 64, 2048 rows of 8192: 220 us for 235; 16 x 100 of 1000: 41 for 43), the split's not
-// (48 tokens at 4000, fp32: 45.9 for 44.5).
+// (2048 rows of 8192: 287 us for 304, heads of 64 226 for 236), the split's not (48 tokens at
+// 4000, heads of 64, fp32: 45.8 for 44.8).
 template <int NT, bool MASKED, bool HINT>
 __device__ __forceinline__ bool weights(half8_t (&wf)[NT], RowState& st, bool& lifts,
                                         const floatx4_t (&sc)[kTiles], const Scales& s,
@@ -494,9 +494,10 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, s
 // Bound by the cache's bytes, each read once: 32 tokens at 16384 (40 query on 8 KV heads of
 // 128, bf16) 188 us for 1.11 GB, 5.9 TB/s where a large copy moves 5.2; its loads with
 // nothing behind them take as long.  Where there is less to read the start, the first loads'
-// latency and the join show: 48 tokens at up to 4000 (heads of 64) 37 us for 162 MB, one at
+// latency and the join show: 48 tokens at up to 4000 (heads of 64) 36 us for 162 MB, one at
 // 16384 (fp32) 14 us for 35 MB.  Three wavefronts a SIMD for heads of 128 (two with two fp16
-// terms), four for heads of 64; 256 / 512 / 768 / 1024 workgroups: 289 / 203 / 195 / 231 us
+// terms), four for heads of 64 (with two terms for 12 bytes a lane in scratch: a call of 32 tokens at
+// 16384 99 us, with three wavefronts and none 124; 48 at 4000 44 and 43); 256 / 512 / 768 / 1024 workgroups: 289 / 203 / 195 / 231 us
 // of the first case, which is why a launch splits no further than fills the chip once.
 template <int HD, int NT>
 __global__ __launch_bounds__(256)
@@ -631,9 +632,9 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_
 // Two buffers: the next chunk's codes are on their way while this one is multiplied, and one
 // barrier a chunk parts a buffer's readers from its next writers.
 //
-// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 298 us in bf16, 807 TFLOP/s
-// of products where a large fp16 product reaches 1300; 495 us with two fp16 terms.  No unit is
-// full: the vector units are busy 53% of the time, the matrix cores 32%, and a wavefront waits
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 288 us in bf16, 836 TFLOP/s
+// of products where a large fp16 product reaches 1300; 477 us with two fp16 terms.  No unit is
+// full: the vector units are busy 52% of the time, the matrix cores 32%, and a wavefront waits
 // for operands, products or the other one (the registers allow two a SIMD).  Eight vector
 // instructions fewer for 512 scores, and priorities of the products or the weights, changed
 // nothing; the next products ahead of the weights need more registers than there are.

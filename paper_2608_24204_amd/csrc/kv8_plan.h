@@ -20,19 +20,19 @@ struct Kv8Plan {
   int ntile, nsplit;
 };
 // Which kernel, from the rows x heads of a KV head, the workgroups of 128 of them and the
-// 16 rows x 32 positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us,
-// split / 64 rows / 128 rows):
-//  - below 128 rows the split: 16 new rows of each of 8 sequences of 2000: 24 / 25 / 33;
-//    16 of 8000 positions: 20 / 23 / 29;
+// 16 rows x 32 positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us a
+// call, split / 64 rows / 128 rows):
+//  - below 128 rows the split: 16 new rows of each of 8 sequences of 2000: 28 / 28 / 33;
+//    16 of 8000 positions: 21 / 23 / 29;
 //  - where 128 rows fill the chip, or have long contexts to split: 2048 of 8192 positions:
-//    634 / 392 / 300; 16 x 100 of 1000: 64 / 54 / 52; 128 of 8000: 57 / 49 / 49;
-//  - a chip half full: 64 rows: 1024 of 1024: 41 / 32 / 58; 32 x 32 of 300: 30 / 19 / 22;
-//  - few workgroups and little to do: the split: 333 of 333: 12 / 16 / 23; 256 of 512:
-//    12 / 18 / 25.
+//    636 / 379 / 288; 16 x 100 of 1000: 87 / 66 / 53; 128 of 8000: 57 / 48 / 48;
+//  - a chip half full: 64 rows: 1024 of 1024: 39 / 29 / 57; 32 x 32 of 300: 32 / 19 / 22;
+//  - few workgroups and little to do: the split: 333 of 333: 13 / 16 / 22; 256 of 512:
+//    13 / 17 / 25.
 // With two terms 128 rows' operands and results leave no registers to hold a chunk's operands
-// in: 64 rows in their place (64 / 128 rows: 2048 of 2048: 93 / 125; 8 x 500 of 1000: 105 / 127;
-// 128 of 8000: 56 / 62; 2048 of 8192: 493 / 477, of 16384: 1038 / 997).
-// (The farthest from the best of 24 such: 32 of 4000 in 4 sequences, 36 for 32.)
+// in: 64 rows in their place (64 / 128 rows, while there were both: 2048 of 2048: 93 / 125;
+// 8 x 500 of 1000: 105 / 127; 128 of 8000: 56 / 62; 2048 of 8192: 493 / 477, of 16384: 1038 / 997).
+// (The farthest from the best of 24 such: 32 of 4000 in 4 sequences, 37 for 34.)
 constexpr int kTileRows = 128, kFull = 400, kHalf = 200;
 constexpr double kMuch = 60000;
 inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int max_rows, int max_length) {
