@@ -196,6 +196,24 @@ def test_rows_whose_every_score_is_minus_infinity(ops, name, dtype):
                  seen=lambda j: j % 5 == 0)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_of_one_position_and_scores_of_infinity(ops, dtype):
+    """One, two and three positions: an infinite query element over a key element of either sign is
+    NaN, for single tokens and for a prompt whose first row sees one position."""
+    for rows in (None, [1, 2, 3]):
+        bt = Batch(ops, [1, 2, 3], rows, n_kv=1, hd=128, page=16, seed=31)
+        v = rnd(bt.rng, 6, 1, 128, dtype=F32)
+        k = torch.ones_like(v)
+        for sign in (1.0, -1.0):
+            k[:, :, 9] = sign
+            store(bt, k, v)
+            for inf in (float("inf"), -float("inf")):
+                q = rnd(bt.rng, bt.n_rows, 3, 128, dtype=dtype)
+                q[:, 1, 9] = inf
+                out = attend(bt, q)
+                assert out[:, 1].isnan().all() and out[:, ::2].isfinite().all(), (rows, sign, inf)
+
+
 # ------------------------------------------------------------------ the longest contexts
 @pytest.mark.parametrize("rows", [None, 200])
 def test_contexts_of_all_positions_that_32_bits_count(ops, rows):
