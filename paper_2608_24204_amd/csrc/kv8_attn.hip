@@ -496,9 +496,10 @@ __device__ __forceinline__ void leave(const Kv8Attn& a, int nsplit, int split, s
 // nothing behind them take as long.  Where there is less to read the start, the first loads'
 // latency and the join show: 48 tokens at up to 4000 (heads of 64) 36 us for 162 MB, one at
 // 16384 (fp32) 14 us for 35 MB.  Three wavefronts a SIMD for heads of 128 (two with two fp16
-// terms), four for heads of 64 (with two terms for 12 bytes a lane in scratch: a call of 32 tokens at
-// 16384 99 us, with three wavefronts and none 124; 48 at 4000 44 and 43); 256 / 512 / 768 / 1024 workgroups: 289 / 203 / 195 / 231 us
-// of the first case, which is why a launch splits no further than fills the chip once.
+// terms), four for heads of 64 (with two terms for 12 bytes a lane in scratch: a call of 32 tokens
+// at 16384 99 us, with three wavefronts and none 124; 48 at 4000 44 and 43).  256 / 512 / 768 /
+// 1024 workgroups: 289 / 203 / 195 / 231 us of the first case, which is why a launch splits no
+// further than fills the chip once.
 template <int HD, int NT>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NT == 1 ? 3 : 2))) void k_kv8_attn_split(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
