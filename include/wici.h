@@ -406,8 +406,8 @@ wici_status wici_stream_read_noalloc(const void* d_buf, size_t bytes, int32_t gr
 
 /* ---- Operators on caller-owned device tensors (no model) -------------------------
  *
- * Rotary positions, an 8-bit paged KV cache and causal attention over it, for callers
- * that run their own layers.  Conventions of these calls:
+ * Rotary positions, paged KV caches of 8 and of 4 bits and causal attention over them, for
+ * callers that run their own layers.  Conventions of these calls:
  *  - every pointer marked device is device memory of the stream's GPU; tensors stay with
  *    the caller, and the calls allocate nothing;
  *  - a call enqueues on hip_stream (NULL: the null stream of the current device) and
@@ -529,6 +529,45 @@ wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batc
  * heads, of any of the two types each; out may be q only if they are the same rows exactly.
  * workspace: device, 16-byte aligned, undefined before and after. */
 wici_status wici_kv8_attend(const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,
+                            float scale, wici_head_rows q, wici_head_rows out, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
+/* The same with four bits a value: about half of wici_kv8's bytes.  The calls take the same
+ * descriptors and follow the same rules as wici_kv8's; the pool is 16-byte aligned and of
+ * wici_kv4_bytes bytes.  For each page, keys then values, and each KV head, it holds a block of
+ * page * head_dim / 2 bytes of codes and then page * head_dim / 32 scale bytes.  A code stands for
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} (bit 3 the sign, bits 0-2 which) times 2^(byte - 127), byte being
+ * the scale byte of its 32 neighbouring dimensions.  A stored row of head_dim values x has, for
+ * each 32 of them with a = max |x_d|,
+ *   the least exponent e of -60 .. 125 with a <= 7 2^e,
+ *   codes of the nearest to x_d 2^-e, ties to the even code (more than 6: 6).
+ * A row holding an infinity or a NaN is stored as all NaN (every scale byte 255).  A byte of codes
+ * holds dimensions 2 j (low bits) and 2 j + 1.  Key bytes lie as [page][head_dim / 2], their scales
+ * as [page][head_dim / 32]; value bytes as [page / 4][head_dim / 2][4], their scales as
+ * [page / 4][head_dim / 32][4]: those of four neighbouring positions side by side.  34 (64
+ * dimensions) or 68 (128) bytes for each position, head, key or value. */
+typedef wici_kv8 wici_kv4;
+
+/* Bytes of a pool. */
+wici_status wici_kv4_bytes(const wici_kv4* cache, size_t* bytes);
+
+/* As wici_kv8_append. */
+wici_status wici_kv4_append(const wici_kv4* cache, const wici_kv8_batch* batch,
+                            const wici_rope_tab* rope, int32_t n_heads, wici_head_rows q,
+                            wici_head_rows q_out, wici_head_rows k, wici_head_rows v,
+                            void* hip_stream);
+
+/* As wici_kv8_read. */
+wici_status wici_kv4_read(const wici_kv4* cache, const wici_kv8_batch* batch, wici_head_rows k,
+                          wici_head_rows v, void* hip_stream);
+
+/* As wici_kv8_attend_workspace. */
+wici_status wici_kv4_attend_workspace(const wici_kv4* cache, const wici_kv8_batch* batch,
+                                      int32_t n_heads, size_t* bytes);
+
+/* As wici_kv8_attend.  The cached values are exact in the matrix products; where q and out are
+ * bf16, q is too and the weights are within 2^-16, else both are within 2^-24. */
+wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream);
 

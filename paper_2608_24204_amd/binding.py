@@ -33,7 +33,8 @@ EXPORTED = ["wici_create", "wici_memory_requirements", "wici_bind_memory", "wici
             "wici_load_weights_cached", "wici_bind_memory_shared", "wici_decode_batch",
             "wici_stream_read", "wici_stream_read_noalloc", "wici_last_error", "wici_destroy",
             "wici_set_rope", "wici_rope_table", "wici_rope_rows", "wici_kv8_bytes", "wici_kv8_append",
-            "wici_kv8_read", "wici_kv8_attend_workspace", "wici_kv8_attend"]
+            "wici_kv8_read", "wici_kv8_attend_workspace", "wici_kv8_attend", "wici_kv4_bytes",
+            "wici_kv4_append", "wici_kv4_read", "wici_kv4_attend_workspace", "wici_kv4_attend"]
 
 
 class WiciConfig(ctypes.Structure):
@@ -132,19 +133,19 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "wici_rope_table": ([ctypes.POINTER(WiciRope), ctypes.c_int64, P, P, P], ctypes.c_int),
         "wici_rope_rows": ([ctypes.POINTER(WiciRopeTab), i32, i32, i32, P, WiciHeadRows,
                             WiciHeadRows, P], ctypes.c_int),
-        "wici_kv8_bytes": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(sz)], ctypes.c_int),
-        "wici_kv8_append": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch),
-                             ctypes.POINTER(WiciRopeTab), i32, WiciHeadRows, WiciHeadRows,
-                             WiciHeadRows, WiciHeadRows, P], ctypes.c_int),
-        "wici_kv8_read": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), WiciHeadRows,
-                           WiciHeadRows, P], ctypes.c_int),
-        "wici_kv8_attend_workspace": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), i32,
-                                       ctypes.POINTER(sz)], ctypes.c_int),
-        "wici_kv8_attend": ([ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch), i32,
-                             ctypes.c_float, WiciHeadRows, WiciHeadRows, P, sz, P], ctypes.c_int),
         "wici_last_error": ([P], ctypes.c_char_p),
         "wici_destroy": ([P], None),
     }
+    rows, kv, batch = WiciHeadRows, ctypes.POINTER(WiciKv8), ctypes.POINTER(WiciKv8Batch)
+    for bits in (8, 4):
+        sig.update({
+            f"wici_kv{bits}_bytes": ([kv, ctypes.POINTER(sz)], ctypes.c_int),
+            f"wici_kv{bits}_append": ([kv, batch, ctypes.POINTER(WiciRopeTab), i32, rows, rows, rows,
+                                       rows, P], ctypes.c_int),
+            f"wici_kv{bits}_read": ([kv, batch, rows, rows, P], ctypes.c_int),
+            f"wici_kv{bits}_attend_workspace": ([kv, batch, i32, ctypes.POINTER(sz)], ctypes.c_int),
+            f"wici_kv{bits}_attend": ([kv, batch, i32, ctypes.c_float, rows, rows, P, sz, P],
+                                      ctypes.c_int)})
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
         f.argtypes = args

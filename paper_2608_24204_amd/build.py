@@ -21,6 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["gemv.hip", "misc.hip", "attention.hip", "gemm.hip", "batch.hip", "kv8.hip", "kv8_attn.hip",
+           "kv4.hip", "kv4_attn.hip",
            "model.cpp", "ops.cpp", "quant.cpp", "cache.cpp", "noalloc.cpp"]
 
 FLAGS = [
@@ -36,7 +37,7 @@ FLAGS = [
 # registers (not the accumulation registers), so the output rows that the softmax
 # rescales are not copied between the two register files on every key block.
 _VGPR_RESULTS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA = {"attention.hip": _VGPR_RESULTS, "kv8_attn.hip": _VGPR_RESULTS}
+EXTRA = {"attention.hip": _VGPR_RESULTS, "kv8_attn.hip": _VGPR_RESULTS, "kv4_attn.hip": _VGPR_RESULTS}
 
 
 def _run(cmd, verbose):

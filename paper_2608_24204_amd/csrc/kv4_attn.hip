@@ -1,0 +1,431 @@
+// Causal grouped-query attention over the 4-bit key-value cache.
+//
+// Mathematics.  For a row with query q over positions j with key rows k_j and value rows v_j:
+//   y_j = (q . k_j) scale log2(e),   out = sum_j 2^(y_j - ref) v_j / sum_j 2^(y_j - ref),
+// `ref` running with the largest y_j (an online softmax): it moves only when a weight would pass
+// 2^8, to the largest score so far.  A cached value is one of 8 small numbers times a power of two,
+// exact in bf16 over fp32's whole range, so both products run on the bf16 matrix cores with the
+// scales inside their operands: one conversion instruction makes two operands of a byte and a
+// scale.  q and the weights enter as NQ and NW bf16 terms: bf16 queries are exact in one, and two
+// hold a weight to 2^-16, far inside a bf16 output's rounding; three hold either to fp32's own.
+// Scores, weights, sums and the output are fp32.
+//
+// A value row that is NaN (scale bytes 255) must not reach rows that do not see it, and a product
+// with a weight of zero would: its operands are made with another scale, and the weights of the
+// rows that do see it are NaN instead.
+//
+// Layout.  S^T = K Q^T and O^T = V^T W^T on v_mfma_f32_16x16x32_bf16, as over the 8-bit cache:
+// lane l holds query row l % 16 in both results, a tile of S^T leaves it with positions
+// 4 (l / 16) .. + 3, and those are the positions that the second product takes from it.  For the
+// keys a lane takes position l % 16 and a quarter of the dimensions, within one group's scale;
+// for the values four positions of hd / 16 neighbouring dimensions, and their four scales.
+#include <algorithm>
+
+#include "kv4.h"
+#include "kv4_plan.h"
+#include "kv_attn.h"
+#include "launch.h"
+
+namespace wici {
+
+constexpr float kMostAhead = 8.f;  // of a score to its row's reference, past which that moves
+
+// The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
+struct RowState4 {
+  float ref = kNoRef, sum = 0.f;  // sum over this lane's positions
+};
+// Output of 16 rows: tile u, element i: dimension (HD / 16) (4 (l / 16) + i) + u.
+template <int HD>
+using RowOut4 = floatx4_t[HD / 16];
+
+// Byte i of a word of scales as the power of two that it stands for.
+__device__ __forceinline__ float scale_of(unsigned w, int i) {
+  return __uint_as_float((i ? w >> (8 * i) & 0xffu : w & 0xffu) << 23);
+}
+template <int BYTE>
+__device__ __forceinline__ unsigned pair_of(unsigned w, float scale) {
+  return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, BYTE));
+}
+// A word of key codes, eight dimensions of a position, as an operand.
+__device__ __forceinline__ bf16x8_t keys8(unsigned w, float scale) {
+  return __builtin_bit_cast(bf16x8_t, make_uint4(pair_of<0>(w, scale), pair_of<1>(w, scale),
+                                                 pair_of<2>(w, scale), pair_of<3>(w, scale)));
+}
+// A word of value codes, four positions of a pair of dimensions: the positions of the first
+// dimension (lo) and of the second.
+__device__ __forceinline__ void values4(unsigned w, const float (&s)[4], uint2& lo, uint2& hi) {
+  const unsigned a = pair_of<0>(w, s[0]), b = pair_of<1>(w, s[1]), c = pair_of<2>(w, s[2]),
+                 d = pair_of<3>(w, s[3]);
+  lo = make_uint2(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u));
+  hi = make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
+}
+// Which of a word's four positions are NaN (scale byte 255; 253 and 254, which memory never
+// appended to may hold, are taken as it: 4 times theirs is infinite), as bits; their scales become 1.
+__device__ __forceinline__ unsigned take_nans(unsigned& w) {
+  const bool maybe = (w & w << 1 & 0x80808080u) != 0;  // some scale of 2^65 and more
+  unsigned nan = 0;
+  if (__builtin_expect(__any(maybe), false)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((w >> (8 * i) & 0xffu) > (unsigned)kKv4MostByte) {
+        nan |= 1u << i;
+        w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
+      }
+  }
+  return nan;
+}
+
+// The codes and scales of a step, as one lane holds them.
+template <int HD>
+struct Step4 {
+  unsigned k[kTiles][HD / 32], ks[kTiles];  // position l % 16, dimensions (HD / 4) (l / 16) ..
+  unsigned v[kTiles][HD / 32], vs[kTiles];  // positions 4 (l / 16) .. + 3, dimensions (HD / 16) (l % 16) ..
+};
+template <int HD>
+__device__ __forceinline__ void fetch_codes(unsigned (&w)[HD / 32], __amdgpu_buffer_rsrc_t r,
+                                            int lane_at, int at) {
+  if constexpr (HD == 128) {
+    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0);
+    w[0] = v[0]; w[1] = v[1];
+  }
+}
+// One KV head of a pool: its key block in page 0, and the bytes from page to page and from a
+// key block to its value block.
+template <int HD>
+struct HeadAt4 {
+  const char* base;
+  uint32_t page, values;
+  __device__ __forceinline__ HeadAt4(const Kv8& c, const Kv8Seq& q, int h)
+      : base(q.base + kv4_block_at(0, 0, h, c.n_kv, 1 << c.page_shift, HD)),
+        page(2 * c.n_kv * (uint32_t)kv4_block_bytes(1 << c.page_shift, HD)),
+        values(page / 2) {}
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const Kv8& c, int phys, int which) const {
+    return rsrc(base + (uint64_t)(uint32_t)max(phys, 0) * page + (which ? values : 0),
+                kv4_block_bytes(1 << c.page_shift, HD));
+  }
+};
+template <int HD>
+__device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const HeadAt4<HD>& at,
+                                           const Pages& p, int step, int lane) {
+  const int page = 1 << c.page_shift, pos = lane & 15, d = (lane >> 4) * (HD / 4);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const int slot = (step * kStep + 16 * t) & (page - 1);
+    const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0);
+    fetch_codes<HD>(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
+    s.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(b, pos * (HD / kKv4Group) + d / kKv4Group,
+                                                  kv4_key_scale_at(slot, 0, page, HD), 0);
+  }
+}
+template <int HD>
+__device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const HeadAt4<HD>& at,
+                                             const Pages& p, int step, int lane) {
+  const int page = 1 << c.page_shift, pos = 4 * (lane >> 4), d = (lane & 15) * (HD / 16);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const int slot = (step * kStep + 16 * t) & (page - 1);
+    const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 1);
+    fetch_codes<HD>(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
+    s.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, pos * (HD / kKv4Group) + 4 * (d / kKv4Group),
+                                                   kv4_value_scale_at(slot, 0, page, HD), 0);
+  }
+}
+
+// S^T of one step: sc[t][i] is the product of position 16 t + 4 (l / 16) + i with row l % 16.
+template <int HD, int NQ>
+__device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>& s,
+                                        const bf16x8_t (&qf)[NQ][HD / 32]) {
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    const float scale = __uint_as_float(s.ks[t] << 23);
+    sc[t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+      const bf16x8_t a = keys8(s.k[t][d], scale);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[n][d], sc[t], 0, 0, 0);
+    }
+  }
+}
+
+// The weights of 32 positions from their products (a score is product * unit), as NW bf16 terms.
+// MASKED: some row does not see every position: row l % 16 sees those below `seen`, of the tiles
+// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  Returns whether a row's
+// reference moved: the output so far is then to be multiplied by `corr`.
+template <int NW, bool MASKED>
+__device__ __forceinline__ bool weights4(bf16x8_t (&wf)[NW], RowState4& st,
+                                         const floatx4_t (&sc)[kTiles], const Pages& p, float unit,
+                                         unsigned nan, int seen, int lane, float& corr) {
+#pragma clang fp contract(off)  // of two scores that are equal and huge the difference is zero
+  const int left = seen - 4 * (lane >> 4);
+  auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
+  float y[4 * kTiles], d[4 * kTiles], most;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[4 * t + i] = on(t, i) ? sc[t][i] * unit : -INFINITY;
+  if (__builtin_expect(__any(nan != 0), false)) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (on(t, i) && (nan >> (4 * t + i) & 1)) y[4 * t + i] = __uint_as_float(0x7fc00000u);
+  }
+  auto against = [&]() {
+    most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4 * kTiles; ++i) {
+      d[i] = y[i] - st.ref;
+      most = __builtin_elementwise_maximum(most, d[i]);  // NaN if one is
+    }
+  };
+  against();
+  const bool move = __any(!(most <= kMostAhead));
+  if (move) {
+    // (by a row's own scores alone: other rows' change nothing in it)
+    float z = y[0];
+#pragma unroll
+    for (int i = 1; i < 4 * kTiles; ++i) z = fmaxf(z, y[i]);
+    z = fmaxf(z, __shfl_xor(z, 16));
+    z = fmaxf(z, __shfl_xor(z, 32));
+    const float ref = z - st.ref > kMostAhead ? z : st.ref;
+    corr = ref == st.ref ? 1.f : __builtin_amdgcn_exp2f(st.ref - ref);
+    st.sum *= corr;
+    st.ref = ref;
+    against();
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4 * kTiles; ++i) {
+    float rest = __builtin_amdgcn_exp2f(d[i]);
+    sum += rest;
+#pragma unroll
+    for (int n = 0; n < NW; ++n) {
+      wf[n][i] = (__bf16)rest;
+      rest -= (float)wf[n][i];
+    }
+  }
+  st.sum += sum;
+  return move;
+}
+
+// O^T += V^T W^T of one step; vs: the scales, NaN ones replaced.
+template <int HD, int NW>
+__device__ __forceinline__ void add_values4(RowOut4<HD>& o, const Step4<HD>& s,
+                                            const unsigned (&vs)[kTiles],
+                                            const bf16x8_t (&wf)[NW]) {
+  float f[kTiles][4];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[t][i] = scale_of(vs[t], i);
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) {
+    uint2 a0, a1, b0, b1;
+    values4(s.v[0][d], f[0], a0, b0);
+    values4(s.v[1][d], f[1], a1, b1);
+    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, make_uint4(a0.x, a0.y, a1.x, a1.y));
+    const bf16x8_t b = __builtin_bit_cast(bf16x8_t, make_uint4(b0.x, b0.y, b1.x, b1.y));
+#pragma unroll
+    for (int n = 0; n < NW; ++n) {
+      o[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, wf[n], o[2 * d], 0, 0, 0);
+      o[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, wf[n], o[2 * d + 1], 0, 0, 0);
+    }
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void rescale4(RowOut4<HD>& o, float f) {
+#pragma unroll
+  for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[u][i] *= f;
+}
+
+// 16 query rows (row l % 16 of the tile, zero where `on` is false) as NQ bf16 terms.
+template <int HD, int NQ>
+__device__ __forceinline__ void load_queries4(const HeadRows& q, int64_t at, bool on, int lane,
+                                              bf16x8_t (&qf)[NQ][HD / 32]) {
+  at += (lane >> 4) * (HD / 4);
+  if (NQ == 1 || q.bf16) {
+    uint4 raw[HD / 32];
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+      raw[d] = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(q.p) + at + 8 * d);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) {
+      qf[0][d] = __builtin_bit_cast(bf16x8_t, on ? raw[d] : make_uint4(0, 0, 0, 0));
+#pragma unroll
+      for (int n = 1; n < NQ; ++n) qf[n][d] = bf16x8_t{};
+    }
+  } else {
+    float v[HD / 32][8];
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) load8(static_cast<const float*>(q.p) + at + 8 * d, v[d]);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float rest = on ? v[d][i] : 0.f;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          qf[n][d][i] = (__bf16)rest;
+          rest -= (float)qf[n][d][i];
+        }
+      }
+  }
+}
+
+// ------------------------------------------------------------------- split over positions
+// Workgroup (KV head, sequence, split): four wavefronts take the split's steps of 32
+// positions in turn for a tile of 16 of the sequence's rows x query heads of the group
+// (row r: new row r / G, query head r % G), and are joined at the end.  Splits take
+// groups of four steps in turn, so one launch serves any length evenly.  With one
+// split the output is written here, otherwise (ref, sum, output) is left for the merge.
+template <int HD, int NQ, int NW>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_attn_split(
+    Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit, int ntile) {
+  __shared__ float s_o[4][16][HD + 4];
+  __shared__ float s_ref[4][16], s_sum[4][16];
+  const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
+  const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, G = a.n_q / c.n_kv;
+  const Kv8Seq q = uniform(kv8_seq(c, r, b));
+  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+  const size_t parts = (size_t)r.n_rows * a.n_q * nsplit;
+  // the wavefront's first steps do not depend on the length, so that their pages are
+  // looked up beside it
+  const HeadAt4<HD> kv(c, q, h);
+  const int s0 = 4 * split + wave;
+  const Entries e0 = find(c, q, s0), e1 = find(c, q, s0 + 4 * nsplit);
+
+  for (int tile = tile0; tile * 16 < q.rows * G; tile += ntile) {
+    const int qr = 16 * tile + r16, row = qr / G, head = h * G + qr % G;
+    const bool on = row < q.rows;
+    const int rc = min(row, q.rows - 1);
+    // a row sees the positions up to its own; the tile's last row sees the most
+    const int last = min((16 * tile + 15) / G, q.rows - 1), first = 16 * tile / G;
+    auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
+    const int limit = on ? seen(row) : 0, steps = kv8_steps(seen(last), kStep);
+    // steps that all 16 rows see whole
+    const int whole = 16 * tile + 15 < q.rows * G ? seen(first) / kStep : 0;
+
+    // the next step's keys are requested once this one's are multiplied, its values
+    // likewise, and its pages (which those addresses wait for) a step earlier
+    const int stride = 4 * nsplit;
+    int s = s0;
+    bf16x8_t qf[NQ][HD / 32];
+    load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf);
+    const float unit = a.scale * kLog2e;
+    RowState4 st;
+    RowOut4<HD> o;
+#pragma unroll
+    for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    if (s < steps) {
+      Step4<HD> x;
+      Pages now = named(c, e0);
+      Entries later = e1;
+      load_keys4<HD>(x, c, kv, now, s, lane);
+      load_values4<HD>(x, c, kv, now, s, lane);
+      for (;;) {
+        floatx4_t sc[kTiles];
+        scores4<HD, NQ>(sc, x, qf);
+        const int then = s + stride;
+        const Pages next = named(c, later);
+        if (then < steps) load_keys4<HD>(x, c, kv, next, then, lane);
+        unsigned vs[kTiles], nan = 0;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          vs[t] = x.vs[t];
+          nan |= take_nans(vs[t]) << (4 * t);
+        }
+        bf16x8_t wf[NW];
+        float corr = 1.f;
+        const bool move =
+            s < whole && now.all()
+                ? weights4<NW, false>(wf, st, sc, now, unit, nan, 0, lane, corr)
+                : weights4<NW, true>(wf, st, sc, now, unit, nan, limit - s * kStep, lane, corr);
+        if (move) rescale4<HD>(o, corr);
+        add_values4<HD, NW>(o, x, vs, wf);
+        if (then >= steps) break;
+        load_values4<HD>(x, c, kv, next, then, lane);
+        now = next;
+        later = find(c, q, then + stride);
+        s = then;
+      }
+    }
+    // join the wavefronts
+    st.sum += __shfl_xor(st.sum, 16);
+    st.sum += __shfl_xor(st.sum, 32);
+    note_no_weight(st.ref, st.sum, c, q, limit, s0 * kStep, seen(last), lane);
+    const int me = fresh(lane), mr = me & 15, mg = me >> 4;
+    if (mg == 0) {
+      s_ref[wave][mr] = st.ref;
+      s_sum[wave][mr] = st.sum;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int u = 0; u < HD / 16; u += 4)
+        *reinterpret_cast<float4*>(&s_o[wave][mr][HD / 16 * (4 * mg + i) + u]) =
+            make_float4(o[u][i], o[u + 1][i], o[u + 2][i], o[u + 3][i]);
+    __syncthreads();
+    for (int x = fresh(threadIdx.x); x < 16 * HD / 4; x += 256) {
+      const int rr = x / (HD / 4), d = 4 * (x % (HD / 4)), tr = 16 * tile + rr;
+      if (tr >= q.rows * G) continue;
+      float ref = s_ref[0][rr];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
+      float sum = 0.f, all[4] = {};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
+        const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
+        sum += f * s_sum[w][rr];
+        all[0] += f * v.x; all[1] += f * v.y; all[2] += f * v.z; all[3] += f * v.w;
+      }
+      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, 0.f, sum, all);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------- launcher
+size_t kv4_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
+                       int max_length) {
+  const Kv8Plan p = kv4_plan(hd, 1, n_q, n_kv, n_seqs, max_rows, max_length);
+  return p.nsplit == 1 ? 0 : kv8_part_floats((size_t)n_rows * n_q * p.nsplit, hd);
+}
+
+template <int HD>
+static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
+  // one term of the query and two of the weights where queries and output are bf16, else three
+  const bool single = a.q.bf16 && a.out.p && a.out.bf16;
+  const Kv8Plan p = kv4_plan(HD, single ? 1 : 3, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
+  const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
+  if (gx > 0x7fffffff || r.n_seqs > 65535 || (p.nsplit > 1 && !a.work)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)gx, r.n_seqs);
+  const int edge = p.nsplit == 1 ? last : last & kFirst;
+#define WICI_ATTN(...) \
+  launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
+  if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2>);
+  else WICI_ATTN(k_kv4_attn_split<HD, 3, 3>);
+#undef WICI_ATTN
+  if (p.nsplit > 1) return launch_kv_attn_merge(HD, c, r, a, p.nsplit, st, last & kLast);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_attn(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st,
+                           int edge) {
+  if (a.hd == 128) return attn4<128>(c, r, a, st, edge);
+  if (a.hd == 64) return attn4<64>(c, r, a, st, edge);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace wici

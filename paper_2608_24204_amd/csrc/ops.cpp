@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "../../include/wici.h"
+#include "kv4.h"
 #include "kv8.h"
 #include "rope.h"
 
@@ -117,6 +118,90 @@ int most_length(const wici_kv8* c, const wici_kv8_batch* b) {
 
 wici_status status(hipError_t e) { return e == hipSuccess ? WICI_OK : WICI_E_HIP; }
 
+// The calls over a cache of 8 or 4 bits a value.
+size_t block_bytes(int bits, const wici_kv8* c) {
+  return bits == 8 ? wici::kv8_block_bytes(c->page, c->head_dim)
+                   : wici::kv4_block_bytes(c->page, c->head_dim);
+}
+wici_status cache_bytes(int bits, const wici_kv8* cache, size_t* bytes) {
+  if (!geometry_ok(cache) || !bytes) return WICI_E_ARG;
+  *bytes = (size_t)cache->n_pages * 2 * cache->n_kv_heads * block_bytes(bits, cache);
+  return WICI_OK;
+}
+
+wici_status append(int bits, const wici_kv8* cache, const wici_kv8_batch* batch,
+                   const wici_rope_tab* rope, int32_t n_heads, const wici_head_rows& q,
+                   const wici_head_rows& q_out, const wici_head_rows& k, const wici_head_rows& v,
+                   void* hip_stream) {
+  if (!call_ok(cache, batch) || (rope && !tab_ok(rope, cache->head_dim))) return WICI_E_ARG;
+  const int hd = cache->head_dim;
+  if (q.data && (!rope || n_heads < 1 || n_heads > 1024)) return WICI_E_ARG;
+  if (!units_ok(batch->n_rows, (q.data ? n_heads : 0) + 2 * cache->n_kv_heads)) return WICI_E_ARG;
+  if (empty(batch)) return WICI_OK;
+  if (!rows_ok(k, cache->n_kv_heads, hd) || !rows_ok(v, cache->n_kv_heads, hd) ||
+      (q.data && (!rows_ok(q, n_heads, hd) || !rows_ok(q_out, n_heads, hd))))
+    return WICI_E_ARG;
+  OnDeviceOf dev(hip_stream);
+  if (!dev.ok()) return WICI_E_HIP;
+  const auto launch = bits == 8 ? wici::launch_kv8_append : wici::launch_kv4_append;
+  return status(launch(hd, cache_of(cache), batch_of(batch), tab_of(rope), n_heads, rows_of(q),
+                       rows_of(q_out), 1.0f, rows_of(k), rows_of(v),
+                       static_cast<hipStream_t>(hip_stream), 3));
+}
+
+wici_status read(int bits, const wici_kv8* cache, const wici_kv8_batch* batch,
+                 const wici_head_rows& k, const wici_head_rows& v, void* hip_stream) {
+  if (!call_ok(cache, batch) || !units_ok(batch->n_rows, 2 * cache->n_kv_heads)) return WICI_E_ARG;
+  if (empty(batch)) return WICI_OK;
+  if ((!k.data && !v.data) || (k.data && !rows_ok(k, cache->n_kv_heads, cache->head_dim)) ||
+      (v.data && !rows_ok(v, cache->n_kv_heads, cache->head_dim)))
+    return WICI_E_ARG;
+  OnDeviceOf dev(hip_stream);
+  if (!dev.ok()) return WICI_E_HIP;
+  const auto launch = bits == 8 ? wici::launch_kv8_read : wici::launch_kv4_read;
+  return status(launch(cache->head_dim, cache_of(cache), batch_of(batch), rows_of(k), rows_of(v),
+                       static_cast<hipStream_t>(hip_stream)));
+}
+
+wici_status attend_workspace(int bits, const wici_kv8* cache, const wici_kv8_batch* batch,
+                             int32_t n_heads, size_t* bytes) {
+  if (!bytes || !geometry_ok(cache) || !batch_shape_ok(cache, batch) || n_heads < 1 ||
+      n_heads > 1024 || n_heads % cache->n_kv_heads ||
+      (int64_t)batch->n_rows * n_heads > kMostAttended)
+    return WICI_E_ARG;
+  const auto floats = bits == 8 ? wici::kv8_attn_floats : wici::kv4_attn_floats;
+  *bytes = empty(batch) ? 0
+                        : 4 * floats(cache->head_dim, n_heads, cache->n_kv_heads, batch->n_seqs,
+                                     batch->n_rows, most_rows(batch), most_length(cache, batch));
+  return WICI_OK;
+}
+
+wici_status attend(int bits, const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,
+                   float scale, const wici_head_rows& q, const wici_head_rows& out,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+  size_t need = 0;
+  if (!call_ok(cache, batch) || !std::isfinite(scale) ||
+      attend_workspace(bits, cache, batch, n_heads, &need) != WICI_OK)
+    return WICI_E_ARG;
+  if (empty(batch)) return WICI_OK;
+  if (!rows_ok(q, n_heads, cache->head_dim) || !rows_ok(out, n_heads, cache->head_dim) ||
+      (need && (!aligned(workspace) || workspace_bytes < need)))
+    return WICI_E_ARG;
+  OnDeviceOf dev(hip_stream);
+  if (!dev.ok()) return WICI_E_HIP;
+  wici::Kv8Attn a{};
+  a.hd = cache->head_dim;
+  a.n_q = n_heads;
+  a.scale = scale;
+  a.q = rows_of(q);
+  a.out = rows_of(out);
+  a.max_rows = most_rows(batch);
+  a.max_length = most_length(cache, batch);
+  a.work = static_cast<float*>(workspace);
+  const auto launch = bits == 8 ? wici::launch_kv8_attn : wici::launch_kv4_attn;
+  return status(launch(cache_of(cache), batch_of(batch), a, static_cast<hipStream_t>(hip_stream), 3));
+}
+
 }  // namespace
 
 extern "C" {
@@ -148,81 +233,57 @@ wici_status wici_rope_rows(const wici_rope_tab* rope, int32_t head_dim, int32_t 
 }
 
 wici_status wici_kv8_bytes(const wici_kv8* cache, size_t* bytes) {
-  if (!geometry_ok(cache) || !bytes) return WICI_E_ARG;
-  *bytes = (size_t)cache->n_pages * 2 * cache->n_kv_heads *
-           wici::kv8_block_bytes(cache->page, cache->head_dim);
-  return WICI_OK;
+  return cache_bytes(8, cache, bytes);
 }
 
 wici_status wici_kv8_append(const wici_kv8* cache, const wici_kv8_batch* batch,
                             const wici_rope_tab* rope, int32_t n_heads, wici_head_rows q,
                             wici_head_rows q_out, wici_head_rows k, wici_head_rows v,
                             void* hip_stream) {
-  if (!call_ok(cache, batch) || (rope && !tab_ok(rope, cache->head_dim))) return WICI_E_ARG;
-  const int hd = cache->head_dim;
-  if (q.data && (!rope || n_heads < 1 || n_heads > 1024)) return WICI_E_ARG;
-  if (!units_ok(batch->n_rows, (q.data ? n_heads : 0) + 2 * cache->n_kv_heads)) return WICI_E_ARG;
-  if (empty(batch)) return WICI_OK;
-  if (!rows_ok(k, cache->n_kv_heads, hd) || !rows_ok(v, cache->n_kv_heads, hd) ||
-      (q.data && (!rows_ok(q, n_heads, hd) || !rows_ok(q_out, n_heads, hd))))
-    return WICI_E_ARG;
-  OnDeviceOf dev(hip_stream);
-  if (!dev.ok()) return WICI_E_HIP;
-  return status(wici::launch_kv8_append(hd, cache_of(cache), batch_of(batch), tab_of(rope), n_heads,
-                                        rows_of(q), rows_of(q_out), 1.0f, rows_of(k), rows_of(v),
-                                        static_cast<hipStream_t>(hip_stream)));
+  return append(8, cache, batch, rope, n_heads, q, q_out, k, v, hip_stream);
 }
 
 wici_status wici_kv8_read(const wici_kv8* cache, const wici_kv8_batch* batch, wici_head_rows k,
                           wici_head_rows v, void* hip_stream) {
-  if (!call_ok(cache, batch) || !units_ok(batch->n_rows, 2 * cache->n_kv_heads)) return WICI_E_ARG;
-  if (empty(batch)) return WICI_OK;
-  if ((!k.data && !v.data) || (k.data && !rows_ok(k, cache->n_kv_heads, cache->head_dim)) ||
-      (v.data && !rows_ok(v, cache->n_kv_heads, cache->head_dim)))
-    return WICI_E_ARG;
-  OnDeviceOf dev(hip_stream);
-  if (!dev.ok()) return WICI_E_HIP;
-  return status(wici::launch_kv8_read(cache->head_dim, cache_of(cache), batch_of(batch), rows_of(k),
-                                      rows_of(v), static_cast<hipStream_t>(hip_stream)));
+  return read(8, cache, batch, k, v, hip_stream);
 }
 
 wici_status wici_kv8_attend_workspace(const wici_kv8* cache, const wici_kv8_batch* batch,
                                       int32_t n_heads, size_t* bytes) {
-  if (!bytes || !geometry_ok(cache) || !batch_shape_ok(cache, batch) || n_heads < 1 ||
-      n_heads > 1024 || n_heads % cache->n_kv_heads ||
-      (int64_t)batch->n_rows * n_heads > kMostAttended)
-    return WICI_E_ARG;
-  *bytes = empty(batch) ? 0
-                        : 4 * wici::kv8_attn_floats(cache->head_dim, n_heads, cache->n_kv_heads,
-                                                    batch->n_seqs, batch->n_rows, most_rows(batch),
-                                                    most_length(cache, batch));
-  return WICI_OK;
+  return attend_workspace(8, cache, batch, n_heads, bytes);
 }
 
 wici_status wici_kv8_attend(const wici_kv8* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream) {
-  size_t need = 0;
-  if (!call_ok(cache, batch) || !std::isfinite(scale) ||
-      wici_kv8_attend_workspace(cache, batch, n_heads, &need) != WICI_OK)
-    return WICI_E_ARG;
-  if (empty(batch)) return WICI_OK;
-  if (!rows_ok(q, n_heads, cache->head_dim) || !rows_ok(out, n_heads, cache->head_dim) ||
-      (need && (!aligned(workspace) || workspace_bytes < need)))
-    return WICI_E_ARG;
-  OnDeviceOf dev(hip_stream);
-  if (!dev.ok()) return WICI_E_HIP;
-  wici::Kv8Attn a{};
-  a.hd = cache->head_dim;
-  a.n_q = n_heads;
-  a.scale = scale;
-  a.q = rows_of(q);
-  a.out = rows_of(out);
-  a.max_rows = most_rows(batch);
-  a.max_length = most_length(cache, batch);
-  a.work = static_cast<float*>(workspace);
-  return status(wici::launch_kv8_attn(cache_of(cache), batch_of(batch), a,
-                                      static_cast<hipStream_t>(hip_stream)));
+  return attend(8, cache, batch, n_heads, scale, q, out, workspace, workspace_bytes, hip_stream);
+}
+
+wici_status wici_kv4_bytes(const wici_kv4* cache, size_t* bytes) {
+  return cache_bytes(4, cache, bytes);
+}
+
+wici_status wici_kv4_append(const wici_kv4* cache, const wici_kv8_batch* batch,
+                            const wici_rope_tab* rope, int32_t n_heads, wici_head_rows q,
+                            wici_head_rows q_out, wici_head_rows k, wici_head_rows v,
+                            void* hip_stream) {
+  return append(4, cache, batch, rope, n_heads, q, q_out, k, v, hip_stream);
+}
+
+wici_status wici_kv4_read(const wici_kv4* cache, const wici_kv8_batch* batch, wici_head_rows k,
+                          wici_head_rows v, void* hip_stream) {
+  return read(4, cache, batch, k, v, hip_stream);
+}
+
+wici_status wici_kv4_attend_workspace(const wici_kv4* cache, const wici_kv8_batch* batch,
+                                      int32_t n_heads, size_t* bytes) {
+  return attend_workspace(4, cache, batch, n_heads, bytes);
+}
+
+wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, int32_t n_heads,
+                            float scale, wici_head_rows q, wici_head_rows out, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  return attend(4, cache, batch, n_heads, scale, q, out, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

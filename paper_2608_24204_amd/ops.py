@@ -1,5 +1,5 @@
-"""Operators on torch tensors: rotary positions, the 8-bit paged KV cache and causal
-attention over it (the model-free calls of include/wici.h).
+"""Operators on torch tensors: rotary positions, paged KV caches of 8 and 4 bits and causal
+attention over them (the model-free calls of include/wici.h).
 
 Argument marshalling only: every operator is a HIP kernel of libwici.so.  Tensors are on
 one HIP GPU; a call enqueues on ``stream`` (default: the current stream of the tensors' GPU)
@@ -9,7 +9,7 @@ that stream.  Every call may be captured into a HIP graph.  The operators have n
 tensor that requires one is refused where gradients are recorded.
 
     table = ops.rope_table(n_pos, dim, base=500000.0, scaling="bands", factor=8, original=8192)
-    cache = ops.KvCache.empty(n_pages, n_kv_heads, head_dim, page_table)
+    cache = ops.KvCache.empty(n_pages, n_kv_heads, head_dim, page_table, bits=8)
     q = cache.append(k, v, length, rope=table, q=q)      # one token of every sequence
     out = cache.attend(q, length)
 """
@@ -227,43 +227,57 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     return out
 
 
+def _row_bytes(bits: int, head_dim: int) -> int:
+    """Bytes of a cached row: its codes and its scales."""
+    if bits not in (8, 4):
+        raise ValueError(f"bits {bits} (8 or 4)")
+    return head_dim + 4 if bits == 8 else head_dim // 2 + head_dim // 32
+
+
 class KvCache:
-    """An 8-bit paged KV cache (wici_kv8): ``pool`` uint8 [n_pages, 2, n_kv_heads,
-    page * (head_dim + 4)] and ``table`` int32 [n_seqs, max_pages] naming each sequence's
-    pages in order.  Both stay the caller's: pages are handed out by writing the table.
+    """A paged KV cache of 8 bits a value and a scale a row (wici_kv8), or of 4 bits and a scale
+    for each 32 dimensions (``bits=4``, wici_kv4): ``pool`` uint8 [n_pages, 2, n_kv_heads,
+    page * row] with rows of head_dim + 4 or head_dim / 2 + head_dim / 32 bytes, and ``table``
+    int32 [n_seqs, max_pages] naming each sequence's pages in order.  Both stay the caller's:
+    pages are handed out by writing the table.
 
     ``length`` [n_seqs] (int32) counts each sequence's positions, the call's new rows
     included; without ``row_start`` [n_seqs + 1] (int32) a sequence has one new row, else rows
     row_start[b] .. row_start[b + 1].  Rows of no sequence are not used, and not written in
     outputs (a new output tensor holds nothing in particular there)."""
 
-    def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, page: int, head_dim: int):
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, *, page: int, head_dim: int,
+                 bits: int = 8):
         device = _on_gpu(pool, "pool")
+        block = page * _row_bytes(bits, head_dim)
         if pool.dtype != torch.uint8 or pool.dim() != 4 or not pool.is_contiguous() or \
-                pool.shape[1] != 2 or pool.shape[3] != page * (head_dim + 4):
+                pool.shape[1] != 2 or pool.shape[3] != block:
             raise ValueError(f"pool: {pool.dtype} {tuple(pool.shape)}, expected contiguous uint8 "
-                             f"[n_pages, 2, n_kv_heads, {page * (head_dim + 4)}]")
+                             f"[n_pages, 2, n_kv_heads, {block}]")
         if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1 or \
                 table.shape[1] < 1 or table.device != device:
             raise ValueError(f"table: {table.dtype} {tuple(table.shape)}, expected int32 "
                              "[n_seqs, max_pages] on the pool's GPU")
         self.pool, self.table, self.page, self.head_dim = pool, table, page, head_dim
-        self.n_kv_heads, self.device = pool.shape[2], device
+        self.n_kv_heads, self.device, self.bits = pool.shape[2], device, bits
         self.lib = binding.load_library()
+        size_of, self._append, self._read, self._attend, self._attend_workspace = (
+            getattr(self.lib, f"wici_kv{bits}_{call}")
+            for call in ("bytes", "append", "read", "attend", "attend_workspace"))
         stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
         self._c = binding.WiciKv8(pool.data_ptr(), pool.shape[0], page, self.n_kv_heads, head_dim,
                                   table.data_ptr(), stride, table.shape[1])
         size = ctypes.c_size_t()
-        _check(self.lib.wici_kv8_bytes(ctypes.byref(self._c), ctypes.byref(size)),
+        _check(size_of(ctypes.byref(self._c), ctypes.byref(size)),
                f"KvCache: page {page}, head_dim {head_dim}, {self.n_kv_heads} KV heads")
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, table: torch.Tensor,
-              page: int = 64) -> "KvCache":
+              page: int = 64, bits: int = 8) -> "KvCache":
         """A cache with a new pool on the table's GPU."""
-        pool = torch.empty(n_pages, 2, n_kv_heads, page * (head_dim + 4), dtype=torch.uint8,
-                           device=_on_gpu(table, "table"))
-        return cls(pool, table, page=page, head_dim=head_dim)
+        pool = torch.empty(n_pages, 2, n_kv_heads, page * _row_bytes(bits, head_dim),
+                           dtype=torch.uint8, device=_on_gpu(table, "table"))
+        return cls(pool, table, page=page, head_dim=head_dim, bits=bits)
 
     def _on(self, stream, *tensors):
         return _launch_on(stream, self.device, self.pool, self.table, *tensors)
@@ -284,7 +298,7 @@ class KvCache:
         """Quantise the rows k and v [rows, n_kv_heads, head_dim] into the cache.  With ``rope``
         the keys are rotated at their positions first, and ``q`` [rows, heads, head_dim] into
         ``q_out`` (default: a new tensor like q; q itself is allowed), which is returned
-        (None without q).  wici_kv8_append."""
+        (None without q).  wici_kv8_append, wici_kv4_append."""
         n, d, dev = k.shape[0], self.head_dim, self.device
         if v.shape[0] != n or (q is not None and q.shape[0] != n):
             raise ValueError("k, v and q have different numbers of rows")
@@ -308,7 +322,7 @@ class KvCache:
                 else:
                     qo = _rows(q_out, heads, d, "q_out", dev)
             kr, vr = _rows(k, self.n_kv_heads, d, "k", dev), _rows(v, self.n_kv_heads, d, "v", dev)
-            _check(self.lib.wici_kv8_append(
+            _check(self._append(
                 self._c, self._batch(n, length, row_start), None if rope is None else rope._c, heads,
                 qr, qo, kr, vr, raw),
                 "append (strides multiples of 8, 16-byte aligned rows, rope.dim <= head_dim)")
@@ -320,7 +334,7 @@ class KvCache:
              k: torch.Tensor | None = None, v: torch.Tensor | None = None, stream=None):
         """The values the cache holds for the rows: (k, v), each [rows, n_kv_heads, head_dim].  New
         tensors of ``dtype`` with ``n_rows`` rows (default: one a sequence) unless given.
-        wici_kv8_read."""
+        wici_kv8_read, wici_kv4_read."""
         dev, d = self.device, self.head_dim
         if n_rows is None:
             n_rows = k.shape[0] if k is not None else v.shape[0] if v is not None else \
@@ -338,7 +352,7 @@ class KvCache:
                 else:
                     rows += [x, _rows(x, self.n_kv_heads, d, name, dev)]
             k, kr, v, vr = rows
-            _check(self.lib.wici_kv8_read(self._c, self._batch(n_rows, length, row_start), kr, vr,
+            _check(self._read(self._c, self._batch(n_rows, length, row_start), kr, vr,
                                           raw),
                    "read (strides multiples of 8, 16-byte aligned rows)")
             if given:
@@ -354,7 +368,7 @@ class KvCache:
         defaults to head_dim^-1/2.  ``max_rows`` and ``max_length`` (the most new rows and
         positions of a sequence, 0: unknown) only shape the launch.  ``out`` (default: a new
         tensor like q) and ``workspace`` (uint8, attend_workspace bytes; default: a new one) may
-        be given.  wici_kv8_attend."""
+        be given.  wici_kv8_attend, wici_kv4_attend."""
         dev, d = self.device, self.head_dim
         if q.dim() != 3:
             raise ValueError(f"q: shape {tuple(q.shape)}, expected [rows, heads, {d}]")
@@ -376,7 +390,7 @@ class KvCache:
             elif workspace.device != dev or not workspace.is_contiguous():
                 raise ValueError(f"workspace: contiguous on {dev} expected")
             size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-            st = self.lib.wici_kv8_attend(
+            st = self._attend(
                 self._c, b, heads, d ** -0.5 if scale is None else scale, qr, outr,
                 None if workspace is None else workspace.data_ptr(), size, raw)
             if st:
@@ -388,7 +402,7 @@ class KvCache:
 
     def _workspace(self, batch, heads: int) -> int:
         size = ctypes.c_size_t()
-        st = self.lib.wici_kv8_attend_workspace(self._c, batch, heads, size)
+        st = self._attend_workspace(self._c, batch, heads, size)
         if st:
             _check(st, f"attend: {heads} query heads on {self.n_kv_heads}")
         return size.value
