@@ -406,8 +406,9 @@ wici_status wici_stream_read_noalloc(const void* d_buf, size_t bytes, int32_t gr
 
 /* ---- Operators on caller-owned device tensors (no model) -------------------------
  *
- * Rotary positions, paged KV caches of 8 and of 4 bits and causal attention over them, for
- * callers that run their own layers.  Conventions of these calls:
+ * Rotary positions, paged KV caches of 8 and of 4 bits, causal attention over them, and the
+ * step of a beam search (its selection, and the caches in its order), for callers that run their
+ * own layers.  Conventions of these calls:
  *  - every pointer marked device is device memory of the stream's GPU; tensors stay with
  *    the caller, and the calls allocate nothing;
  *  - a call enqueues on hip_stream (NULL: the null stream of the current device) and
@@ -570,6 +571,45 @@ wici_status wici_kv4_attend_workspace(const wici_kv4* cache, const wici_kv8_batc
 wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream);
+
+/* One step of n beam searches of `beams` beams each (1 .. 64; n beams at most 65535).  Row
+ * b beams + i of the logits (device, WICI_F32 or WICI_BF16, rows row_stride elements apart, of any
+ * alignment of their type; vocab at most 2^24) belongs to beam i of search b, which has the score
+ * scores[b beams + i] so far (device).  The continuation of beam i by word v has the score
+ *   scores[b beams + i] + z_v - log sum_u e^(z_u)        (z the row's logits)
+ * formed in 64 bits, and the k (1 .. 64) greatest of each search's beams x vocab are returned in
+ * falling order, [n][k] each (device): the scores rounded to fp32, the beam that each continues
+ * (0 .. beams - 1) and the word.  Equal scores of one beam: the lowest word first (within a beam the
+ * order is the logits'); of several: the lowest beam first.  A logit of minus infinity is a word that
+ * is not chosen, a score of minus infinity a beam that is not alive, whose row may hold anything.
+ * Where fewer than k are left the rest are -1, -1 and minus infinity.  A NaN or a positive infinity,
+ * in the score of a beam or the logits of one that is alive, makes all k of the search -1, -1 and
+ * NaN.  out_scores may be scores where k is beams.  workspace: device, 16-byte aligned, undefined
+ * before and after. */
+wici_status wici_beam_workspace(int32_t n, int32_t beams, int32_t vocab, int32_t dtype, int32_t k,
+                                size_t* bytes);
+wici_status wici_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t n,
+                             int32_t beams, int32_t vocab, const float* scores, int32_t k,
+                             float* out_scores, int32_t* out_parent, int32_t* out_token,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The page tables of n searches' beams put in the order of a selection: beam i of search b (sequence
+ * b beams + i of `table`, device [n beams][table_stride], which is written) goes on from the
+ * positions of beam parent[b beams + i] (device).  All beams of a search have one length, read at its
+ * first (length, device [n beams]).  Of its pages, those that are full are shared: the beam's
+ * entries become its parent's.  The partial page after them, if there is one, is copied whole into
+ * the page named by spare[b beams + i] (device), in each of the n_pools pools (host array of device
+ * pointers: the layers' caches, all of `bits` (8 or 4) and the geometry of `cache`, whose own pool
+ * and table are not used); that page takes the partial one's place in the beam's table, and the
+ * beam's own former partial page becomes its spare.  So n beams spares, pages that no table names,
+ * serve all steps until the partial pages are full.  A beam that is its own parent keeps its pages,
+ * and so does one whose parent is not among 0 .. beams - 1.  A parent's entry that names no page is
+ * taken over as it is, with nothing copied or exchanged; a spare that names none takes its place in
+ * the table, with nothing copied. */
+wici_status wici_beam_reorder(const wici_kv8* cache, int32_t bits, void* const* pools,
+                              int32_t n_pools, int32_t n, int32_t beams, const int32_t* parent,
+                              const int32_t* length, int32_t* table, int32_t* spare,
+                              void* hip_stream);
 
 /* Message of the last failed call on this model ("" if none).  Valid until the
  * next call on the model. */

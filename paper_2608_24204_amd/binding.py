@@ -34,7 +34,8 @@ EXPORTED = ["wici_create", "wici_memory_requirements", "wici_bind_memory", "wici
             "wici_stream_read", "wici_stream_read_noalloc", "wici_last_error", "wici_destroy",
             "wici_set_rope", "wici_rope_table", "wici_rope_rows", "wici_kv8_bytes", "wici_kv8_append",
             "wici_kv8_read", "wici_kv8_attend_workspace", "wici_kv8_attend", "wici_kv4_bytes",
-            "wici_kv4_append", "wici_kv4_read", "wici_kv4_attend_workspace", "wici_kv4_attend"]
+            "wici_kv4_append", "wici_kv4_read", "wici_kv4_attend_workspace", "wici_kv4_attend",
+            "wici_beam_workspace", "wici_beam_select", "wici_beam_reorder"]
 
 
 class WiciConfig(ctypes.Structure):
@@ -133,6 +134,11 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
         "wici_rope_table": ([ctypes.POINTER(WiciRope), ctypes.c_int64, P, P, P], ctypes.c_int),
         "wici_rope_rows": ([ctypes.POINTER(WiciRopeTab), i32, i32, i32, P, WiciHeadRows,
                             WiciHeadRows, P], ctypes.c_int),
+        "wici_beam_workspace": ([i32, i32, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "wici_beam_select": ([P, i32, ctypes.c_int64, i32, i32, i32, P, i32, P, P, P, P, sz, P],
+                             ctypes.c_int),
+        "wici_beam_reorder": ([ctypes.POINTER(WiciKv8), i32, P, i32, i32, i32, P, P, P, P, P],
+                              ctypes.c_int),
         "wici_last_error": ([P], ctypes.c_char_p),
         "wici_destroy": ([P], None),
     }

@@ -21,7 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["gemv.hip", "misc.hip", "attention.hip", "gemm.hip", "batch.hip", "kv8.hip", "kv8_attn.hip",
-           "kv4.hip", "kv4_attn.hip",
+           "kv4.hip", "kv4_attn.hip", "beam.hip",
            "model.cpp", "ops.cpp", "quant.cpp", "cache.cpp", "noalloc.cpp"]
 
 FLAGS = [

@@ -6,6 +6,8 @@
 #include <cmath>
 
 #include "../../include/wici.h"
+#include "beam.h"
+#include "beam_plan.h"
 #include "kv4.h"
 #include "kv8.h"
 #include "rope.h"
@@ -117,6 +119,11 @@ int most_length(const wici_kv8* c, const wici_kv8_batch* b) {
 }
 
 wici_status status(hipError_t e) { return e == hipSuccess ? WICI_OK : WICI_E_HIP; }
+
+bool words(const void* p) { return p && (uintptr_t)p % 4 == 0; }
+bool beam_ok(int32_t n, int32_t beams) {
+  return n >= 0 && beams >= 1 && beams <= wici::kMostBeams && (int64_t)n * beams <= wici::kMostRows;
+}
 
 // The calls over a cache of 8 or 4 bits a value.
 size_t block_bytes(int bits, const wici_kv8* c) {
@@ -284,6 +291,60 @@ wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, 
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream) {
   return attend(4, cache, batch, n_heads, scale, q, out, workspace, workspace_bytes, hip_stream);
+}
+
+wici_status wici_beam_workspace(int32_t n, int32_t beams, int32_t vocab, int32_t dtype, int32_t k,
+                                size_t* bytes) {
+  if (!bytes || !beam_ok(n, beams) || vocab < 1 || vocab > wici::kMostVocab || k < 1 ||
+      k > wici::kMostChosen || (dtype != WICI_F32 && dtype != WICI_BF16))
+    return WICI_E_ARG;
+  *bytes = n == 0 ? 0
+                  : wici::beam_space(wici::beam_plan(vocab, dtype == WICI_BF16), (int64_t)n * beams, k)
+                        .bytes;
+  return WICI_OK;
+}
+
+wici_status wici_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t n,
+                             int32_t beams, int32_t vocab, const float* scores, int32_t k,
+                             float* out_scores, int32_t* out_parent, int32_t* out_token,
+                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+  size_t need = 0;
+  if (wici_beam_workspace(n, beams, vocab, dtype, k, &need) != WICI_OK) return WICI_E_ARG;
+  if (n == 0) return WICI_OK;
+  const uintptr_t size = dtype == WICI_BF16 ? 2 : 4;
+  if (!logits || (uintptr_t)logits % size || !words(scores) || !words(out_scores) ||
+      !words(out_parent) || !words(out_token) || row_stride > (int64_t)1 << 40 ||
+      ((int64_t)n * beams > 1 && row_stride < vocab) || !aligned(workspace) || workspace_bytes < need)
+    return WICI_E_ARG;
+  OnDeviceOf dev(hip_stream);
+  if (!dev.ok()) return WICI_E_HIP;
+  return status(wici::launch_beam_select(
+      wici::BeamSelect{logits, dtype == WICI_BF16, row_stride, n, beams, vocab, k, scores, out_scores,
+                       out_parent, out_token, static_cast<char*>(workspace)},
+      static_cast<hipStream_t>(hip_stream)));
+}
+
+wici_status wici_beam_reorder(const wici_kv8* cache, int32_t bits, void* const* pools,
+                              int32_t n_pools, int32_t n, int32_t beams, const int32_t* parent,
+                              const int32_t* length, int32_t* table, int32_t* spare,
+                              void* hip_stream) {
+  if ((bits != 8 && bits != 4) || !geometry_ok(cache) || !beam_ok(n, beams) || cache->max_pages < 1 ||
+      cache->max_pages > (1 << 24) || n_pools < 0 || n_pools > 65535 || (n_pools && !pools))
+    return WICI_E_ARG;
+  const int64_t seqs = (int64_t)n * beams;
+  if ((seqs > 1 && cache->table_stride < cache->max_pages) || cache->table_stride < 0)
+    return WICI_E_ARG;
+  for (int i = 0; i < n_pools; ++i)
+    if (!aligned(pools[i])) return WICI_E_ARG;
+  if (n == 0) return WICI_OK;
+  if (!words(parent) || !words(length) || !words(table) || !words(spare)) return WICI_E_ARG;
+  OnDeviceOf dev(hip_stream);
+  if (!dev.ok()) return WICI_E_HIP;
+  wici::Kv8 c = cache_of(cache);
+  c.table = table;
+  return status(wici::launch_beam_reorder(
+      c, 2 * cache->n_kv_heads * block_bytes(bits, cache), pools, n_pools, n, beams, parent, length,
+      table, spare, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

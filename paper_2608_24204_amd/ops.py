@@ -1,5 +1,6 @@
-"""Operators on torch tensors: rotary positions, paged KV caches of 8 and 4 bits and causal
-attention over them (the model-free calls of include/wici.h).
+"""Operators on torch tensors: rotary positions, paged KV caches of 8 and 4 bits, causal
+attention over them, and a beam search's selection and reordering of such caches (the model-free
+calls of include/wici.h).
 
 Argument marshalling only: every operator is a HIP kernel of libwici.so.  Tensors are on
 one HIP GPU; a call enqueues on ``stream`` (default: the current stream of the tensors' GPU)
@@ -12,6 +13,8 @@ tensor that requires one is refused where gradients are recorded.
     cache = ops.KvCache.empty(n_pages, n_kv_heads, head_dim, page_table, bits=8)
     q = cache.append(k, v, length, rope=table, q=q)      # one token of every sequence
     out = cache.attend(q, length)
+    scores, parent, token = ops.beam_select(logits, scores)
+    ops.beam_reorder(caches, parent, length, spare)      # caches: the layers'
 """
 
 from __future__ import annotations
@@ -412,3 +415,85 @@ class KvCache:
         """Bytes of workspace attend needs for such a call (0: none)."""
         return self._workspace(binding.WiciKv8Batch(n_seqs, n_rows, 1 if row_start else None, None,
                                                     max_rows, max_length), heads)
+
+
+def beam_workspace(n: int, beams: int, vocab: int, dtype: torch.dtype, k: int) -> int:
+    """Bytes of workspace beam_select needs for such a call."""
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype {dtype} (float32 or bfloat16)")
+    size = ctypes.c_size_t()
+    _check(binding.load_library().wici_beam_workspace(n, beams, vocab, _DTYPES[dtype], k, size),
+           f"beam_select: {n} searches of {beams} beams, {vocab} words, {k} chosen")
+    return size.value
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int | None = None, *,
+                workspace: torch.Tensor | None = None, stream=None):
+    """The ``k`` (default: as many as beams) best continuations of each of n beam searches:
+    (scores float32, parent int32, token int32), each [n, k], best first.  ``logits``
+    [n * beams, vocab] (rows of any stride), ``scores`` [n, beams] float32: each beam's so far
+    (minus infinity: not alive).  A continuation adds its word's log-probability; the order is that
+    of 64-bit sums, ties the lowest beam's and word's.  Where fewer than k are left the parents and
+    tokens are -1.  ``workspace`` (uint8, beam_workspace bytes; default: a new one) may be given.
+    wici_beam_select."""
+    device = _on_gpu(logits, "logits")
+    if scores.dim() != 2 or scores.dtype != torch.float32 or not scores.is_contiguous() or \
+            scores.device != device:
+        raise ValueError(f"scores: {scores.dtype} {tuple(scores.shape)} on {scores.device}, expected "
+                         f"contiguous float32 [n, beams] on {device}")
+    n, beams = scores.shape
+    if logits.dim() != 2 or logits.shape[0] != n * beams or logits.shape[1] < 1:
+        raise ValueError(f"logits: shape {tuple(logits.shape)}, expected [{n * beams}, vocab]")
+    vocab = logits.shape[1]
+    if vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the words of a row must lie side by side")
+    if logits.requires_grad or scores.requires_grad:
+        _no_gradient("logits" if logits.requires_grad else "scores")
+    k = beams if k is None else k
+    need = beam_workspace(n, beams, vocab, logits.dtype, k)
+    with _launch_on(stream, device, logits, scores, workspace) as raw:
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: contiguous on {device} expected")
+        out = torch.empty(n, k, dtype=torch.float32, device=device)
+        parent, token = (torch.empty(n, k, dtype=torch.int32, device=device) for _ in range(2))
+        st = binding.load_library().wici_beam_select(
+            logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0), n, beams, vocab,
+            scores.data_ptr(), k, out.data_ptr(), parent.data_ptr(), token.data_ptr(),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), raw)
+        if st:
+            _check(st, f"beam_select: {need} workspace bytes (rows of stride {logits.stride(0)})")
+    return out, parent, token
+
+
+def beam_reorder(caches, parent: torch.Tensor, length: torch.Tensor, spare: torch.Tensor, *,
+                 stream=None) -> None:
+    """The caches (a KvCache or a list of them: layers of one table and geometry) in the order of a
+    selection: beam i of search b goes on from beam ``parent`` [n, beams] (int32) [b, i].  Sequence
+    b * beams + i of the table is that beam's, and ``length`` [n * beams] (int32) counts its
+    positions (one length a search).  Full pages are shared through the table; a partial last one is
+    copied into the beam's page of ``spare`` [n * beams] (int32), and the beam's own becomes its
+    spare: table and spare are written.  wici_beam_reorder."""
+    caches = [caches] if isinstance(caches, KvCache) else list(caches)
+    if not caches:
+        raise ValueError("caches: none")
+    c = caches[0]
+    for x in caches[1:]:
+        if (x.table.data_ptr(), x.table.shape, x.table.stride(), x.pool.shape, x.page, x.bits,
+                x.device) != (c.table.data_ptr(), c.table.shape, c.table.stride(), c.pool.shape,
+                              c.page, c.bits, c.device):
+            raise ValueError("caches: of one table and geometry expected")
+    if parent.dim() != 2:
+        raise ValueError(f"parent: shape {tuple(parent.shape)}, expected [n, beams]")
+    n, beams = parent.shape
+    if n * beams > c.table.shape[0]:
+        raise ValueError(f"parent: {n * beams} sequences, the table has {c.table.shape[0]}")
+    p = _ints(parent, (n, beams), "parent", c.device)
+    at, sp = (_ints(x, (n * beams,), name, c.device) for x, name in ((length, "length"), (spare, "spare")))
+    pools = (ctypes.c_void_p * len(caches))(*(x.pool.data_ptr() for x in caches))
+    with _launch_on(stream, c.device, c.table, parent, length, spare, *(x.pool for x in caches)) as raw:
+        _check(c.lib.wici_beam_reorder(c._c, c.bits, pools, len(caches), n, beams, p, at,
+                                       c.table.data_ptr(), sp, raw),
+               f"beam_reorder: {n} searches of {beams} beams")
+        _written([c.table, spare, *(x.pool for x in caches)])
