@@ -396,6 +396,230 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
   }
 }
 
+// ------------------------------------------------------------------- prompts: row tiles
+// Workgroup (KV head, tile of 64 or 128 rows x query heads, split, sequence): each of four
+// wavefronts holds a quarter of the rows and takes every chunk of 64 positions of the split.  The
+// codes of a chunk become bf16 operands once for all four, in LDS, lane by lane as the products
+// read them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers:
+// the next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
+// parts a buffer's readers from its next writers.
+template <int HD, int NQ, int NW, int kRowTiles>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+                                                            int ntile) {
+  constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles, VW = HD / 64;
+  __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
+  __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
+  __shared__ unsigned s_nan[2][kChunkTiles / 2][4];  // of the values: two tiles, lane / 16
+  const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
+  const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int r16 = lane & 15, g = lane >> 4, G = a.n_q / c.n_kv;
+  const Kv8Seq q = uniform(kv8_seq(c, r, b));
+  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
+  const int page = 1 << c.page_shift;
+  const size_t parts = (size_t)r.n_rows * a.n_q * nsplit;
+  const int total = q.rows * G, tiles = (total + kRows - 1) / kRows;
+  const HeadAt4<HD> kv(c, q, h);
+  const float unit = a.scale * kLog2e;
+  const bool two_a_cu = gridDim.x > kCus && gridDim.x * gridDim.y <= 2 * kCus && tiles <= ntile;
+
+  for (int back = tile0; back < tiles; back += ntile) {
+    // From the last tile back; with two workgroups a CU, the second half from the first tile
+    // on, so that a CU's two see about as many positions together as any other's.
+    const int first = (tiles + 1) / 2;
+    const int tile = two_a_cu && back >= first ? back - first : tiles - 1 - back;
+    const int row0 = kRows * tile, mine = row0 + 16 * kRowTiles * wave;
+    auto seen = [&](int rr) { return kv8_seen(q.len, q.rows, rr, cap); };
+    // positions this wavefront's rows see at most and at least
+    const int most = mine < total ? seen(min((mine + 16 * kRowTiles - 1) / G, q.rows - 1)) : 0;
+    const int least = mine + 16 * kRowTiles <= total ? seen(mine / G) : 0;
+    const int all = seen(min((row0 + kRows - 1) / G, q.rows - 1));  // of the workgroup's rows
+    const int chunks = kv8_steps(all, kChunkPos), per = (chunks + nsplit - 1) / nsplit;
+    const int c0 = min(split * per, chunks), c1 = min(c0 + per, chunks);
+
+    RowState4 st[kRowTiles];
+    RowOut4<HD> o[kRowTiles];
+#pragma unroll
+    for (int x = 0; x < kRowTiles; ++x)
+#pragma unroll
+      for (int u = 0; u < DT; ++u) o[x][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+
+    // what this wavefront brings of a chunk: the keys of tile `wave`; of the pair of tiles
+    // wave / 2 the values of half of each lane's dimensions
+    unsigned kc[DS], ks, vc[2][VW], vs[2];
+    int phys[kChunkTiles], later[kChunkTiles];
+    const int pair = wave >> 1, half = wave & 1;
+    const bool whole_chunk = c.page_shift >= 6;  // one page holds a chunk
+    auto find = [&](int chunk) {
+      later[0] = entry(c, q, (uint32_t)chunk * kChunkPos);
+      if (!whole_chunk)
+#pragma unroll
+        for (int t = 1; t < kChunkTiles; ++t)
+          later[t] = entry(c, q, (uint32_t)chunk * kChunkPos + 16 * t);
+    };
+    auto look = [&]() {
+      phys[0] = kv8_named(later[0], c.n_pages);
+#pragma unroll
+      for (int t = 1; t < kChunkTiles; ++t)
+        phys[t] = whole_chunk ? phys[0] : kv8_named(later[t], c.n_pages);
+    };
+    auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
+      const int j0 = chunk * kChunkPos;
+      // p[t], with bits: a choice between the elements would put them into memory
+      auto pick = [&](int t) {
+        const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
+        return lo ^ ((lo ^ hi) & -(t >> 1));
+      };
+      auto keys = [&](__amdgpu_buffer_rsrc_t b, int slot) {
+        const int d = g * (HD / 4);
+        fetch_codes<HD>(kc, b, kv4_key_at(r16, d, HD), kv4_key_at(slot, 0, HD));
+        ks = __builtin_amdgcn_raw_buffer_load_b8(b, r16 * (HD / kKv4Group) + d / kKv4Group,
+                                                 kv4_key_scale_at(slot, 0, page, HD), 0);
+      };
+      auto values = [&](int t, __amdgpu_buffer_rsrc_t b, int slot) {
+        const int d = r16 * (HD / 16) + half * (HD / 32);
+        const int at = kv4_value_at(4 * g, d, HD), from = kv4_value_at(slot, 0, HD);
+        if constexpr (VW == 2) {
+          const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, at, from, 0);
+          vc[t][0] = w[0];
+          vc[t][1] = w[1];
+        } else {
+          vc[t][0] = __builtin_amdgcn_raw_buffer_load_b32(b, at, from, 0);
+        }
+        vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, 4 * g * (HD / kKv4Group) + 4 * (d / kKv4Group),
+                                                     kv4_value_scale_at(slot, 0, page, HD), 0);
+      };
+      if (whole_chunk) {
+        const int slot = j0 & (page - 1);
+        keys(kv.buffer(c, p[0], 0), slot + 16 * wave);
+        const __amdgpu_buffer_rsrc_t b = kv.buffer(c, p[0], 1);
+        values(0, b, slot + 32 * pair);
+        values(1, b, slot + 32 * pair + 16);
+      } else {
+        keys(kv.buffer(c, pick(wave), 0), (j0 + 16 * wave) & (page - 1));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          values(t, kv.buffer(c, pick(2 * pair + t), 1), (j0 + 32 * pair + 16 * t) & (page - 1));
+      }
+    };
+    auto convert = [&](int buf) {
+      const float scale = __uint_as_float(ks << 23);
+#pragma unroll
+      for (int d = 0; d < DS; ++d)
+        s_k[buf][wave][d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
+      const unsigned nan = take_nans(vs[0]) | take_nans(vs[1]) << 4;
+      float f[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[t][i] = scale_of(vs[t], i);
+#pragma unroll
+      for (int d = 0; d < VW; ++d) {
+        uint2 a0, a1, b0, b1;
+        values4(vc[0][d], f[0], a0, b0);
+        values4(vc[1][d], f[1], a1, b1);
+        s_v[buf][pair][2 * (half * VW + d)][lane] = make_uint4(a0.x, a0.y, a1.x, a1.y);
+        s_v[buf][pair][2 * (half * VW + d) + 1][lane] = make_uint4(b0.x, b0.y, b1.x, b1.y);
+      }
+      if (half == 0 && r16 == 0) s_nan[buf][pair][g] = nan;
+    };
+
+    if (c0 < c1) {
+      find(c0);
+      look();
+      bring(phys, c0);
+      find(c0 + 1);
+    }
+    bf16x8_t qf[kRowTiles][NQ][DS];
+    int limit[kRowTiles];  // positions each row sees
+#pragma unroll
+    for (int x = 0; x < kRowTiles; ++x) {
+      const int qr = mine + 16 * x + r16, row = qr / G, rc = min(row, q.rows - 1);
+      const bool on = qr < total;
+      limit[x] = on ? seen(row) : 0;
+      load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + (h * G + qr % G) * a.q.head_stride,
+                            on, lane, qf[x]);
+    }
+    for (int ch = c0; ch < c1; ++ch) {
+      const int buf = (ch - c0) & 1;
+      int now[kChunkTiles];
+#pragma unroll
+      for (int t = 0; t < kChunkTiles; ++t) now[t] = phys[t];
+      look();
+      find(ch + 2);
+      convert(buf);
+      if (ch + 1 < c1) bring(phys, ch + 1);
+      __syncthreads();
+      if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
+#pragma unroll
+      for (int p = 0; p < kChunkTiles / 2; ++p) {
+        const int j0 = ch * kChunkPos + 32 * p;
+        Pages pg;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) pg.phys[t] = now[2 * p + t];
+        const unsigned nan = s_nan[buf][p][g];
+        // Row tile after row tile: the matrix cores work on one's products while the vector
+        // units turn the other's scores into weights.
+        floatx4_t x[kRowTiles][kTiles];
+        bf16x8_t op[DT];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int d = 0; d < DS; ++d)
+            op[t * DS + d] = __builtin_bit_cast(bf16x8_t, s_k[buf][2 * p + t][d][lane]);
+#pragma unroll
+        for (int y = 0; y < kRowTiles; ++y)
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < DS; ++d)
+#pragma unroll
+              for (int n = 0; n < NQ; ++n)
+                x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[t * DS + d], qf[y][n][d],
+                                                                  x[y][t], 0, 0, 0);
+          }
+#pragma unroll
+        for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(bf16x8_t, s_v[buf][p][u][lane]);
+        const bool whole = least - j0 >= kStep && pg.all();
+#pragma unroll
+        for (int y = 0; y < kRowTiles; ++y) {
+          float corr = 1.f;
+          bf16x8_t wf[NW];
+          const bool move =
+              whole ? weights4<NW, false>(wf, st[y], x[y], pg, unit, nan, 0, lane, corr)
+                    : weights4<NW, true>(wf, st[y], x[y], pg, unit, nan, limit[y] - j0, lane, corr);
+          if (move) rescale4<HD>(o[y], corr);
+#pragma unroll
+          for (int u = 0; u < DT; ++u)
+#pragma unroll
+            for (int n = 0; n < NW; ++n)
+              o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[u], wf[n], o[y][u], 0, 0, 0);
+        }
+      }
+    }
+    __syncthreads();  // the buffers are free for the next tile
+    const int me = fresh(lane), mg = me >> 4;
+#pragma unroll
+    for (int y = 0; y < kRowTiles; ++y) {
+      st[y].sum += __shfl_xor(st[y].sum, 16);
+      st[y].sum += __shfl_xor(st[y].sum, 32);
+      note_no_weight(st[y].ref, st[y].sum, c, q, limit[y], (uint32_t)c0 * kChunkPos, most, lane);
+      const int qr = mine + 16 * y + (me & 15);
+      if (qr >= total) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < DT; u += 4) {
+          float v[4] = {o[y][u][i], o[y][u + 1][i], o[y][u + 2][i], o[y][u + 3][i]};
+          leave(a, nsplit, split, parts, q.row0 + qr / G, h * G + qr % G,
+                DT * (4 * mg + i) + u, st[y].ref, 0.f, st[y].sum, v);
+        }
+    }
+  }
+}
+
 // ------------------------------------------------------------------- launcher
 size_t kv4_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int max_rows,
                        int max_length) {
@@ -414,8 +638,15 @@ static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStr
   const int edge = p.nsplit == 1 ? last : last & kFirst;
 #define WICI_ATTN(...) \
   launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
-  if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2>);
-  else WICI_ATTN(k_kv4_attn_split<HD, 3, 3>);
+  if (p.row_tiles == 2) {
+    WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 2>);
+  } else if (p.row_tiles == 1) {
+    if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1>);
+    else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1>);
+  } else {
+    if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2>);
+    else WICI_ATTN(k_kv4_attn_split<HD, 3, 3>);
+  }
 #undef WICI_ATTN
   if (p.nsplit > 1) return launch_kv_attn_merge(HD, c, r, a, p.nsplit, st, last & kLast);
   return hipGetLastError();
