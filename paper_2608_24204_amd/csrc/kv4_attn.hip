@@ -3,7 +3,7 @@
 // Mathematics.  For a row with query q over positions j with key rows k_j and value rows v_j:
 //   y_j = (q . k_j) scale log2(e),   out = sum_j 2^(y_j - ref) v_j / sum_j 2^(y_j - ref),
 // `ref` running with the largest y_j (an online softmax): it moves only when a weight would pass
-// 2^8, to the largest score so far.  A cached value is one of 8 small numbers times a power of two,
+// 2^8 times its size when `ref` was set.  A cached value is one of 8 small numbers times a power of two,
 // exact in bf16 over fp32's whole range, so both products run on the bf16 matrix cores with the
 // scales inside their operands: one conversion instruction makes two operands of a byte and a
 // scale.  q and the weights enter as NQ and NW bf16 terms: bf16 queries are exact in one, and two
@@ -20,6 +20,7 @@
 // keys a lane takes position l % 16 and a quarter of the dimensions, within one group's scale;
 // for the values four positions of hd / 16 neighbouring dimensions, and their four scales.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.h"
 #include "kv4_plan.h"
@@ -28,7 +29,17 @@
 
 namespace wici {
 
-constexpr float kMostAhead = 8.f;  // of a score to its row's reference, past which that moves
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+template <typename T> struct ElemOf;
+template <> struct ElemOf<bf16x8_t> { typedef __bf16 type; };
+template <> struct ElemOf<half8_t> { typedef _Float16 type; };
+template <typename T> using Elem_t = typename ElemOf<T>::type;
+
+constexpr float kAhead = 8.f;       // log2 by which weights may pass their size when `ref` is set:
+constexpr float kTopBf16 = 0.f;     // 2^0 for bf16 weights, 2^6 for fp16 ones (2^14 then fits, and
+constexpr float kTopHalf = 6.f;     // fp16's least step is 2^-30 of the largest)
+constexpr float kTopHuge = -32.f;   // of rows that have met values of 2^100 and more: 2^-32, so
+constexpr int kHugeByte = 227;      // that sums of 2^24 of the largest stay in fp32
 
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
 struct RowState4 {
@@ -52,27 +63,50 @@ __device__ __forceinline__ bf16x8_t keys8(unsigned w, float scale) {
                                                  pair_of<2>(w, scale), pair_of<3>(w, scale)));
 }
 // A word of value codes, four positions of a pair of dimensions: the positions of the first
-// dimension (lo) and of the second.
+// dimension (lo) and of the second, as bf16 or fp16.
+template <int BYTE, bool HALF>
+__device__ __forceinline__ unsigned pair_as(unsigned w, float scale) {
+  if constexpr (HALF)
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, BYTE));
+  else
+    return pair_of<BYTE>(w, scale);
+}
+template <bool HALF>
 __device__ __forceinline__ void values4(unsigned w, const float (&s)[4], uint2& lo, uint2& hi) {
-  const unsigned a = pair_of<0>(w, s[0]), b = pair_of<1>(w, s[1]), c = pair_of<2>(w, s[2]),
-                 d = pair_of<3>(w, s[3]);
+  const unsigned a = pair_as<0, HALF>(w, s[0]), b = pair_as<1, HALF>(w, s[1]),
+                 c = pair_as<2, HALF>(w, s[2]), d = pair_as<3, HALF>(w, s[3]);
   lo = make_uint2(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u));
   hi = make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
 }
 // Which of a word's four positions are NaN (scale byte 255; 253 and 254, which memory never
 // appended to may hold, are taken as it: 4 times theirs is infinite), as bits; their scales become 1.
-__device__ __forceinline__ unsigned take_nans(unsigned& w) {
+// `large`: whether the wavefront has a scale of 2^100 and more.
+__device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large) {
   const bool maybe = (w & w << 1 & 0x80808080u) != 0;  // some scale of 2^65 and more
   unsigned nan = 0;
   if (__builtin_expect(__any(maybe), false)) {
+    bool big = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if ((w >> (8 * i) & 0xffu) > (unsigned)kKv4MostByte) {
+    for (int i = 0; i < 4; ++i) {
+      const unsigned byte = w >> (8 * i) & 0xffu;
+      if (byte > (unsigned)kKv4MostByte) {
         nan |= 1u << i;
         w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
+      } else {
+        big |= byte >= (unsigned)kHugeByte;
       }
+    }
+    large |= __any(big);
   }
   return nan;
+}
+
+// A word's scales from position `left` on become 1, or all where the page is absent: what nobody
+// sees is finite in the products, and no result depends on it.
+__device__ __forceinline__ void leave_seen(unsigned& w, bool there, int left) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (!there || i >= left) w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
 }
 
 // The codes and scales of a step, as one lane holds them.
@@ -134,6 +168,13 @@ __device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const H
   }
 }
 
+__device__ __forceinline__ floatx4_t product(bf16x8_t a, bf16x8_t b, floatx4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4_t product(half8_t a, half8_t b, floatx4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 // S^T of one step: sc[t][i] is the product of position 16 t + 4 (l / 16) + i with row l % 16.
 template <int HD, int NQ>
 __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>& s,
@@ -152,14 +193,15 @@ __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>
   }
 }
 
-// The weights of 32 positions from their products (a score is product * unit), as NW bf16 terms.
-// MASKED: some row does not see every position: row l % 16 sees those below `seen`, of the tiles
-// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  Returns whether a row's
-// reference moved: the output so far is then to be multiplied by `corr`.
-template <int NW, bool MASKED>
-__device__ __forceinline__ bool weights4(bf16x8_t (&wf)[NW], RowState4& st,
-                                         const floatx4_t (&sc)[kTiles], const Pages& p, float unit,
-                                         unsigned nan, int seen, int lane, float& corr) {
+// The weights of 32 positions from their products (a score is product * unit), as NW terms of type
+// T.  MASKED: some row does not see every position: row l % 16 sees those below `seen`, of the tiles
+// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  A row's reference is set
+// `top` below its largest score, and moves when a score is kAhead and more above that.  Returns
+// whether one moved: the output so far is then to be multiplied by `corr`.
+template <typename T, int NW, bool MASKED>
+__device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, const floatx4_t (&sc)[kTiles],
+                                         const Pages& p, float unit, unsigned nan, float top,
+                                         int seen, int lane, float& corr) {
 #pragma clang fp contract(off)  // of two scores that are equal and huge the difference is zero
   const int left = seen - 4 * (lane >> 4);
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
@@ -184,15 +226,15 @@ __device__ __forceinline__ bool weights4(bf16x8_t (&wf)[NW], RowState4& st,
     }
   };
   against();
-  const bool move = __any(!(most <= kMostAhead));
-  if (move) {
+  const bool move = __any(!(most <= top + kAhead));
+  if (__builtin_expect(move, false)) {
     // (by a row's own scores alone: other rows' change nothing in it)
     float z = y[0];
 #pragma unroll
     for (int i = 1; i < 4 * kTiles; ++i) z = fmaxf(z, y[i]);
     z = fmaxf(z, __shfl_xor(z, 16));
     z = fmaxf(z, __shfl_xor(z, 32));
-    const float ref = z - st.ref > kMostAhead ? z : st.ref;
+    const float ref = z - st.ref > top + kAhead ? z - top : st.ref;
     corr = ref == st.ref ? 1.f : __builtin_amdgcn_exp2f(st.ref - ref);
     st.sum *= corr;
     st.ref = ref;
@@ -205,7 +247,7 @@ __device__ __forceinline__ bool weights4(bf16x8_t (&wf)[NW], RowState4& st,
     sum += rest;
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
-      wf[n][i] = (__bf16)rest;
+      wf[n][i] = (Elem_t<T>)rest;
       rest -= (float)wf[n][i];
     }
   }
@@ -226,8 +268,8 @@ __device__ __forceinline__ void add_values4(RowOut4<HD>& o, const Step4<HD>& s,
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) {
     uint2 a0, a1, b0, b1;
-    values4(s.v[0][d], f[0], a0, b0);
-    values4(s.v[1][d], f[1], a1, b1);
+    values4<false>(s.v[0][d], f[0], a0, b0);
+    values4<false>(s.v[1][d], f[1], a1, b1);
     const bf16x8_t a = __builtin_bit_cast(bf16x8_t, make_uint4(a0.x, a0.y, a1.x, a1.y));
     const bf16x8_t b = __builtin_bit_cast(bf16x8_t, make_uint4(b0.x, b0.y, b1.x, b1.y));
 #pragma unroll
@@ -244,6 +286,15 @@ __device__ __forceinline__ void rescale4(RowOut4<HD>& o, float f) {
   for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[u][i] *= f;
+}
+
+// The references `top` above what they were (set for 2^from): the output and the sum accordingly.
+template <int HD>
+__device__ __forceinline__ void lower(RowOut4<HD>& o, RowState4& st, float from) {
+  const float f = __builtin_amdgcn_exp2f(kTopHuge - from);
+  if (st.ref != kNoRef) st.ref += from - kTopHuge;
+  st.sum *= f;
+  rescale4<HD>(o, f);
 }
 
 // 16 query rows (row l % 16 of the tile, zero where `on` is false) as NQ bf16 terms.
@@ -323,6 +374,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
     bf16x8_t qf[NQ][HD / 32];
     load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf);
     const float unit = a.scale * kLog2e;
+    float top = kTopBf16;
     RowState4 st;
     RowOut4<HD> o;
 #pragma unroll
@@ -340,17 +392,26 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
         const Pages next = named(c, later);
         if (then < steps) load_keys4<HD>(x, c, kv, next, then, lane);
         unsigned vs[kTiles], nan = 0;
+        bool large = false;
+        const bool clear = s < whole && now.all();
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
           vs[t] = x.vs[t];
-          nan |= take_nans(vs[t]) << (4 * t);
+          if (!clear)
+            leave_seen(vs[t], now.phys[t] >= 0, seen(last) - s * kStep - (16 * t + 4 * (lane >> 4)));
+          nan |= take_nans(vs[t], large) << (4 * t);
+        }
+        if (__builtin_expect(large, false) && top != kTopHuge) {
+          top = kTopHuge;
+          lower<HD>(o, st, kTopBf16);
         }
         bf16x8_t wf[NW];
         float corr = 1.f;
         const bool move =
-            s < whole && now.all()
-                ? weights4<NW, false>(wf, st, sc, now, unit, nan, 0, lane, corr)
-                : weights4<NW, true>(wf, st, sc, now, unit, nan, limit - s * kStep, lane, corr);
+            clear
+                ? weights4<bf16x8_t, NW, false>(wf, st, sc, now, unit, nan, top, 0, lane, corr)
+                : weights4<bf16x8_t, NW, true>(wf, st, sc, now, unit, nan, top, limit - s * kStep, lane,
+                                               corr);
         if (move) rescale4<HD>(o, corr);
         add_values4<HD, NW>(o, x, vs, wf);
         if (then >= steps) break;
@@ -408,9 +469,11 @@ __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                             int ntile) {
   constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles, VW = HD / 64;
+  enum Kind { kTooWide = 1, kNans = 2, kLarge = 4 };
   __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
   __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
-  __shared__ unsigned s_nan[2][kChunkTiles / 2][4];  // of the values: two tiles, lane / 16
+  __shared__ int s_kind[2][kChunkTiles / 2];         // of the values of two tiles: Kind,
+  __shared__ unsigned s_nan[2][kChunkTiles / 2][4];  // and which are NaN, by lane / 16
   const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
   const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -440,6 +503,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 
     RowState4 st[kRowTiles];
     RowOut4<HD> o[kRowTiles];
+    float top = NQ > 1 ? kTopBf16 : kTopHalf;
 #pragma unroll
     for (int x = 0; x < kRowTiles; ++x)
 #pragma unroll
@@ -503,34 +567,48 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
           values(t, kv.buffer(c, pick(2 * pair + t), 1), (j0 + 32 * pair + 16 * t) & (page - 1));
       }
     };
-    auto convert = [&](int buf) {
+    // The operands of the chunk that is here; whether the values' scales do for `halves`.
+    auto convert = [&](int buf, int ch, const int (&now)[kChunkTiles], auto halves) {
       const float scale = __uint_as_float(ks << 23);
 #pragma unroll
       for (int d = 0; d < DS; ++d)
         s_k[buf][wave][d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
-      const unsigned nan = take_nans(vs[0]) | take_nans(vs[1]) << 4;
-      float f[2][4];
+      // (in the last chunk, and in pages that are not there)
+      const int left = all - ch * kChunkPos;
+      const int p0 = now[0] ^ ((now[0] ^ now[2]) & -pair), p1 = now[1] ^ ((now[1] ^ now[3]) & -pair);
+      if (left < kChunkPos || (p0 | p1) < 0) {
+        leave_seen(vs[0], p0 >= 0, left - (32 * pair + 4 * g));
+        leave_seen(vs[1], p1 >= 0, left - (32 * pair + 16 + 4 * g));
+      }
+      bool large = false;
+      const unsigned nan = take_nans(vs[0], large) | take_nans(vs[1], large) << 4;
+      int kind = large ? kLarge : 0;
+      if (__any(nan != 0)) {
+        kind |= kNans;
+        if (half == 0 && r16 == 0) s_nan[buf][pair][g] = nan;
+      }
+      float f[2][4], least = INFINITY, largest = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[t][i] = scale_of(vs[t], i);
+        for (int i = 0; i < 4; ++i) {
+          f[t][i] = scale_of(vs[t], i);
+          least = fminf(least, f[t][i]);
+          largest = fmaxf(largest, f[t][i]);
+        }
+      // (both wavefronts of the pair see all its scales)
+      if (halves.value && __any(!(least >= 0x1p-23f && largest <= 0x1p13f))) kind |= kTooWide;
 #pragma unroll
       for (int d = 0; d < VW; ++d) {
         uint2 a0, a1, b0, b1;
-        values4(vc[0][d], f[0], a0, b0);
-        values4(vc[1][d], f[1], a1, b1);
+        values4<halves.value>(vc[0][d], f[0], a0, b0);
+        values4<halves.value>(vc[1][d], f[1], a1, b1);
         s_v[buf][pair][2 * (half * VW + d)][lane] = make_uint4(a0.x, a0.y, a1.x, a1.y);
         s_v[buf][pair][2 * (half * VW + d) + 1][lane] = make_uint4(b0.x, b0.y, b1.x, b1.y);
       }
-      if (half == 0 && r16 == 0) s_nan[buf][pair][g] = nan;
+      if (half == 0 && lane == 0) s_kind[buf][pair] = kind;
     };
 
-    if (c0 < c1) {
-      find(c0);
-      look();
-      bring(phys, c0);
-      find(c0 + 1);
-    }
     bf16x8_t qf[kRowTiles][NQ][DS];
     int limit[kRowTiles];  // positions each row sees
 #pragma unroll
@@ -541,63 +619,90 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
       load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + (h * G + qr % G) * a.q.head_stride,
                             on, lane, qf[x]);
     }
-    for (int ch = c0; ch < c1; ++ch) {
-      const int buf = (ch - c0) & 1;
-      int now[kChunkTiles];
-#pragma unroll
-      for (int t = 0; t < kChunkTiles; ++t) now[t] = phys[t];
+    // The chunks from `from` on, with the values and weights as halves or as NW bf16 terms; returns
+    // the first chunk that it does not take: one whose values do not fit halves.
+    auto take = [&](int from, auto halves) -> int {
+      typedef std::conditional_t<halves.value, half8_t, bf16x8_t> Value;
+      constexpr int N = halves.value ? 1 : NW;
+      if (from >= c1) return from;
+      find(from);
       look();
-      find(ch + 2);
-      convert(buf);
-      if (ch + 1 < c1) bring(phys, ch + 1);
-      __syncthreads();
-      if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
+      bring(phys, from);
+      find(from + 1);
+      for (int ch = from; ch < c1; ++ch) {
+        const int buf = (ch - from) & 1;
+        int now[kChunkTiles];
 #pragma unroll
-      for (int p = 0; p < kChunkTiles / 2; ++p) {
-        const int j0 = ch * kChunkPos + 32 * p;
-        Pages pg;
+        for (int t = 0; t < kChunkTiles; ++t) now[t] = phys[t];
+        look();
+        find(ch + 2);
+        convert(buf, ch, now, halves);
+        if (ch + 1 < c1) bring(phys, ch + 1);
+        __syncthreads();
+        const int kinds[2] = {uniform(s_kind[buf][0]), uniform(s_kind[buf][1])};
+        if (halves.value && __builtin_expect((kinds[0] | kinds[1]) & kTooWide, false)) return ch;
+        if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) pg.phys[t] = now[2 * p + t];
-        const unsigned nan = s_nan[buf][p][g];
-        // Row tile after row tile: the matrix cores work on one's products while the vector
-        // units turn the other's scores into weights.
-        floatx4_t x[kRowTiles][kTiles];
-        bf16x8_t op[DT];
+        for (int p = 0; p < kChunkTiles / 2; ++p) {
+          const int j0 = ch * kChunkPos + 32 * p;
+          Pages pg;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
+          for (int t = 0; t < kTiles; ++t) pg.phys[t] = now[2 * p + t];
+          unsigned nan = 0;
+          if (__builtin_expect(kinds[p], false)) {
+            if (kinds[p] & kNans) nan = s_nan[buf][p][g];
+            if (!halves.value && (kinds[p] & kLarge) && top != kTopHuge) {
 #pragma unroll
-          for (int d = 0; d < DS; ++d)
-            op[t * DS + d] = __builtin_bit_cast(bf16x8_t, s_k[buf][2 * p + t][d][lane]);
-#pragma unroll
-        for (int y = 0; y < kRowTiles; ++y)
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t) {
-            x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int d = 0; d < DS; ++d)
-#pragma unroll
-              for (int n = 0; n < NQ; ++n)
-                x[y][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[t * DS + d], qf[y][n][d],
-                                                                  x[y][t], 0, 0, 0);
+              for (int y = 0; y < kRowTiles; ++y) lower<HD>(o[y], st[y], top);
+              top = kTopHuge;
+            }
           }
+          // Row tile after row tile: the matrix cores work on one's products while the vector
+          // units turn the other's scores into weights.
+          floatx4_t x[kRowTiles][kTiles];
+          uint4 op[DT];
 #pragma unroll
-        for (int u = 0; u < DT; ++u) op[u] = __builtin_bit_cast(bf16x8_t, s_v[buf][p][u][lane]);
-        const bool whole = least - j0 >= kStep && pg.all();
+          for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int y = 0; y < kRowTiles; ++y) {
-          float corr = 1.f;
-          bf16x8_t wf[NW];
-          const bool move =
-              whole ? weights4<NW, false>(wf, st[y], x[y], pg, unit, nan, 0, lane, corr)
-                    : weights4<NW, true>(wf, st[y], x[y], pg, unit, nan, limit[y] - j0, lane, corr);
-          if (move) rescale4<HD>(o[y], corr);
+            for (int d = 0; d < DS; ++d) op[t * DS + d] = s_k[buf][2 * p + t][d][lane];
 #pragma unroll
-          for (int u = 0; u < DT; ++u)
+          for (int y = 0; y < kRowTiles; ++y)
 #pragma unroll
-            for (int n = 0; n < NW; ++n)
-              o[y][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[u], wf[n], o[y][u], 0, 0, 0);
+            for (int t = 0; t < kTiles; ++t) {
+              x[y][t] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int d = 0; d < DS; ++d)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                  x[y][t] = product(__builtin_bit_cast(bf16x8_t, op[t * DS + d]), qf[y][n][d], x[y][t]);
+            }
+#pragma unroll
+          for (int u = 0; u < DT; ++u) op[u] = s_v[buf][p][u][lane];
+          const bool whole = least - j0 >= kStep && pg.all();
+#pragma unroll
+          for (int y = 0; y < kRowTiles; ++y) {
+            float corr = 1.f;
+            Value wf[N];
+            const bool move =
+                whole ? weights4<Value, N, false>(wf, st[y], x[y], pg, unit, nan, top, 0, lane, corr)
+                      : weights4<Value, N, true>(wf, st[y], x[y], pg, unit, nan, top, limit[y] - j0, lane,
+                                                 corr);
+            if (__builtin_expect(move, false)) rescale4<HD>(o[y], corr);
+#pragma unroll
+            for (int u = 0; u < DT; ++u)
+#pragma unroll
+              for (int n = 0; n < N; ++n)
+                o[y][u] = product(__builtin_bit_cast(Value, op[u]), wf[n], o[y][u]);
+          }
         }
       }
+      return c1;
+    };
+    int at = c0;
+    if (NQ == 1) at = take(at, std::integral_constant<bool, true>());
+    if (NQ > 1 || __builtin_expect(at < c1, false)) {
+      __syncthreads();  // (what was made of this chunk is read no more)
+      take(at, std::integral_constant<bool, false>());
     }
     __syncthreads();  // the buffers are free for the next tile
     const int me = fresh(lane), mg = me >> 4;

@@ -6,12 +6,15 @@ bf16 result with the rounding of that answer).  Attention: with S the largest su
 of a row and A the output with |v| in place of v, a score is off by at most e = 64 2^-24 S + 2^-20
 (a sum of 128 products in fp32, with the roundings of a third bf16 term of the query, of the
 factor and of the difference; the exponential's argument and result), which moves a weight and the
-sum by e each; a weight is off by at most 2^-16 (two bf16 terms, bf16 rows: half a step is 2^-8,
-twice) or 2^-24 (three) of itself; the sums over n positions add at most (64 + n / 16) roundings of
+sum by e each; a weight is off by at most 2^-24 of itself (three bf16 terms), for bf16 rows 2^-16 (two:
+half a step is 2^-8, twice), and for bf16 rows of prompts 2^-11 (one fp16 term) or 2^-31 of the row's
+largest weight (half of fp16's least step, 2^-24, with that at 2^6 or more: n 2^-31 of the largest |v| at
+most in all); the sums over n positions add at most (64 + n / 16) roundings of
 2^-24 A, and those of several terms as many again; and the result is rounded once, by eps / 2 of
 itself.  Weights are fp32 (and their terms bf16) with the largest at 1 or more: one below 2^-126, or a
 term below it, may count as zero, which is off by at most 2^-126 |v| a position and term, of a sum
-of at least 1: 3 n 2^-126 of the largest |v| that the row sees."""
+of at least 1: 3 n 2^-126 of the largest |v| that the row sees.  Rows that have met values of 2^100
+hold their largest weight at 2^-32 (what is summed would else leave fp32), and 2^-126 is 2^-94 of it."""
 
 from __future__ import annotations
 
@@ -56,16 +59,21 @@ def sub_batch(lens, rows, start):
     return bt
 
 
-def tolerance(want, mag, dots, n, single, out_dtype):
+def tolerance(want, mag, dots, n, single, out_dtype, top=0.0, prompt=False):
+    """top: the largest |v| that each row sees (broadcast to `want`)."""
     e = 64 * 2.0 ** -24 * dots + 2.0 ** -20
-    rel = 2 * e + (2.0 ** -16 if single else 2.0 ** -24) + 2 * (64 + n / 16) * 2.0 ** -24
-    return mag * rel[..., None] + abs(want) * (torch.finfo(out_dtype).eps / 2) + 1e-30
+    weight = 2.0 ** -24 if not single else 2.0 ** -11 if prompt else 2.0 ** -16
+    rel = 2 * e + weight + 2 * (64 + n / 16) * 2.0 ** -24
+    lost = 3 * n * (2.0 ** -126 + (top >= 2.0 ** 100) * 2.0 ** -94) + \
+        (n * 2.0 ** -31 if single and prompt else 0.0)
+    return mag * rel[..., None] + abs(want) * (torch.finfo(out_dtype).eps / 2) + lost * top + 1e-30
 
 
 def check_attend(bt, q, out, K, V, scale, seen=None):
     """out [n_rows, heads, hd] of q against the definition, for every row of the batch."""
     qn, on = f64(q), f64(out)
     single = q.dtype == BF16 and out.dtype == BF16
+    prompt = max(bt.rows) > 1
     for b, (n, r) in enumerate(zip(bt.lens, bt.rows)):
         at = slice(bt.start[b], bt.start[b] + r)
         pos = np.arange(n - r, n)
@@ -73,10 +81,10 @@ def check_attend(bt, q, out, K, V, scale, seen=None):
         if seen is not None:
             sees &= seen(b, np.arange(n))[None]
         want, mag, dots = oracle.attend_rows(qn[at], K[b], V[b], sees, scale)
-        tol = tolerance(want, mag, dots, n, single, out.dtype)
-        if r:
-            top = np.where(sees, np.abs(V[b]).max((1, 2))[None], 0.0).max(1)
-            tol = tol + (3 * n * 2.0 ** -126 * top)[:, None, None]
+        if not r:
+            continue
+        top = np.where(sees, np.abs(V[b]).max((1, 2))[None], 0.0).max(1)[:, None, None]
+        tol = tolerance(want, mag, dots, n, single, out.dtype, top, prompt)
         err = np.abs(on[at] - want)
         assert np.all(err <= tol), (b, float(np.max(err / tol)))
 
@@ -227,7 +235,14 @@ def test_every_kernel(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dty
     K, V = bt.fill(dtype=BF16)
     q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype, scale=1.5)
     out = bt.cache.attend(q, bt.length, row_start=bt.row_start, max_rows=rows)
-    for b, (n, r) in enumerate(zip(lens, new)):
+    check_on_gpu(bt, q, out, K, V)
+
+
+def check_on_gpu(bt, q, out, K, V):
+    """Against float64 on the GPU, all rows."""
+    n_kv, hd, dtype = bt.n_kv, bt.hd, q.dtype
+    G = q.shape[1] // n_kv
+    for b, (n, r) in enumerate(zip(bt.lens, bt.rows)):
         if not r:
             continue
         at = slice(bt.start[b], bt.start[b] + r)
@@ -238,9 +253,37 @@ def test_every_kernel(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dty
         p = x.masked_fill(late, float("-inf")).softmax(-1)
         want, mag = p @ v, p @ v.abs()
         dots = (qq.abs() @ k.abs().transpose(-1, -2).contiguous()).amax(-1) * hd ** -0.5
-        tol = tolerance(want, mag, dots, n, dtype == BF16, dtype)
+        top = v.abs().amax(-1).cummax(-1).values[..., n - r:, None]
+        tol = tolerance(want, mag, dots, n, dtype == BF16, out.dtype, top, True)
         err = (out[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3) - want).abs()
         assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("n_seqs,rows,length,n_kv,G,hd,entries,page", PLAN_CASES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("where", ["early", "late", "here and there"])
+def test_values_past_halves(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dtype, where):
+    """Value rows of zeros, of 1e-12 and up to fp32's end, in every kernel: before, after and among
+    ordinary ones."""
+    lens = [max(rows, length - 7 * b) for b in range(min(n_seqs, 9))]
+    lens += [max(rows, length)] * (n_seqs - len(lens))
+    need = -(-max(lens) // page)
+    bt = Batch4(ops, lens, [rows] * n_seqs, n_kv=n_kv, hd=hd, page=page, seed=rows + n_seqs,
+                extra_pages=entries - need)
+    n = sum(lens)
+    k, v = (rnd(bt.rng, n, n_kv, hd, dtype=F32) for _ in "kv")
+    at = np.concatenate([np.arange(x) for x in lens])
+    odd = {"early": at < 3, "late": at >= length - rows // 2 - 2,
+           "here and there": bt.rng.random(n) < 0.05}[where]
+    size = np.where(odd, bt.rng.choice([0.0, 1e-12, 1e7, 1e25, 3e36], n), 1.0)
+    if where == "early":
+        size[at == 0] = 1e38 / 4
+    v *= torch.from_numpy(size.astype(np.float32)).cuda()[:, None, None]
+    K, V = bt.store(k, v)
+    q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype, scale=1.5)
+    out = bt.cache.attend(q, bt.length, row_start=bt.row_start, max_rows=rows)
+    assert out.isfinite().all()
+    check_on_gpu(bt, q, out, K, V)
 
 
 @pytest.mark.parametrize("rows", [None, [3, 16, 700]])
@@ -413,7 +456,7 @@ def test_scores_past_the_range(ops, dtype, rows):
         want, mag, dots = oracle.attend_rows(f64(qq[:late, 1:]), K[0], V[0],
                                              (np.arange(700)[None] <= (700 - n + np.arange(late))[:, None]) & keep,
                                              0.125)
-        tol = tolerance(want, mag, dots, 700, dtype == BF16, dtype)
+        tol = tolerance(want, mag, dots, 700, dtype == BF16, dtype, 10.0, True)
         assert np.all(np.abs(f64(out[:late, 1:]) - want) <= tol)
     k[:, 0, 0] = 2e38
     bt.store(k, v)
