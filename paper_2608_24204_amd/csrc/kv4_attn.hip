@@ -35,11 +35,15 @@ template <> struct ElemOf<bf16x8_t> { typedef __bf16 type; };
 template <> struct ElemOf<half8_t> { typedef _Float16 type; };
 template <typename T> using Elem_t = typename ElemOf<T>::type;
 
-constexpr float kAhead = 8.f;       // log2 by which weights may pass their size when `ref` is set:
-constexpr float kTopBf16 = 0.f;     // 2^0 for bf16 weights, 2^6 for fp16 ones (2^14 then fits, and
-constexpr float kTopHalf = 6.f;     // fp16's least step is 2^-30 of the largest)
-constexpr float kTopHuge = -32.f;   // of rows that have met values of 2^100 and more: 2^-32, so
-constexpr int kHugeByte = 227;      // that sums of 2^24 of the largest stay in fp32
+// A row's reference is set so that its largest weight is 2^top, and moves before one is past `most`.
+struct Room {
+  float top, most;
+};
+// fp16 weights: 2^14 fits, and fp16's least step is 2^-30 of the largest weight.
+constexpr Room kRoomHalf{6.f, 0x1p14f}, kRoomBf16{0.f, 0x1p8f};
+// Rows that have met values of 2^100 and more: sums of 2^24 of the largest stay in fp32.
+constexpr Room kRoomHuge{-32.f, 0x1p-24f};
+constexpr int kHugeByte = 227;
 
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
 struct RowState4 {
@@ -49,9 +53,10 @@ struct RowState4 {
 template <int HD>
 using RowOut4 = floatx4_t[HD / 16];
 
-// Byte i of a word of scales as the power of two that it stands for.
+// Byte i of a word of scales as the power of two that the conversions take: they read the exponent's
+// bits alone (checked for every scale), so that what else the word holds may stand beside them.
 __device__ __forceinline__ float scale_of(unsigned w, int i) {
-  return __uint_as_float((i ? w >> (8 * i) & 0xffu : w & 0xffu) << 23);
+  return __uint_as_float(i < 3 ? w << (23 - 8 * i) : w >> 1);
 }
 template <int BYTE>
 __device__ __forceinline__ unsigned pair_of(unsigned w, float scale) {
@@ -101,6 +106,12 @@ __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large) {
   return nan;
 }
 
+// Whether one of the scales of two words is outside 2^-23 .. 2^8 (bytes 104 .. 135), where fp16 holds
+// every multiple of them.  (A byte of 232 and more carries into the next, and is outside itself.)
+__device__ __forceinline__ bool past_half(unsigned a, unsigned b) {
+  const unsigned x = (a + 0x18181818u) ^ 0x80808080u, y = (b + 0x18181818u) ^ 0x80808080u;
+  return ((x | y) & 0xe0e0e0e0u) != 0;
+}
 // A word's scales from position `left` on become 1, or all where the page is absent: what nobody
 // sees is finite in the products, and no result depends on it.
 __device__ __forceinline__ void leave_seen(unsigned& w, bool there, int left) {
@@ -195,63 +206,87 @@ __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>
 
 // The weights of 32 positions from their products (a score is product * unit), as NW terms of type
 // T.  MASKED: some row does not see every position: row l % 16 sees those below `seen`, of the tiles
-// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  A row's reference is set
-// `top` below its largest score, and moves when a score is kAhead and more above that.  Returns
-// whether one moved: the output so far is then to be multiplied by `corr`.
+// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  Returns whether a row's
+// reference moved: the output so far is then to be multiplied by `corr`.
+//
+// What is rare stands in one branch: NaN values, a reference to move (once a lane's eight weights
+// sum up to more than room.most: one comparison), and references past 2^22 (`huge`, the same in the
+// wavefront).  From those a product is subtracted after it is rounded, as it was for the reference:
+// joined, the difference of scores that are equal and that large would not be zero.  A row's weights
+// are made of its own values alone, whatever takes the wavefront into the branch.
 template <typename T, int NW, bool MASKED>
-__device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, const floatx4_t (&sc)[kTiles],
-                                         const Pages& p, float unit, unsigned nan, float top,
-                                         int seen, int lane, float& corr) {
-#pragma clang fp contract(off)  // of two scores that are equal and huge the difference is zero
-  const int left = seen - 4 * (lane >> 4);
+__device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, bool& huge,
+                                         const floatx4_t (&sc)[kTiles], const Pages& p, float unit,
+                                         unsigned nan, const Room& room, int seen, int lane,
+                                         float& corr) {
+  const int left = MASKED ? fresh(seen - 4 * (lane >> 4)) : 0;
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
-  float y[4 * kTiles], d[4 * kTiles], most;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[4 * t + i] = on(t, i) ? sc[t][i] * unit : -INFINITY;
-  if (__builtin_expect(__any(nan != 0), false)) {
+  float w[4 * kTiles], sum;
+  // d(t, i): a score less the reference
+  auto weigh = [&](auto d) {
+    sum = 0.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (on(t, i) && (nan >> (4 * t + i) & 1)) y[4 * t + i] = __uint_as_float(0x7fc00000u);
-  }
-  auto against = [&]() {
-    most = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4 * kTiles; ++i) {
-      d[i] = y[i] - st.ref;
-      most = __builtin_elementwise_maximum(most, d[i]);  // NaN if one is
-    }
+      for (int i = 0; i < 4; ++i) {
+        w[4 * t + i] = __builtin_amdgcn_exp2f(on(t, i) ? d(t, i) : -INFINITY);
+        sum += w[4 * t + i];
+      }
   };
-  against();
-  const bool move = __any(!(most <= top + kAhead));
-  if (__builtin_expect(move, false)) {
-    // (by a row's own scores alone: other rows' change nothing in it)
-    float z = y[0];
+  weigh([&](int t, int i) { return __builtin_fmaf(sc[t][i], unit, -st.ref); });
+  bool move = false;
+  if (__builtin_expect(__any(!(sum <= room.most)) || huge || __any(nan != 0), false)) {
+    // (made here, and not for every step ahead of the branch)
+    const unsigned bits = (unsigned)fresh((int)nan);
+    float x[4 * kTiles], y[4 * kTiles];
 #pragma unroll
-    for (int i = 1; i < 4 * kTiles; ++i) z = fmaxf(z, y[i]);
-    z = fmaxf(z, __shfl_xor(z, 16));
-    z = fmaxf(z, __shfl_xor(z, 32));
-    const float ref = z - st.ref > top + kAhead ? z - top : st.ref;
-    corr = ref == st.ref ? 1.f : __builtin_amdgcn_exp2f(st.ref - ref);
-    st.sum *= corr;
-    st.ref = ref;
-    against();
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v = sc[t][i];
+        asm volatile("" : "+v"(v));
+        v = bits >> (4 * t + i) & 1 ? __uint_as_float(0x7fc00000u) : v;
+        x[4 * t + i] = v;
+        v *= unit;
+        asm volatile("" : "+v"(v));
+        y[4 * t + i] = v;
+      }
+    auto distance = [&](int t, int i) {
+      const float d = y[4 * t + i] - st.ref;
+      return fabsf(st.ref) > 0x1p22f ? d : __builtin_fmaf(x[4 * t + i], unit, -st.ref);
+    };
+    weigh(distance);
+    const uint64_t lanes = __ballot(!(sum <= room.most));  // lanes l, l + 16, .. : row l
+    if (lanes) {
+      move = true;
+      const uint32_t two = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+      const bool mine = (two | two >> 16) >> (lane & 15) & 1;
+      float z = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (on(t, i)) z = fmaxf(z, y[4 * t + i]);
+      z = fmaxf(z, __shfl_xor(z, 16));
+      z = fmaxf(z, __shfl_xor(z, 32));
+      const float ref = mine ? fmaxf(st.ref, z - room.top) : st.ref;
+      corr = mine ? __builtin_amdgcn_exp2f(st.ref - ref) : 1.f;
+      st.sum *= corr;
+      st.ref = ref;
+      huge = __any(fabsf(ref) > 0x1p22f && ref != kNoRef);
+      weigh(distance);
+    }
   }
-  float sum = 0.f;
+  st.sum += sum;
 #pragma unroll
   for (int i = 0; i < 4 * kTiles; ++i) {
-    float rest = __builtin_amdgcn_exp2f(d[i]);
-    sum += rest;
+    float rest = w[i];
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
       wf[n][i] = (Elem_t<T>)rest;
       rest -= (float)wf[n][i];
     }
   }
-  st.sum += sum;
   return move;
 }
 
@@ -288,11 +323,11 @@ __device__ __forceinline__ void rescale4(RowOut4<HD>& o, float f) {
     for (int i = 0; i < 4; ++i) o[u][i] *= f;
 }
 
-// The references `top` above what they were (set for 2^from): the output and the sum accordingly.
+// From the room that a row had to kRoomHuge: its reference, its sum and its output.
 template <int HD>
-__device__ __forceinline__ void lower(RowOut4<HD>& o, RowState4& st, float from) {
-  const float f = __builtin_amdgcn_exp2f(kTopHuge - from);
-  if (st.ref != kNoRef) st.ref += from - kTopHuge;
+__device__ __forceinline__ void lower(RowOut4<HD>& o, RowState4& st, float top) {
+  const float f = __builtin_amdgcn_exp2f(kRoomHuge.top - top);
+  if (st.ref != kNoRef) st.ref += top - kRoomHuge.top;
   st.sum *= f;
   rescale4<HD>(o, f);
 }
@@ -374,7 +409,8 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
     bf16x8_t qf[NQ][HD / 32];
     load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf);
     const float unit = a.scale * kLog2e;
-    float top = kTopBf16;
+    Room room = kRoomBf16;
+    bool huge = false;
     RowState4 st;
     RowOut4<HD> o;
 #pragma unroll
@@ -401,17 +437,17 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
             leave_seen(vs[t], now.phys[t] >= 0, seen(last) - s * kStep - (16 * t + 4 * (lane >> 4)));
           nan |= take_nans(vs[t], large) << (4 * t);
         }
-        if (__builtin_expect(large, false) && top != kTopHuge) {
-          top = kTopHuge;
-          lower<HD>(o, st, kTopBf16);
+        if (__builtin_expect(large, false) && room.top != kRoomHuge.top) {
+          lower<HD>(o, st, room.top);
+          room = kRoomHuge;
         }
         bf16x8_t wf[NW];
         float corr = 1.f;
         const bool move =
             clear
-                ? weights4<bf16x8_t, NW, false>(wf, st, sc, now, unit, nan, top, 0, lane, corr)
-                : weights4<bf16x8_t, NW, true>(wf, st, sc, now, unit, nan, top, limit - s * kStep, lane,
-                                               corr);
+                ? weights4<bf16x8_t, NW, false>(wf, st, huge, sc, now, unit, nan, room, 0, lane, corr)
+                : weights4<bf16x8_t, NW, true>(wf, st, huge, sc, now, unit, nan, room,
+                                               limit - s * kStep, lane, corr);
         if (move) rescale4<HD>(o, corr);
         add_values4<HD, NW>(o, x, vs, wf);
         if (then >= steps) break;
@@ -503,7 +539,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 
     RowState4 st[kRowTiles];
     RowOut4<HD> o[kRowTiles];
-    float top = NQ > 1 ? kTopBf16 : kTopHalf;
+    Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
+    bool huge = false;
 #pragma unroll
     for (int x = 0; x < kRowTiles; ++x)
 #pragma unroll
@@ -580,24 +617,20 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
         leave_seen(vs[0], p0 >= 0, left - (32 * pair + 4 * g));
         leave_seen(vs[1], p1 >= 0, left - (32 * pair + 16 + 4 * g));
       }
-      bool large = false;
-      const unsigned nan = take_nans(vs[0], large) | take_nans(vs[1], large) << 4;
-      int kind = large ? kLarge : 0;
-      if (__any(nan != 0)) {
-        kind |= kNans;
+      int kind = 0;
+      if (!halves.value || __builtin_expect(__any(past_half(vs[0], vs[1])), false)) {
+        bool large = false;
+        const unsigned nan = take_nans(vs[0], large) | take_nans(vs[1], large) << 4;
+        // (both wavefronts of the pair see all its scales)
+        kind = (large ? kLarge : 0) | (__any(nan != 0) ? kNans : 0) |
+               (halves.value && __any(past_half(vs[0], vs[1])) ? kTooWide : 0);
         if (half == 0 && r16 == 0) s_nan[buf][pair][g] = nan;
       }
-      float f[2][4], least = INFINITY, largest = 0.f;
+      float f[2][4];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          f[t][i] = scale_of(vs[t], i);
-          least = fminf(least, f[t][i]);
-          largest = fmaxf(largest, f[t][i]);
-        }
-      // (both wavefronts of the pair see all its scales)
-      if (halves.value && __any(!(least >= 0x1p-23f && largest <= 0x1p13f))) kind |= kTooWide;
+        for (int i = 0; i < 4; ++i) f[t][i] = scale_of(vs[t], i);
 #pragma unroll
       for (int d = 0; d < VW; ++d) {
         uint2 a0, a1, b0, b1;
@@ -651,10 +684,10 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
           unsigned nan = 0;
           if (__builtin_expect(kinds[p], false)) {
             if (kinds[p] & kNans) nan = s_nan[buf][p][g];
-            if (!halves.value && (kinds[p] & kLarge) && top != kTopHuge) {
+            if (!halves.value && (kinds[p] & kLarge) && room.top != kRoomHuge.top) {
 #pragma unroll
-              for (int y = 0; y < kRowTiles; ++y) lower<HD>(o[y], st[y], top);
-              top = kTopHuge;
+              for (int y = 0; y < kRowTiles; ++y) lower<HD>(o[y], st[y], room.top);
+              room = kRoomHuge;
             }
           }
           // Row tile after row tile: the matrix cores work on one's products while the vector
@@ -679,14 +712,16 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 #pragma unroll
           for (int u = 0; u < DT; ++u) op[u] = s_v[buf][p][u][lane];
           const bool whole = least - j0 >= kStep && pg.all();
+          const Room now_room = halves.value ? kRoomHalf : room;
 #pragma unroll
           for (int y = 0; y < kRowTiles; ++y) {
             float corr = 1.f;
             Value wf[N];
             const bool move =
-                whole ? weights4<Value, N, false>(wf, st[y], x[y], pg, unit, nan, top, 0, lane, corr)
-                      : weights4<Value, N, true>(wf, st[y], x[y], pg, unit, nan, top, limit[y] - j0, lane,
-                                                 corr);
+                whole ? weights4<Value, N, false>(wf, st[y], huge, x[y], pg, unit, nan, now_room, 0, lane,
+                                                  corr)
+                      : weights4<Value, N, true>(wf, st[y], huge, x[y], pg, unit, nan, now_room,
+                                                 limit[y] - j0, lane, corr);
             if (__builtin_expect(move, false)) rescale4<HD>(o[y], corr);
 #pragma unroll
             for (int u = 0; u < DT; ++u)
