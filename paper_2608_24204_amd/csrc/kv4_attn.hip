@@ -106,11 +106,10 @@ __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large) {
   return nan;
 }
 
-// Whether one of the scales of two words is outside 2^-23 .. 2^8 (bytes 104 .. 135), where fp16 holds
+// Whether one of a word's scales is outside 2^-23 .. 2^8 (bytes 104 .. 135), where fp16 holds
 // every multiple of them.  (A byte of 232 and more carries into the next, and is outside itself.)
-__device__ __forceinline__ bool past_half(unsigned a, unsigned b) {
-  const unsigned x = (a + 0x18181818u) ^ 0x80808080u, y = (b + 0x18181818u) ^ 0x80808080u;
-  return ((x | y) & 0xe0e0e0e0u) != 0;
+__device__ __forceinline__ bool past_half(unsigned w) {
+  return ((w + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u;
 }
 // A word's scales from position `left` on become 1, or all where the page is absent: what nobody
 // sees is finite in the products, and no result depends on it.
@@ -126,15 +125,17 @@ struct Step4 {
   unsigned k[kTiles][HD / 32], ks[kTiles];  // position l % 16, dimensions (HD / 4) (l / 16) ..
   unsigned v[kTiles][HD / 32], vs[kTiles];  // positions 4 (l / 16) .. + 3, dimensions (HD / 16) (l % 16) ..
 };
-template <int HD>
-__device__ __forceinline__ void fetch_codes(unsigned (&w)[HD / 32], __amdgpu_buffer_rsrc_t r,
-                                            int lane_at, int at) {
-  if constexpr (HD == 128) {
+template <int N>
+__device__ __forceinline__ void fetch_words(unsigned (&w)[N], __amdgpu_buffer_rsrc_t r, int lane_at,
+                                            int at) {
+  if constexpr (N == 4) {
     const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0);
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-  } else {
+  } else if constexpr (N == 2) {
     const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0);
     w[0] = v[0]; w[1] = v[1];
+  } else {
+    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane_at, at, 0);
   }
 }
 // One KV head of a pool: its key block in page 0, and the bytes from page to page and from a
@@ -160,7 +161,7 @@ __device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const Hea
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0);
-    fetch_codes<HD>(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
+    fetch_words(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
     s.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(b, pos * (HD / kKv4Group) + d / kKv4Group,
                                                   kv4_key_scale_at(slot, 0, page, HD), 0);
   }
@@ -173,7 +174,7 @@ __device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const H
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 1);
-    fetch_codes<HD>(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
+    fetch_words(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
     s.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, pos * (HD / kKv4Group) + 4 * (d / kKv4Group),
                                                    kv4_value_scale_at(slot, 0, page, HD), 0);
   }
@@ -500,16 +501,17 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
 // read them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers:
 // the next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
 // parts a buffer's readers from its next writers.
-template <int HD, int NQ, int NW, int kRowTiles>
-__global__ __launch_bounds__(256)
-__attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+template <int HD, int NQ, int NW, int kRowTiles, int kWaves>
+__global__ __launch_bounds__(64 * kWaves)
+__attribute__((amdgpu_waves_per_eu(kWaves == 8 && kRowTiles == 1 ? 4 : 2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                             int ntile) {
-  constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles, VW = HD / 64;
+  constexpr int DS = HD / 32, DT = HD / 16, kRows = kWaves * 16 * kRowTiles;
+  constexpr int kParts = kWaves / kChunkTiles, PW = DS / kParts;  // wavefronts a tile, words of one
   enum Kind { kTooWide = 1, kNans = 2, kLarge = 4 };
   __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
   __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
-  __shared__ int s_kind[2][kChunkTiles / 2];         // of the values of two tiles: Kind,
-  __shared__ unsigned s_nan[2][kChunkTiles / 2][4];  // and which are NaN, by lane / 16
+  __shared__ __align__(16) int s_kind[2][kChunkTiles];         // of a tile's values: Kind,
+  __shared__ unsigned s_nan[2][kChunkTiles][4];  // and which are NaN, by lane / 16
   const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
   const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -546,11 +548,11 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 #pragma unroll
       for (int u = 0; u < DT; ++u) o[x][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
-    // what this wavefront brings of a chunk: the keys of tile `wave`; of the pair of tiles
-    // wave / 2 the values of half of each lane's dimensions
-    unsigned kc[DS], ks, vc[2][VW], vs[2];
+    // what this wavefront brings of a chunk: keys and values of one tile, all or half of each
+    // lane's dimensions
+    unsigned kc[PW], ks, vc[PW], vs;
     int phys[kChunkTiles], later[kChunkTiles];
-    const int pair = wave >> 1, half = wave & 1;
+    const int mine_t = wave / kParts, part = wave % kParts;
     const bool whole_chunk = c.page_shift >= 6;  // one page holds a chunk
     auto find = [&](int chunk) {
       later[0] = entry(c, q, (uint32_t)chunk * kChunkPos);
@@ -572,74 +574,48 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
         const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
         return lo ^ ((lo ^ hi) & -(t >> 1));
       };
-      auto keys = [&](__amdgpu_buffer_rsrc_t b, int slot) {
-        const int d = g * (HD / 4);
-        fetch_codes<HD>(kc, b, kv4_key_at(r16, d, HD), kv4_key_at(slot, 0, HD));
-        ks = __builtin_amdgcn_raw_buffer_load_b8(b, r16 * (HD / kKv4Group) + d / kKv4Group,
-                                                 kv4_key_scale_at(slot, 0, page, HD), 0);
-      };
-      auto values = [&](int t, __amdgpu_buffer_rsrc_t b, int slot) {
-        const int d = r16 * (HD / 16) + half * (HD / 32);
-        const int at = kv4_value_at(4 * g, d, HD), from = kv4_value_at(slot, 0, HD);
-        if constexpr (VW == 2) {
-          const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, at, from, 0);
-          vc[t][0] = w[0];
-          vc[t][1] = w[1];
-        } else {
-          vc[t][0] = __builtin_amdgcn_raw_buffer_load_b32(b, at, from, 0);
-        }
-        vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, 4 * g * (HD / kKv4Group) + 4 * (d / kKv4Group),
-                                                     kv4_value_scale_at(slot, 0, page, HD), 0);
-      };
-      if (whole_chunk) {
-        const int slot = j0 & (page - 1);
-        keys(kv.buffer(c, p[0], 0), slot + 16 * wave);
-        const __amdgpu_buffer_rsrc_t b = kv.buffer(c, p[0], 1);
-        values(0, b, slot + 32 * pair);
-        values(1, b, slot + 32 * pair + 16);
-      } else {
-        keys(kv.buffer(c, pick(wave), 0), (j0 + 16 * wave) & (page - 1));
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          values(t, kv.buffer(c, pick(2 * pair + t), 1), (j0 + 32 * pair + 16 * t) & (page - 1));
-      }
+      const int phys = whole_chunk ? p[0] : pick(mine_t), slot = (j0 + 16 * mine_t) & (page - 1);
+      const __amdgpu_buffer_rsrc_t kb = kv.buffer(c, phys, 0), vb = kv.buffer(c, phys, 1);
+      const int dk = g * (HD / 4) + part * (8 * PW), dv = r16 * (HD / 16) + part * (2 * PW);
+      fetch_words(kc, kb, kv4_key_at(r16, dk, HD), kv4_key_at(slot, 0, HD));
+      ks = __builtin_amdgcn_raw_buffer_load_b8(kb, r16 * (HD / kKv4Group) + dk / kKv4Group,
+                                               kv4_key_scale_at(slot, 0, page, HD), 0);
+      fetch_words(vc, vb, kv4_value_at(4 * g, dv, HD), kv4_value_at(slot, 0, HD));
+      vs = __builtin_amdgcn_raw_buffer_load_b32(vb, 4 * g * (HD / kKv4Group) + 4 * (dv / kKv4Group),
+                                                kv4_value_scale_at(slot, 0, page, HD), 0);
     };
     // The operands of the chunk that is here; whether the values' scales do for `halves`.
     auto convert = [&](int buf, int ch, const int (&now)[kChunkTiles], auto halves) {
       const float scale = __uint_as_float(ks << 23);
 #pragma unroll
-      for (int d = 0; d < DS; ++d)
-        s_k[buf][wave][d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
+      for (int d = 0; d < PW; ++d)
+        s_k[buf][mine_t][part * PW + d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
       // (in the last chunk, and in pages that are not there)
       const int left = all - ch * kChunkPos;
-      const int p0 = now[0] ^ ((now[0] ^ now[2]) & -pair), p1 = now[1] ^ ((now[1] ^ now[3]) & -pair);
-      if (left < kChunkPos || (p0 | p1) < 0) {
-        leave_seen(vs[0], p0 >= 0, left - (32 * pair + 4 * g));
-        leave_seen(vs[1], p1 >= 0, left - (32 * pair + 16 + 4 * g));
-      }
+      const int lo = now[0] ^ ((now[0] ^ now[1]) & -(mine_t & 1)), hi = now[2] ^ ((now[2] ^ now[3]) & -(mine_t & 1));
+      const int there = lo ^ ((lo ^ hi) & -(mine_t >> 1));
+      if (left < kChunkPos || there < 0) leave_seen(vs, there >= 0, left - (16 * mine_t + 4 * g));
       int kind = 0;
-      if (!halves.value || __builtin_expect(__any(past_half(vs[0], vs[1])), false)) {
+      if (!halves.value || __builtin_expect(__any(past_half(vs)), false)) {
         bool large = false;
-        const unsigned nan = take_nans(vs[0], large) | take_nans(vs[1], large) << 4;
-        // (both wavefronts of the pair see all its scales)
+        const unsigned nan = take_nans(vs, large);
+        // (both wavefronts of a tile see all its scales)
         kind = (large ? kLarge : 0) | (__any(nan != 0) ? kNans : 0) |
-               (halves.value && __any(past_half(vs[0], vs[1])) ? kTooWide : 0);
-        if (half == 0 && r16 == 0) s_nan[buf][pair][g] = nan;
+               (halves.value && __any(past_half(vs)) ? kTooWide : 0);
+        if (part == 0 && r16 == 0) s_nan[buf][mine_t][g] = nan;
       }
-      float f[2][4];
+      float f[4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < 4; ++i) f[i] = scale_of(vs, i);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[t][i] = scale_of(vs[t], i);
-#pragma unroll
-      for (int d = 0; d < VW; ++d) {
-        uint2 a0, a1, b0, b1;
-        values4<halves.value>(vc[0][d], f[0], a0, b0);
-        values4<halves.value>(vc[1][d], f[1], a1, b1);
-        s_v[buf][pair][2 * (half * VW + d)][lane] = make_uint4(a0.x, a0.y, a1.x, a1.y);
-        s_v[buf][pair][2 * (half * VW + d) + 1][lane] = make_uint4(b0.x, b0.y, b1.x, b1.y);
+      for (int d = 0; d < PW; ++d) {
+        uint2 lo2, hi2;
+        values4<halves.value>(vc[d], f, lo2, hi2);
+        uint4* to = &s_v[buf][mine_t >> 1][2 * (part * PW + d)][lane];
+        reinterpret_cast<uint2*>(to)[mine_t & 1] = lo2;
+        reinterpret_cast<uint2*>(to + 64)[mine_t & 1] = hi2;
       }
-      if (half == 0 && lane == 0) s_kind[buf][pair] = kind;
+      if (part == 0 && lane == 0) s_kind[buf][mine_t] = kind;
     };
 
     bf16x8_t qf[kRowTiles][NQ][DS];
@@ -672,7 +648,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
         convert(buf, ch, now, halves);
         if (ch + 1 < c1) bring(phys, ch + 1);
         __syncthreads();
-        const int kinds[2] = {uniform(s_kind[buf][0]), uniform(s_kind[buf][1])};
+        const int4 k4 = *reinterpret_cast<const int4*>(s_kind[buf]);
+        const int kinds[2] = {uniform(k4.x | k4.y), uniform(k4.z | k4.w)};
         if (halves.value && __builtin_expect((kinds[0] | kinds[1]) & kTooWide, false)) return ch;
         if (ch * kChunkPos >= most) continue;  // past this wavefront's rows
 #pragma unroll
@@ -683,7 +660,10 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
           for (int t = 0; t < kTiles; ++t) pg.phys[t] = now[2 * p + t];
           unsigned nan = 0;
           if (__builtin_expect(kinds[p], false)) {
-            if (kinds[p] & kNans) nan = s_nan[buf][p][g];
+            if (kinds[p] & kNans)
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t)
+                if (uniform(s_kind[buf][2 * p + t]) & kNans) nan |= s_nan[buf][2 * p + t][g] << (4 * t);
             if (!halves.value && (kinds[p] & kLarge) && room.top != kRoomHuge.top) {
 #pragma unroll
               for (int y = 0; y < kRowTiles; ++y) lower<HD>(o[y], st[y], room.top);
@@ -779,10 +759,10 @@ static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStr
 #define WICI_ATTN(...) \
   launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
   if (p.row_tiles == 2) {
-    WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 2>);
+    WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 2, 4>);
   } else if (p.row_tiles == 1) {
-    if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1>);
-    else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1>);
+    if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1, 4>);
+    else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1, 4>);
   } else {
     if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2>);
     else WICI_ATTN(k_kv4_attn_split<HD, 3, 3>);
