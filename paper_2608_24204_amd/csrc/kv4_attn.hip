@@ -148,19 +148,21 @@ struct HeadAt4 {
       : base(q.base + kv4_block_at(0, 0, h, c.n_kv, 1 << c.page_shift, HD)),
         page(2 * c.n_kv * (uint32_t)kv4_block_bytes(1 << c.page_shift, HD)),
         values(page / 2) {}
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const Kv8& c, int phys, int which) const {
+  // (on: false reads as zeros, from no memory)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const Kv8& c, int phys, int which,
+                                                           bool on = true) const {
     return rsrc(base + (uint64_t)(uint32_t)max(phys, 0) * page + (which ? values : 0),
-                kv4_block_bytes(1 << c.page_shift, HD));
+                on ? kv4_block_bytes(1 << c.page_shift, HD) : 0);
   }
 };
 template <int HD>
 __device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const HeadAt4<HD>& at,
-                                           const Pages& p, int step, int lane) {
+                                           const Pages& p, int step, int lane, bool on) {
   const int page = 1 << c.page_shift, pos = lane & 15, d = (lane >> 4) * (HD / 4);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
-    const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0);
+    const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0, on);
     fetch_words(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
     s.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(b, pos * (HD / kKv4Group) + d / kKv4Group,
                                                   kv4_key_scale_at(slot, 0, page, HD), 0);
@@ -292,10 +294,10 @@ __device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, bool& huge,
 }
 
 // O^T += V^T W^T of one step; vs: the scales, NaN ones replaced.
-template <int HD, int NW>
+template <int HD, typename T, int NW>
 __device__ __forceinline__ void add_values4(RowOut4<HD>& o, const Step4<HD>& s,
-                                            const unsigned (&vs)[kTiles],
-                                            const bf16x8_t (&wf)[NW]) {
+                                            const unsigned (&vs)[kTiles], const T (&wf)[NW]) {
+  constexpr bool kHalf = std::is_same<T, half8_t>::value;
   float f[kTiles][4];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
@@ -304,14 +306,14 @@ __device__ __forceinline__ void add_values4(RowOut4<HD>& o, const Step4<HD>& s,
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) {
     uint2 a0, a1, b0, b1;
-    values4<false>(s.v[0][d], f[0], a0, b0);
-    values4<false>(s.v[1][d], f[1], a1, b1);
-    const bf16x8_t a = __builtin_bit_cast(bf16x8_t, make_uint4(a0.x, a0.y, a1.x, a1.y));
-    const bf16x8_t b = __builtin_bit_cast(bf16x8_t, make_uint4(b0.x, b0.y, b1.x, b1.y));
+    values4<kHalf>(s.v[0][d], f[0], a0, b0);
+    values4<kHalf>(s.v[1][d], f[1], a1, b1);
+    const T a = __builtin_bit_cast(T, make_uint4(a0.x, a0.y, a1.x, a1.y));
+    const T b = __builtin_bit_cast(T, make_uint4(b0.x, b0.y, b1.x, b1.y));
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
-      o[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, wf[n], o[2 * d], 0, 0, 0);
-      o[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, wf[n], o[2 * d + 1], 0, 0, 0);
+      o[2 * d] = product(a, wf[n], o[2 * d]);
+      o[2 * d + 1] = product(b, wf[n], o[2 * d + 1]);
     }
   }
 }
@@ -410,7 +412,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
     bf16x8_t qf[NQ][HD / 32];
     load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf);
     const float unit = a.scale * kLog2e;
-    Room room = kRoomBf16;
+    Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
     bool huge = false;
     RowState4 st;
     RowOut4<HD> o;
@@ -418,45 +420,65 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
     for (int u = 0; u < HD / 16; ++u) o[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     if (s < steps) {
       Step4<HD> x;
-      Pages now = named(c, e0);
+      Pages now = named(c, e0), next;
       Entries later = e1;
-      load_keys4<HD>(x, c, kv, now, s, lane);
+      floatx4_t sc[kTiles];
+      bool scored = false;  // this step's scores are made, and the next one's keys requested
+      load_keys4<HD>(x, c, kv, now, s, lane, true);
       load_values4<HD>(x, c, kv, now, s, lane);
-      for (;;) {
-        floatx4_t sc[kTiles];
-        scores4<HD, NQ>(sc, x, qf);
-        const int then = s + stride;
-        const Pages next = named(c, later);
-        if (then < steps) load_keys4<HD>(x, c, kv, next, then, lane);
-        unsigned vs[kTiles], nan = 0;
-        bool large = false;
-        const bool clear = s < whole && now.all();
+      // The steps from here on, with the values and weights as halves or as NW bf16 terms; returns
+      // whether none is left: halves end before the first step whose values do not fit them.
+      auto take = [&](auto halves) -> bool {
+        typedef std::conditional_t<halves.value, half8_t, bf16x8_t> Value;
+        constexpr int N = halves.value ? 1 : NW;
+        for (;;) {
+          const int then = s + stride;
+          if (halves.value || !scored) {
+            scores4<HD, NQ>(sc, x, qf);
+            next = named(c, later);
+            // (in any case: what follows would else wait for whatever may be requested here)
+            load_keys4<HD>(x, c, kv, next, then, lane, then < steps);
+          }
+          scored = false;
+          const bool clear = s < whole && now.all();
+          unsigned vs[kTiles], nan = 0;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          vs[t] = x.vs[t];
-          if (!clear)
-            leave_seen(vs[t], now.phys[t] >= 0, seen(last) - s * kStep - (16 * t + 4 * (lane >> 4)));
-          nan |= take_nans(vs[t], large) << (4 * t);
-        }
-        if (__builtin_expect(large, false) && room.top != kRoomHuge.top) {
-          lower<HD>(o, st, room.top);
-          room = kRoomHuge;
-        }
-        bf16x8_t wf[NW];
-        float corr = 1.f;
-        const bool move =
-            clear
-                ? weights4<bf16x8_t, NW, false>(wf, st, huge, sc, now, unit, nan, room, 0, lane, corr)
-                : weights4<bf16x8_t, NW, true>(wf, st, huge, sc, now, unit, nan, room,
+          for (int t = 0; t < kTiles; ++t) {
+            vs[t] = x.vs[t];
+            if (!clear)
+              leave_seen(vs[t], now.phys[t] >= 0, seen(last) - s * kStep - (16 * t + 4 * (lane >> 4)));
+          }
+          if (!halves.value || __builtin_expect(__any(past_half(vs[0]) || past_half(vs[1])), false)) {
+            bool large = false;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) nan |= take_nans(vs[t], large) << (4 * t);
+            if (halves.value && __any(past_half(vs[0]) || past_half(vs[1]))) {
+              scored = true;
+              return false;
+            }
+            if (__builtin_expect(large, false) && room.top != kRoomHuge.top) {
+              lower<HD>(o, st, room.top);
+              room = kRoomHuge;
+            }
+          }
+          const Room now_room = halves.value ? kRoomHalf : room;
+          Value wf[N];
+          float corr = 1.f;
+          const bool move =
+              clear ? weights4<Value, N, false>(wf, st, huge, sc, now, unit, nan, now_room, 0, lane, corr)
+                    : weights4<Value, N, true>(wf, st, huge, sc, now, unit, nan, now_room,
                                                limit - s * kStep, lane, corr);
-        if (move) rescale4<HD>(o, corr);
-        add_values4<HD, NW>(o, x, vs, wf);
-        if (then >= steps) break;
-        load_values4<HD>(x, c, kv, next, then, lane);
-        now = next;
-        later = find(c, q, then + stride);
-        s = then;
-      }
+          if (__builtin_expect(move, false)) rescale4<HD>(o, corr);
+          add_values4<HD>(o, x, vs, wf);
+          if (then >= steps) return true;
+          load_values4<HD>(x, c, kv, next, then, lane);
+          now = next;
+          later = find(c, q, then + stride);
+          s = then;
+        }
+      };
+      if (NQ > 1 || __builtin_expect(!take(std::integral_constant<bool, true>()), false))
+        take(std::integral_constant<bool, false>());
     }
     // join the wavefronts
     st.sum += __shfl_xor(st.sum, 16);

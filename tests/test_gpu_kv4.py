@@ -6,10 +6,10 @@ bf16 result with the rounding of that answer).  Attention: with S the largest su
 of a row and A the output with |v| in place of v, a score is off by at most e = 64 2^-24 S + 2^-20
 (a sum of 128 products in fp32, with the roundings of a third bf16 term of the query, of the
 factor and of the difference; the exponential's argument and result), which moves a weight and the
-sum by e each; a weight is off by at most 2^-24 of itself (three bf16 terms), for bf16 rows 2^-16 (two:
-half a step is 2^-8, twice), and for bf16 rows of prompts 2^-11 (one fp16 term) or 2^-31 of the row's
-largest weight (half of fp16's least step, 2^-24, with that at 2^6 or more: n 2^-31 of the largest |v| at
-most in all); the sums over n positions add at most (64 + n / 16) roundings of
+sum by e each; a weight is off by at most 2^-24 of itself (three bf16 terms), for bf16 rows 2^-11 (one
+fp16 term; two bf16 terms where the values' scales do not fit fp16: 2^-16) or 2^-31 of the row's largest
+weight (half of fp16's least step, 2^-24, with that at 2^6 or more: n 2^-31 of the largest |v| at most
+in all); the sums over n positions add at most (64 + n / 16) roundings of
 2^-24 A, and those of several terms as many again; and the result is rounded once, by eps / 2 of
 itself.  Weights are fp32 (and their terms bf16) with the largest at 1 or more: one below 2^-126, or a
 term below it, may count as zero, which is off by at most 2^-126 |v| a position and term, of a sum
@@ -59,13 +59,13 @@ def sub_batch(lens, rows, start):
     return bt
 
 
-def tolerance(want, mag, dots, n, single, out_dtype, top=0.0, prompt=False):
+def tolerance(want, mag, dots, n, single, out_dtype, top=0.0):
     """top: the largest |v| that each row sees (broadcast to `want`)."""
     e = 64 * 2.0 ** -24 * dots + 2.0 ** -20
-    weight = 2.0 ** -24 if not single else 2.0 ** -11 if prompt else 2.0 ** -16
+    weight = 2.0 ** -11 if single else 2.0 ** -24
     rel = 2 * e + weight + 2 * (64 + n / 16) * 2.0 ** -24
     lost = 3 * n * (2.0 ** -126 + (top >= 2.0 ** 100) * 2.0 ** -94) + \
-        (n * 2.0 ** -31 if single and prompt else 0.0)
+        (n * 2.0 ** -31 if single else 0.0)
     return mag * rel[..., None] + abs(want) * (torch.finfo(out_dtype).eps / 2) + lost * top + 1e-30
 
 
@@ -73,7 +73,6 @@ def check_attend(bt, q, out, K, V, scale, seen=None):
     """out [n_rows, heads, hd] of q against the definition, for every row of the batch."""
     qn, on = f64(q), f64(out)
     single = q.dtype == BF16 and out.dtype == BF16
-    prompt = max(bt.rows) > 1
     for b, (n, r) in enumerate(zip(bt.lens, bt.rows)):
         at = slice(bt.start[b], bt.start[b] + r)
         pos = np.arange(n - r, n)
@@ -84,7 +83,7 @@ def check_attend(bt, q, out, K, V, scale, seen=None):
         if not r:
             continue
         top = np.where(sees, np.abs(V[b]).max((1, 2))[None], 0.0).max(1)[:, None, None]
-        tol = tolerance(want, mag, dots, n, single, out.dtype, top, prompt)
+        tol = tolerance(want, mag, dots, n, single, out.dtype, top)
         err = np.abs(on[at] - want)
         assert np.all(err <= tol), (b, float(np.max(err / tol)))
 
@@ -254,7 +253,7 @@ def check_on_gpu(bt, q, out, K, V):
         want, mag = p @ v, p @ v.abs()
         dots = (qq.abs() @ k.abs().transpose(-1, -2).contiguous()).amax(-1) * hd ** -0.5
         top = v.abs().amax(-1).cummax(-1).values[..., n - r:, None]
-        tol = tolerance(want, mag, dots, n, dtype == BF16, out.dtype, top, True)
+        tol = tolerance(want, mag, dots, n, dtype == BF16, out.dtype, top)
         err = (out[at].double().view(r, n_kv, G, hd).permute(1, 2, 0, 3) - want).abs()
         assert (err <= tol).all(), (b, float((err / tol).max()))
 
@@ -456,7 +455,7 @@ def test_scores_past_the_range(ops, dtype, rows):
         want, mag, dots = oracle.attend_rows(f64(qq[:late, 1:]), K[0], V[0],
                                              (np.arange(700)[None] <= (700 - n + np.arange(late))[:, None]) & keep,
                                              0.125)
-        tol = tolerance(want, mag, dots, 700, dtype == BF16, dtype, 10.0, True)
+        tol = tolerance(want, mag, dots, 700, dtype == BF16, dtype, 10.0)
         assert np.all(np.abs(f64(out[:late, 1:]) - want) <= tol)
     k[:, 0, 0] = 2e38
     bt.store(k, v)
