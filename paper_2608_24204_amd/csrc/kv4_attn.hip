@@ -125,17 +125,19 @@ struct Step4 {
   unsigned k[kTiles][HD / 32], ks[kTiles];  // position l % 16, dimensions (HD / 4) (l / 16) ..
   unsigned v[kTiles][HD / 32], vs[kTiles];  // positions 4 (l / 16) .. + 3, dimensions (HD / 16) (l % 16) ..
 };
-template <int N>
+// (ONCE: not kept in the caches.)
+template <bool ONCE = false, int N>
 __device__ __forceinline__ void fetch_words(unsigned (&w)[N], __amdgpu_buffer_rsrc_t r, int lane_at,
                                             int at) {
+  constexpr int kNonTemporal = ONCE ? 2 : 0;
   if constexpr (N == 4) {
-    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, 0);
+    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, at, kNonTemporal);
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
   } else if constexpr (N == 2) {
-    const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, 0);
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_at, at, kNonTemporal);
     w[0] = v[0]; w[1] = v[1];
   } else {
-    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane_at, at, 0);
+    w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane_at, at, kNonTemporal);
   }
 }
 // One KV head of a pool: its key block in page 0, and the bytes from page to page and from a
@@ -155,7 +157,7 @@ struct HeadAt4 {
                 on ? kv4_block_bytes(1 << c.page_shift, HD) : 0);
   }
 };
-template <int HD>
+template <int HD, bool ONCE>
 __device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const HeadAt4<HD>& at,
                                            const Pages& p, int step, int lane, bool on) {
   const int page = 1 << c.page_shift, pos = lane & 15, d = (lane >> 4) * (HD / 4);
@@ -163,12 +165,12 @@ __device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const Hea
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0, on);
-    fetch_words(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
+    fetch_words<ONCE>(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
     s.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(b, pos * (HD / kKv4Group) + d / kKv4Group,
                                                   kv4_key_scale_at(slot, 0, page, HD), 0);
   }
 }
-template <int HD>
+template <int HD, bool ONCE>
 __device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const HeadAt4<HD>& at,
                                              const Pages& p, int step, int lane) {
   const int page = 1 << c.page_shift, pos = 4 * (lane >> 4), d = (lane & 15) * (HD / 16);
@@ -176,7 +178,7 @@ __device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const H
   for (int t = 0; t < kTiles; ++t) {
     const int slot = (step * kStep + 16 * t) & (page - 1);
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 1);
-    fetch_words(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
+    fetch_words<ONCE>(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
     s.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, pos * (HD / kKv4Group) + 4 * (d / kKv4Group),
                                                    kv4_value_scale_at(slot, 0, page, HD), 0);
   }
@@ -375,7 +377,8 @@ __device__ __forceinline__ void load_queries4(const HeadRows& q, int64_t at, boo
 // (row r: new row r / G, query head r % G), and are joined at the end.  Splits take
 // groups of four steps in turn, so one launch serves any length evenly.  With one
 // split the output is written here, otherwise (ref, sum, output) is left for the merge.
-template <int HD, int NQ, int NW>
+// ONCE: nobody reads a code again.
+template <int HD, int NQ, int NW, bool ONCE>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_attn_split(
     Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit, int ntile) {
@@ -424,8 +427,8 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
       Entries later = e1;
       floatx4_t sc[kTiles];
       bool scored = false;  // this step's scores are made, and the next one's keys requested
-      load_keys4<HD>(x, c, kv, now, s, lane, true);
-      load_values4<HD>(x, c, kv, now, s, lane);
+      load_keys4<HD, ONCE>(x, c, kv, now, s, lane, true);
+      load_values4<HD, ONCE>(x, c, kv, now, s, lane);
       // The steps from here on, with the values and weights as halves or as NW bf16 terms; returns
       // whether none is left: halves end before the first step whose values do not fit them.
       auto take = [&](auto halves) -> bool {
@@ -437,7 +440,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
             scores4<HD, NQ>(sc, x, qf);
             next = named(c, later);
             // (in any case: what follows would else wait for whatever may be requested here)
-            load_keys4<HD>(x, c, kv, next, then, lane, then < steps);
+            load_keys4<HD, ONCE>(x, c, kv, next, then, lane, then < steps);
           }
           scored = false;
           const bool clear = s < whole && now.all();
@@ -471,7 +474,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
           if (__builtin_expect(move, false)) rescale4<HD>(o, corr);
           add_values4<HD>(o, x, vs, wf);
           if (then >= steps) return true;
-          load_values4<HD>(x, c, kv, next, then, lane);
+          load_values4<HD, ONCE>(x, c, kv, next, then, lane);
           now = next;
           later = find(c, q, then + stride);
           s = then;
@@ -786,8 +789,17 @@ static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStr
     if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1, 4>);
     else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1, 4>);
   } else {
-    if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2>);
-    else WICI_ATTN(k_kv4_attn_split<HD, 3, 3>);
+    // Codes that one tile of rows reads are read past the caches (heads of 128: 48 tokens at up to
+    // 4000 positions 42.4 us for 46.0, 32 at 16384 103.6 for 119; heads of 64: 34.4 for 32.6, so
+    // not there; 4 x 16 rows, four tiles, of 8000 31.9 for 29.9).
+    constexpr bool kMay = HD == 128;
+    if (kMay && p.ntile == 1) {
+      if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2, kMay>);
+      else WICI_ATTN(k_kv4_attn_split<HD, 3, 3, kMay>);
+    } else {
+      if (single) WICI_ATTN(k_kv4_attn_split<HD, 1, 2, false>);
+      else WICI_ATTN(k_kv4_attn_split<HD, 3, 3, false>);
+    }
   }
 #undef WICI_ATTN
   if (p.nsplit > 1) return launch_kv_attn_merge(HD, c, r, a, p.nsplit, st, last & kLast);
