@@ -20,9 +20,9 @@ def beam_select(logits, scores, k):
         top = z.max()
         if top == -np.inf:
             continue
-        lse = top + np.log(np.exp(z - top).sum())
+        lse = np.log(np.exp(z - top).sum())
         best = np.lexsort((np.arange(len(z)), -z))[:k]
-        found += [(-(c + (z[v] - lse)), i, r, int(v)) for r, v in enumerate(best) if z[v] > -np.inf]
+        found += [(-(c + ((z[v] - top) - lse)), i, r, int(v)) for r, v in enumerate(best) if z[v] > -np.inf]
     found = sorted(found)[:k]
     out = np.full(k, -np.inf), np.full(k, -1), np.full(k, -1)
     for r, (s, i, _, v) in enumerate(found):

@@ -1,8 +1,9 @@
 // Beam search: the k best continuations of each search, and the caches' pages put in their order.
 //
 // A continuation of beam i (score c_i, logits z_i) by word v has the score
-//   s_iv = c_i + z_iv - L_i,   L_i = log sum_u e^(z_iu),
-// and of all (i, v) of a search the k greatest are chosen, equal ones by the lowest (i, v).
+//   s_iv = c_i + ((z_iv - m_i) - L_i),   m_i = max_u z_iu,   L_i = log sum_u e^(z_iu - m_i),
+// and of all (i, v) of a search the k greatest are chosen, equal ones by the lowest (i, v).  (In this
+// order beams whose logits are alike up to a constant have equal scores, not nearly equal ones.)
 //
 // Within a beam the order is that of the logits and needs no L_i; between beams it does, and two
 // continuations may be as near each other as numbers of 24 bits get: L_i and s_iv are formed in 64
@@ -66,23 +67,22 @@ struct Logits {
   }
 };
 
-// e^x for x <= 0 to 2^-37 of itself (what is below e^-200 counts as that): x = n ln 2 + r with
-// |r| <= ln 2 / 2, and the first ten terms of e^r, of which the next is (ln 2 / 2)^10 / 10! = 7e-12.
+// e^x for x <= 0 to 2^-34 of itself (what is below e^-200 counts as that): x = n ln 2 + r with
+// |r| <= ln 2 / 2, and the polynomial of degree 7 that meets e^r at the eight Chebyshev nodes of that
+// range.  Added to 1.5 2^52, n stands in the sum's low bits.
 __device__ __forceinline__ double exp_below(double x) {
   x = fmax(x, -200.0);
-  const double n = __builtin_rint(x * 1.4426950408889634074);
-  const double r = __builtin_fma(n, -0.69314718055994530942, x);
-  double p = 1.0 / 362880;
-  p = __builtin_fma(p, r, 1.0 / 40320);
-  p = __builtin_fma(p, r, 1.0 / 5040);
-  p = __builtin_fma(p, r, 1.0 / 720);
-  p = __builtin_fma(p, r, 1.0 / 120);
-  p = __builtin_fma(p, r, 1.0 / 24);
-  p = __builtin_fma(p, r, 1.0 / 6);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  return __builtin_ldexp(p, (int)n);
+  const double t = __builtin_fma(x, 1.4426950408889634074, 0x1.8p52);
+  const double r = __builtin_fma(t - 0x1.8p52, -0.69314718055994530942, x);
+  double p = 0.000199075693109263;
+  p = __builtin_fma(p, r, 0.0013948578326463854);
+  p = __builtin_fma(p, r, 0.008333283538708377);
+  p = __builtin_fma(p, r, 0.041666218319291876);
+  p = __builtin_fma(p, r, 0.16666666786308587);
+  p = __builtin_fma(p, r, 0.5000000107729166);
+  p = __builtin_fma(p, r, 0.999999999995509);
+  p = __builtin_fma(p, r, 0.9999999999595618);
+  return __builtin_ldexp(p, (int)__builtin_bit_cast(uint64_t, t));
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -159,31 +159,53 @@ __device__ __forceinline__ float value_of(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t index_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
 
-__device__ __forceinline__ uint64_t other_lane(uint64_t v, int m) {
-  const uint32_t lo = __shfl_xor((int)(uint32_t)v, m), hi = __shfl_xor((int)(uint32_t)(v >> 32), m);
-  return (uint64_t)hi << 32 | lo;
+// The key of lane l ^ M.  Within 16 lanes by data-parallel moves of the vector unit, past them by its
+// exchange of rows: the LDS crossbar would cost several times as much a step.
+template <int CTRL, int BANKS>
+__device__ __forceinline__ uint32_t move_lanes(uint32_t old, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, BANKS, false);
 }
-// One step of a bitonic network over the 64 lanes: of lanes l and l ^ m the one with bit m clear
-// keeps the larger key where `down`.
-__device__ __forceinline__ uint64_t exchange(uint64_t v, int m, bool larger) {
-  const uint64_t w = other_lane(v, m);
-  return (v > w) == larger ? v : w;
+template <int M>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v) {
+  if constexpr (M == 1) return move_lanes<kDppXor1, 0xf>(v, v);
+  else if constexpr (M == 2) return move_lanes<kDppXor2, 0xf>(v, v);
+  else if constexpr (M == 4)  // four lanes on (banks 0 and 2) or back (1 and 3)
+    return move_lanes<0x114, 0xa>(move_lanes<0x104, 0x5>(v, v), v);
+  else if constexpr (M == 8) return move_lanes<0x128, 0xf>(v, v);  // eight around the row
+  else if constexpr (M == 16) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? p[0] : p[1];
+  } else {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? p[0] : p[1];
+  }
+}
+template <int M>
+__device__ __forceinline__ uint64_t other_lane(uint64_t v) {
+  return (uint64_t)other_lane<M>((uint32_t)(v >> 32)) << 32 | other_lane<M>((uint32_t)v);
+}
+// Steps of a bitonic network over the 64 lanes: of lanes l and l ^ M the one with bit M clear keeps
+// the larger key where the run of RUN lanes falls (64: everywhere).
+template <int RUN, int M>
+__device__ __forceinline__ uint64_t steps64(uint64_t v, int lane) {
+  const uint64_t w = other_lane<M>(v);
+  const bool larger = ((lane & M) == 0) == (RUN == 64 || (lane & RUN) == 0);
+  v = (v > w) == larger ? v : w;
+  if constexpr (M > 1) return steps64<RUN, M / 2>(v, lane);
+  else return v;
 }
 // The lanes' keys in falling order.
 __device__ __forceinline__ uint64_t sort64(uint64_t v, int lane) {
-#pragma unroll
-  for (int run = 2; run <= 64; run *= 2)
-#pragma unroll
-    for (int m = run / 2; m >= 1; m /= 2)
-      v = exchange(v, m, ((lane & m) == 0) == ((lane & run) == 0 || run == 64));
-  return v;
+  v = steps64<2, 1>(v, lane);
+  v = steps64<4, 2>(v, lane);
+  v = steps64<8, 4>(v, lane);
+  v = steps64<16, 8>(v, lane);
+  v = steps64<32, 16>(v, lane);
+  return steps64<64, 32>(v, lane);
 }
 // The first 64 of two falling lists, in falling order; w: the other list's key of lane 63 - l.
 __device__ __forceinline__ uint64_t merge64(uint64_t v, uint64_t w, int lane) {
-  v = v > w ? v : w;
-#pragma unroll
-  for (int m = 32; m >= 1; m /= 2) v = exchange(v, m, (lane & m) == 0);
-  return v;
+  return steps64<64, 32>(v > w ? v : w, lane);
 }
 // The first 64 of the lists of `waves` wavefronts, to the first one.
 template <int WAVES>
@@ -201,8 +223,14 @@ __device__ __forceinline__ uint64_t merge_waves(uint64_t v, uint64_t (*list)[64]
   return v;
 }
 
+// Between a wavefront's writes to its part of LDS and its reads of them by other lanes.
+__device__ __forceinline__ void own_writes() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // ------------------------------------------------------------------- a beam's first k
-// One workgroup a row: L_i, and the row's first k logits with their words.
+// One workgroup a row: m_i and L_i, and the row's first k logits with their words.
 constexpr int kRowWaves = kMostGroups / 64;
 template <bool BF16>
 __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, BeamPlan p,
@@ -210,6 +238,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
                                                             const float* __restrict__ tops,
                                                             const float* __restrict__ groups,
                                                             double* __restrict__ lse,
+                                                            float* __restrict__ row_top,
                                                             float* __restrict__ out_z,
                                                             int32_t* __restrict__ out_index) {
   constexpr int E = Logits<BF16>::E;
@@ -245,7 +274,12 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
   uint64_t best = 0;
   int held = 0;
   uint64_t* hold = s_hold[wave];
-  auto take = [&](uint64_t k) { best = merge64(best, other_lane(sort64(k, lane), 63), lane); };
+  // (falling lists both: one of them turned around)
+  auto take = [&](uint64_t k) {
+    hold[lane] = sort64(k, lane);
+    own_writes();
+    best = merge64(best, hold[63 - lane], lane);
+  };
   for (int g = wave; g < n_groups; g += kRowWaves) {
     const int64_t group = index_of(s_list[0][g]);
     for (int l = 0; l < p.per_group; ++l) {
@@ -261,19 +295,17 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
         if (on) hold[held + __popcll(lanes & ((1ull << lane) - 1))] = key;
         held += __popcll(lanes);
         if (held >= 64) {
-          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-          __builtin_amdgcn_wave_barrier();
+          own_writes();
           take(hold[lane]);
           held -= 64;
           const uint64_t rest = hold[64 + lane];
-          __builtin_amdgcn_wave_barrier();
+          own_writes();
           hold[lane] = rest;
         }
       }
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+  own_writes();
   if (held) take(lane < held ? hold[lane] : 0);
   __syncthreads();  // s_list is read no more
   best = merge_waves<kRowWaves>(best, s_list, wave, lane);
@@ -287,7 +319,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
     double all = s_sum[0];
 #pragma unroll
     for (int w = 1; w < kRowWaves; ++w) all += s_sum[w];
-    lse[row] = most == -INFINITY && all == 0.0 ? 0.0 : (double)most + log(all);
+    lse[row] = most == -INFINITY && all == 0.0 ? 0.0 : log(all);
+    row_top[row] = most;
   }
 }
 
@@ -296,6 +329,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
 // own list and, by bisection, in each other.  Equal scores: the lower beam first.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_beam_join(BeamSelect a, const double* __restrict__ lse,
+                                                       const float* __restrict__ row_top,
                                                        const float* __restrict__ z,
                                                        const int32_t* __restrict__ index) {
   __shared__ double s_score[kMostBeams * kMostChosen];
@@ -314,7 +348,7 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamSelect a, const doubl
     // (a beam that is not alive may hold anything)
     if (live && (!(c < INFINITY) || l != l)) s_bad = 1;
     const bool on = live && zz != -INFINITY;
-    s_score[x] = on ? (double)c + ((double)zz - l) : -INFINITY;
+    s_score[x] = on ? (double)c + (((double)zz - (double)row_top[row]) - l) : -INFINITY;
     if (on) atomicAdd(&s_count[i], 1);
   }
   __syncthreads();
@@ -361,20 +395,22 @@ hipError_t launch_beam_select(const BeamSelect& a, hipStream_t st) {
   double* lse = reinterpret_cast<double*>(a.work + s.lse);
   float* tops = reinterpret_cast<float*>(a.work + s.top);
   float* groups = reinterpret_cast<float*>(a.work + s.group);
+  float* row_top = reinterpret_cast<float*>(a.work + s.row_top);
   float* z = reinterpret_cast<float*>(a.work + s.z);
   int32_t* index = reinterpret_cast<int32_t*>(a.work + s.index);
   const dim3 scan((p.units + 3) / 4, (unsigned)rows);
 #define WICI_BEAM(B)                                                                            \
   launch_k(k_beam_scan<B>, scan, dim3(256), 0, st, kFirst, a, p, sums, tops, groups);           \
   launch_k(k_beam_rows<B>, dim3((unsigned)rows), dim3(64 * kRowWaves), 0, st, 0, a, p, sums, tops, \
-           groups, lse, z, index)
+           groups, lse, row_top, z, index)
   if (a.bf16) {
     WICI_BEAM(true);
   } else {
     WICI_BEAM(false);
   }
 #undef WICI_BEAM
-  launch_k(k_beam_join<256>, dim3(a.n), dim3(256), 0, st, kLast, a, lse, z, index);
+  launch_k(k_beam_join<256>, dim3(a.n), dim3(256), 0, st, kLast, a, lse, row_top,
+           z, index);
   return hipGetLastError();
 }
 

@@ -37,6 +37,7 @@ inline BeamPlan beam_plan(int vocab, bool bf16) {
 struct BeamSpace {
   size_t sum, lse;        // double [rows][units], [rows]
   size_t top, group;      // float [rows][units], [rows][groups]
+  size_t row_top;         // float [rows]
   size_t z, index;        // float, int32 [rows][k]
   size_t bytes;
 };
@@ -52,6 +53,7 @@ inline BeamSpace beam_space(const BeamPlan& p, int64_t rows, int k) {
   s.lse = take(8 * (size_t)rows);
   s.top = take(4 * (size_t)rows * p.units);
   s.group = take(4 * (size_t)rows * p.groups);
+  s.row_top = take(4 * (size_t)rows);
   s.z = take(4 * (size_t)rows * k);
   s.index = take(4 * (size_t)rows * k);
   s.bytes = at;

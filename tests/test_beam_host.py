@@ -33,7 +33,7 @@ def test_workspaces():
                 groups, units = -(-loads // per), -(-loads // max(per, 8))
                 assert groups <= 1024 and units <= groups
                 want = sum(-(-x // 16) * 16 for x in (8 * rows * units, 8 * rows, 4 * rows * units,
-                                                      4 * rows * groups, 4 * rows * k, 4 * rows * k))
+                                                      4 * rows * groups, 4 * rows, 4 * rows * k, 4 * rows * k))
                 assert need(rows, 1, vocab, dtype, k) == want
     assert need(0, 4, 100, binding.WICI_F32, 4) == 0
     for bad in ((-1, 4, 100, 0, 4), (1, 0, 100, 0, 4), (1, 65, 100, 0, 4), (1, 4, 0, 0, 4), (1, 4, (1 << 24) + 1, 0, 4),
