@@ -31,39 +31,67 @@ struct Logits {
   const char* base;  // aligned address at or before the row's first element
   int head;          // elements between
   int vocab;
+  int from, to;      // the blocks that lie in the row whole: from .. to - 1
   __device__ __forceinline__ Logits(const void* p, int64_t row_stride, int row, int vocab_)
       : vocab(vocab_) {
     const char* first = static_cast<const char*>(p) + row * row_stride * (BF16 ? 2 : 4);
     const int off = (int)(reinterpret_cast<uintptr_t>(first) & 15);
     base = first - off;
     head = off / (BF16 ? 2 : 4);
+    from = head != 0;
+    to = (head + vocab) / E;
   }
-  // The block's elements, -inf where it has none; the first one's index.
-  __device__ __forceinline__ int block(int64_t b, float (&z)[E]) const {
-    const int64_t at = b * E - head;
-    if (at >= 0 && at + E <= vocab) {
-      const uint4 w = *reinterpret_cast<const uint4*>(base + 16 * b);
+  __device__ __forceinline__ int index(int b) const { return b * E - head; }  // of its first element
+  __device__ __forceinline__ uint4 whole(int b) const {
+    return *reinterpret_cast<const uint4*>(base + 16 * (int64_t)b);
+  }
+  __device__ __forceinline__ void unpack(const uint4& w, float (&z)[E]) const {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = (&w.x)[i];
-        if constexpr (BF16) {
-          z[2 * i] = __uint_as_float(x << 16);
-          z[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
-        } else {
-          z[i] = __uint_as_float(x);
-        }
-      }
-    } else {  // a row's first or last block, or past it
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        z[i] = -INFINITY;
-        if (at + i >= 0 && at + i < vocab) {
-          if constexpr (BF16) z[i] = bf16_to_f32(reinterpret_cast<const bf16_t*>(base + 16 * b)[i]);
-          else z[i] = reinterpret_cast<const float*>(base + 16 * b)[i];
-        }
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = (&w.x)[i];
+      if constexpr (BF16) {
+        z[2 * i] = __uint_as_float(x << 16);
+        z[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
+      } else {
+        z[i] = __uint_as_float(x);
       }
     }
-    return (int)at;
+  }
+  // A block of which only some elements are the row's (its first or last), element by element; -inf
+  // where it has none.
+  __device__ __forceinline__ void part(int b, float (&z)[E]) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = index(b) + i;
+      z[i] = -INFINITY;
+      if (at >= 0 && at < vocab) {
+        if constexpr (BF16) z[i] = bf16_to_f32(reinterpret_cast<const bf16_t*>(base + 16 * (int64_t)b)[i]);
+        else z[i] = reinterpret_cast<const float*>(base + 16 * (int64_t)b)[i];
+      }
+    }
+  }
+  __device__ __forceinline__ bool partly(int b) const {
+    return (b == 0 && from == 1) || (b == to && index(b) < vocab);
+  }
+  // N blocks, `step` apart from b on: those that are whole requested together.
+  template <int N>
+  __device__ __forceinline__ void blocks(int b, int step, float (&z)[N][E]) const {
+    uint4 w[N];
+    const bool any = from < to;  // (the same in every lane)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      w[n] = any ? whole(min(max(b + n * step, from), to - 1)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) unpack(w[n], z[n]);
+    if (__all(b >= from && b + (N - 1) * step < to)) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = b + n * step;
+      if (at < from || at >= to)
+#pragma unroll
+        for (int i = 0; i < E; ++i) z[n][i] = -INFINITY;
+      if (partly(at)) part(at, z[n]);
+    }
   }
 };
 
@@ -106,25 +134,22 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamSelect a, BeamPlan p, dou
   double sum = 0.0;  // of this lane, against `top`
   bool bad = false;
   for (int l0 = 0; l0 < p.per_unit; l0 += kLoads) {
-    const int64_t first = (int64_t)unit * p.per_unit + l0;
+    const int first = unit * p.per_unit + l0;
     float x[kLoads][E];
-#pragma unroll
-    for (int l = 0; l < kLoads; ++l) z.block((first + l) * 64 + lane, x[l]);
+    z.template blocks<kLoads>(first * 64 + lane, 64, x);
     float most[kLoads], now = top;
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
       most[l] = x[l][0];
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        bad |= !(x[l][i] < INFINITY);
-        most[l] = fmaxf(most[l], x[l][i]);
-      }
+      for (int i = 1; i < E; ++i) most[l] = __builtin_elementwise_maximum(most[l], x[l][i]);
+      bad |= !(most[l] < INFINITY);  // (NaN if one is)
       most[l] = wave_max(most[l]);
       now = fmaxf(now, most[l]);
       group = fmaxf(group, most[l]);
-      const int64_t load = first + l + 1;
+      const int load = first + l + 1;
       if ((load & (p.per_group - 1)) == 0) {  // the group's last
-        const int64_t g = load / p.per_group - 1;
+        const int g = load / p.per_group - 1;
         if (lane == 0 && g < p.groups) groups[(size_t)row * p.groups + g] = group;
         group = -INFINITY;
       }
@@ -281,15 +306,16 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
     best = merge64(best, hold[63 - lane], lane);
   };
   for (int g = wave; g < n_groups; g += kRowWaves) {
-    const int64_t group = index_of(s_list[0][g]);
+    const int group = (int)index_of(s_list[0][g]);
     for (int l = 0; l < p.per_group; ++l) {
-      float x[E];
-      const int at = z.block((group * p.per_group + l) * 64 + lane, x);
+      float x[1][E];
+      const int b = (group * p.per_group + l) * 64 + lane, at = z.index(b);
+      z.template blocks<1>(b, 0, x);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         // (a block's places outside the row are -inf, as masked words are: neither is a candidate)
-        const uint64_t key = key_of(x[i], (uint32_t)(at + i));
-        const bool on = x[i] != -INFINITY && (uint32_t)(key >> 32) >= least;
+        const uint64_t key = key_of(x[0][i], (uint32_t)(at + i));
+        const bool on = x[0][i] != -INFINITY && (uint32_t)(key >> 32) >= least;
         const uint64_t lanes = __ballot(on);
         if (!lanes) continue;
         if (on) hold[held + __popcll(lanes & ((1ull << lane) - 1))] = key;
@@ -308,6 +334,13 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
   own_writes();
   if (held) take(lane < held ? hold[lane] : 0);
   __syncthreads();  // s_list is read no more
+  if (t == 64 * kRowWaves - 1) {  // (of a wavefront that the merge needs only once)
+    double all = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < kRowWaves; ++w) all += s_sum[w];
+    lse[row] = most == -INFINITY && all == 0.0 ? 0.0 : log(all);
+    row_top[row] = most;
+  }
   best = merge_waves<kRowWaves>(best, s_list, wave, lane);
   if (wave) return;
   if (lane < a.k) {
@@ -315,70 +348,67 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_beam_rows(BeamSelect a, Beam
     out_z[at] = best ? value_of(best) : -INFINITY;
     out_index[at] = best ? (int)index_of(best) : -1;
   }
-  if (lane == 0) {
-    double all = s_sum[0];
-#pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) all += s_sum[w];
-    lse[row] = most == -INFINITY && all == 0.0 ? 0.0 : log(all);
-    row_top[row] = most;
-  }
 }
 
 // ------------------------------------------------------------------- a search's first k
 // Of the beams' lists, each in falling order: a candidate's place is the number before it in its
-// own list and, by bisection, in each other.  Equal scores: the lower beam first.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_beam_join(BeamSelect a, const double* __restrict__ lse,
-                                                       const float* __restrict__ row_top,
-                                                       const float* __restrict__ z,
-                                                       const int32_t* __restrict__ index) {
+// own list and, by bisection, in each other: a work-item finds one of those numbers.  Equal scores: the
+// lower beam first.
+constexpr int kJoin = 1024;
+__global__ __launch_bounds__(kJoin) void k_beam_join(BeamSelect a, const double* __restrict__ lse,
+                                                     const float* __restrict__ row_top,
+                                                     const float* __restrict__ z,
+                                                     const int32_t* __restrict__ index) {
   __shared__ double s_score[kMostBeams * kMostChosen];
+  __shared__ int s_place[kMostBeams * kMostChosen];
   __shared__ int s_count[kMostBeams];  // live candidates of a beam: the first ones of its list
-  __shared__ int s_bad;
+  __shared__ int s_bad, s_all;
   const int b = blockIdx.x, W = a.beams, k = a.k, t = threadIdx.x;
   if (t < W) s_count[t] = 0;
-  if (t == 0) s_bad = 0;
+  if (t == 0) s_bad = s_all = 0;
   __syncthreads();
-  for (int x = t; x < W * k; x += THREADS) {
-    const int i = x / k;
+  for (int x = t; x < W * k; x += kJoin) {
+    const int i = x / k, r = x % k;
     const size_t row = (size_t)b * W + i;
-    const float c = a.scores[row], zz = z[row * k + x % k];
+    const float c = a.scores[row], zz = z[row * k + r], top = row_top[row];
     const double l = lse[row];
     const bool live = c != -INFINITY;
     // (a beam that is not alive may hold anything)
     if (live && (!(c < INFINITY) || l != l)) s_bad = 1;
     const bool on = live && zz != -INFINITY;
-    s_score[x] = on ? (double)c + (((double)zz - (double)row_top[row]) - l) : -INFINITY;
-    if (on) atomicAdd(&s_count[i], 1);
+    s_score[x] = on ? (double)c + (((double)zz - (double)top) - l) : -INFINITY;
+    s_place[x] = r;
+    if (on) {
+      atomicAdd(&s_count[i], 1);
+      atomicAdd(&s_all, 1);
+    }
   }
   __syncthreads();
   const bool bad = s_bad != 0;
-  int all = 0;
-  for (int i = 0; i < W; ++i) all += s_count[i];
   const size_t to = (size_t)b * k;
-  if (t < k && (bad || t >= all)) {
+  if (t < k && (bad || t >= s_all)) {
     a.out_scores[to + t] = bad ? __uint_as_float(0x7fc00000u) : -INFINITY;
     a.out_parent[to + t] = a.out_token[to + t] = -1;
   }
   if (bad) return;
-  for (int x = t; x < W * k; x += THREADS) {
-    const int i = x / k, r = x % k;
-    if (r >= s_count[i]) continue;
+  for (int y = t; y < W * k * W; y += kJoin) {
+    const int j = y / (W * k), x = y % (W * k), i = x / k;
+    if (i == j || x % k >= s_count[i]) continue;
     const double s = s_score[x];
-    int place = r;
-    for (int j = 0; j < W && place < k; ++j) {
-      if (j == i) continue;
-      int lo = 0, hi = s_count[j];  // candidates before lo are before this one, from hi on not
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        const double m = s_score[j * k + mid];
-        if (m > s || (m == s && j < i)) lo = mid + 1;
-        else hi = mid;
-      }
-      place += lo;
+    int lo = 0, hi = s_count[j];  // candidates before lo are before this one, from hi on not
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      const double m = s_score[j * k + mid];
+      if (m > s || (m == s && j < i)) lo = mid + 1;
+      else hi = mid;
     }
-    if (place >= k) continue;
-    a.out_scores[to + place] = (float)s;
+    atomicAdd(&s_place[x], lo);
+  }
+  __syncthreads();
+  for (int x = t; x < W * k; x += kJoin) {
+    const int i = x / k, r = x % k, place = s_place[x];
+    if (r >= s_count[i] || place >= k) continue;
+    a.out_scores[to + place] = (float)s_score[x];
     a.out_parent[to + place] = i;
     a.out_token[to + place] = index[((size_t)b * W + i) * k + r];
   }
@@ -409,7 +439,7 @@ hipError_t launch_beam_select(const BeamSelect& a, hipStream_t st) {
     WICI_BEAM(false);
   }
 #undef WICI_BEAM
-  launch_k(k_beam_join<256>, dim3(a.n), dim3(256), 0, st, kLast, a, lse, row_top,
+  launch_k(k_beam_join, dim3(a.n), dim3(kJoin), 0, st, kLast, a, lse, row_top,
            z, index);
   return hipGetLastError();
 }
