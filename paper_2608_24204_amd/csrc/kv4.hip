@@ -18,6 +18,17 @@ __device__ __forceinline__ char* kv4_block_of(const Kv8& c, const RowAt& w, int 
                   : w.base + kv4_block_at(phys, which, h, c.n_kv, 1 << c.page_shift, HD);
 }
 
+// The largest of a unit's values, by data-parallel moves (a lane and its mirror within 2, 4, 8 and 16).
+template <int CTRL>
+__device__ __forceinline__ unsigned max_with(unsigned v) {
+  return max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false));
+}
+template <int LPU>
+__device__ __forceinline__ unsigned most_of(unsigned v) {
+  v = max_with<kDppHalfMirror>(max_with<kDppXor2>(max_with<kDppXor1>(v)));
+  return LPU == 16 ? max_with<kDppMirror>(v) : v;
+}
+
 // The codes of a lane's two runs of four dimensions (run a in the low half), and the unit's scale
 // bytes, of group g in byte g.  A lane's runs may belong to two groups, and a group to the first
 // members of pairs here and the second ones there: every group's maximum is taken over the unit.
@@ -35,7 +46,7 @@ __device__ __forceinline__ unsigned quantise4(const float (&x)[8], const Runs& r
   scales = 0;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    const unsigned m = unit_max<LPU>(max(ga == g ? ma : 0u, gb == g ? mb : 0u));
+    const unsigned m = most_of<LPU>(max(ga == g ? ma : 0u, gb == g ? mb : 0u));
     const unsigned byte = (unsigned)kv4_scale_byte(m);
     most = max(most, m);
     scales |= byte << (8 * g);

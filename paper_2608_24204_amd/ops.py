@@ -19,8 +19,10 @@ tensor that requires one is refused where gradients are recorded.
 
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes
+import functools
 
 import torch
 
@@ -268,6 +270,8 @@ class KvCache:
             getattr(self.lib, f"wici_kv{bits}_{call}")
             for call in ("bytes", "append", "read", "attend", "attend_workspace"))
         stride = table.stride(0) if table.shape[0] > 1 else table.shape[1]
+        # what caches that are layers of one model have in common
+        self._layers = (table.data_ptr(), tuple(table.shape), stride, tuple(pool.shape), page, bits, device)
         self._c = binding.WiciKv8(pool.data_ptr(), pool.shape[0], page, self.n_kv_heads, head_dim,
                                   table.data_ptr(), stride, table.shape[1])
         size = ctypes.c_size_t()
@@ -417,6 +421,7 @@ class KvCache:
                                                     max_rows, max_length), heads)
 
 
+@functools.lru_cache(maxsize=64)
 def beam_workspace(n: int, beams: int, vocab: int, dtype: torch.dtype, k: int) -> int:
     """Bytes of workspace beam_select needs for such a call."""
     if dtype not in _DTYPES:
@@ -479,11 +484,8 @@ def beam_reorder(caches, parent: torch.Tensor, length: torch.Tensor, spare: torc
     if not caches:
         raise ValueError("caches: none")
     c = caches[0]
-    for x in caches[1:]:
-        if (x.table.data_ptr(), x.table.shape, x.table.stride(), x.pool.shape, x.page, x.bits,
-                x.device) != (c.table.data_ptr(), c.table.shape, c.table.stride(), c.pool.shape,
-                              c.page, c.bits, c.device):
-            raise ValueError("caches: of one table and geometry expected")
+    if any(x._layers != c._layers for x in caches):
+        raise ValueError("caches: of one table and geometry expected")
     if parent.dim() != 2:
         raise ValueError(f"parent: shape {tuple(parent.shape)}, expected [n, beams]")
     n, beams = parent.shape
@@ -491,9 +493,11 @@ def beam_reorder(caches, parent: torch.Tensor, length: torch.Tensor, spare: torc
         raise ValueError(f"parent: {n * beams} sequences, the table has {c.table.shape[0]}")
     p = _ints(parent, (n, beams), "parent", c.device)
     at, sp = (_ints(x, (n * beams,), name, c.device) for x, name in ((length, "length"), (spare, "spare")))
-    pools = (ctypes.c_void_p * len(caches))(*(x.pool.data_ptr() for x in caches))
-    with _launch_on(stream, c.device, c.table, parent, length, spare, *(x.pool for x in caches)) as raw:
-        _check(c.lib.wici_beam_reorder(c._c, c.bits, pools, len(caches), n, beams, p, at,
-                                       c.table.data_ptr(), sp, raw),
+    pools = [x.pool for x in caches]
+    at_pools = array.array("Q", [x.data_ptr() for x in pools])
+    with _launch_on(stream, c.device, c.table, parent, length, spare,
+                    *(pools if stream is not None else ())) as raw:
+        _check(c.lib.wici_beam_reorder(c._c, c.bits, at_pools.buffer_info()[0], len(pools), n, beams, p,
+                                       at, c.table.data_ptr(), sp, raw),
                f"beam_reorder: {n} searches of {beams} beams")
-        _written([c.table, spare, *(x.pool for x in caches)])
+        _written([c.table, spare, *pools])
