@@ -11,7 +11,7 @@
 // exponentials cost as much as reading bf16 logits does, at the rate of a 32-bit multiply-add each
 // step.
 //
-// One pass over the logits (k_beam_scan) leaves, for each unit of 8 KiB, its largest logit and the
+// One pass over the logits (k_beam_scan) leaves, for each unit of 2 KiB, its largest logit and the
 // sum of exponentials against it, and for each group of 64 x 16 bytes (more of a vocabulary past
 // 2^18 fp32 logits) its largest logit.  The k first elements of a row are in the k groups with the
 // largest maxima (of equal maxima the first groups): any other group has k elements before its

@@ -30,7 +30,7 @@ def test_workspaces():
                 per = 1
                 while -(-loads // per) > 1024:
                     per *= 2
-                groups, units = -(-loads // per), -(-loads // max(per, 8))
+                groups, units = -(-loads // per), -(-loads // max(per, 2))
                 assert groups <= 1024 and units <= groups
                 want = sum(-(-x // 16) * 16 for x in (8 * rows * units, 8 * rows, 4 * rows * units,
                                                       4 * rows * groups, 4 * rows, 4 * rows * k, 4 * rows * k))

@@ -14,6 +14,7 @@ import pytest
 
 import oracle
 from paper_2608_24204_amd import binding
+from tests.test_gpu_kv8 import PLAN_CASES
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 GXX = shutil.which("g++")
@@ -154,3 +155,17 @@ def test_refusals():
     for b in (batch(n_seqs=0, n_rows=0), ):
         assert lib.wici_kv4_append(cache(), b, None, 0, none, none, none, none, None) == 0
         assert lib.wici_kv4_attend(cache(), b, 4, 1.0, none, none, None, 0, None) == 0
+
+
+def test_the_gpu_tests_meet_every_kernel(ask):
+    """The attention's kernels (a split of few rows, of one tile of them or more; tiles of 64 and of 128
+    rows), with and without partial results to merge, for both head sizes, bf16 and other rows."""
+    seen = set()
+    for n_seqs, rows, length, n_kv, G, hd, entries, page in PLAN_CASES:
+        for terms in (1, 3):
+            (kind, ntile, nsplit), = ask([("plan", hd, terms, n_kv * G, n_kv, n_seqs, rows, entries * page)])
+            seen.add((hd, terms, kind, nsplit > 1, ntile > 1 if kind == 0 else None))
+    # (tiles of 64 rows of bf16 are taken where the chip is half full: nothing is left to split)
+    assert seen == {(hd, t, k, s, m) for hd in (64, 128) for t, k, s, m in (
+        (1, 0, False, True), (1, 0, True, False), (1, 1, False, None), (1, 2, False, None), (1, 2, True, None),
+        (3, 0, False, True), (3, 0, True, False), (3, 1, False, None), (3, 1, True, None))}
