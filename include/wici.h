@@ -566,8 +566,10 @@ wici_status wici_kv4_read(const wici_kv4* cache, const wici_kv8_batch* batch, wi
 wici_status wici_kv4_attend_workspace(const wici_kv4* cache, const wici_kv8_batch* batch,
                                       int32_t n_heads, size_t* bytes);
 
-/* As wici_kv8_attend.  The cached values are exact in the matrix products; where q and out are
- * bf16, q is too and the weights are within 2^-16, else both are within 2^-24. */
+/* As wici_kv8_attend.  Cached keys, and values, are exact in the matrix products.  Where q and out
+ * are bf16, q is too and a weight is within 2^-11 of itself or 2^-31 of the row's largest; else both are
+ * within 2^-24.  A weight 2^-126 and less of its row's largest may count as nothing (2^-94, in rows that
+ * have met values of 2^100 and more). */
 wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream);

@@ -65,7 +65,8 @@ __device__ __forceinline__ unsigned quantise4(const float (&x)[8], const Runs& r
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], fb, 3);
 }
 
-// As the append to the 8-bit cache: a unit takes R neighbouring rows of one head, requested before
+// As the append to the 8-bit cache (and as far from its bytes: 2048 rows of 8 heads of 128, bf16, 8.7
+// us for 8.4 MB in and 2.2 out; 48 rows of fp32 with 32 rotated query heads 4.4): a unit takes R neighbouring rows of one head, requested before
 // their places are known; four rows of a prompt that are the four positions of a value word write
 // it whole.
 template <int HD, int R>
@@ -163,6 +164,7 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv8 c, Kv8Rows r, RopeTab ro
   }
 }
 
+// 2048 rows of 8 heads of 128 to fp32 9.0 us for 2.2 MB in and 16.8 out; 48 rows 3.9.
 template <int HD, int R>
 __global__ __launch_bounds__(256) void k_kv4_read(Kv8 c, Kv8Rows r, HeadRows k, HeadRows v) {
   constexpr int LPU = HD / 8, UPB = 256 / LPU;

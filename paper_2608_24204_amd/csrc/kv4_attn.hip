@@ -2,23 +2,29 @@
 //
 // Mathematics.  For a row with query q over positions j with key rows k_j and value rows v_j:
 //   y_j = (q . k_j) scale log2(e),   out = sum_j 2^(y_j - ref) v_j / sum_j 2^(y_j - ref),
-// `ref` running with the largest y_j (an online softmax): it moves only when a weight would pass
-// 2^8 times its size when `ref` was set.  A cached value is one of 8 small numbers times a power of two,
-// exact in bf16 over fp32's whole range, so both products run on the bf16 matrix cores with the
-// scales inside their operands: one conversion instruction makes two operands of a byte and a
-// scale.  q and the weights enter as NQ and NW bf16 terms: bf16 queries are exact in one, and two
-// hold a weight to 2^-16, far inside a bf16 output's rounding; three hold either to fp32's own.
-// Scores, weights, sums and the output are fp32.
+// `ref` running with the largest y_j (an online softmax): it moves only when weights outgrow the size
+// at which it was set (Room).  A cached value is one of 8 small numbers times a power of two, exact in
+// bf16 over fp32's whole range: one conversion instruction makes two operands of a byte and a scale,
+// and the scales need no arithmetic of their own.  The keys' product runs on the bf16 matrix cores,
+// with the query as NQ bf16 terms: one for bf16 rows (exact), else three (2^-24).  Weights and values of
+// bf16 rows enter the second product as one fp16 term while the values' scales are 2^-23 .. 2^8, so
+// that fp16 holds them exactly (a weight to 2^-11, an eighth of the output's own rounding, or to 2^-31
+// of the row's largest); where they are not, and for other rows, as NW bf16 terms (two, 2^-16, or
+// three, 2^-24).  Scores, weights, sums and the output are fp32.
+//
+// (The matrix instruction that takes 4-bit operands with their scales as they lie would need queries
+// in 8 bits, two terms for bf16 ones at the same rate, and was measured to keep only about 2^-14 of the
+// largest product in its sums of 32.)
 //
 // A value row that is NaN (scale bytes 255) must not reach rows that do not see it, and a product
 // with a weight of zero would: its operands are made with another scale, and the weights of the
 // rows that do see it are NaN instead.
 //
-// Layout.  S^T = K Q^T and O^T = V^T W^T on v_mfma_f32_16x16x32_bf16, as over the 8-bit cache:
-// lane l holds query row l % 16 in both results, a tile of S^T leaves it with positions
-// 4 (l / 16) .. + 3, and those are the positions that the second product takes from it.  For the
-// keys a lane takes position l % 16 and a quarter of the dimensions, within one group's scale;
-// for the values four positions of hd / 16 neighbouring dimensions, and their four scales.
+// Layout.  S^T = K Q^T and O^T = V^T W^T on 16x16x32 products, as over the 8-bit cache: lane l holds
+// query row l % 16 in both results, a tile of S^T leaves it with positions 4 (l / 16) .. + 3, and those
+// are the positions that the second product takes from it.  For the keys a lane takes position l % 16
+// and a quarter of the dimensions, within one group's scale; for the values four positions of hd / 16
+// neighbouring dimensions, and their four scales.
 #include <algorithm>
 #include <type_traits>
 
@@ -378,6 +384,14 @@ __device__ __forceinline__ void load_queries4(const HeadRows& q, int64_t at, boo
 // groups of four steps in turn, so one launch serves any length evenly.  With one
 // split the output is written here, otherwise (ref, sum, output) is left for the merge.
 // ONCE: nobody reads a code again.
+//
+// Bound by the cache's bytes, each read once: 32 tokens at 16384 (40 query on 8 KV heads of 128, bf16)
+// 93 us for 570 MB, 6.1 TB/s where a large copy moves 4.9-5.2; the loads with nothing behind them take
+// 92.  There the vector units are busy 53% of the time (17 instructions of a tile's 70 make keys, 36
+// values).  Where there is less to read, latencies show: 48 tokens at up to 4000 (heads of 64) 28.7 us
+// for 81 MB, one at 16384 (fp32) 12.8 us for 18 MB.  Three wavefronts a SIMD for heads of 128 (two with
+// three terms), four for heads of 64: one more changed nothing (114 for 112, 37.8 for 36.7 us), nor did
+// steps of 64 positions (124 for 120, 37.0 for 37.0).
 template <int HD, int NQ, int NW, bool ONCE>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_attn_split(
@@ -522,16 +536,23 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
 // ------------------------------------------------------------------- prompts: row tiles
 // Workgroup (KV head, tile of 64 or 128 rows x query heads, split, sequence): each of four
 // wavefronts holds a quarter of the rows and takes every chunk of 64 positions of the split.  The
-// codes of a chunk become bf16 operands once for all four, in LDS, lane by lane as the products
-// read them (16 bytes a lane, no bank met twice): a wavefront converts a quarter.  Two buffers:
-// the next chunk's codes are on their way while this one is multiplied, and one barrier a chunk
-// parts a buffer's readers from its next writers.
-template <int HD, int NQ, int NW, int kRowTiles, int kWaves>
-__global__ __launch_bounds__(64 * kWaves)
-__attribute__((amdgpu_waves_per_eu(kWaves == 8 && kRowTiles == 1 ? 4 : 2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
+// codes of a chunk become operands once for all four, in LDS, lane by lane as the products read
+// them (16 bytes a lane): a wavefront converts one of the four tiles.  Two buffers: the next chunk's
+// codes are on their way while this one is multiplied, and one barrier a chunk parts a buffer's
+// readers from its next writers.
+//
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 280 us in bf16, 860 TFLOP/s of
+// products where a large product reaches 1150-1300.  No unit is full: matrix cores 34%, vector units
+// 45%, LDS 26% of the time; the two wavefronts a SIMD that the registers allow wait for each other's
+// units and on LDS.  Two bf16 terms of every weight took 366 us; eight wavefronts of 16 rows a
+// workgroup, four a SIMD, 346 (they spill); the next chunk's operands made between this one's two
+// steps 289.
+template <int HD, int NQ, int NW, int kRowTiles>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit,
                                                             int ntile) {
-  constexpr int DS = HD / 32, DT = HD / 16, kRows = kWaves * 16 * kRowTiles;
-  constexpr int kParts = kWaves / kChunkTiles, PW = DS / kParts;  // wavefronts a tile, words of one
+  constexpr int DS = HD / 32, DT = HD / 16, kRows = 4 * 16 * kRowTiles;
+  static_assert(kChunkTiles == 4, "a wavefront brings one tile of a chunk");
   enum Kind { kTooWide = 1, kNans = 2, kLarge = 4 };
   __shared__ uint4 s_k[2][kChunkTiles][DS][64];      // keys: tile, 32 dimensions, lane
   __shared__ uint4 s_v[2][kChunkTiles / 2][DT][64];  // values: two tiles, 16 dimensions, lane
@@ -573,11 +594,9 @@ __attribute__((amdgpu_waves_per_eu(kWaves == 8 && kRowTiles == 1 ? 4 : 2))) void
 #pragma unroll
       for (int u = 0; u < DT; ++u) o[x][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
-    // what this wavefront brings of a chunk: keys and values of one tile, all or half of each
-    // lane's dimensions
-    unsigned kc[PW], ks, vc[PW], vs;
+    // what this wavefront brings of a chunk: the keys and values of one tile
+    unsigned kc[DS], ks, vc[DS], vs;
     int phys[kChunkTiles], later[kChunkTiles];
-    const int mine_t = wave / kParts, part = wave % kParts;
     const bool whole_chunk = c.page_shift >= 6;  // one page holds a chunk
     auto find = [&](int chunk) {
       later[0] = entry(c, q, (uint32_t)chunk * kChunkPos);
@@ -592,16 +611,16 @@ __attribute__((amdgpu_waves_per_eu(kWaves == 8 && kRowTiles == 1 ? 4 : 2))) void
       for (int t = 1; t < kChunkTiles; ++t)
         phys[t] = whole_chunk ? phys[0] : kv8_named(later[t], c.n_pages);
     };
+    // p[t], with bits: a choice between the elements would put them into memory
+    auto pick = [](const int (&p)[kChunkTiles], int t) {
+      const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
+      return lo ^ ((lo ^ hi) & -(t >> 1));
+    };
     auto bring = [&](const int (&p)[kChunkTiles], int chunk) {
       const int j0 = chunk * kChunkPos;
-      // p[t], with bits: a choice between the elements would put them into memory
-      auto pick = [&](int t) {
-        const int lo = p[0] ^ ((p[0] ^ p[1]) & -(t & 1)), hi = p[2] ^ ((p[2] ^ p[3]) & -(t & 1));
-        return lo ^ ((lo ^ hi) & -(t >> 1));
-      };
-      const int phys = whole_chunk ? p[0] : pick(mine_t), slot = (j0 + 16 * mine_t) & (page - 1);
+      const int phys = whole_chunk ? p[0] : pick(p, wave), slot = (j0 + 16 * wave) & (page - 1);
       const __amdgpu_buffer_rsrc_t kb = kv.buffer(c, phys, 0), vb = kv.buffer(c, phys, 1);
-      const int dk = g * (HD / 4) + part * (8 * PW), dv = r16 * (HD / 16) + part * (2 * PW);
+      const int dk = g * (HD / 4), dv = r16 * (HD / 16);
       fetch_words(kc, kb, kv4_key_at(r16, dk, HD), kv4_key_at(slot, 0, HD));
       ks = __builtin_amdgcn_raw_buffer_load_b8(kb, r16 * (HD / kKv4Group) + dk / kKv4Group,
                                                kv4_key_scale_at(slot, 0, page, HD), 0);
@@ -613,34 +632,32 @@ __attribute__((amdgpu_waves_per_eu(kWaves == 8 && kRowTiles == 1 ? 4 : 2))) void
     auto convert = [&](int buf, int ch, const int (&now)[kChunkTiles], auto halves) {
       const float scale = __uint_as_float(ks << 23);
 #pragma unroll
-      for (int d = 0; d < PW; ++d)
-        s_k[buf][mine_t][part * PW + d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
+      for (int d = 0; d < DS; ++d)
+        s_k[buf][wave][d][lane] = __builtin_bit_cast(uint4, keys8(kc[d], scale));
       // (in the last chunk, and in pages that are not there)
       const int left = all - ch * kChunkPos;
-      const int lo = now[0] ^ ((now[0] ^ now[1]) & -(mine_t & 1)), hi = now[2] ^ ((now[2] ^ now[3]) & -(mine_t & 1));
-      const int there = lo ^ ((lo ^ hi) & -(mine_t >> 1));
-      if (left < kChunkPos || there < 0) leave_seen(vs, there >= 0, left - (16 * mine_t + 4 * g));
+      const int there = pick(now, wave);
+      if (left < kChunkPos || there < 0) leave_seen(vs, there >= 0, left - (16 * wave + 4 * g));
       int kind = 0;
       if (!halves.value || __builtin_expect(__any(past_half(vs)), false)) {
         bool large = false;
         const unsigned nan = take_nans(vs, large);
-        // (both wavefronts of a tile see all its scales)
         kind = (large ? kLarge : 0) | (__any(nan != 0) ? kNans : 0) |
                (halves.value && __any(past_half(vs)) ? kTooWide : 0);
-        if (part == 0 && r16 == 0) s_nan[buf][mine_t][g] = nan;
+        if (r16 == 0) s_nan[buf][wave][g] = nan;
       }
       float f[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = scale_of(vs, i);
 #pragma unroll
-      for (int d = 0; d < PW; ++d) {
-        uint2 lo2, hi2;
-        values4<halves.value>(vc[d], f, lo2, hi2);
-        uint4* to = &s_v[buf][mine_t >> 1][2 * (part * PW + d)][lane];
-        reinterpret_cast<uint2*>(to)[mine_t & 1] = lo2;
-        reinterpret_cast<uint2*>(to + 64)[mine_t & 1] = hi2;
+      for (int d = 0; d < DS; ++d) {
+        uint2 lo, hi;
+        values4<halves.value>(vc[d], f, lo, hi);
+        uint4* to = &s_v[buf][wave >> 1][2 * d][lane];
+        reinterpret_cast<uint2*>(to)[wave & 1] = lo;
+        reinterpret_cast<uint2*>(to + 64)[wave & 1] = hi;
       }
-      if (part == 0 && lane == 0) s_kind[buf][mine_t] = kind;
+      if (lane == 0) s_kind[buf][wave] = kind;
     };
 
     bf16x8_t qf[kRowTiles][NQ][DS];
@@ -774,7 +791,7 @@ size_t kv4_attn_floats(int hd, int n_q, int n_kv, int n_seqs, int n_rows, int ma
 
 template <int HD>
 static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStream_t st, int last) {
-  // one term of the query and two of the weights where queries and output are bf16, else three
+  // bf16 queries and output: one term of the query, one or two of the weights; else three
   const bool single = a.q.bf16 && a.out.p && a.out.bf16;
   const Kv8Plan p = kv4_plan(HD, single ? 1 : 3, a.n_q, c.n_kv, r.n_seqs, a.max_rows, a.max_length);
   const int64_t gx = (int64_t)c.n_kv * p.nsplit * p.ntile;
@@ -784,10 +801,10 @@ static hipError_t attn4(const Kv8& c, const Kv8Rows& r, const Kv8Attn& a, hipStr
 #define WICI_ATTN(...) \
   launch_k((__VA_ARGS__), grid, dim3(256), 0, st, edge, c, r, a, p.nsplit, p.ntile)
   if (p.row_tiles == 2) {
-    WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 2, 4>);
+    WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 2>);
   } else if (p.row_tiles == 1) {
-    if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1, 4>);
-    else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1, 4>);
+    if (single) WICI_ATTN(k_kv4_attn_tile<HD, 1, 2, 1>);
+    else WICI_ATTN(k_kv4_attn_tile<HD, 3, 3, 1>);
   } else {
     // Codes that one tile of rows reads are read past the caches (heads of 128: 48 tokens at up to
     // 4000 positions 42.4 us for 46.0, 32 at 16384 103.6 for 119; heads of 64: 34.4 for 32.6, so
