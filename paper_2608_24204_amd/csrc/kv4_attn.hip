@@ -169,7 +169,7 @@ __device__ __forceinline__ void load_keys4(Step4<HD>& s, const Kv8& c, const Hea
   const int page = 1 << c.page_shift, pos = lane & 15, d = (lane >> 4) * (HD / 4);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    const int slot = (step * kStep + 16 * t) & (page - 1);
+    const int slot = (int)(((uint32_t)step * kStep + 16 * t) & (uint32_t)(page - 1));
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 0, on);
     fetch_words<ONCE>(s.k[t], b, kv4_key_at(pos, d, HD), kv4_key_at(slot, 0, HD));
     s.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(b, pos * (HD / kKv4Group) + d / kKv4Group,
@@ -182,7 +182,7 @@ __device__ __forceinline__ void load_values4(Step4<HD>& s, const Kv8& c, const H
   const int page = 1 << c.page_shift, pos = 4 * (lane >> 4), d = (lane & 15) * (HD / 16);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    const int slot = (step * kStep + 16 * t) & (page - 1);
+    const int slot = (int)(((uint32_t)step * kStep + 16 * t) & (uint32_t)(page - 1));
     const __amdgpu_buffer_rsrc_t b = at.buffer(c, p.phys[t], 1);
     fetch_words<ONCE>(s.v[t], b, kv4_value_at(pos, d, HD), kv4_value_at(slot, 0, HD));
     s.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(b, pos * (HD / kKv4Group) + 4 * (d / kKv4Group),
