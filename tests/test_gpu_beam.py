@@ -386,3 +386,46 @@ def test_a_beam_search_over_two_layers(ops, bits, graph):
                     at = slice(sq * (i + 1), (sq + 1) * (i + 1))
                     assert np.array_equal(f64(rk[at]), values(k).astype(np.float32))
                     assert np.array_equal(f64(rv[at]), values(x[:, G * H + H:]).astype(np.float32))
+
+
+def test_scores_written_in_place(ops):
+    """The C call with its scores as output, as a captured search step may keep them."""
+    from paper_2608_24204_amd import binding
+    rng = np.random.default_rng(21)
+    z, c = rnd(rng, 20, 5000, dtype=BF16), rnd(rng, 5, 4, dtype=F32)
+    want = ops.beam_select(z, c)
+    p, t = (torch.empty(5, 4, dtype=torch.int32, device="cuda") for _ in "pt")
+    ws = torch.empty(ops.beam_workspace(5, 4, 5000, BF16, 4), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream()
+    st = binding.load_library().wici_beam_select(
+        z.data_ptr(), binding.WICI_BF16, 5000, 5, 4, 5000, c.data_ptr(), 4, c.data_ptr(), p.data_ptr(),
+        t.data_ptr(), ws.data_ptr(), ws.numel(), s.cuda_stream)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((c, p, t), want))
+
+
+def test_reordering_on_a_named_stream_and_in_a_graph(ops):
+    """Captured once and replayed as lengths and parents change in place; two layers of 8 bits."""
+    rng = np.random.default_rng(22)
+    caches, table, spare = make_caches(ops, rng, 3, 4, 4, 2, 64, 16, 8, 2)
+    other, table2, spare2 = make_caches(ops, np.random.default_rng(22), 3, 4, 4, 2, 64, 16, 8, 2)
+    parent, length = ints([[0] * 4] * 3), ints([5] * 12)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ops.beam_reorder(caches, parent, length, spare, stream=s)
+    ops.beam_reorder(other, parent, length, spare2)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        ops.beam_reorder(caches, parent, length, spare)
+    for at in (6, 16, 17, 40, 64):
+        parent.copy_(ints(rng.integers(-1, 5, (3, 4)).tolist()))
+        length.fill_(at)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        ops.beam_reorder(other, parent, length, spare2)
+        torch.cuda.synchronize()
+        assert torch.equal(table, table2) and torch.equal(spare, spare2)
+        assert all(torch.equal(a.pool, b.pool) for a, b in zip(caches, other))
