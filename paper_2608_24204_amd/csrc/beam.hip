@@ -7,8 +7,8 @@
 //
 // Within a beam the order is that of the logits and needs no L_i; between beams it does, and two
 // continuations may be as near each other as numbers of 24 bits get: L_i and s_iv are formed in 64
-// bits, so that which of them is chosen does not hang on how a sum was split.  64-bit multiply-adds
-// run at the rate of 32-bit ones here.
+// bits, and from parts of a row that its length alone decides, so that beams that are alike have the
+// same ones.  64-bit multiply-adds run at the rate of 32-bit ones here.
 //
 // One pass over the logits (k_beam_scan) leaves, for each unit of 2 KiB, its largest logit and the
 // sum of exponentials against it, and for each group of 64 x 16 bytes (more of a vocabulary past
@@ -24,25 +24,22 @@
 namespace wici {
 
 // ------------------------------------------------------------------- elements
+// A row as blocks of E elements, counted from its first one wherever that lies: rows that are alike
+// are cut alike, and have the same sums to the last bit.  (Loads of 16 bytes take any alignment.)
 template <bool BF16>
 struct Logits {
   static constexpr int E = BF16 ? 8 : 4;  // of a block of 16 bytes
-  const char* base;  // aligned address at or before the row's first element
-  int head;          // elements between
+  const char* base;
   int vocab;
-  int from, to;      // the blocks that lie in the row whole: from .. to - 1
+  int to;  // the blocks that the row has whole: 0 .. to - 1
   __device__ __forceinline__ Logits(const void* p, int64_t row_stride, int row, int vocab_)
-      : vocab(vocab_) {
-    const char* first = static_cast<const char*>(p) + row * row_stride * (BF16 ? 2 : 4);
-    const int off = (int)(reinterpret_cast<uintptr_t>(first) & 15);
-    base = first - off;
-    head = off / (BF16 ? 2 : 4);
-    from = head != 0;
-    to = (head + vocab) / E;
-  }
-  __device__ __forceinline__ int index(int b) const { return b * E - head; }  // of its first element
+      : base(static_cast<const char*>(p) + row * row_stride * (BF16 ? 2 : 4)), vocab(vocab_),
+        to(vocab_ / E) {}
+  __device__ __forceinline__ int index(int b) const { return b * E; }  // of its first element
   __device__ __forceinline__ uint4 whole(int b) const {
-    return *reinterpret_cast<const uint4*>(base + 16 * (int64_t)b);
+    uint4 w;
+    __builtin_memcpy(&w, base + 16 * (int64_t)b, 16);
+    return w;
   }
   __device__ __forceinline__ void unpack(const uint4& w, float (&z)[E]) const {
 #pragma unroll
@@ -56,40 +53,34 @@ struct Logits {
       }
     }
   }
-  // A block of which only some elements are the row's (its first or last), element by element; -inf
-  // where it has none.
+  // The block that the row ends in, element by element; -inf where it has none.
   __device__ __forceinline__ void part(int b, float (&z)[E]) const {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const int at = index(b) + i;
       z[i] = -INFINITY;
-      if (at >= 0 && at < vocab) {
-        if constexpr (BF16) z[i] = bf16_to_f32(reinterpret_cast<const bf16_t*>(base + 16 * (int64_t)b)[i]);
-        else z[i] = reinterpret_cast<const float*>(base + 16 * (int64_t)b)[i];
+      if (index(b) + i < vocab) {
+        if constexpr (BF16) z[i] = bf16_to_f32(reinterpret_cast<const bf16_t*>(base)[index(b) + i]);
+        else z[i] = reinterpret_cast<const float*>(base)[index(b) + i];
       }
     }
-  }
-  __device__ __forceinline__ bool partly(int b) const {
-    return (b == 0 && from == 1) || (b == to && index(b) < vocab);
   }
   // N blocks, `step` apart from b on: those that are whole requested together.
   template <int N>
   __device__ __forceinline__ void blocks(int b, int step, float (&z)[N][E]) const {
     uint4 w[N];
-    const bool any = from < to;  // (the same in every lane)
+    const bool any = to > 0;  // (the same in every lane)
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-      w[n] = any ? whole(min(max(b + n * step, from), to - 1)) : make_uint4(0, 0, 0, 0);
+    for (int n = 0; n < N; ++n) w[n] = any ? whole(min(b + n * step, to - 1)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int n = 0; n < N; ++n) unpack(w[n], z[n]);
-    if (__all(b >= from && b + (N - 1) * step < to)) return;
+    if (__all(b + (N - 1) * step < to)) return;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int at = b + n * step;
-      if (at < from || at >= to)
+      if (at >= to)
 #pragma unroll
         for (int i = 0; i < E; ++i) z[n][i] = -INFINITY;
-      if (partly(at)) part(at, z[n]);
+      if (at == to) part(at, z[n]);
     }
   }
 };

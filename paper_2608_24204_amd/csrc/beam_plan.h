@@ -12,9 +12,10 @@ constexpr int kMostRows = 65535;    // searches x beams: a grid's second dimensi
 constexpr int kLoads = 2;           // 16-byte loads of a lane at a time (8: 35.3 us for 33.0)
 constexpr int kMostGroups = 1024;   // whose maxima one workgroup takes, one a work-item
 
-// A row of `vocab` logits as 16-byte blocks from the aligned address at or before its start: the
-// blocks of 64 lanes are one load, `per_group` loads (a power of two) one group, whose maximum is
-// kept, and `per_unit` of them, whole groups, one wavefront's unit.
+// A row of `vocab` logits as 16-byte blocks from its first one on: the blocks of 64 lanes are one load,
+// `per_group` loads (a power of two) one group, whose maximum is kept, and `per_unit` of them, whole
+// groups, one wavefront's unit.  Counted is up to one block more than a row has (it holds nothing): as
+// many as a row of any alignment has of aligned ones, for which programs keep workspaces.
 struct BeamPlan {
   int in_block;   // elements of a block
   int per_group, per_unit;
@@ -23,7 +24,7 @@ struct BeamPlan {
 inline BeamPlan beam_plan(int vocab, bool bf16) {
   BeamPlan p;
   p.in_block = bf16 ? 8 : 4;
-  const int64_t blocks = ((int64_t)vocab + 2 * (p.in_block - 1)) / p.in_block;  // wherever it starts
+  const int64_t blocks = ((int64_t)vocab + 2 * (p.in_block - 1)) / p.in_block;
   const int64_t loads = (blocks + 63) / 64;
   p.per_group = 1;
   while ((loads + p.per_group - 1) / p.per_group > kMostGroups) p.per_group *= 2;
