@@ -579,7 +579,8 @@ wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, 
  * alignment of their type; vocab at most 2^24) belongs to beam i of search b, which has the score
  * scores[b beams + i] so far (device).  The continuation of beam i by word v has the score
  *   scores[b beams + i] + z_v - log sum_u e^(z_u)        (z the row's logits)
- * formed in 64 bits, and the k (1 .. 64) greatest of each search's beams x vocab are returned in
+ * formed in 64 bits (exponentials and the logarithm to 2^-52, sums to 2^-53 an addition; rows that are alike
+ * have the same), and the k (1 .. 64) greatest of each search's beams x vocab are returned in
  * falling order, [n][k] each (device): the scores rounded to fp32, the beam that each continues
  * (0 .. beams - 1) and the word.  Equal scores of one beam: the lowest word first (within a beam the
  * order is the logits'); of several: the lowest beam first.  A logit of minus infinity is a word that
