@@ -221,8 +221,8 @@ __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>
 // reference moved: the output so far is then to be multiplied by `corr`.
 //
 // What is rare stands in one branch: NaN values, a reference to move (once a lane's eight weights
-// sum up to more than room.most: one comparison), and references past 2^22 (`huge`, the same in the
-// wavefront).  From those a product is subtracted after it is rounded, as it was for the reference:
+// sum up to more than room.most: one comparison), and references past 2^22 (`huge`: one of these 16
+// rows has such a one).  From those a product is subtracted after it is rounded, as it was for the reference:
 // joined, the difference of scores that are equal and that large would not be zero.  A row's weights
 // are made of its own values alone, whatever takes the wavefront into the branch.
 template <typename T, int NW, bool MASKED>
@@ -588,11 +588,13 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
     RowState4 st[kRowTiles];
     RowOut4<HD> o[kRowTiles];
     Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
-    bool huge = false;
+    bool huge[kRowTiles];
 #pragma unroll
-    for (int x = 0; x < kRowTiles; ++x)
+    for (int x = 0; x < kRowTiles; ++x) {
+      huge[x] = false;
 #pragma unroll
       for (int u = 0; u < DT; ++u) o[x][u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
 
     // what this wavefront brings of a chunk: the keys and values of one tile
     unsigned kc[DS], ks, vc[DS], vs;
@@ -740,9 +742,9 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
             float corr = 1.f;
             Value wf[N];
             const bool move =
-                whole ? weights4<Value, N, false>(wf, st[y], huge, x[y], pg, unit, nan, now_room, 0, lane,
-                                                  corr)
-                      : weights4<Value, N, true>(wf, st[y], huge, x[y], pg, unit, nan, now_room,
+                whole ? weights4<Value, N, false>(wf, st[y], huge[y], x[y], pg, unit, nan, now_room, 0,
+                                                  lane, corr)
+                      : weights4<Value, N, true>(wf, st[y], huge[y], x[y], pg, unit, nan, now_room,
                                                  limit[y] - j0, lane, corr);
             if (__builtin_expect(move, false)) rescale4<HD>(o[y], corr);
 #pragma unroll

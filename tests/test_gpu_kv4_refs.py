@@ -1,0 +1,47 @@
+"""Attention over the 4-bit cache where scores are too large for a reference to hold a shift, and where
+values are so large that sums of them leave fp32."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_kv4 import Batch4, check_on_gpu
+from tests.test_gpu_kv8 import BF16, F32, PLAN_CASES, ints, ops, rnd, torch  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def case(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, values, **kw):
+    """Contexts of one key throughout; `values` (positions) -> factors of normal values."""
+    need = -(-length // page)
+    bt = Batch4(ops, [length] * n_seqs, [rows] * n_seqs, n_kv=n_kv, hd=hd, page=page, seed=rows + n_seqs,
+                extra_pages=entries - need)
+    n = n_seqs * length
+    k = rnd(bt.rng, 1, n_kv, hd, dtype=F32).expand(n, n_kv, hd).contiguous()
+    v = rnd(bt.rng, n, n_kv, hd, dtype=F32)
+    size = values(np.arange(n) % length).astype(np.float32)
+    v *= torch.from_numpy(size).cuda()[:, None, None]
+    return bt, *bt.store(k, v)
+
+
+def check_alike(bt, q, K, V, **kw):
+    """Equal scores weigh alike: as those of queries of zero."""
+    out = bt.cache.attend(q, bt.length, row_start=bt.row_start, **kw)
+    assert out.isfinite().all()
+    check_on_gpu(bt, torch.zeros_like(q), out, K, V)
+
+
+@pytest.mark.parametrize("n_seqs,rows,length,n_kv,G,hd,entries,page", PLAN_CASES + [(1, 200, 700, 4, 5, 64, 2100, 128)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_scores_beside_ordinary_ones(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dtype):
+    """Tiles of 16 rows x heads of large queries in turn with ordinary ones, either first, and every
+    other row: what a row's neighbours are does not matter."""
+    bt, K, V = case(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, lambda j: 1.0 + 0 * j)
+    of_row = np.arange(n_seqs * rows) % rows
+    place = of_row[:, None] * G + np.arange(n_kv * G) % G       # among the rows x heads of a KV head
+    for pick in (place // 16 % 2 == 0, place // 16 % 2 == 1, place % 2 == 0):
+        for size in (3e6, 3e7, 1.7e8):
+            q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype)
+            q *= torch.from_numpy(np.where(pick, size, 1.0).astype(np.float32)).cuda().to(dtype)[..., None]
+            check_alike(bt, q, K, V, max_rows=rows)
