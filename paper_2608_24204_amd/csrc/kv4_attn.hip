@@ -42,13 +42,14 @@ template <> struct ElemOf<half8_t> { typedef _Float16 type; };
 template <typename T> using Elem_t = typename ElemOf<T>::type;
 
 // A row's reference is set so that its largest weight is 2^top, and moves before one is past `most`.
+// Once a wavefront has met values of 2^100 and more its rows' outputs hold 2^-lift of their sums, for
+// which the weights are multiplied by that: sums of 2^24 of the largest values stay in fp32.  (Not by
+// other references: those of large scores are too coarse to hold such a shift.)
 struct Room {
-  float top, most;
+  float top, most, lift;
 };
 // fp16 weights: 2^14 fits, and fp16's least step is 2^-30 of the largest weight.
-constexpr Room kRoomHalf{6.f, 0x1p14f}, kRoomBf16{0.f, 0x1p8f};
-// Rows that have met values of 2^100 and more: sums of 2^24 of the largest stay in fp32.
-constexpr Room kRoomHuge{-32.f, 0x1p-24f};
+constexpr Room kRoomHalf{6.f, 0x1p14f, 38.f}, kRoomBf16{0.f, 0x1p8f, 32.f};
 constexpr int kHugeByte = 227;
 
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
@@ -217,8 +218,9 @@ __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>
 
 // The weights of 32 positions from their products (a score is product * unit), as NW terms of type
 // T.  MASKED: some row does not see every position: row l % 16 sees those below `seen`, of the tiles
-// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  Returns whether a row's
-// reference moved: the output so far is then to be multiplied by `corr`.
+// that are there.  nan: the positions (bit 4 t + i) whose weight is NaN.  The terms are those of 2^-lift
+// of the weights (the same in the wavefront; 0 for halves).  Returns whether a row's reference moved:
+// the output so far is then to be multiplied by `corr`.
 //
 // What is rare stands in one branch: NaN values, a reference to move (once a lane's eight weights
 // sum up to more than room.most: one comparison), and references past 2^22 (`huge`: one of these 16
@@ -228,8 +230,8 @@ __device__ __forceinline__ void scores4(floatx4_t (&sc)[kTiles], const Step4<HD>
 template <typename T, int NW, bool MASKED>
 __device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, bool& huge,
                                          const floatx4_t (&sc)[kTiles], const Pages& p, float unit,
-                                         unsigned nan, const Room& room, int seen, int lane,
-                                         float& corr) {
+                                         unsigned nan, const Room& room, float lift, int seen,
+                                         int lane, float& corr) {
   const int left = MASKED ? fresh(seen - 4 * (lane >> 4)) : 0;
   auto on = [&](int t, int i) { return !MASKED || (p.phys[t] >= 0 && 16 * t + i < left); };
   float w[4 * kTiles], sum;
@@ -289,6 +291,13 @@ __device__ __forceinline__ bool weights4(T (&wf)[NW], RowState4& st, bool& huge,
     }
   }
   st.sum += sum;
+  if constexpr (!std::is_same<T, half8_t>::value) {
+    if (__builtin_expect(lift != 0.f, false)) {
+      const float down = __builtin_amdgcn_exp2f(-lift);
+#pragma unroll
+      for (int i = 0; i < 4 * kTiles; ++i) w[i] *= down;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 4 * kTiles; ++i) {
     float rest = w[i];
@@ -332,15 +341,6 @@ __device__ __forceinline__ void rescale4(RowOut4<HD>& o, float f) {
   for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[u][i] *= f;
-}
-
-// From the room that a row had to kRoomHuge: its reference, its sum and its output.
-template <int HD>
-__device__ __forceinline__ void lower(RowOut4<HD>& o, RowState4& st, float top) {
-  const float f = __builtin_amdgcn_exp2f(kRoomHuge.top - top);
-  if (st.ref != kNoRef) st.ref += top - kRoomHuge.top;
-  st.sum *= f;
-  rescale4<HD>(o, f);
 }
 
 // 16 query rows (row l % 16 of the tile, zero where `on` is false) as NQ bf16 terms.
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_attn_split(
     Kv8 c, Kv8Rows r, Kv8Attn a, int nsplit, int ntile) {
   __shared__ float s_o[4][16][HD + 4];
-  __shared__ float s_ref[4][16], s_sum[4][16];
+  __shared__ float s_ref[4][16], s_sum[4][16], s_lift[4];
   const int h = blockIdx.x % c.n_kv, split = blockIdx.x / c.n_kv % nsplit;
   const int tile0 = blockIdx.x / (c.n_kv * nsplit), b = blockIdx.y;
   const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -429,7 +429,8 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
     bf16x8_t qf[NQ][HD / 32];
     load_queries4<HD, NQ>(a.q, (q.row0 + rc) * a.q.row_stride + head * a.q.head_stride, on, lane, qf);
     const float unit = a.scale * kLog2e;
-    Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
+    constexpr Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
+    float lift = 0.f;
     bool huge = false;
     RowState4 st;
     RowOut4<HD> o;
@@ -473,17 +474,16 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
               scored = true;
               return false;
             }
-            if (__builtin_expect(large, false) && room.top != kRoomHuge.top) {
-              lower<HD>(o, st, room.top);
-              room = kRoomHuge;
+            if (__builtin_expect(large, false) && lift == 0.f) {
+              lift = room.lift;
+              rescale4<HD>(o, __builtin_amdgcn_exp2f(-lift));
             }
           }
-          const Room now_room = halves.value ? kRoomHalf : room;
           Value wf[N];
           float corr = 1.f;
           const bool move =
-              clear ? weights4<Value, N, false>(wf, st, huge, sc, now, unit, nan, now_room, 0, lane, corr)
-                    : weights4<Value, N, true>(wf, st, huge, sc, now, unit, nan, now_room,
+              clear ? weights4<Value, N, false>(wf, st, huge, sc, now, unit, nan, room, lift, 0, lane, corr)
+                    : weights4<Value, N, true>(wf, st, huge, sc, now, unit, nan, room, lift,
                                                limit - s * kStep, lane, corr);
           if (__builtin_expect(move, false)) rescale4<HD>(o, corr);
           add_values4<HD>(o, x, vs, wf);
@@ -506,6 +506,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
       s_ref[wave][mr] = st.ref;
       s_sum[wave][mr] = st.sum;
     }
+    if (lane == 0) s_lift[wave] = lift;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -519,15 +520,25 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
       float ref = s_ref[0][rr];
 #pragma unroll
       for (int w = 1; w < 4; ++w) ref = fmaxf(ref, s_ref[w][rr]);
-      float sum = 0.f, all[4] = {};
+      float sum = 0.f, up = 0.f, all[4] = {};
+      const bool lifts = s_lift[0] + s_lift[1] + s_lift[2] + s_lift[3] != 0.f;
+      if (__builtin_expect(lifts, false)) {
+        // the least with which no wavefront's output is multiplied by 2 or more
+        up = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) up = fmaxf(up, s_lift[w] + (s_ref[w][rr] - ref));
+        up = floorf(up);
+      }
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
+        float f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref);
         const float4 v = *reinterpret_cast<const float4*>(&s_o[w][rr][d]);
         sum += f * s_sum[w][rr];
+        if (__builtin_expect(lifts, false))
+          f = __builtin_amdgcn_exp2f(s_ref[w][rr] - ref + (s_lift[w] - up));
         all[0] += f * v.x; all[1] += f * v.y; all[2] += f * v.z; all[3] += f * v.w;
       }
-      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, 0.f, sum, all);
+      leave(a, nsplit, split, parts, q.row0 + tr / G, h * G + tr % G, d, ref, up, sum, all);
     }
     __syncthreads();
   }
@@ -587,7 +598,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 
     RowState4 st[kRowTiles];
     RowOut4<HD> o[kRowTiles];
-    Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
+    constexpr Room room = NQ > 1 ? kRoomBf16 : kRoomHalf;
+    float lift = 0.f;
     bool huge[kRowTiles];
 #pragma unroll
     for (int x = 0; x < kRowTiles; ++x) {
@@ -708,10 +720,11 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 #pragma unroll
               for (int t = 0; t < kTiles; ++t)
                 if (uniform(s_kind[buf][2 * p + t]) & kNans) nan |= s_nan[buf][2 * p + t][g] << (4 * t);
-            if (!halves.value && (kinds[p] & kLarge) && room.top != kRoomHuge.top) {
+            if (!halves.value && (kinds[p] & kLarge) && lift == 0.f) {
+              lift = room.lift;
 #pragma unroll
-              for (int y = 0; y < kRowTiles; ++y) lower<HD>(o[y], st[y], room.top);
-              room = kRoomHuge;
+              for (int y = 0; y < kRowTiles; ++y)
+                rescale4<HD>(o[y], __builtin_amdgcn_exp2f(-lift));
             }
           }
           // Row tile after row tile: the matrix cores work on one's products while the vector
@@ -736,15 +749,14 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
 #pragma unroll
           for (int u = 0; u < DT; ++u) op[u] = s_v[buf][p][u][lane];
           const bool whole = least - j0 >= kStep && pg.all();
-          const Room now_room = halves.value ? kRoomHalf : room;
 #pragma unroll
           for (int y = 0; y < kRowTiles; ++y) {
             float corr = 1.f;
             Value wf[N];
             const bool move =
-                whole ? weights4<Value, N, false>(wf, st[y], huge[y], x[y], pg, unit, nan, now_room, 0,
+                whole ? weights4<Value, N, false>(wf, st[y], huge[y], x[y], pg, unit, nan, room, lift, 0,
                                                   lane, corr)
-                      : weights4<Value, N, true>(wf, st[y], huge[y], x[y], pg, unit, nan, now_room,
+                      : weights4<Value, N, true>(wf, st[y], huge[y], x[y], pg, unit, nan, room, lift,
                                                  limit[y] - j0, lane, corr);
             if (__builtin_expect(move, false)) rescale4<HD>(o[y], corr);
 #pragma unroll
@@ -778,7 +790,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
         for (int u = 0; u < DT; u += 4) {
           float v[4] = {o[y][u][i], o[y][u + 1][i], o[y][u + 2][i], o[y][u + 3][i]};
           leave(a, nsplit, split, parts, q.row0 + qr / G, h * G + qr % G,
-                DT * (4 * mg + i) + u, st[y].ref, 0.f, st[y].sum, v);
+                DT * (4 * mg + i) + u, st[y].ref, lift, st[y].sum, v);
         }
     }
   }

@@ -45,3 +45,17 @@ def test_large_scores_beside_ordinary_ones(ops, n_seqs, rows, length, n_kv, G, h
             q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype)
             q *= torch.from_numpy(np.where(pick, size, 1.0).astype(np.float32)).cuda().to(dtype)[..., None]
             check_alike(bt, q, K, V, max_rows=rows)
+
+
+@pytest.mark.parametrize("n_seqs,rows,length,n_kv,G,hd,entries,page",
+                         PLAN_CASES + [(3, 1, 3000, 2, 2, 64, 190, 16), (3, 1, 3000, 2, 2, 128, 190, 16)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_values_midway_under_large_scores(ops, n_seqs, rows, length, n_kv, G, hd, entries, page, dtype):
+    """Ordinary values first, ones past 2^100 and to fp32's end later: the positions before them weigh what
+    they did."""
+    for late, big in ((1 - rows / length / 2, 2.0 ** 101), (0.7, 2.0 ** 124)):
+        bt, K, V = case(ops, n_seqs, rows, length, n_kv, G, hd, entries, page,
+                        lambda j: np.where(j >= late * length, big, 1.0))
+        for size in (1.0, 3e6, 2.0 ** 28, 1e9, 3e10):
+            q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype) * size
+            check_alike(bt, q, K, V, max_rows=rows)
