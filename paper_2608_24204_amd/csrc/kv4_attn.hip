@@ -42,15 +42,28 @@ template <> struct ElemOf<half8_t> { typedef _Float16 type; };
 template <typename T> using Elem_t = typename ElemOf<T>::type;
 
 // A row's reference is set so that its largest weight is 2^top, and moves before one is past `most`.
-// Once a wavefront has met values of 2^100 and more its rows' outputs hold 2^-lift of their sums, for
-// which the weights are multiplied by that: sums of 2^24 of the largest values stay in fp32.  (Not by
-// other references: those of large scores are too coarse to hold such a shift.)
 struct Room {
-  float top, most, lift;
+  float top, most;
+  int log_most;
 };
 // fp16 weights: 2^14 fits, and fp16's least step is 2^-30 of the largest weight.
-constexpr Room kRoomHalf{6.f, 0x1p14f, 38.f}, kRoomBf16{0.f, 0x1p8f, 32.f};
-constexpr int kHugeByte = 227;
+constexpr Room kRoomHalf{6.f, 0x1p14f, 14}, kRoomBf16{0.f, 0x1p8f, 8};
+// Once a wavefront has met large values its rows' outputs hold 2^-lift of their sums, for which the
+// weights are multiplied by that.  (Not by other references: those of large scores are too coarse to
+// hold such a shift.)  A lane's eight weights sum up to at most `most`, so n <= 2^lg positions add up to at
+// most 2^(lg - 3) most times the largest value, 6 times the largest scale, and the joins may double that.
+//  - Values are large from a scale of 2^e on that leaves 2^(lg - 3 + log_most + 1) 6 2^(e - 1) below
+//    2^128: e = 128 - log_most - lg; at most 2^100, which contexts of 2^14 positions need (2^20 for
+//    weights in bf16).
+//  - With the largest scale, 2^125, 2^(lg - 3 + log_most + 1 - lift) 6 2^125 is below 2^128 for lift = lg +
+//    log_most - 2; contexts below 2^26 positions take that of 2^26.
+__device__ __forceinline__ int log_of(int n) { return 32 - __builtin_clz((unsigned)max(n, 2) - 1); }
+__device__ __forceinline__ int large_byte(const Room& room, int n) {
+  return 127 + min(128 - room.log_most - log_of(n), 100);
+}
+__device__ __forceinline__ float lift_of(const Room& room, int n) {
+  return (float)(max(log_of(n), 26) + room.log_most - 2);
+}
 
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
 struct RowState4 {
@@ -92,8 +105,8 @@ __device__ __forceinline__ void values4(unsigned w, const float (&s)[4], uint2& 
 }
 // Which of a word's four positions are NaN (scale byte 255; 253 and 254, which memory never
 // appended to may hold, are taken as it: 4 times theirs is infinite), as bits; their scales become 1.
-// `large`: whether the wavefront has a scale of 2^100 and more.
-__device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large) {
+// `large`: whether the wavefront has a scale that is large for rows of n positions.
+__device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large, const Room& room, int n) {
   const bool maybe = (w & w << 1 & 0x80808080u) != 0;  // some scale of 2^65 and more
   unsigned nan = 0;
   if (__builtin_expect(__any(maybe), false)) {
@@ -105,7 +118,7 @@ __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large) {
         nan |= 1u << i;
         w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
       } else {
-        big |= byte >= (unsigned)kHugeByte;
+        big |= byte >= (unsigned)large_byte(room, n);
       }
     }
     large |= __any(big);
@@ -469,13 +482,13 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
           if (!halves.value || __builtin_expect(__any(past_half(vs[0]) || past_half(vs[1])), false)) {
             bool large = false;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) nan |= take_nans(vs[t], large) << (4 * t);
+            for (int t = 0; t < kTiles; ++t) nan |= take_nans(vs[t], large, room, seen(last)) << (4 * t);
             if (halves.value && __any(past_half(vs[0]) || past_half(vs[1]))) {
               scored = true;
               return false;
             }
             if (__builtin_expect(large, false) && lift == 0.f) {
-              lift = room.lift;
+              lift = lift_of(room, seen(last));
               rescale4<HD>(o, __builtin_amdgcn_exp2f(-lift));
             }
           }
@@ -655,7 +668,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
       int kind = 0;
       if (!halves.value || __builtin_expect(__any(past_half(vs)), false)) {
         bool large = false;
-        const unsigned nan = take_nans(vs, large);
+        const unsigned nan = take_nans(vs, large, room, all);
         kind = (large ? kLarge : 0) | (__any(nan != 0) ? kNans : 0) |
                (halves.value && __any(past_half(vs)) ? kTooWide : 0);
         if (r16 == 0) s_nan[buf][wave][g] = nan;
@@ -721,7 +734,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
               for (int t = 0; t < kTiles; ++t)
                 if (uniform(s_kind[buf][2 * p + t]) & kNans) nan |= s_nan[buf][2 * p + t][g] << (4 * t);
             if (!halves.value && (kinds[p] & kLarge) && lift == 0.f) {
-              lift = room.lift;
+              lift = lift_of(room, all);
 #pragma unroll
               for (int y = 0; y < kRowTiles; ++y)
                 rescale4<HD>(o[y], __builtin_amdgcn_exp2f(-lift));

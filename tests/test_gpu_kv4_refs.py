@@ -59,3 +59,30 @@ def test_large_values_midway_under_large_scores(ops, n_seqs, rows, length, n_kv,
         for size in (1.0, 3e6, 2.0 ** 28, 1e9, 3e10):
             q = rnd(bt.rng, bt.n_rows, n_kv * G, hd, dtype=dtype) * size
             check_alike(bt, q, K, V, max_rows=rows)
+
+
+@pytest.mark.parametrize("rows", [None, 200])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lg,exponent", [(21, 99), (27, 99), (28, 125)])
+def test_long_contexts_of_large_values(ops, rows, dtype, lg, exponent):
+    """2^lg positions that all hold +-6 2^exponent, the first page with scores 4.9 ln 2 below the others' or
+    all with the same: their mean, though fp32 does not hold their sum.  A lane adds at most 2^28 / (32 x
+    128) = 2^16 times to each of its two sums, each time within 2^-24: 2^-7 in all."""
+    hd, page, n = 64, 128, 2 ** lg
+    table = torch.ones(1, n // page, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    cache = ops.KvCache.empty(2, 1, hd, table, page=page, bits=4)
+    k = torch.zeros(256, 1, hd, device="cuda")
+    k[128:, 0, 0] = 4.0
+    v = torch.full((256, 1, hd), 6 * 2.0 ** exponent, device="cuda")
+    v[:, :, 1::2] *= -1
+    ops.KvCache(cache.pool, ints([[0, 1]]), page=page, head_dim=hd, bits=4).append(
+        k, v, ints([256]), row_start=ints([0, 256]))
+    r = rows or 1
+    q = torch.zeros(r, 1, hd, device="cuda", dtype=dtype)
+    q[:, 0, 0] = 1.0
+    kw = {} if rows is None else dict(row_start=ints([0, rows]), max_rows=rows)
+    for scale in (0.0, 4.9 * np.log(2.0) / 4):
+        out = cache.attend(q, ints([n]), scale=scale, **kw).double()
+        want = v[0].double()
+        assert ((out - want).abs() <= want.abs() * (2.0 ** -7 + 2.0 ** -8)).all()
