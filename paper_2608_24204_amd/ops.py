@@ -7,7 +7,8 @@ one HIP GPU; a call enqueues on ``stream`` (default: the current stream of the t
 and returns without waiting.  On a stream other than the current one the caller orders the
 inputs' producers before the call, as for any torch operation; results are allocated on
 that stream.  Every call may be captured into a HIP graph.  The operators have no gradients: a
-tensor that requires one is refused where gradients are recorded.
+tensor that requires one is refused where gradients are recorded, and one with a forward-mode
+tangent always.
 
     table = ops.rope_table(n_pos, dim, base=500000.0, scaling="bands", factor=8, original=8192)
     cache = ops.KvCache.empty(n_pages, n_kv_heads, head_dim, page_table, bits=8)
@@ -25,6 +26,7 @@ import ctypes
 import functools
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import binding
 from .binding import WICI_BF16, WICI_F32, WICI_OK, WiciError
@@ -53,11 +55,20 @@ def _check(st: int, what: str) -> None:
         raise WiciError(st, what)
 
 
-def _no_gradient(name: str) -> None:
-    """For a tensor that requires a gradient."""
-    if torch.is_grad_enabled():
+def _tracked(x: torch.Tensor) -> bool:
+    """Whether x may have a gradient to lose (0.1 us)."""
+    return x.requires_grad or _forward._current_level >= 0
+
+
+def _no_gradient(name: str, x: torch.Tensor) -> None:
+    """Refuses a tracked x that requires a gradient where gradients are recorded, or that carries a
+    forward-mode tangent."""
+    if x.requires_grad and torch.is_grad_enabled():
         raise RuntimeError(f"{name}: requires a gradient, which these operators do not have (call "
                            "them under torch.no_grad(), or detach)")
+    if _forward.unpack_dual(x).tangent is not None:
+        raise RuntimeError(f"{name}: has a forward-mode gradient, which these operators do not have "
+                           "(detach)")
 
 
 def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> HeadRows:
@@ -66,8 +77,8 @@ def _rows(x: torch.Tensor, heads: int, head_dim: int, name: str, device) -> Head
     dtype = _DTYPES.get(x.dtype)
     if dtype is None:
         raise TypeError(f"{name}: dtype {x.dtype} (float32 or bfloat16)")
-    if x.requires_grad:
-        _no_gradient(name)
+    if _tracked(x):
+        _no_gradient(name, x)
     shape = x.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected [rows, {heads}, {head_dim}]")
@@ -161,6 +172,11 @@ class RopeTable:
         self._c = binding.WiciRopeTab(cos.data_ptr(), sin.data_ptr(), cos.shape[0], self.dim,
                                       LAYOUTS[layout])
 
+    def _no_gradients(self, name: str) -> None:
+        for x in (self.cos, self.sin):
+            if _tracked(x):
+                _no_gradient(name, x)
+
 
 def rope_spec(dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "plain",
               factor: float = 1.0, original: float = 0.0, low: float = 0.0,
@@ -207,8 +223,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, table: RopeTable,
     n, h, d = x.shape
     if table.device != device:
         raise ValueError(f"table: on {table.device}, expected {device}")
-    if table.cos.requires_grad or table.sin.requires_grad:
-        _no_gradient("table")
+    table._no_gradients("table")
     lib = binding.load_library()
     with _launch_on(stream, device, x, positions, out, table.cos, table.sin) as raw:
         xr = _rows(x, h, d, "x", device)
@@ -313,8 +328,8 @@ class KvCache:
             raise ValueError("q is only rotated: it needs rope")
         if rope is not None and rope.device != dev:
             raise ValueError(f"rope: on {rope.device}, expected {dev}")
-        if rope is not None and (rope.cos.requires_grad or rope.sin.requires_grad):
-            _no_gradient("rope")
+        if rope is not None:
+            rope._no_gradients("rope")
         with self._on(stream, k, v, length, row_start, q, q_out, rope and rope.cos,
                       rope and rope.sin) as raw:
             qr, qo, heads, given = _NO_ROWS, _NO_ROWS, 0, q is not None and q_out is not None
@@ -452,8 +467,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int | None = None
     vocab = logits.shape[1]
     if vocab > 1 and logits.stride(1) != 1:
         raise ValueError("logits: the words of a row must lie side by side")
-    if logits.requires_grad or scores.requires_grad:
-        _no_gradient("logits" if logits.requires_grad else "scores")
+    for name, x in (("logits", logits), ("scores", scores)):
+        if _tracked(x):
+            _no_gradient(name, x)
     k = beams if k is None else k
     need = beam_workspace(n, beams, vocab, logits.dtype, k)
     with _launch_on(stream, device, logits, scores, workspace) as raw:
