@@ -605,9 +605,14 @@ wici_status wici_beam_select(const void* logits, int32_t dtype, int64_t row_stri
  * the page named by spare[b beams + i] (device), in each of the n_pools pools (host array of device
  * pointers: the layers' caches, all of `bits` (8 or 4) and the geometry of `cache`, whose own pool
  * and table are not used); that page takes the partial one's place in the beam's table, and the
- * beam's own former partial page becomes its spare.  So n beams spares, pages that no table names,
- * serve all steps until the partial pages are full.  A beam that is its own parent keeps its pages,
- * and so does one whose parent is not among 0 .. beams - 1.  A parent's entry that names no page is
+ * beam's own former partial page becomes its spare.  So n beams spares serve all steps until the
+ * partial pages are full.  The caller sees to it that the pages in the tables' partial places and the
+ * spares are all different, and that no other entry in use names one of them: a page that two beams
+ * write on, or that is one's partial page and another's spare, would be overwritten under the other.
+ * They stay so from step to step.  A search whose prompt lies in the pages of one beam begins by a
+ * reordering with that beam as every parent, the others' tables naming a page of their own each in the
+ * partial place.  A beam that is its own parent keeps its pages, and so does one whose parent is not
+ * among 0 .. beams - 1.  A parent's entry that names no page is
  * taken over as it is, with nothing copied or exchanged; a spare that names none takes its place in
  * the table, with nothing copied. */
 wici_status wici_beam_reorder(const wici_kv8* cache, int32_t bits, void* const* pools,

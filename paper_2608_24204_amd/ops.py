@@ -495,7 +495,12 @@ def beam_reorder(caches, parent: torch.Tensor, length: torch.Tensor, spare: torc
     b * beams + i of the table is that beam's, and ``length`` [n * beams] (int32) counts its
     positions (one length a search).  Full pages are shared through the table; a partial last one is
     copied into the beam's page of ``spare`` [n * beams] (int32), and the beam's own becomes its
-    spare: table and spare are written.  wici_beam_reorder."""
+    spare: table and spare are written.
+
+    The partial pages and the spares have to be different pages, named by no other entry in use
+    (they stay so).  A search begins from a prompt in the pages of its first beam by
+    ``parent`` 0 throughout, each other beam's table naming a page of its own where the prompt's
+    partial one stands.  wici_beam_reorder."""
     caches = [caches] if isinstance(caches, KvCache) else list(caches)
     if not caches:
         raise ValueError("caches: none")
