@@ -451,11 +451,12 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int | None = None
                 workspace: torch.Tensor | None = None, stream=None):
     """The ``k`` (default: as many as beams) best continuations of each of n beam searches:
     (scores float32, parent int32, token int32), each [n, k], best first.  ``logits``
-    [n * beams, vocab] (rows of any stride), ``scores`` [n, beams] float32: each beam's so far
-    (minus infinity: not alive).  A continuation adds its word's log-probability; the order is that
-    of scores formed in 64 bits (to some 2^-53), ties the lowest beam's and word's.  Where fewer
-    than k are left the parents and tokens are -1.  ``workspace`` (uint8, beam_workspace bytes;
-    default: a new one) may be given.  wici_beam_select."""
+    [n * beams, vocab] (rows of their own: vocab or more elements apart, anywhere), ``scores``
+    [n, beams] float32: each beam's so far (minus infinity: not alive).  A continuation adds its
+    word's log-probability; the order is that of scores formed in 64 bits (to some 2^-53), ties the
+    lowest beam's and word's.  Where fewer than k are left the parents and tokens are -1.
+    ``workspace`` (uint8, beam_workspace bytes; default: a new one) may be given.
+    wici_beam_select."""
     device = _on_gpu(logits, "logits")
     if scores.dim() != 2 or scores.dtype != torch.float32 or not scores.is_contiguous() or \
             scores.device != device:
