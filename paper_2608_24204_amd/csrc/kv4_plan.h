@@ -5,9 +5,6 @@
 
 namespace wici {
 
-// Workgroups of the split that the chip holds at once: 4, 3 or 2 wavefronts a SIMD.
-inline int resident4(int hd, int terms) { return kCus * (hd == 64 ? 4 : terms == 1 ? 3 : 2); }
-
 // Which kernel, from the rows x heads of a KV head, the workgroups of 128 of them and the 16 rows x 32
 // positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us a call, split / 64 rows
 // / 128 rows):
@@ -34,21 +31,7 @@ inline Kv8Plan kv4_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int ma
   if (terms > 1) p.row_tiles = std::min(p.row_tiles, 1);
   const int64_t per = p.row_tiles ? 64 * p.row_tiles : 16;
   p.ntile = std::max(1, (int)((rows + per - 1) / per));
-  const int64_t blocks = heads * p.ntile;
-  const int64_t want =
-      std::min<int64_t>((p.row_tiles ? 2 * kCus : resident4(hd, terms)) / blocks, 128);
-  if (want <= 1) {
-    p.nsplit = 1;
-  } else if (p.row_tiles) {
-    // eight chunks a split at least: partial results of 128 rows are the larger traffic
-    const int64_t most = ((int64_t)max_length + 8 * kChunkPos - 1) / (8 * kChunkPos);
-    p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
-  } else {
-    // each wavefront as many steps
-    const int64_t steps = ((int64_t)max_length + kStep - 1) / kStep;
-    const int64_t each = steps <= 16 ? 4 : (steps + 4 * want - 1) / (4 * want);
-    p.nsplit = (int)std::max<int64_t>(1, (steps + 4 * each - 1) / (4 * each));
-  }
+  p.nsplit = kv_splits(hd, terms, p.row_tiles, heads * p.ntile, max_length);
   return p;
 }
 

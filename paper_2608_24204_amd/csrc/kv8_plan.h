@@ -19,6 +19,23 @@ struct Kv8Plan {
   int row_tiles;  // prompts: tiles of 16 rows a wavefront; 0: a split of few rows
   int ntile, nsplit;
 };
+// The splits of the positions of `blocks` workgroups (of either cache).
+inline int kv_splits(int hd, int terms, int row_tiles, int64_t blocks, int max_length) {
+  const int64_t want = std::min<int64_t>((row_tiles ? 2 * kCus : resident(hd, terms)) / blocks, 128);
+  if (want <= 1) return 1;
+  if (row_tiles) {
+    // eight chunks a split at least: partial results of 128 rows are the larger traffic
+    const int64_t most = ((int64_t)max_length + 8 * kChunkPos - 1) / (8 * kChunkPos);
+    return (int)std::max<int64_t>(1, std::min(want, most));
+  }
+  // Each wavefront as many steps: one at 16384 positions (8 bits a value) 16.4 us with 64 splits of two
+  // steps a wavefront, 17.6 with the 96 that the chip holds.  Up to 512 positions, four
+  // steps, no split: 256 7.7 us (one split) for 9.1 (two, and the merge), 512 9.5 for 9.1,
+  // and a call's host work 3 us less; 700 would be 11.0 for 9.1.
+  const int64_t steps = ((int64_t)max_length + kStep - 1) / kStep;
+  const int64_t each = steps <= 16 ? 4 : (steps + 4 * want - 1) / (4 * want);
+  return (int)std::max<int64_t>(1, (steps + 4 * each - 1) / (4 * each));
+}
 // Which kernel, from the rows x heads of a KV head, the workgroups of 128 of them and the
 // 16 rows x 32 positions that all of them multiply (32 query on 8 KV heads of 128, bf16, us a
 // call, split / 64 rows / 128 rows):
@@ -48,24 +65,7 @@ inline Kv8Plan kv8_plan(int hd, int terms, int n_q, int n_kv, int n_seqs, int ma
   if (terms == 2) p.row_tiles = std::min(p.row_tiles, 1);
   const int64_t per = p.row_tiles ? 64 * p.row_tiles : 16;
   p.ntile = std::max(1, (int)((rows + per - 1) / per));
-  const int64_t blocks = heads * p.ntile;
-  const int64_t want =
-      std::min<int64_t>((p.row_tiles ? 2 * kCus : resident(hd, terms)) / blocks, 128);
-  if (want <= 1) {
-    p.nsplit = 1;
-  } else if (p.row_tiles) {
-    // eight chunks a split at least: partial results of 128 rows are the larger traffic
-    const int64_t most = ((int64_t)max_length + 8 * kChunkPos - 1) / (8 * kChunkPos);
-    p.nsplit = (int)std::max<int64_t>(1, std::min(want, most));
-  } else {
-    // Each wavefront as many steps: one at 16384 positions 16.4 us with 64 splits of two
-    // steps a wavefront, 17.6 with the 96 that the chip holds.  Up to 512 positions, four
-    // steps, no split: 256 7.7 us (one split) for 9.1 (two, and the merge), 512 9.5 for 9.1,
-    // and a call's host work 3 us less; 700 would be 11.0 for 9.1.
-    const int64_t steps = ((int64_t)max_length + kStep - 1) / kStep;
-    const int64_t each = steps <= 16 ? 4 : (steps + 4 * want - 1) / (4 * want);
-    p.nsplit = (int)std::max<int64_t>(1, (steps + 4 * each - 1) / (4 * each));
-  }
+  p.nsplit = kv_splits(hd, terms, p.row_tiles, heads * p.ntile, max_length);
   return p;
 }
 
