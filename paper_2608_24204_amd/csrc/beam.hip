@@ -88,8 +88,8 @@ struct Logits {
 // e^x for x <= 0 to 2^-52 + |x| 2^-54 of itself, and 1 for 0 (what is below e^-200 counts as that): x =
 // n ln 2 + r with |r| <= ln 2 / 2, and 1 + r + r^2 p(r) with the polynomial p of degree 9 that meets
 // (e^r - 1 - r) / r^2 at the ten Chebyshev nodes of that range (2^-55).  Added to 1.5 2^52, n stands in
-// the sum's low bits; it goes into the exponent, which stays in its range.  (A degree of 7 with errors of
-// 2^-34 reached the scores: words that are all but certain came out at 1e-10 above or below theirs.)
+// the sum's low bits; it goes into the exponent, which stays in its range.  (A degree of 7, errors of 2^-34,
+// took 19.7 us for 23.0 below and reached the scores: those of all but certain words were 1e-10 off.)
 __device__ __forceinline__ double exp_below(double x) {
   x = fmax(x, -200.0);
   const double t = __builtin_fma(x, 1.4426950408889634074, 0x1.8p52);
@@ -118,8 +118,8 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // ------------------------------------------------------------------- the pass over the logits
 // A wavefront takes a unit, kLoads blocks a lane at a time.  A NaN or an infinity makes the sum NaN.
 //
-// Bound by the exponentials: 16 instructions an element, two of them at half rate.  128 rows of 152064
-// bf16 logits 19.7 us for 39 MB (the instructions alone 11, the bytes 7.5), 4 of 128256 in fp32 3.9.
+// Bound by the exponentials: 19 instructions an element, vector units busy 85% of the time.  128 rows of
+// 152064 bf16 logits 23.0 us for 39 MB (the instructions alone 15, the bytes 7.5), 4 of 128256 in fp32 3.9.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_beam_scan(BeamSelect a, BeamPlan p, double* __restrict__ sums,
                                                    float* __restrict__ tops,

@@ -10,7 +10,9 @@
 // bf16 rows enter the second product as one fp16 term while the values' scales are 2^-23 .. 2^8, so
 // that fp16 holds them exactly (a weight to 2^-11, an eighth of the output's own rounding, or to 2^-31
 // of the row's largest); where they are not, and for other rows, as NW bf16 terms (two, 2^-16, or
-// three, 2^-24).  Scores, weights, sums and the output are fp32.
+// three, 2^-24).  A wavefront that has met such a step goes on in bf16; groups of zeros, whose scale is
+// the least, do that too (2048 rows of 8192 positions 369 us for 282).  Scores, weights, sums and the
+// output are fp32.
 //
 // (The matrix instruction that takes 4-bit operands with their scales as they lie would need queries
 // in 8 bits, two terms for bf16 ones at the same rate, and was measured to keep only about 2^-14 of the
@@ -399,8 +401,8 @@ __device__ __forceinline__ void load_queries4(const HeadRows& q, int64_t at, boo
 // ONCE: nobody reads a code again.
 //
 // Bound by the cache's bytes, each read once: 32 tokens at 16384 (40 query on 8 KV heads of 128, bf16)
-// 93 us for 570 MB, 6.1 TB/s where a large copy moves 4.9-5.2; the loads with nothing behind them take
-// 92.  There the vector units are busy 53% of the time (17 instructions of a tile's 70 make keys, 36
+// 93 us for 570 MB, 6.1 TB/s where a large copy moves 4.8-5.2; the loads with nothing behind them take
+// 92.  There the vector units are busy 54% of the time (17 instructions of a tile's 70 make keys, 36
 // values).  Where there is less to read, latencies show: 48 tokens at up to 4000 (heads of 64) 28.7 us
 // for 81 MB, one at 16384 (fp32) 12.8 us for 18 MB.  Three wavefronts a SIMD for heads of 128 (two with
 // three terms), four for heads of 64: one more changed nothing (114 for 112, 37.8 for 36.7 us), nor did
@@ -565,10 +567,10 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
 // codes are on their way while this one is multiplied, and one barrier a chunk parts a buffer's
 // readers from its next writers.
 //
-// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 280 us in bf16, 860 TFLOP/s of
-// products where a large product reaches 1150-1300.  No unit is full: matrix cores 34%, vector units
-// 45%, LDS 26% of the time; the two wavefronts a SIMD that the registers allow wait for each other's
-// units and on LDS.  Two bf16 terms of every weight took 366 us; eight wavefronts of 16 rows a
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 282 us in bf16, 853 TFLOP/s of
+// products where a large product reaches 1100-1300.  No unit is full: matrix cores 36%, vector units
+// 42%, LDS 33% of the time (a seventh of that bank conflicts: a tile's values are written 8 bytes a
+// lane); the two wavefronts a SIMD that the registers allow wait for each other's units and on LDS.  Two bf16 terms of every weight took 366 us; eight wavefronts of 16 rows a
 // workgroup, four a SIMD, 346 (they spill); the next chunk's operands made between this one's two
 // steps 289.
 template <int HD, int NQ, int NW, int kRowTiles>

@@ -388,7 +388,9 @@ class KvCache:
         """Causal attention of the rows q [rows, heads, head_dim] over the cache (append first):
         a row sees its sequence's positions up to its own; zeros where that is none.  ``scale``
         defaults to head_dim^-1/2.  ``max_rows`` and ``max_length`` (the most new rows and
-        positions of a sequence, 0: unknown) only shape the launch.  ``out`` (default: a new
+        positions of a sequence, 0: unknown) only shape the launch.  Where q and out are bfloat16 a
+        weight enters the products to 11 bits (an eighth of the output's own rounding), else to 22
+        or more; sums are float32.  ``out`` (default: a new
         tensor like q) and ``workspace`` (uint8, attend_workspace bytes; default: a new one) may
         be given.  wici_kv8_attend, wici_kv4_attend."""
         dev, d = self.device, self.head_dim
