@@ -570,7 +570,7 @@ wici_status wici_kv4_attend_workspace(const wici_kv4* cache, const wici_kv8_batc
  * are bf16, q is too and a weight is within 2^-11 of itself or 2^-31 of the row's largest; else both are
  * within 2^-24.  A weight 2^-126 and less of its row's largest may count as nothing.  In rows that have met
  * values of 2^100 and more (of 2^114 / n and more, where they see n > 2^14 positions) that is 2^-94, for
- * n > 2^26 2^-120 n: sums of any such values stay within fp32. */
+ * n > 2^25 2^-119 n: sums of any such values stay within fp32. */
 wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, int32_t n_heads,
                             float scale, wici_head_rows q, wici_head_rows out, void* workspace,
                             size_t workspace_bytes, void* hip_stream);

@@ -43,30 +43,6 @@ template <> struct ElemOf<bf16x8_t> { typedef __bf16 type; };
 template <> struct ElemOf<half8_t> { typedef _Float16 type; };
 template <typename T> using Elem_t = typename ElemOf<T>::type;
 
-// A row's reference is set so that its largest weight is 2^top, and moves before one is past `most`.
-struct Room {
-  float top, most;
-  int log_most;
-};
-// fp16 weights: 2^14 fits, and fp16's least step is 2^-30 of the largest weight.
-constexpr Room kRoomHalf{6.f, 0x1p14f, 14}, kRoomBf16{0.f, 0x1p8f, 8};
-// Once a wavefront has met large values its rows' outputs hold 2^-lift of their sums, for which the
-// weights are multiplied by that.  (Not by other references: those of large scores are too coarse to
-// hold such a shift.)  A lane's eight weights sum up to at most `most`, so n <= 2^lg positions add up to at
-// most 2^(lg - 3) most times the largest value, 6 times the largest scale, and the joins may double that.
-//  - Values are large from a scale of 2^e on that leaves 2^(lg - 3 + log_most + 1) 6 2^(e - 1) below
-//    2^128: e = 128 - log_most - lg; at most 2^100, which contexts of 2^14 positions need (2^20 for
-//    weights in bf16).
-//  - With the largest scale, 2^125, 2^(lg - 3 + log_most + 1 - lift) 6 2^125 is below 2^128 for lift = lg +
-//    log_most - 2; contexts below 2^26 positions take that of 2^26.
-__device__ __forceinline__ int log_of(int n) { return 32 - __builtin_clz((unsigned)max(n, 2) - 1); }
-__device__ __forceinline__ int large_byte(const Room& room, int n) {
-  return 127 + min(128 - room.log_most - log_of(n), 100);
-}
-__device__ __forceinline__ float lift_of(const Room& room, int n) {
-  return (float)(max(log_of(n), 26) + room.log_most - 2);
-}
-
 // The state of 16 query rows over the positions a wavefront has taken: lane l, row l % 16.
 struct RowState4 {
   float ref = kNoRef, sum = 0.f;  // sum over this lane's positions
@@ -120,7 +96,7 @@ __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large, const Ro
         nan |= 1u << i;
         w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
       } else {
-        big |= byte >= (unsigned)large_byte(room, n);
+        big |= byte >= (unsigned)kv4_large_byte(room, n);
       }
     }
     large |= __any(big);
@@ -490,7 +466,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
               return false;
             }
             if (__builtin_expect(large, false) && lift == 0.f) {
-              lift = lift_of(room, seen(last));
+              lift = (float)kv4_lift(room, seen(last));
               rescale4<HD>(o, __builtin_amdgcn_exp2f(-lift));
             }
           }
@@ -736,7 +712,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
               for (int t = 0; t < kTiles; ++t)
                 if (uniform(s_kind[buf][2 * p + t]) & kNans) nan |= s_nan[buf][2 * p + t][g] << (4 * t);
             if (!halves.value && (kinds[p] & kLarge) && lift == 0.f) {
-              lift = lift_of(room, all);
+              lift = (float)kv4_lift(room, all);
 #pragma unroll
               for (int y = 0; y < kRowTiles; ++y)
                 rescale4<HD>(o[y], __builtin_amdgcn_exp2f(-lift));

@@ -41,4 +41,33 @@ WICI_HD int kv4_scale_byte(uint32_t most) {
   return byte < kKv4LeastByte ? kKv4LeastByte : byte > kKv4MostByte ? kKv4MostByte : byte;
 }
 
+// A row's reference is set so that its largest weight is 2^top, and moves before a lane's eight weights
+// sum up to more than most = 2^log_most.
+struct Room {
+  float top, most;
+  int log_most;
+};
+// fp16 weights: 2^14 fits, and fp16's least step is 2^-30 of the largest weight.
+constexpr Room kRoomHalf{6.f, 0x1p14f, 14}, kRoomBf16{0.f, 0x1p8f, 8};
+
+// Once a wavefront has met large values its rows' outputs hold 2^-lift of their sums, for which the
+// weights are multiplied by that.  (Not by other references: those of large scores are too coarse to
+// hold such a shift.)  n <= 2^lg positions add up to at most 2^(lg - 3) most times the largest value, 6
+// times the largest scale.
+//  - Values are large from a scale of 2^e on that leaves 2^(lg - 3) most 6 2^(e - 1) below 2^127: e = 128 -
+//    log_most - lg; at most 2^100, which contexts of 2^14 positions need (2^20 for weights in bf16).  The
+//    joins take what is not lifted by factors of at most 1.
+//  - With the largest scale, 2^125, 2^(lg - 3 - lift) most 6 2^125 is below 2^126 for lift = lg + log_most -
+//    1; contexts below 2^25 positions take that of 2^25.  Two joins, of wavefronts and of splits, take
+//    what is lifted by less than 2 each, where the largest reference is that of an output that is not.
+WICI_HD int kv4_log_of(int n) { return n < 2 ? 1 : 32 - __builtin_clz((unsigned)n - 1u); }
+WICI_HD int kv4_large_byte(const Room& room, int n) {
+  const int e = 128 - room.log_most - kv4_log_of(n);
+  return 127 + (e < 100 ? e : 100);
+}
+WICI_HD int kv4_lift(const Room& room, int n) {
+  const int lg = kv4_log_of(n);
+  return (lg < 25 ? 25 : lg) + room.log_most - 1;
+}
+
 }  // namespace wici
