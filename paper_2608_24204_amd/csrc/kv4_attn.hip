@@ -83,7 +83,9 @@ __device__ __forceinline__ void values4(unsigned w, const float (&s)[4], uint2& 
 }
 // Which of a word's four positions are NaN (scale byte 255; 253 and 254, which memory never
 // appended to may hold, are taken as it: 4 times theirs is infinite), as bits; their scales become 1.
-// `large`: whether the wavefront has a scale that is large for rows of n positions.
+// `large`: whether the wavefront has a scale that is large for rows of n positions (asked where LARGE: one
+// that fits halves is not; asked everywhere, 2048 rows of 8192 positions took 286 us for 282).
+template <bool LARGE>
 __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large, const Room& room, int n) {
   const bool maybe = (w & w << 1 & 0x80808080u) != 0;  // some scale of 2^65 and more
   unsigned nan = 0;
@@ -95,11 +97,11 @@ __device__ __forceinline__ unsigned take_nans(unsigned& w, bool& large, const Ro
       if (byte > (unsigned)kKv4MostByte) {
         nan |= 1u << i;
         w = (w & ~(0xffu << (8 * i))) | 127u << (8 * i);
-      } else {
+      } else if constexpr (LARGE) {
         big |= byte >= (unsigned)kv4_large_byte(room, n);
       }
     }
-    large |= __any(big);
+    if constexpr (LARGE) large |= __any(big);
   }
   return nan;
 }
@@ -460,7 +462,7 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
           if (!halves.value || __builtin_expect(__any(past_half(vs[0]) || past_half(vs[1])), false)) {
             bool large = false;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) nan |= take_nans(vs[t], large, room, seen(last)) << (4 * t);
+            for (int t = 0; t < kTiles; ++t) nan |= take_nans<!halves.value>(vs[t], large, room, seen(last)) << (4 * t);
             if (halves.value && __any(past_half(vs[0]) || past_half(vs[1]))) {
               scored = true;
               return false;
@@ -646,7 +648,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_attn_tile(Kv8 c, Kv8Rows r, K
       int kind = 0;
       if (!halves.value || __builtin_expect(__any(past_half(vs)), false)) {
         bool large = false;
-        const unsigned nan = take_nans(vs, large, room, all);
+        const unsigned nan = take_nans<!halves.value>(vs, large, room, all);
         kind = (large ? kLarge : 0) | (__any(nan != 0) ? kNans : 0) |
                (halves.value && __any(past_half(vs)) ? kTooWide : 0);
         if (r16 == 0) s_nan[buf][wave][g] = nan;
