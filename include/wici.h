@@ -576,9 +576,10 @@ wici_status wici_kv4_attend(const wici_kv4* cache, const wici_kv8_batch* batch, 
                             size_t workspace_bytes, void* hip_stream);
 
 /* One step of n beam searches of `beams` beams each (1 .. 64; n beams at most 65535).  Row
- * b beams + i of the logits (device, WICI_F32 or WICI_BF16, rows row_stride elements apart, vocab or more
- * unless there is one row, of any alignment of their type; vocab at most 2^24) belongs to beam i of search b, which has the score
- * scores[b beams + i] so far (device).  The continuation of beam i by word v has the score
+ * b beams + i of the logits (device, WICI_F32 or WICI_BF16, of any alignment of their type; rows
+ * row_stride elements apart, vocab or more unless there is one; vocab at most 2^24) belongs to beam i
+ * of search b, which has the score scores[b beams + i] so far (device).  The continuation of beam i by
+ * word v has the score
  *   scores[b beams + i] + z_v - log sum_u e^(z_u)        (z the row's logits)
  * formed in 64 bits (exponentials and the logarithm to 2^-52, sums to 2^-53 an addition; rows that are alike
  * have the same), and the k (1 .. 64) greatest of each search's beams x vocab are returned in

@@ -11,7 +11,7 @@
 // that fp16 holds them exactly (a weight to 2^-11, an eighth of the output's own rounding, or to 2^-31
 // of the row's largest); where they are not, and for other rows, as NW bf16 terms (two, 2^-16, or
 // three, 2^-24).  A wavefront that has met such a step goes on in bf16; groups of zeros, whose scale is
-// the least, do that too (2048 rows of 8192 positions 369 us for 282).  Scores, weights, sums and the
+// the least, do that too (2048 rows of 8192 positions 366 us for 280).  Scores, weights, sums and the
 // output are fp32.
 //
 // (The matrix instruction that takes 4-bit operands with their scales as they lie would need queries
@@ -545,9 +545,9 @@ __attribute__((amdgpu_waves_per_eu(HD == 64 ? 4 : NQ == 1 ? 3 : 2))) void k_kv4_
 // codes are on their way while this one is multiplied, and one barrier a chunk parts a buffer's
 // readers from its next writers.
 //
-// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 282 us in bf16, 853 TFLOP/s of
+// 2048 rows of 8192 positions (32 query on 8 KV heads of 128) take 280 us in bf16, 859 TFLOP/s of
 // products where a large product reaches 1100-1300.  No unit is full: matrix cores 36%, vector units
-// 42%, LDS 33% of the time (a seventh of that bank conflicts: a tile's values are written 8 bytes a
+// 43%, LDS 33% of the time (a seventh of that bank conflicts: a tile's values are written 8 bytes a
 // lane); the two wavefronts a SIMD that the registers allow wait for each other's units and on LDS.  Two bf16 terms of every weight took 366 us; eight wavefronts of 16 rows a
 // workgroup, four a SIMD, 346 (they spill); the next chunk's operands made between this one's two
 // steps 289.
